@@ -67,7 +67,7 @@ typedef enum { GRACEKV_F32 = 0, GRACEKV_BF16 = 1 } gracekv_dtype;
 /* Version of this interface (structures and signatures).  A binding must
  * refuse a library whose gracekv_abi_version() differs from the value it was
  * written for: argument lists shift silently across versions. */
-#define GRACEKV_ABI_VERSION 11
+#define GRACEKV_ABI_VERSION 12
 
 /* Shapes and hyperparameters.  gracekv_default_config fills the paper's
  * defaults (App. A and B); the caller then sets the shape fields. */
@@ -379,6 +379,119 @@ gracekv_status gracekv_decode_attention(const gracekv_config* cfg, const void* q
 gracekv_status gracekv_decode_attention_noalloc(const gracekv_config* cfg, const void* q, const int64_t* offsets,
                                                 const void* K_out, const void* V_out, const float* logm_out,
                                                 const void* K, const void* V, float* out, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Around the compression, one layer at a time: the attention of a prompt (whose
+ * keys and values are what is compressed), a paged cache for the tokens that come
+ * after it, and the attention of the next token over both.
+ *
+ * These calls follow the conventions above (device pointers of the caller's,
+ * 16-byte aligned; nothing allocated or synchronised; argument errors before
+ * anything is enqueued) and take no gracekv_config: their shapes come in the
+ * structures below.  Types: GRACEKV_BF16 and GRACEKV_F32; d: 64 or 128; any H / G.
+ * Strides are in elements and multiples of 16 bytes; the elements of a head are
+ * contiguous.  Logits are q.k / sqrt(d), softmax statistics are fp32; bf16
+ * probabilities are rounded to bf16 in the product with the values.  The outputs are of
+ * the inputs' type, lse = log sum exp of the logits is fp32 (natural logarithm;
+ * NULL: not wanted).  A query with no key has the output 0 and lse -inf; a masked or
+ * absent key and its value never reach an output, whatever they hold.  Every call may
+ * be captured in a HIP graph; lengths and tables are read when it runs. */
+
+/* Causal attention over packed prompts. */
+typedef struct {
+  int32_t dtype, G, H, d;           /* gracekv_dtype, KV heads, query heads, head dim */
+  int32_t n_seq;                    /* sequences */
+  int32_t reserved;                 /* 0 */
+  int64_t n_q, n_k;                 /* rows of Q and out; rows of K and V (below 2^31) */
+  int64_t q_tok, q_head, k_tok, k_head, v_tok, v_head, out_tok, out_head; /* strides */
+} gracekv_prompt_config;
+
+/* Workspace of gracekv_prompt_attention (bytes; 0 where the rows fill the chip). */
+gracekv_status gracekv_prompt_ws_bytes(const gracekv_prompt_config* cfg, size_t* ws_bytes);
+
+/* Sequence b has the query rows cu_q[b] .. cu_q[b+1] - 1 and the key rows cu_k[b] ..
+ * cu_k[b+1] - 1.  Its last query stands at its last key: query i of Lq sees the keys
+ * j <= i + Lk - Lq, so Lq = Lk is a whole prompt, Lq < Lk a later piece of one (the
+ * question's window, a chunk), and with Lq > Lk the first queries see nothing.
+ *   Q          [n_q] rows x H heads (strides q_tok, q_head); K, V [n_k] x G
+ *   cu_q, cu_k [n_seq + 1] int32, ascending; places outside [0, n_q] and [0, n_k]
+ *              are held inside, a descending pair is an empty sequence
+ *   out        [n_q] x H (strides out_tok, out_head); not an input's memory
+ *   lse        [n_q][H] fp32 or NULL
+ *   ws         gracekv_prompt_ws_bytes bytes (NULL where that is 0); calls that
+ *              overlap on one workspace race
+ * Rows outside every sequence are left as they are. */
+gracekv_status gracekv_prompt_attention(const gracekv_prompt_config* cfg, const void* Q, const void* K, const void* V,
+                                        const int32_t* cu_q, const int32_t* cu_k, void* out, float* lse, void* ws,
+                                        size_t ws_bytes, void* stream);
+
+/* A paged cache of one layer.  K_pages and V_pages hold n_pages pages of page_size
+ * tokens, page i at element i * page_stride, each [G][page_size][d].  Row b of
+ * block_table [n_seq][table_width] int32 names the pages of sequence b in order: its
+ * token t lies in page block_table[b][t / page_size].  An id outside [0, n_pages) is
+ * no page: nothing is written there, and its tokens do not take part in attention. */
+typedef struct {
+  int32_t dtype, G, H, d;
+  int32_t n_seq;
+  int32_t page_size;                /* 16, 32, 64, 128 or 256 */
+  int32_t table_width;
+  int32_t reserved;                 /* 0 */
+  int64_t n_pages, page_stride;     /* page_stride >= G * page_size * d, a multiple of 16 bytes */
+} gracekv_page_config;
+
+/* New tokens of gracekv_cache_append. */
+typedef struct {
+  int64_t n_new;                    /* rows of k, v (and q, q_out), below 2^31 */
+  int64_t rope_rows;                /* rows of rope_cos, rope_sin */
+  int64_t k_tok, k_head, v_tok, v_head, q_tok, q_head, qout_tok, qout_head; /* strides */
+} gracekv_append_config;
+
+/* Keys and values of new tokens into the pages, the keys rotated on the way, and the
+ * rotated queries of the same tokens: token cu_new[b] + i of the rows goes to place
+ * start[b] + i of sequence b.
+ *   k, v       [n_new] x G;  q, q_out [n_new] x H, or both NULL (q_out may be q itself,
+ *              with the same strides)
+ *   start      [n_seq] int32: tokens that sequence b holds already
+ *   cu_new     [n_seq + 1] int32, as cu_q above
+ *   pos        [n_new] int32: row of rope_cos, rope_sin ([rope_rows][d/2] fp32, as
+ *              above) that turns the token's key and query; all three NULL: nothing is
+ *              turned (keys that are rotated already)
+ * A token whose place has no page, or whose position is outside the tables, is left out:
+ * neither its key and value nor its rotated query is written.  Two tokens with one place race.
+ * Products and sums of the rotation are fp32, rounded once. */
+gracekv_status gracekv_cache_append(const gracekv_page_config* cfg, const gracekv_append_config* rows, const void* k,
+                                    const void* v, const void* q, const int32_t* block_table, const int32_t* start,
+                                    const int32_t* cu_new, const int32_t* pos, const float* rope_cos,
+                                    const float* rope_sin, void* K_pages, void* V_pages, void* q_out, void* stream);
+
+/* Workspace of gracekv_paged_attention (bytes). */
+gracekv_status gracekv_paged_ws_bytes(const gracekv_page_config* cfg, size_t* ws_bytes);
+
+/* Packed entries in front of the pages: rows start[b*G+g] .. + count[b*G+g] - 1 of the
+ * arrays are entries of (sequence b, KV head g), with logits q.k / sqrt(d) + logm; an
+ * entry with logm = -inf has no weight.  For one sequence these are gracekv_pack's
+ * outputs as they stand: layer l takes start = offsets + l*G and count = counts + l*G.
+ * Starts and counts that leave [0, rows] are held inside. */
+typedef struct {
+  const int64_t* start;             /* [n_seq * G] */
+  const int64_t* count;             /* [n_seq * G] */
+  const void* K;                    /* [rows][d] (cfg->dtype) */
+  const void* V;
+  const float* logm;                /* [rows] */
+  int64_t rows;
+} gracekv_prefix;
+
+/* Attention of one token of every sequence over the first seq_len[b] tokens of its
+ * pages, and over its packed entries (prefix not NULL).
+ *   q          [n_seq] rows x [H][d], rows q_tok elements apart, rotated already
+ *   seq_len    [n_seq] int32, held to [0, table_width * page_size]
+ *   prefix     host structure, read by the call, or NULL
+ *   out        [n_seq][H][d] (cfg->dtype); lse [n_seq][H] fp32 or NULL
+ *   ws         gracekv_paged_ws_bytes bytes; calls that overlap on one workspace race */
+gracekv_status gracekv_paged_attention(const gracekv_page_config* cfg, const void* q, int64_t q_tok, const void* K_pages,
+                                       const void* V_pages, const int32_t* block_table, const int32_t* seq_len,
+                                       const gracekv_prefix* prefix, void* out, float* lse, void* ws, size_t ws_bytes,
+                                       void* stream);
 
 /* Layout check of the cross-lane instructions used by the kernels: computes
  * a 16x16 product from fixed inputs with the fp32 16x16x4 (which = 0), the

@@ -8,6 +8,7 @@
 #include <vector>
 
 #include "common.h"
+#include "serve.h"
 
 using namespace gkv;
 
@@ -571,6 +572,121 @@ gracekv_status gracekv_decode_attention_noalloc(const gracekv_config* c, const v
   const Dims dm = make_dims(*c, p);
   if (decode_ws_bytes(dm, decode_parts(dm)) > (size_t)GRACEKV_DECODE_SCRATCH_BYTES) return GRACEKV_ERR_WORKSPACE;
   return hip_status(launch_decode_noalloc(dm, q, offsets, K_out, V_out, logm_out, K, V, out, (hipStream_t)stream));
+}
+
+// ---- attention over prompts and pages ----
+static bool heads_ok(int dtype, int G, int H, int n_seq) {
+  return (dtype == GRACEKV_F32 || dtype == GRACEKV_BF16) && G >= 1 && H >= 1 && H % G == 0 && n_seq >= 1;
+}
+// a stride: rows stay 16-byte aligned and go upwards
+static bool stride_ok(int dtype, int64_t s) { return s >= 0 && s % (dtype == GRACEKV_BF16 ? 8 : 4) == 0; }
+
+static gracekv_status prompt_dims(const gracekv_prompt_config* c, PromptDims* pd) {
+  if (!c) return GRACEKV_ERR_INVALID_ARG;
+  if (!heads_ok(c->dtype, c->G, c->H, c->n_seq) || c->reserved != 0) return GRACEKV_ERR_INVALID_ARG;
+  if (c->n_q < 0 || c->n_k < 0 || c->n_q > 0x7fffffff || c->n_k > 0x7fffffff) return GRACEKV_ERR_INVALID_ARG;
+  for (int64_t s : {c->q_tok, c->q_head, c->k_tok, c->k_head, c->v_tok, c->v_head, c->out_tok, c->out_head})
+    if (!stride_ok(c->dtype, s)) return GRACEKV_ERR_INVALID_ARG;
+  if ((c->out_tok == 0 && c->n_q > 1) || (c->out_head == 0 && c->H > 1)) return GRACEKV_ERR_INVALID_ARG;   // rows on rows
+  if (c->d != 64 && c->d != 128) return GRACEKV_ERR_UNSUPPORTED;
+  *pd = PromptDims{c->dtype, c->G, c->H, c->d, c->H / c->G, c->n_seq, c->n_q, c->n_k, c->q_tok, c->q_head,
+                   c->k_tok, c->k_head, c->v_tok, c->v_head, c->out_tok, c->out_head};
+  if (prompt_items(*pd) > 0x7fffffff || c->H > 65535 * 8) return GRACEKV_ERR_UNSUPPORTED;   // one launch
+  return GRACEKV_OK;
+}
+
+gracekv_status gracekv_prompt_ws_bytes(const gracekv_prompt_config* c, size_t* ws_bytes) {
+  PromptDims pd;
+  const gracekv_status s = prompt_dims(c, &pd);
+  if (s != GRACEKV_OK) return s;
+  if (!ws_bytes) return GRACEKV_ERR_INVALID_ARG;
+  *ws_bytes = prompt_ws_bytes(pd);
+  return GRACEKV_OK;
+}
+
+gracekv_status gracekv_prompt_attention(const gracekv_prompt_config* c, const void* Q, const void* K, const void* V,
+                                        const int32_t* cu_q, const int32_t* cu_k, void* out, float* lse, void* ws,
+                                        size_t ws_bytes, void* stream) {
+  PromptDims pd;
+  const gracekv_status s = prompt_dims(c, &pd);
+  if (s != GRACEKV_OK) return s;
+  if (!cu_q || !cu_k || (c->n_q > 0 && (!Q || !out)) || (c->n_k > 0 && (!K || !V))) return GRACEKV_ERR_INVALID_ARG;
+  if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(out)) return GRACEKV_ERR_INVALID_ARG;
+  const size_t need = prompt_ws_bytes(pd);
+  if (need && (!ws || !aligned16(ws))) return GRACEKV_ERR_INVALID_ARG;
+  if (ws_bytes < need) return GRACEKV_ERR_WORKSPACE;
+  return hip_status(launch_prompt(pd, Q, K, V, cu_q, cu_k, out, lse, ws, (hipStream_t)stream));
+}
+
+static gracekv_status page_dims(const gracekv_page_config* c, PageDims* pg) {
+  if (!c) return GRACEKV_ERR_INVALID_ARG;
+  if (!heads_ok(c->dtype, c->G, c->H, c->n_seq) || c->reserved != 0) return GRACEKV_ERR_INVALID_ARG;
+  if (c->table_width < 1 || c->n_pages < 1) return GRACEKV_ERR_INVALID_ARG;
+  if (c->d != 64 && c->d != 128) return GRACEKV_ERR_UNSUPPORTED;
+  int shift = 4;
+  while (shift < 9 && (1 << shift) != c->page_size) ++shift;
+  if (shift == 9) return GRACEKV_ERR_UNSUPPORTED;
+  const int64_t page = (int64_t)c->G * c->page_size * c->d;
+  if (c->page_stride < page || !stride_ok(c->dtype, c->page_stride) || c->n_pages > INT64_MAX / 4 / c->page_stride)
+    return GRACEKV_ERR_INVALID_ARG;
+  *pg = PageDims{c->dtype, c->G, c->H, c->d, c->H / c->G, c->n_seq, shift, c->table_width, c->n_pages, c->page_stride};
+  // one launch: rows (sequence, KV head) in x, query heads in y; lengths are int32
+  if ((int64_t)c->n_seq * c->G > (1 << 24) || c->H > 65535 || ((int64_t)c->table_width << shift) > 0x7fffffff)
+    return GRACEKV_ERR_UNSUPPORTED;
+  return GRACEKV_OK;
+}
+
+gracekv_status gracekv_cache_append(const gracekv_page_config* c, const gracekv_append_config* r, const void* k,
+                                    const void* v, const void* q, const int32_t* block_table, const int32_t* start,
+                                    const int32_t* cu_new, const int32_t* pos, const float* rope_cos,
+                                    const float* rope_sin, void* K_pages, void* V_pages, void* q_out, void* stream) {
+  PageDims pg;
+  const gracekv_status s = page_dims(c, &pg);
+  if (s != GRACEKV_OK) return s;
+  if (!r || (r->n_new > 0 && (!k || !v)) || !block_table || !start || !cu_new || !K_pages || !V_pages) return GRACEKV_ERR_INVALID_ARG;
+  if (!q != !q_out) return GRACEKV_ERR_INVALID_ARG;
+  if (!pos != !rope_cos || !pos != !rope_sin) return GRACEKV_ERR_INVALID_ARG;
+  if (!aligned16(k) || !aligned16(v) || !aligned16(q) || !aligned16(K_pages) || !aligned16(V_pages) || !aligned16(q_out) ||
+      !aligned16(rope_cos) || !aligned16(rope_sin))
+    return GRACEKV_ERR_INVALID_ARG;
+  if (r->n_new < 0 || r->n_new > 0x7fffffff || r->rope_rows < 0) return GRACEKV_ERR_INVALID_ARG;
+  for (int64_t x : {r->k_tok, r->k_head, r->v_tok, r->v_head, r->q_tok, r->q_head, r->qout_tok, r->qout_head})
+    if (!stride_ok(c->dtype, x)) return GRACEKV_ERR_INVALID_ARG;
+  if (q && ((r->qout_tok == 0 && r->n_new > 1) || (r->qout_head == 0 && c->H > 1))) return GRACEKV_ERR_INVALID_ARG;
+  const AppendDims ap{r->n_new, r->rope_rows, r->k_tok, r->k_head, r->v_tok, r->v_head, r->q_tok, r->q_head, r->qout_tok, r->qout_head};
+  return hip_status(launch_append(pg, ap, k, v, q, block_table, start, cu_new, pos, rope_cos, rope_sin, K_pages, V_pages, q_out,
+                                  (hipStream_t)stream));
+}
+
+gracekv_status gracekv_paged_ws_bytes(const gracekv_page_config* c, size_t* ws_bytes) {
+  PageDims pg;
+  const gracekv_status s = page_dims(c, &pg);
+  if (s != GRACEKV_OK) return s;
+  if (!ws_bytes) return GRACEKV_ERR_INVALID_ARG;
+  *ws_bytes = paged_ws_bytes(pg);
+  return GRACEKV_OK;
+}
+
+gracekv_status gracekv_paged_attention(const gracekv_page_config* c, const void* q, int64_t q_tok, const void* K_pages,
+                                       const void* V_pages, const int32_t* block_table, const int32_t* seq_len,
+                                       const gracekv_prefix* prefix, void* out, float* lse, void* ws, size_t ws_bytes,
+                                       void* stream) {
+  PageDims pg;
+  const gracekv_status s = page_dims(c, &pg);
+  if (s != GRACEKV_OK) return s;
+  if (!q || !K_pages || !V_pages || !block_table || !seq_len || !out || !ws) return GRACEKV_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(K_pages) || !aligned16(V_pages) || !aligned16(out) || !aligned16(ws))
+    return GRACEKV_ERR_INVALID_ARG;
+  if (!stride_ok(c->dtype, q_tok)) return GRACEKV_ERR_INVALID_ARG;
+  PrefixView px{nullptr, nullptr, nullptr, nullptr, nullptr, 0};
+  if (prefix) {
+    if (!prefix->start || !prefix->count || !prefix->K || !prefix->V || !prefix->logm || !aligned16(prefix->K) ||
+        !aligned16(prefix->V) || prefix->rows < 0 || prefix->rows > (int64_t)1 << 34)
+      return GRACEKV_ERR_INVALID_ARG;
+    px = PrefixView{prefix->start, prefix->count, prefix->K, prefix->V, prefix->logm, prefix->rows};
+  }
+  if (ws_bytes < paged_ws_bytes(pg)) return GRACEKV_ERR_WORKSPACE;
+  return hip_status(launch_paged(pg, q_tok, q, K_pages, V_pages, block_table, seq_len, px, out, lse, ws, (hipStream_t)stream));
 }
 
 gracekv_status gracekv_selftest_mfma(int32_t which, float* out, void* stream) {

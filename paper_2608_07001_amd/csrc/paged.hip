@@ -1,0 +1,473 @@
+// Attention of one new token of every sequence over its pages, and over the packed
+// entries of its compressed context in front of them.
+//
+// For sequence b and query head h (KV head g = h / hpg) the entries are
+//   (a) rows [start, start + count) of the packed arrays (b, g), logits q.k / sqrt(d) + log m
+//   (b) the first len[b] tokens of its pages, logits q.k / sqrt(d)
+// and out = sum e^x v / sum e^x, lse = log sum e^x; no entry: 0 and -inf.
+//
+// The work is a stream over keys and values, each read once for all query heads of its
+// group: bound by HBM.  Sequences differ in length, and how long they are is known on
+// the device only, so the split is made there: every row (b, g) is cut into tiles of 16
+// or 32 entries, a chunk is so many tiles that the chunks of all rows fill the grid
+// once, and workgroup w finds its chunk by a scan over the rows' lengths.  A row of one
+// chunk is finished by its workgroup; the others leave a partial state each, merged by
+// k_paged_combine.
+//
+// A wave takes whole tiles.  Logits are formed transposed, S^T = K Q^T (entries x heads,
+// 16x16 matrix tiles, heads past the group's zero), keys straight from memory as the
+// product's operand.  A lane then holds four entries of one head, which is the operand
+// layout of the second product O^T = V^T P^T: probabilities never cross lanes.  V^T needs
+// the same four entries of one dimension; a lane loads those entries' rows (16 bytes
+// each) and pairs the halves up in registers, row i of product j being dimension 8 i + j.
+// No LDS before the waves are merged.  For bf16 the probabilities are rounded to bf16
+// (nearest even) as the second product's operand, while their sum takes them unrounded:
+// each weight is off by at most 2^-9 of itself, at random, like the output's own rounding.
+// fp32 caches use the fp32 matrix instructions.
+#include "serve.h"
+
+namespace gkv {
+
+constexpr int PA_T = 256;
+constexpr int PA_W = PA_T / 64;
+constexpr int PA_HEADS = 16;       // query heads of a workgroup
+constexpr int PA_MIN = PA_W;       // tiles of the shortest chunk: one a wave
+constexpr int PA_TARGET = 1024;    // chunks that the rows are cut into (beside one a row)
+
+static size_t al256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// workspace: per row (first chunk, chunks), then per chunk and head (max, sum), then the
+// partial outputs [chunk][hpg][d]
+struct PagedWs {
+  int2* rows;
+  float2* ml;
+  float* o;
+  size_t bytes;
+};
+static PagedWs paged_view(void* base, const PageDims& pg) {
+  const size_t R = (size_t)pg.n_seq * pg.G, chunks = R + PA_TARGET;
+  char* p = (char*)base;
+  PagedWs w;
+  size_t o = 0;
+  w.rows = (int2*)(p + o);
+  o += al256(R * 8);
+  w.ml = (float2*)(p + o);
+  o += al256(chunks * pg.hpg * 8);
+  w.o = (float*)(p + o);
+  o += chunks * pg.hpg * pg.d * 4;
+  w.bytes = o;
+  return w;
+}
+size_t paged_ws_bytes(const PageDims& pg) { return paged_view(nullptr, pg).bytes; }
+
+// inclusive sum over the workgroup's threads; `total`: of all of them
+__device__ __forceinline__ int64_t scan_block(int64_t v, int64_t* sh, int64_t& total) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t u = __shfl_up(v, o, 64);
+    if (lane >= o) v += u;
+  }
+  sync_after_lds_stores();
+  if (lane == 63) sh[w] = v;
+  sync_after_lds_stores();
+  int64_t before = 0;
+  total = 0;
+#pragma unroll
+  for (int i = 0; i < PA_W; ++i) {
+    if (i < w) before += sh[i];
+    total += sh[i];
+  }
+  return v + before;
+}
+
+// What a workgroup works on: tiles [t0, t1) of row (b, g); chunk `c` of `chunks`.
+struct Chunk {
+  int b, g, c, chunks, t0, t1;
+};
+
+template <int TILE>
+__device__ __forceinline__ int64_t tiles_of(const PageDims& pg, int64_t len, int64_t count) {
+  const int64_t t = (len + TILE - 1) / TILE + (count + TILE - 1) / TILE;
+  return t > 0 ? t : 1;              // an empty row has a chunk, which writes its zeros
+}
+__device__ __forceinline__ int64_t held_count(const PrefixView& px, int64_t row, int64_t& start) {
+  int64_t s = px.start[row], c = px.count[row];
+  s = s < 0 ? 0 : (s > px.rows ? px.rows : s);
+  c = c < 0 ? 0 : (c > px.rows - s ? px.rows - s : c);
+  start = s;
+  return c;
+}
+
+// The chunk of workgroup blockIdx.x; false past the last.  Rows are looked at as units:
+// (b, g) where a prefix makes their lengths differ, b (G equal rows) otherwise.
+template <int TILE, bool PREFIX>
+__device__ __forceinline__ bool find_chunk(const PageDims& pg, const PrefixView& px, const int32_t* len, Chunk& out) {
+  __shared__ int64_t sh[PA_W];
+  __shared__ int64_t found[3];
+  const int tid = threadIdx.x;
+  const int units = PREFIX ? pg.n_seq * pg.G : pg.n_seq, mult = PREFIX ? 1 : pg.G;
+  auto tiles = [&](int u) -> int64_t {
+    int64_t s = 0;
+    return tiles_of<TILE>(pg, held_len(pg, len[PREFIX ? u / pg.G : u]), PREFIX ? held_count(px, u, s) : 0);
+  };
+  int64_t mine = 0, total;
+  for (int u = tid; u < units; u += PA_T) mine += tiles(u);
+  scan_block(mine, sh, total);
+  total *= mult;
+  const int64_t room = gridDim.x - (int64_t)pg.n_seq * pg.G;      // every row may leave one chunk unfilled
+  int64_t size = (total + room - 1) / room;
+  if (size < PA_MIN) size = PA_MIN;
+  if (tid == 0) found[0] = -1;
+  int64_t base = 0;
+  for (int u0 = 0; u0 < units; u0 += PA_T) {
+    const int u = u0 + tid;
+    const int64_t n = u < units ? tiles(u) : 0, c = (n + size - 1) / size;
+    const int64_t to = base + scan_block(c * mult, sh, total), from = to - c * mult;
+    if (u < units && (int64_t)blockIdx.x >= from && (int64_t)blockIdx.x < to) {
+      found[0] = u;
+      found[1] = blockIdx.x - from;
+      found[2] = n;
+    }
+    base += total;
+    if ((int64_t)blockIdx.x < base) break;
+  }
+  sync_after_lds_stores();
+  // one value for the workgroup: kept in scalar registers
+  const int u = __builtin_amdgcn_readfirstlane((int)found[0]);
+  if (u < 0) return false;
+  const int local = __builtin_amdgcn_readfirstlane((int)found[1]), n = __builtin_amdgcn_readfirstlane((int)found[2]);
+  const int chunks = __builtin_amdgcn_readfirstlane((int)((n + size - 1) / size));
+  out.b = PREFIX ? u / pg.G : u;
+  out.g = PREFIX ? u % pg.G : local / chunks;
+  out.c = PREFIX ? local : local % chunks;
+  out.chunks = chunks;
+  out.t0 = (int)((int64_t)n * out.c / chunks);
+  out.t1 = (int)((int64_t)n * (out.c + 1) / chunks);
+  return true;
+}
+
+template <typename T, int D, int NS, bool PREFIX>
+__global__ __launch_bounds__(PA_T, 2) void k_paged(PageDims pg, int64_t q_tok, const T* __restrict__ q,
+                                                   const T* __restrict__ Kp, const T* __restrict__ Vp,
+                                                   const int32_t* __restrict__ table, const int32_t* __restrict__ len,
+                                                   PrefixView px, T* __restrict__ out, float* __restrict__ lse, PagedWs ws) {
+  constexpr bool BF = sizeof(T) == 2;
+  constexpr int TILE = 16 * NS;
+  constexpr int E = 16 / (int)sizeof(T);      // elements of 16 bytes
+  constexpr int KC = D / 4 / E;               // 16-byte pieces of a lane's quarter of a key
+  constexpr int VD = BF ? D / 16 : 4;         // neighbouring dims of a lane
+  constexpr int VB = BF ? 1 : D / 64;         // ... in so many places of the row
+  constexpr int VW = VD * (int)sizeof(T) / 4; // words of one place
+  __shared__ float sM[PA_W][PA_HEADS], sL[PA_W][PA_HEADS];
+  __shared__ float sO[PA_W][PA_HEADS][D];
+  Chunk ck;
+  if (!find_chunk<TILE, PREFIX>(pg, px, len, ck)) return;
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i16 = lane & 15, g4 = lane >> 4;
+  const int h0 = blockIdx.y * PA_HEADS, heads = min(PA_HEADS, pg.hpg - h0);
+  const int64_t row = (int64_t)ck.b * pg.G + ck.g;
+  const int64_t n_page = held_len(pg, len[ck.b]);
+  int64_t p_start = 0, n_pack = 0;
+  if constexpr (PREFIX) n_pack = held_count(px, row, p_start);
+  const int pack_tiles = (int)((n_pack + TILE - 1) / TILE);
+  const T* PK = (const T*)px.K;
+  const T* PV = (const T*)px.V;
+  constexpr float LOG2E = 1.44269504088896341f;
+  const float scale = 1.0f / sqrtf((float)D);
+
+  // the group's queries: lane (head i16, quarter g4) holds pieces g4, g4 + 4, ... of the row
+  uint4 qv[KC];
+#pragma unroll
+  for (int s = 0; s < KC; ++s)
+    qv[s] = i16 < heads ? *(const uint4*)(q + ck.b * q_tok + ((int64_t)ck.g * pg.hpg + h0 + i16) * D + (4 * s + g4) * E)
+                        : make_uint4(0, 0, 0, 0);
+
+  struct Tile {
+    uint4 k[NS][KC];
+    uint32_t v[NS][4][VB][VW];
+    float lm[NS][4];              // log m; -inf: no weight (absent, or masked by its log m)
+    bool all;                     // every entry there with log m = 0
+  };
+  const int32_t* tab = table + (int64_t)ck.b * pg.width;
+  auto fetch = [&](Tile& t, int ti) {
+    const bool packed = PREFIX && ti < pack_tiles;
+    t.all = !packed;
+#pragma unroll
+    for (int h = 0; h < NS; ++h) {
+      const int64_t e = (int64_t)(packed ? ti : ti - pack_tiles) * TILE + 16 * h;
+      int64_t left = (packed ? n_pack : n_page) - e, at = 0;
+      if (!packed && left > 0) {
+        at = page_row(pg, tab[e >> pg.shift], ck.g, (int)(e & (((int64_t)1 << pg.shift) - 1)));
+        if (at < 0) left = 0;
+      } else if (packed) {
+        at = (p_start + e) * D;
+      }
+      const int n = left > 16 ? 16 : (left < 0 ? 0 : (int)left);
+      t.all &= n == 16;
+      const T* kb = (packed ? PK : Kp) + at;
+      const T* vb = (packed ? PV : Vp) + at;
+      if (n > 0) {                // absent entries read the last one there
+        const T* kr = kb + (int64_t)min(i16, n - 1) * D;
+#pragma unroll
+        for (int s = 0; s < KC; ++s) t.k[h][s] = *(const uint4*)(kr + (4 * s + g4) * E);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const T* vr = vb + (int64_t)min(4 * g4 + r, n - 1) * D;
+#pragma unroll
+          for (int p = 0; p < VB; ++p) {
+            const uint32_t* x = (const uint32_t*)(vr + 64 * p + VD * i16);
+            if constexpr (VW == 4) {
+              const uint4 u = *(const uint4*)x;
+              t.v[h][r][p][0] = u.x; t.v[h][r][p][1] = u.y; t.v[h][r][p][2] = u.z; t.v[h][r][p][3] = u.w;
+            } else {
+              const uint2 u = *(const uint2*)x;
+              t.v[h][r][p][0] = u.x; t.v[h][r][p][1] = u.y;
+            }
+          }
+        }
+      } else {
+#pragma unroll
+        for (int s = 0; s < KC; ++s) t.k[h][s] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int p = 0; p < VB; ++p)
+#pragma unroll
+            for (int x = 0; x < VW; ++x) t.v[h][r][p][x] = 0;
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int i = 4 * g4 + r;
+        t.lm[h][r] = i >= n ? -INFINITY : (packed ? px.logm[p_start + e + i] : 0.f);
+      }
+    }
+  };
+
+  f32x4 o[VB][VD];
+#pragma unroll
+  for (int p = 0; p < VB; ++p)
+#pragma unroll
+    for (int j = 0; j < VD; ++j) o[p][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;               // of head i16; l: this lane's entries only
+
+  auto fold = [&](Tile& t) {
+    float x[NS][4];
+#pragma unroll
+    for (int h = 0; h < NS; ++h) {
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < KC; ++s) {
+        if constexpr (BF) {
+          acc = mfma_bf16_16x16x32(pk8(t.k[h][s]), pk8(qv[s]), acc);
+        } else {
+          const uint32_t a[4] = {t.k[h][s].x, t.k[h][s].y, t.k[h][s].z, t.k[h][s].w};
+          const uint32_t b[4] = {qv[s].x, qv[s].y, qv[s].z, qv[s].w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc = mfma_f32_16x16x4(__uint_as_float(a[i]), __uint_as_float(b[i]), acc);
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[h][r] = acc[r] * scale;
+    }
+    if (!t.all) {
+#pragma unroll
+      for (int h = 0; h < NS; ++h)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const bool none = t.lm[h][r] == -INFINITY;
+          x[h][r] = none ? -INFINITY : x[h][r] + t.lm[h][r];
+          if (none) {             // 0 times an infinity is not 0
+#pragma unroll
+            for (int p = 0; p < VB; ++p)
+#pragma unroll
+              for (int i = 0; i < VW; ++i) t.v[h][r][p][i] = 0;
+          }
+        }
+    }
+    float mx = x[0][0];
+#pragma unroll
+    for (int h = 0; h < NS; ++h)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) mx = fmaxf(mx, x[h][r]);
+    {
+      const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+      mx = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+      const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+      mx = fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+    }
+    if (__any(mx > m)) {
+      const float mn = fmaxf(m, mx);
+      const float c = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - mn) * LOG2E);
+      m = mn;
+      l *= c;
+#pragma unroll
+      for (int p = 0; p < VB; ++p)
+#pragma unroll
+        for (int j = 0; j < VD; ++j) o[p][j] *= c;
+    }
+    const float ms = m == -INFINITY ? 0.f : m;
+    float pr[NS][4];
+#pragma unroll
+    for (int h = 0; h < NS; ++h)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        pr[h][r] = __builtin_amdgcn_exp2f((x[h][r] - ms) * LOG2E);
+        l += pr[h][r];
+      }
+    if constexpr (BF) {
+      static_assert(!BF || NS == 2, "two tiles of 16 make one product of 32");
+      const s16x8 pb = pk8(make_uint4(pack_bf16(pr[0][0], pr[0][1]), pack_bf16(pr[0][2], pr[0][3]),
+                                      pack_bf16(pr[1][0], pr[1][1]), pack_bf16(pr[1][2], pr[1][3])));
+#pragma unroll
+      for (int j = 0; j < VD; ++j) {
+        const uint32_t sel = (j & 1) ? 0x07060302u : 0x05040100u;
+        uint32_t a[4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int r = 0; r < 2; ++r)
+            a[2 * h + r] = __builtin_amdgcn_perm(t.v[h][2 * r + 1][0][j / 2], t.v[h][2 * r][0][j / 2], sel);
+        o[0][j] = mfma_bf16_16x16x32(pk8(make_uint4(a[0], a[1], a[2], a[3])), pb, o[0][j]);
+      }
+    } else {
+#pragma unroll
+      for (int h = 0; h < NS; ++h)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int p = 0; p < VB; ++p)
+#pragma unroll
+            for (int j = 0; j < VD; ++j)
+              o[p][j] = mfma_f32_16x16x4(__uint_as_float(t.v[h][r][p][j]), pr[h][r], o[p][j]);
+    }
+  };
+
+  // the next tile in flight while one is folded in; two places that take turns
+  Tile ta, tb;
+  int ti = ck.t0 + w;
+  if (ti < ck.t1) fetch(ta, ti);
+  while (ti < ck.t1) {
+    if (ti + PA_W < ck.t1) fetch(tb, ti + PA_W);
+    fold(ta);
+    ti += PA_W;
+    if (ti >= ck.t1) break;
+    if (ti + PA_W < ck.t1) fetch(ta, ti + PA_W);
+    fold(tb);
+    ti += PA_W;
+  }
+#pragma unroll
+  for (int p = 0; p < VB; ++p)
+#pragma unroll
+    for (int j = 0; j < VD; ++j) mfma_done(o[p][j]);
+  l = col_sum4(l);
+  // row 4 g4 + r of product (p, j) is dimension 64 p + VD (4 g4 + r) + j, column i16 the head
+  if (g4 == 0) { sM[w][i16] = m; sL[w][i16] = l; }
+#pragma unroll
+  for (int p = 0; p < VB; ++p)
+#pragma unroll
+    for (int j = 0; j < VD; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sO[w][i16][64 * p + VD * (4 * g4 + r) + j] = o[p][j][r];
+  sync_after_lds_stores();
+  const bool whole = ck.chunks == 1;
+  if (tid == 0 && ck.c == 0 && blockIdx.y == 0) ws.rows[row] = make_int2((int)blockIdx.x, ck.chunks);
+  for (int i = tid; i < heads * D; i += PA_T) {
+    const int h = i / D, dd = i % D;
+    float M = -INFINITY;
+#pragma unroll
+    for (int x = 0; x < PA_W; ++x) M = fmaxf(M, sM[x][h]);
+    float S = 0.f, O = 0.f;
+#pragma unroll
+    for (int x = 0; x < PA_W; ++x) {
+      const float c = sM[x][h] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((sM[x][h] - M) * LOG2E);
+      S += sL[x][h] * c;
+      O += c == 0.f ? 0.f : sO[x][h][dd] * c;
+    }
+    const int64_t hd = (int64_t)ck.g * pg.hpg + h0 + h;
+    if (whole) {
+      stf(out, ((int64_t)ck.b * pg.H + hd) * D + dd, S > 0.f ? O / S : S);     // nothing: 0; NaN stays
+      if (lse && dd == 0) lse[(int64_t)ck.b * pg.H + hd] = M + logf(S);
+    } else {
+      const int64_t part = (int64_t)blockIdx.x * pg.hpg + h0 + h;
+      ws.o[part * D + dd] = O;
+      if (dd == 0) ws.ml[part] = make_float2(M, S);
+    }
+  }
+}
+
+// One workgroup per (row, head): the chunks' states, D lanes over the dims and the rest
+// over the chunks.
+template <typename T, int D>
+__global__ __launch_bounds__(PA_T) void k_paged_combine(PageDims pg, PagedWs ws, T* __restrict__ out, float* __restrict__ lse) {
+  constexpr int GR = PA_T / D;
+  constexpr float LOG2E = 1.44269504088896341f;
+  __shared__ float sS[GR], sO[GR][D], sW[PA_W];
+  const int64_t row = blockIdx.x;
+  const int h = blockIdx.y, tid = threadIdx.x, gr = tid / D, dd = tid % D;
+  const int2 ch = ws.rows[row];
+  if (ch.y <= 1) return;
+  const int64_t base = (int64_t)ch.x * pg.hpg + h;
+  float M = -INFINITY;
+  for (int c = tid; c < ch.y; c += PA_T) M = fmaxf(M, ws.ml[base + (int64_t)c * pg.hpg].x);
+  M = wave_max(M);
+  if ((tid & 63) == 0) sW[tid >> 6] = M;
+  sync_after_lds_stores();
+#pragma unroll
+  for (int x = 0; x < PA_W; ++x) M = fmaxf(M, sW[x]);
+  float S = 0.f, O = 0.f;
+#pragma unroll 4
+  for (int c = gr; c < ch.y; c += GR) {
+    const int64_t part = base + (int64_t)c * pg.hpg;
+    const float2 ml = ws.ml[part];
+    const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ml.x - M) * LOG2E);
+    const float ov = ws.o[part * D + dd];
+    S += ml.y * f;
+    O += f == 0.f ? 0.f : ov * f;
+  }
+  sO[gr][dd] = O;
+  if (dd == 0) sS[gr] = S;
+  sync_after_lds_stores();
+  if (gr == 0) {
+#pragma unroll
+    for (int x = 1; x < GR; ++x) {
+      S += sS[x];
+      O += sO[x][dd];
+    }
+    const int64_t b = row / pg.G, hd = (row % pg.G) * pg.hpg + h;
+    stf(out, (b * pg.H + hd) * D + dd, S > 0.f ? O / S : S);
+    if (lse && dd == 0) lse[b * pg.H + hd] = M + logf(S);
+  }
+}
+
+hipError_t launch_paged(const PageDims& pg, int64_t q_tok, const void* q, const void* Kp, const void* Vp,
+                        const int32_t* table, const int32_t* len, const PrefixView& px, void* out, float* lse, void* ws,
+                        hipStream_t st) {
+  const PagedWs v = paged_view(ws, pg);
+  const int64_t R = (int64_t)pg.n_seq * pg.G;
+  auto go = [&](auto type, auto dim, auto sub) {
+    using T = decltype(type);
+    constexpr int D = decltype(dim)::value, NS = decltype(sub)::value;
+    // chunks that the longest rows could make: no larger grid than that
+    const int64_t tiles = R * ((((int64_t)pg.width << pg.shift) + 16 * NS - 1) / (16 * NS)) + (px.K ? px.rows / (16 * NS) + R : 0);
+    const int64_t most = (tiles + PA_MIN - 1) / PA_MIN;
+    const dim3 grid((unsigned)(R + (most < PA_TARGET ? (most > 0 ? most : 1) : PA_TARGET)), (unsigned)((pg.hpg + PA_HEADS - 1) / PA_HEADS));
+    if (px.K)
+      hipLaunchKernelGGL((k_paged<T, D, NS, true>), grid, dim3(PA_T), 0, st, pg, q_tok, (const T*)q, (const T*)Kp, (const T*)Vp, table,
+                         len, px, (T*)out, lse, v);
+    else
+      hipLaunchKernelGGL((k_paged<T, D, NS, false>), grid, dim3(PA_T), 0, st, pg, q_tok, (const T*)q, (const T*)Kp, (const T*)Vp, table,
+                         len, px, (T*)out, lse, v);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((k_paged_combine<T, D>), dim3((unsigned)R, (unsigned)pg.hpg), dim3(PA_T), 0, st, pg, v, (T*)out, lse);
+    return hipGetLastError();
+  };
+  using std::integral_constant;
+  if (pg.dtype == GRACEKV_BF16)
+    return pg.d == 128 ? go(uint16_t{}, integral_constant<int, 128>{}, integral_constant<int, 2>{})
+                       : go(uint16_t{}, integral_constant<int, 64>{}, integral_constant<int, 2>{});
+  return pg.d == 128 ? go(float{}, integral_constant<int, 128>{}, integral_constant<int, 1>{})
+                     : go(float{}, integral_constant<int, 64>{}, integral_constant<int, 2>{});
+}
+
+}  // namespace gkv

@@ -1,0 +1,547 @@
+// Causal attention over packed prompts with grouped query heads.
+//
+// Sequence b has query rows [cu_q[b], cu_q[b+1]) and key rows [cu_k[b], cu_k[b+1]); its
+// last query stands at its last key, so query i sees the keys j <= i + Lk - Lq:
+//   out_i = sum_j softmax_j(q_i.k_j / sqrt(d)) v_j,  lse_i = log sum_j exp(q_i.k_j / sqrt(d))
+// (no key: 0 and -inf).
+//
+// The query heads of a group share their keys, so the rows of a tile are (token, head)
+// pairs, row r = token * hpg + head: any grouping fills the tile, keys and values are
+// loaded once for the group, and the tile spans few tokens, which leaves little work
+// above the diagonal.
+//
+// One pass over the keys with a running maximum and sum.  Products are formed transposed:
+// S^T = K Q^T (keys x rows), then O^T = V^T P^T, because the accumulator of the first
+// holds four neighbouring keys of one row per lane, which (the order of the keys inside a
+// product is free) is the operand of the second: probabilities stay in their lane, and
+// the row's maximum, sum and rescaling are lane-local but for one swap of halves.  Keys
+// and values go through LDS, V^T by the transposing LDS read.
+//
+// A tile that some row of the workgroup sees in part (its diagonal, its end) is staged
+// with values that are not finite replaced by 0, since 0 times an infinity is not 0; rows
+// that do see such a value get it at the end (poison()).
+//
+// bf16 probabilities are rounded to bf16 (nearest even) as operands, their sum takes them
+// unrounded: each weight is off by at most 2^-9 of itself, at random, like the output's
+// own rounding.  fp32 uses the fp32 matrix instructions.
+#include "serve.h"
+
+namespace gkv {
+
+constexpr int PR_T = 256;
+constexpr int PR_W = PR_T / 64;
+constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+__device__ __forceinline__ f32x16 mfma_bf16_32x32x16(uint4 a, uint4 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// the stated wait for the matrix pipeline (mfma_done) for these accumulators
+__device__ __forceinline__ void mfma_done16(f32x16& x) { asm volatile("s_nop 15\n\ts_nop 4" : "+v"(x)); }
+__device__ __forceinline__ void mfma_done16(f32x16& x, f32x16& y) { asm volatile("s_nop 15\n\ts_nop 4" : "+v"(x), "+v"(y)); }
+
+static size_t al256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+template <bool BF> constexpr int tile_rows() { return BF ? 32 * PR_W : 16 * PR_W; }
+template <bool BF> constexpr int tile_keys() { return BF ? 64 : 32; }
+
+// row tiles of all sequences: sequence b's begin at cu_q[b] * hpg / rows + b, which
+// leaves each at least as many as it needs whatever the lengths are
+static int64_t row_tiles(const PromptDims& pd, int rows) { return pd.n_q * pd.hpg / rows + pd.n_seq; }
+
+// Parts that every row tile's keys are cut into: one where the tiles fill the chip twice
+// over, more where they are few, each part holding at least 256 keys of the longest row.
+static int prompt_parts(const PromptDims& pd) {
+  const int rows = pd.dtype == GRACEKV_BF16 ? tile_rows<true>() : tile_rows<false>();
+  const int64_t tiles = row_tiles(pd, rows) * pd.G;
+  const int64_t want = (512 + tiles - 1) / tiles, most = (pd.n_k + 255) / 256;
+  return (int)(want < 1 ? 1 : (want > most ? (most < 1 ? 1 : most) : want));
+}
+int64_t prompt_items(const PromptDims& pd) {
+  return row_tiles(pd, pd.dtype == GRACEKV_BF16 ? tile_rows<true>() : tile_rows<false>()) * prompt_parts(pd) * pd.G;
+}
+size_t prompt_ws_bytes(const PromptDims& pd) {
+  const int P = prompt_parts(pd);
+  if (P == 1) return 0;
+  const size_t n = (size_t)P * pd.n_q * pd.H;
+  return al256(n * 8) + n * pd.d * 4;
+}
+
+// what a workgroup works on
+struct Item {
+  int b, g, part;
+  int64_t q0, lq, k0, lk;      // the sequence's rows
+  int64_t r0, rows;            // first (token, head) row of the tile; rows of the sequence
+  int t0, t1;                  // key tiles [t0, t1)
+};
+
+// The item of workgroup blockIdx.x; false where there is none.  Pairs of one KV head and
+// part are neighbours modulo G, so with G a multiple of 8 a KV head stays on one XCD's
+// L2; the tiles with the most keys come first.
+template <int ROWS, int KEYS>
+__device__ __forceinline__ bool find_item(const PromptDims& pd, const int32_t* cu_q, const int32_t* cu_k, int parts, Item& it) {
+  int64_t bid = blockIdx.x;
+  it.g = (int)(bid % pd.G);
+  bid /= pd.G;
+  it.part = (int)(bid % parts);
+  bid /= parts;
+  const int64_t slot = (int64_t)gridDim.x / pd.G / parts - 1 - bid;
+  auto first = [&](int b) { return span_of(cu_q, b, pd.n_q).a * pd.hpg / ROWS + b; };
+  it.b = find_last(pd.n_seq, [&](int b) { return first(b) <= slot; });
+  const Span sq = span_of(cu_q, it.b, pd.n_q), sk = span_of(cu_k, it.b, pd.n_k);
+  it.q0 = sq.a; it.lq = sq.n; it.k0 = sk.a; it.lk = sk.n;
+  it.rows = sq.n * pd.hpg;
+  it.r0 = (slot - first(it.b)) * ROWS;
+  if (it.r0 < 0 || it.r0 >= it.rows) return false;
+  // keys that the tile's last row sees
+  const int64_t last = (it.r0 + ROWS < it.rows ? it.r0 + ROWS : it.rows) - 1;
+  int64_t n = last / pd.hpg + 1 + sk.n - sq.n;
+  n = n < 0 ? 0 : n;
+  const int64_t tiles = (n + KEYS - 1) / KEYS;
+  it.t0 = (int)(tiles * it.part / parts);
+  it.t1 = (int)(tiles * (it.part + 1) / parts);
+  return true;
+}
+
+// the four 16-bit values of a lane after the transposing read: `p` is the lane's 8 bytes
+// of its group's 4 x 16 block (lanes 4 r .. 4 r + 3: row r), returned is column lane % 16
+__device__ __forceinline__ uint2 lds_read_tr(const uint16_t* p) {
+  auto q = (__attribute__((address_space(3))) s16x4*)p;
+  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(q));
+}
+
+// bf16 pairs / floats with what is not finite replaced by 0; `any` says whether there was
+__device__ __forceinline__ uint32_t finite_bf(uint32_t x, bool& any) {
+  const bool h = (x & 0x7f800000u) == 0x7f800000u, l = (x & 0x7f80u) == 0x7f80u;
+  any |= h | l;
+  return (h ? 0u : x & 0xffff0000u) | (l ? 0u : x & 0xffffu);
+}
+__device__ __forceinline__ uint32_t finite_f(uint32_t x, bool& any) {
+  const bool b = (x & 0x7f800000u) == 0x7f800000u;
+  any |= b;
+  return b ? 0u : x;
+}
+template <bool BF> __device__ __forceinline__ uint4 finite(uint4 x, bool& any) {
+  if constexpr (BF) return make_uint4(finite_bf(x.x, any), finite_bf(x.y, any), finite_bf(x.z, any), finite_bf(x.w, any));
+  else return make_uint4(finite_f(x.x, any), finite_f(x.y, any), finite_f(x.z, any), finite_f(x.w, any));
+}
+
+// place of 16-byte piece c of key row t in a staged tile: neighbouring rows start in
+// other banks, for the reads along a row (16 rows, one piece) and the transposing ones
+// (8 rows, four pieces)
+template <int D> __device__ __forceinline__ int swz(int t, int c) {
+  if constexpr (D == 128) return t * 16 + (c ^ (((t & 3) << 2) | ((t >> 2) & 3)));
+  else return t * 8 + (c ^ ((((t >> 1) & 1) << 2) | ((t >> 2) & 3)));
+}
+
+template <int D>
+__global__ __launch_bounds__(PR_T, 2) void k_prompt_bf(PromptDims pd, int parts, const uint16_t* __restrict__ q,
+                                                       const uint16_t* __restrict__ k, const uint16_t* __restrict__ v,
+                                                       const int32_t* __restrict__ cu_q, const int32_t* __restrict__ cu_k,
+                                                       uint16_t* __restrict__ out, float* __restrict__ lse,
+                                                       float2* __restrict__ pml, float* __restrict__ po) {
+  constexpr int ROWS = tile_rows<true>(), KEYS = tile_keys<true>();
+  constexpr int CH = D / 8;                     // 16-byte pieces of a row
+  constexpr int NL = KEYS * CH / PR_T;          // ... that a thread stages
+  constexpr int KS = D / 16;                    // product steps over the dims
+  constexpr int DT = D / 32;                    // 32-dim tiles of the output
+  __shared__ uint4 sK[2][KEYS * CH], sV[2][KEYS * CH];
+  __shared__ int bad;
+  Item it;
+  if (!find_item<ROWS, KEYS>(pd, cu_q, cu_k, parts, it)) return;
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i32 = lane & 31, half = lane >> 5;
+  const int64_t off = it.lk - it.lq;            // query i sees the keys up to i + off
+  // the lane's row
+  const int64_t row = it.r0 + 32 * w + i32, rowc = row < it.rows ? row : it.rows - 1;
+  const int64_t tok = rowc / pd.hpg;
+  const int head = it.g * pd.hpg + (int)(rowc % pd.hpg);
+  const int64_t see = tok + off;                // its last key
+  // what the wave's and the workgroup's rows see
+  const int64_t wr0 = it.r0 + 32 * w, wr1 = wr0 + 31;
+  const int64_t w_all = (wr0 < it.rows ? wr0 : it.rows - 1) / pd.hpg + off;
+  const int64_t w_any = wr0 < it.rows ? (wr1 < it.rows ? wr1 : it.rows - 1) / pd.hpg + off : -1;
+  const int64_t g_all = it.r0 / pd.hpg + off;
+
+  uint4 qv[KS];
+  {
+    const uint16_t* qp = q + (it.q0 + tok) * pd.q_tok + head * pd.q_head;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) qv[s] = *(const uint4*)(qp + 16 * s + 8 * half);
+  }
+  f32x16 o[DT];
+#pragma unroll
+  for (int t = 0; t < DT; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[t][r] = 0.f;
+  float m = -INFINITY, l = 0.f;                 // base-2 units; l: this lane's keys only
+  const float sc2 = LOG2E / sqrtf((float)D);
+
+  const uint16_t* kp = k + it.k0 * pd.k_tok + it.g * pd.k_head;
+  const uint16_t* vp = v + it.k0 * pd.v_tok + it.g * pd.v_head;
+  uint4 rk[NL], rv[NL];
+  auto load = [&](int t) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int e = tid + PR_T * i, c = e % CH;
+      const int64_t j = (int64_t)t * KEYS + e / CH;
+      const bool in = j < it.lk;
+      rk[i] = in ? *(const uint4*)(kp + j * pd.k_tok + 8 * c) : make_uint4(0, 0, 0, 0);
+      rv[i] = in ? *(const uint4*)(vp + j * pd.v_tok + 8 * c) : make_uint4(0, 0, 0, 0);
+    }
+  };
+  auto store = [&](int buf, int t) {
+    if ((int64_t)t * KEYS + KEYS - 1 > g_all) {
+      bool any = false;
+#pragma unroll
+      for (int i = 0; i < NL; ++i) rv[i] = finite<true>(rv[i], any);
+      if (any) bad = 1;
+    }
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int e = tid + PR_T * i;
+      sK[buf][swz<D>(e / CH, e % CH)] = rk[i];
+      sV[buf][swz<D>(e / CH, e % CH)] = rv[i];
+    }
+  };
+  if (tid == 0) bad = 0;
+  if (it.t0 < it.t1) load(it.t0);
+  sync_after_lds_stores();
+  if (it.t0 < it.t1) store(0, it.t0);
+  for (int t = it.t0; t < it.t1; ++t) {
+    const int buf = (t - it.t0) & 1;
+    sync_after_lds_stores();
+    if (t + 1 < it.t1) load(t + 1);
+    const int64_t j0 = (int64_t)t * KEYS;
+    if (j0 <= w_any) {
+      f32x16 s[2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[b][r] = 0.f;
+#pragma unroll
+        for (int x = 0; x < KS; ++x) s[b] = mfma_bf16_32x32x16(sK[buf][swz<D>(32 * b + i32, 2 * x + half)], qv[x], s[b]);
+      }
+      mfma_done16(s[0], s[1]);
+      // register r of block b: key 32 b + 8 (r / 4) + 4 half + r % 4
+      if (j0 + KEYS - 1 > w_all) {
+        const int rel = (int)(see - j0 < KEYS ? (see - j0 < -1 ? -1 : see - j0) : KEYS) - 4 * half;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (32 * b + 8 * (r / 4) + r % 4 > rel) s[b][r] = -INFINITY;
+      }
+      float mx = s[0][0];
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[b][r]);
+      {
+        const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+        mx = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1])) * sc2;
+      }
+      if (__any(mx > m)) {
+        const float mn = fmaxf(m, mx);
+        const float c = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+        m = mn;
+        l *= c;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[d] *= c;
+      }
+      const float ms = m == -INFINITY ? 0.f : m;
+      uint4 pr[4];
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float e[8];
+#pragma unroll
+          for (int r = 0; r < 8; ++r) e[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][8 * h + r], sc2, -ms));
+          l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+          pr[2 * b + h] = make_uint4(pack_bf16(e[0], e[1]), pack_bf16(e[2], e[3]), pack_bf16(e[4], e[5]), pack_bf16(e[6], e[7]));
+        }
+      const uint16_t* sv = (const uint16_t*)sV[buf];
+      // product step x: keys 16 x + 8 (j / 4) + 4 half + j % 4 in place 8 half + j
+      const int tr = 4 * half + ((lane & 15) >> 2), tc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const uint2 a = lds_read_tr(sv + 8 * swz<D>(16 * x + tr, 4 * d + tc) + 4 * (lane & 1));
+          const uint2 b = lds_read_tr(sv + 8 * swz<D>(16 * x + 8 + tr, 4 * d + tc) + 4 * (lane & 1));
+          o[d] = mfma_bf16_32x32x16(make_uint4(a.x, a.y, b.x, b.y), pr[x], o[d]);
+        }
+    }
+    if (t + 1 < it.t1) store(buf ^ 1, t + 1);
+  }
+#pragma unroll
+  for (int d = 0; d < DT; ++d) mfma_done16(o[d]);
+  sync_after_lds_stores();
+  // values that are not finite in partly seen tiles, for the rows that see them
+  if (bad) {
+    const int64_t from = (g_all + 1) / KEYS * KEYS > (int64_t)it.t0 * KEYS ? (g_all + 1) / KEYS * KEYS : (int64_t)it.t0 * KEYS;
+    const int64_t to = (int64_t)it.t1 * KEYS < it.lk ? (int64_t)it.t1 * KEYS : it.lk;
+    for (int64_t j = from > 0 ? from : 0; j < to; ++j)
+      if (j <= see) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const float x = bf16_to_f32(vp[j * pd.v_tok + 32 * d + 8 * (r / 4) + 4 * half + r % 4]);
+            if (!(fabsf(x) < INFINITY)) o[d][r] += x;
+          }
+      }
+  }
+  {
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+    l = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+  }
+  if (row >= it.rows) return;
+  const int64_t qrow = it.q0 + tok;
+  if (parts > 1) {
+    const int64_t part = ((int64_t)it.part * pd.n_q + qrow) * pd.H + head;
+    if (half == 0) pml[part] = make_float2(m, l);
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        *(float4*)(po + part * D + 32 * d + 8 * r + 4 * half) = make_float4(o[d][4 * r], o[d][4 * r + 1], o[d][4 * r + 2], o[d][4 * r + 3]);
+    return;
+  }
+  const float inv = l > 0.f ? 1.f / l : l;      // no key: the sums are 0; NaN stays
+  uint16_t* op = out + qrow * pd.o_tok + head * pd.o_head;
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      *(uint2*)(op + 32 * d + 8 * r + 4 * half) =
+          make_uint2(pack_bf16(o[d][4 * r] * inv, o[d][4 * r + 1] * inv), pack_bf16(o[d][4 * r + 2] * inv, o[d][4 * r + 3] * inv));
+  if (lse && half == 0) lse[qrow * pd.H + head] = m == -INFINITY ? logf(l) : (m + log2f(l)) * LN2;
+}
+
+// fp32: 16 rows a wave, 32 keys a tile, fp32 matrix instructions
+template <int D>
+__global__ __launch_bounds__(PR_T, 2) void k_prompt_f32(PromptDims pd, int parts, const float* __restrict__ q,
+                                                        const float* __restrict__ k, const float* __restrict__ v,
+                                                        const int32_t* __restrict__ cu_q, const int32_t* __restrict__ cu_k,
+                                                        float* __restrict__ out, float* __restrict__ lse,
+                                                        float2* __restrict__ pml, float* __restrict__ po) {
+  constexpr int ROWS = tile_rows<false>(), KEYS = tile_keys<false>();
+  constexpr int CH = D / 4, NL = KEYS * CH / PR_T, LD = D + 4;
+  constexpr int KC = D / 16, VB = D / 64;
+  __shared__ __align__(16) float sK[KEYS * LD], sV[KEYS * LD];
+  __shared__ int bad;
+  Item it;
+  if (!find_item<ROWS, KEYS>(pd, cu_q, cu_k, parts, it)) return;
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i16 = lane & 15, g4 = lane >> 4;
+  const int64_t off = it.lk - it.lq;
+  const int64_t row = it.r0 + 16 * w + i16, rowc = row < it.rows ? row : it.rows - 1;
+  const int64_t tok = rowc / pd.hpg;
+  const int head = it.g * pd.hpg + (int)(rowc % pd.hpg);
+  const int64_t see = tok + off;
+  const int64_t wr0 = it.r0 + 16 * w, wr1 = wr0 + 15;
+  const int64_t w_all = (wr0 < it.rows ? wr0 : it.rows - 1) / pd.hpg + off;
+  const int64_t w_any = wr0 < it.rows ? (wr1 < it.rows ? wr1 : it.rows - 1) / pd.hpg + off : -1;
+  const int64_t g_all = it.r0 / pd.hpg + off;
+
+  float4 qv[KC];                                // pieces g4, g4 + 4, ... of the row
+  {
+    const float* qp = q + (it.q0 + tok) * pd.q_tok + head * pd.q_head;
+#pragma unroll
+    for (int s = 0; s < KC; ++s) qv[s] = *(const float4*)(qp + 16 * s + 4 * g4);
+  }
+  f32x4 o[VB][4];
+#pragma unroll
+  for (int p = 0; p < VB; ++p)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[p][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+  const float sc2 = LOG2E / sqrtf((float)D);
+  const float* kp = k + it.k0 * pd.k_tok + it.g * pd.k_head;
+  const float* vp = v + it.k0 * pd.v_tok + it.g * pd.v_head;
+  uint4 rk[NL], rv[NL];
+  auto load = [&](int t) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int e = tid + PR_T * i, c = e % CH;
+      const int64_t j = (int64_t)t * KEYS + e / CH;
+      const bool in = j < it.lk;
+      rk[i] = in ? *(const uint4*)(kp + j * pd.k_tok + 4 * c) : make_uint4(0, 0, 0, 0);
+      rv[i] = in ? *(const uint4*)(vp + j * pd.v_tok + 4 * c) : make_uint4(0, 0, 0, 0);
+    }
+  };
+  if (tid == 0) bad = 0;
+  if (it.t0 < it.t1) load(it.t0);
+  for (int t = it.t0; t < it.t1; ++t) {
+    sync_after_lds_stores();
+    if ((int64_t)t * KEYS + KEYS - 1 > g_all) {
+      bool any = false;
+#pragma unroll
+      for (int i = 0; i < NL; ++i) rv[i] = finite<false>(rv[i], any);
+      if (any) bad = 1;
+    }
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int e = tid + PR_T * i;
+      *(uint4*)(sK + e / CH * LD + 4 * (e % CH)) = rk[i];
+      *(uint4*)(sV + e / CH * LD + 4 * (e % CH)) = rv[i];
+    }
+    if (t + 1 < it.t1) load(t + 1);
+    sync_after_lds_stores();
+    const int64_t j0 = (int64_t)t * KEYS;
+    if (j0 > w_any) continue;
+    float x[KEYS / 16][4];
+#pragma unroll
+    for (int b = 0; b < KEYS / 16; ++b) {
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < KC; ++s) {
+        const float4 a = *(const float4*)(sK + (16 * b + i16) * LD + 16 * s + 4 * g4);
+        acc = mfma_f32_16x16x4(a.x, qv[s].x, acc);
+        acc = mfma_f32_16x16x4(a.y, qv[s].y, acc);
+        acc = mfma_f32_16x16x4(a.z, qv[s].z, acc);
+        acc = mfma_f32_16x16x4(a.w, qv[s].w, acc);
+      }
+      mfma_done(acc);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[b][r] = j0 + 16 * b + 4 * g4 + r > see ? -INFINITY : acc[r];
+    }
+    float mx = x[0][0];
+#pragma unroll
+    for (int b = 0; b < KEYS / 16; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) mx = fmaxf(mx, x[b][r]);
+    {
+      const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+      mx = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+      const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+      mx = fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1])) * sc2;
+    }
+    if (__any(mx > m)) {
+      const float mn = fmaxf(m, mx);
+      const float c = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= c;
+#pragma unroll
+      for (int p = 0; p < VB; ++p)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[p][j] *= c;
+    }
+    const float ms = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int b = 0; b < KEYS / 16; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][r], sc2, -ms));
+        l += e;
+#pragma unroll
+        for (int p = 0; p < VB; ++p) {
+          const float4 a = *(const float4*)(sV + (16 * b + 4 * g4 + r) * LD + 64 * p + 4 * i16);
+          o[p][0] = mfma_f32_16x16x4(a.x, e, o[p][0]);
+          o[p][1] = mfma_f32_16x16x4(a.y, e, o[p][1]);
+          o[p][2] = mfma_f32_16x16x4(a.z, e, o[p][2]);
+          o[p][3] = mfma_f32_16x16x4(a.w, e, o[p][3]);
+        }
+      }
+#pragma unroll
+    for (int p = 0; p < VB; ++p) mfma_done(o[p]);
+  }
+  sync_after_lds_stores();
+  // row 4 g4 + r of product (p, j) is dimension 64 p + 4 (4 g4 + r) + j
+  if (bad) {
+    const int64_t from = (g_all + 1) / KEYS * KEYS > (int64_t)it.t0 * KEYS ? (g_all + 1) / KEYS * KEYS : (int64_t)it.t0 * KEYS;
+    const int64_t to = (int64_t)it.t1 * KEYS < it.lk ? (int64_t)it.t1 * KEYS : it.lk;
+    for (int64_t j = from > 0 ? from : 0; j < to; ++j)
+      if (j <= see) {
+#pragma unroll
+        for (int p = 0; p < VB; ++p)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float x = vp[j * pd.v_tok + 64 * p + 4 * (4 * g4 + r) + i];
+              if (!(fabsf(x) < INFINITY)) o[p][i][r] += x;
+            }
+      }
+  }
+  l = col_sum4(l);
+  if (row >= it.rows) return;
+  const int64_t qrow = it.q0 + tok;
+  const int64_t part = ((int64_t)it.part * pd.n_q + qrow) * pd.H + head;
+  const float inv = parts > 1 ? 1.f : (l > 0.f ? 1.f / l : l);
+  float* op = parts > 1 ? po + part * D : out + qrow * pd.o_tok + head * pd.o_head;
+#pragma unroll
+  for (int p = 0; p < VB; ++p)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      *(float4*)(op + 64 * p + 4 * (4 * g4 + r)) = make_float4(o[p][0][r] * inv, o[p][1][r] * inv, o[p][2][r] * inv, o[p][3][r] * inv);
+  if (g4 != 0) return;
+  if (parts > 1) pml[part] = make_float2(m, l);
+  else if (lse) lse[qrow * pd.H + head] = m == -INFINITY ? logf(l) : (m + log2f(l)) * LN2;
+}
+
+// the parts of every (token, head) of the sequences, a lane for four dims
+template <typename T, int D>
+__global__ __launch_bounds__(PR_T) void k_prompt_combine(PromptDims pd, int parts, const int32_t* __restrict__ cu_q,
+                                                         const float2* __restrict__ pml, const float* __restrict__ po,
+                                                         T* __restrict__ out, float* __restrict__ lse) {
+  constexpr int LH = D / 4;                     // lanes of a head
+  const int64_t t = blockIdx.x;
+  const int b = find_span(cu_q, pd.n_seq, t);
+  const Span sp = span_of(cu_q, b, pd.n_q);
+  if (t < sp.a || t >= sp.a + sp.n) return;     // behind the last sequence
+  const int head = blockIdx.y * (PR_T / LH) + threadIdx.x / LH, c = 4 * (threadIdx.x % LH);
+  if (head >= pd.H) return;
+  const int64_t step = pd.n_q * pd.H, at = t * pd.H + head;
+  float M = -INFINITY;
+  for (int p = 0; p < parts; ++p) M = fmaxf(M, pml[at + p * step].x);
+  float S = 0.f, O[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int p = 0; p < parts; ++p) {
+    const float2 ml = pml[at + p * step];
+    const float f = ml.x == -INFINITY ? (ml.y == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(ml.x - M);
+    const float4 x = *(const float4*)(po + (at + p * step) * D + c);
+    if (f == 0.f) continue;
+    S += ml.y * f;
+    O[0] += x.x * f; O[1] += x.y * f; O[2] += x.z * f; O[3] += x.w * f;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) stf(out, t * pd.o_tok + head * pd.o_head + c + i, S > 0.f ? O[i] / S : S);
+  if (lse && c == 0) lse[at] = M == -INFINITY ? logf(S) : (M + log2f(S)) * LN2;
+}
+
+hipError_t launch_prompt(const PromptDims& pd, const void* q, const void* k, const void* v, const int32_t* cu_q,
+                         const int32_t* cu_k, void* out, float* lse, void* ws, hipStream_t st) {
+  if (pd.n_q == 0) return hipSuccess;
+  const int P = prompt_parts(pd);
+  float2* pml = P > 1 ? (float2*)ws : nullptr;
+  float* po = P > 1 ? (float*)((char*)ws + al256((size_t)P * pd.n_q * pd.H * 8)) : nullptr;
+  const bool bf = pd.dtype == GRACEKV_BF16;
+  const dim3 grid((unsigned)prompt_items(pd));
+#define GKV_PROMPT(KERNEL, TT)                                                                                            \
+  hipLaunchKernelGGL(KERNEL, grid, dim3(PR_T), 0, st, pd, P, (const TT*)q, (const TT*)k, (const TT*)v, cu_q, cu_k, (TT*)out, \
+                     lse, pml, po)
+  if (bf) {
+    if (pd.d == 128) GKV_PROMPT(k_prompt_bf<128>, uint16_t); else GKV_PROMPT(k_prompt_bf<64>, uint16_t);
+  } else {
+    if (pd.d == 128) GKV_PROMPT(k_prompt_f32<128>, float); else GKV_PROMPT(k_prompt_f32<64>, float);
+  }
+#undef GKV_PROMPT
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || P == 1) return e;
+  auto join = [&](auto type, auto dim) {
+    using T = decltype(type);
+    constexpr int D = decltype(dim)::value, HB = PR_T / (D / 4);
+    hipLaunchKernelGGL((k_prompt_combine<T, D>), dim3((unsigned)pd.n_q, (unsigned)((pd.H + HB - 1) / HB)), dim3(PR_T), 0, st, pd, P,
+                       cu_q, pml, po, (T*)out, lse);
+  };
+  using std::integral_constant;
+  if (bf) {
+    if (pd.d == 128) join(uint16_t{}, integral_constant<int, 128>{}); else join(uint16_t{}, integral_constant<int, 64>{});
+  } else {
+    if (pd.d == 128) join(float{}, integral_constant<int, 128>{}); else join(float{}, integral_constant<int, 64>{});
+  }
+  return hipGetLastError();
+}
+
+}  // namespace gkv

@@ -16,7 +16,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libgracekv.so")
 
 F32, BF16 = 0, 1
-ABI_VERSION = 11         # GRACEKV_ABI_VERSION this binding is written for
+ABI_VERSION = 12         # GRACEKV_ABI_VERSION this binding is written for
 _STATUS = {0: "ok", -1: "invalid argument", -2: "unsupported configuration", -3: "budget",
            -4: "workspace too small", -5: "HIP error", -6: "numeric fault on the device",
            -7: "the tree buffer holds no build", -8: "malformed slot partition on the device",
@@ -71,10 +71,35 @@ class Plan(ctypes.Structure):
                                                             ("build_ws_bytes", ctypes.c_size_t)])
 
 
+class PromptConfig(ctypes.Structure):
+    """gracekv_prompt_config."""
+    _fields_ = ([(n, ctypes.c_int32) for n in ("dtype", "G", "H", "d", "n_seq", "reserved")]
+                + [(n, ctypes.c_int64) for n in ("n_q", "n_k", "q_tok", "q_head", "k_tok", "k_head", "v_tok", "v_head",
+                                                 "out_tok", "out_head")])
+
+
+class PageConfig(ctypes.Structure):
+    """gracekv_page_config."""
+    _fields_ = ([(n, ctypes.c_int32) for n in ("dtype", "G", "H", "d", "n_seq", "page_size", "table_width", "reserved")]
+                + [(n, ctypes.c_int64) for n in ("n_pages", "page_stride")])
+
+
+class AppendConfig(ctypes.Structure):
+    """gracekv_append_config."""
+    _fields_ = [(n, ctypes.c_int64) for n in ("n_new", "rope_rows", "k_tok", "k_head", "v_tok", "v_head", "q_tok", "q_head",
+                                              "qout_tok", "qout_head")]
+
+
+class PrefixArrays(ctypes.Structure):
+    """gracekv_prefix."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("start", "count", "K", "V", "logm")] + [("rows", ctypes.c_int64)]
+
+
 SYMBOLS = ["gracekv_abi_version", "gracekv_default_config", "gracekv_plan_sizes", "gracekv_status_string", "gracekv_check",
            "gracekv_segment", "gracekv_build_trees", "gracekv_score", "gracekv_select", "gracekv_pack",
            "gracekv_selftest_mfma", "gracekv_decode_ws_bytes", "gracekv_decode_attention", "gracekv_relevance_stats",
-           "gracekv_decode_attention_noalloc", "gracekv_stage_times"]
+           "gracekv_decode_attention_noalloc", "gracekv_stage_times", "gracekv_prompt_ws_bytes", "gracekv_prompt_attention",
+           "gracekv_cache_append", "gracekv_paged_ws_bytes", "gracekv_paged_attention"]
 
 _lib = None
 
@@ -112,6 +137,12 @@ def lib() -> ctypes.CDLL:
         "gracekv_decode_attention": [ctypes.POINTER(Config), P, P, P, P, P, P, P, P, P, S, P],
         "gracekv_decode_attention_noalloc": [ctypes.POINTER(Config), P, P, P, P, P, P, P, P, P],
         "gracekv_stage_times": [P, P],
+        "gracekv_prompt_ws_bytes": [ctypes.POINTER(PromptConfig), ctypes.POINTER(S)],
+        "gracekv_prompt_attention": [ctypes.POINTER(PromptConfig), P, P, P, P, P, P, P, P, S, P],
+        "gracekv_cache_append": [ctypes.POINTER(PageConfig), ctypes.POINTER(AppendConfig), P, P, P, P, P, P, P, P, P, P, P, P, P],
+        "gracekv_paged_ws_bytes": [ctypes.POINTER(PageConfig), ctypes.POINTER(S)],
+        "gracekv_paged_attention": [ctypes.POINTER(PageConfig), P, ctypes.c_int64, P, P, P, P, ctypes.POINTER(PrefixArrays),
+                                    P, P, P, S, P],
     }
     for name, args in sig.items():
         f = getattr(L, name)
@@ -231,6 +262,180 @@ def decode_attention_noalloc(cfg, q, offsets, K_out, V_out, logm_out, K, V, out,
     _ok(lib().gracekv_decode_attention_noalloc(ctypes.byref(cfg), _ptr(q), _ptr(offsets), _ptr(K_out), _ptr(V_out),
                                                _ptr(logm_out), _ptr(K), _ptr(V), _ptr(out), _stream(stream)),
         "decode_attention_noalloc")
+
+
+# ---------------------------------------------------------------------------
+# Around the compression, one layer at a time: prompts, pages and the next token.
+
+_DTYPE = {torch.float32: F32, torch.bfloat16: BF16}
+_TORCH = {v: k for k, v in _DTYPE.items()}
+
+
+def _same(what: str, got, want):
+    if got != want:
+        raise ValueError(f"{what}: got {got}, need {want}")
+
+
+def _tensor(name: str, t: torch.Tensor, dtype: torch.dtype, shape) -> int:
+    """Address of a contiguous tensor of that type and shape on the current device."""
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name}: got {t.dtype} {tuple(t.shape)}{'' if t.is_contiguous() else ', not contiguous'}, "
+                         f"need {dtype} {tuple(shape)}, contiguous")
+    return _here(name, t)
+
+
+def _strided(name: str, t: torch.Tensor, dtype: torch.dtype, shape, tok: int, head: int) -> int:
+    """Address of [rows][heads][d] rows with these strides on the current device."""
+    if t.dtype != dtype or t.shape != shape or t.stride(2) != 1 or _strides(t) != (tok, head):
+        raise ValueError(f"{name}: got {t.dtype} {tuple(t.shape)} with strides {t.stride()}, "
+                         f"need {dtype} {tuple(shape)} with strides {(tok, head, 1)}")
+    return _here(name, t)
+
+
+def _here(name: str, t: torch.Tensor) -> int:
+    if t.device.index != torch.cuda.current_device():      # None on the CPU
+        raise ValueError(f"{name}: on {t.device}, but the current device is cuda:{torch.cuda.current_device()}")
+    return t.data_ptr()
+
+
+def _heads(name: str, t: torch.Tensor):
+    if t.dim() != 3 or t.stride(2) != 1:
+        raise ValueError(f"{name}: need [rows][heads][d] with contiguous heads, got {tuple(t.shape)}, strides {t.stride()}")
+    return t.shape
+
+
+def _dtype_of(name: str, t: torch.Tensor) -> int:
+    if t.dtype not in _DTYPE:
+        raise ValueError(f"{name}: got {t.dtype}, need one of {list(_DTYPE)}")
+    return _DTYPE[t.dtype]
+
+
+def _strides(t: torch.Tensor):
+    """Strides of rows and heads; 0 where there is one, whatever the tensor says."""
+    return t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0
+
+
+def prompt_config(q, k, v, out, n_seq: int) -> PromptConfig:
+    """The shapes and strides of these tensors (q, out [n_q][H][d], k, v [n_k][G][d], any
+    strides of rows and heads) for prompt_attention."""
+    (n_q, H, d), (n_k, G, _) = _heads("q", q), _heads("k", k)
+    _same("k", k.shape[2], d)
+    _same("v", tuple(_heads("v", v)), (n_k, G, d))
+    _same("out", tuple(_heads("out", out)), (n_q, H, d))
+    return PromptConfig(_dtype_of("q", q), G, H, d, n_seq, 0, n_q, n_k, *_strides(q), *_strides(k), *_strides(v), *_strides(out))
+
+
+def prompt_ws_bytes(cfg: PromptConfig) -> int:
+    n = ctypes.c_size_t(0)
+    _ok(lib().gracekv_prompt_ws_bytes(ctypes.byref(cfg), ctypes.byref(n)), "prompt_ws_bytes")
+    return int(n.value)
+
+
+def prompt_attention(cfg: PromptConfig, q, k, v, cu_q, cu_k, out, ws=None, lse=None, stream=None):
+    """Causal attention over packed prompts (gracekv_prompt_attention): ``cfg`` from
+    prompt_config; cu_q, cu_k [n_seq + 1] int32; lse [n_q][H] fp32; ws: prompt_ws_bytes(cfg) bytes."""
+    t, n = _TORCH[cfg.dtype], (cfg.n_seq + 1,)
+    _ok(lib().gracekv_prompt_attention(
+        ctypes.byref(cfg), _strided("q", q, t, (cfg.n_q, cfg.H, cfg.d), cfg.q_tok, cfg.q_head),
+        _strided("k", k, t, (cfg.n_k, cfg.G, cfg.d), cfg.k_tok, cfg.k_head),
+        _strided("v", v, t, (cfg.n_k, cfg.G, cfg.d), cfg.v_tok, cfg.v_head),
+        _tensor("cu_q", cu_q, torch.int32, n), _tensor("cu_k", cu_k, torch.int32, n),
+        _strided("out", out, t, (cfg.n_q, cfg.H, cfg.d), cfg.out_tok, cfg.out_head),
+        None if lse is None else _tensor("lse", lse, torch.float32, (cfg.n_q, cfg.H)),
+        *_workspace(ws), _stream(stream)), "prompt_attention")
+
+
+def _workspace(ws):
+    if ws is None:
+        return None, 0
+    return _tensor("ws", ws, ws.dtype, ws.shape), ws.numel() * ws.element_size()
+
+
+def page_config(K_pages, H: int, block_table) -> PageConfig:
+    """The shapes of a paged cache: K_pages [n_pages][G][page_size][d] (pages any distance
+    apart, each contiguous), block_table [n_seq][table_width] int32, H query heads."""
+    if K_pages.dim() != 4 or block_table.dim() != 2:
+        raise ValueError(f"need [n_pages][G][page_size][d] and [n_seq][table_width], got {tuple(K_pages.shape)}, {tuple(block_table.shape)}")
+    n, G, page, d = K_pages.shape
+    far = K_pages.stride(0) if n > 1 else G * page * d
+    cfg = PageConfig(_dtype_of("K_pages", K_pages), G, H, d, block_table.shape[0], page, block_table.shape[1], 0, n, far)
+    _page_strides("K_pages", cfg, K_pages)
+    return cfg
+
+
+def _page_strides(name: str, cfg: PageConfig, t: torch.Tensor):
+    want = (cfg.page_stride, cfg.page_size * cfg.d, cfg.d, 1)
+    if any(n > 1 and a != b for n, a, b in zip(t.shape, t.stride(), want)):
+        raise ValueError(f"{name}: strides {t.stride()}, need {want}")
+
+
+def _pages(name: str, cfg: PageConfig, t: torch.Tensor) -> int:
+    want = (cfg.n_pages, cfg.G, cfg.page_size, cfg.d)
+    if t.dtype != _TORCH[cfg.dtype] or t.shape != want:
+        raise ValueError(f"{name}: got {t.dtype} {tuple(t.shape)}, need {_TORCH[cfg.dtype]} {want}")
+    _page_strides(name, cfg, t)
+    return _here(name, t)
+
+
+def cache_append(cfg: PageConfig, k, v, K_pages, V_pages, block_table, start, cu_new, pos=None, rope_cos=None, rope_sin=None,
+                 q=None, q_out=None, stream=None):
+    """New tokens into the pages (gracekv_cache_append): k, v [n_new][G][d] and q, q_out
+    [n_new][H][d] with any strides of rows and heads; start [n_seq], cu_new [n_seq + 1],
+    pos [n_new] int32; rope_cos, rope_sin [rope_rows][d/2] fp32."""
+    t = _TORCH[cfg.dtype]
+    n = k.shape[0]
+    rows = AppendConfig(n, 0 if rope_cos is None else rope_cos.shape[0], *_strides(k), *_strides(v),
+                        *(_strides(q) if q is not None else (0, 0)), *(_strides(q_out) if q_out is not None else (0, 0)))
+    opt = lambda name, x, heads, tok, head: None if x is None else _strided(name, x, t, (n, heads, cfg.d), tok, head)  # noqa: E731
+    tab = lambda name, x: None if x is None else _tensor(name, x, torch.float32, (rows.rope_rows, cfg.d // 2))  # noqa: E731
+    _ok(lib().gracekv_cache_append(
+        ctypes.byref(cfg), ctypes.byref(rows), opt("k", k, cfg.G, rows.k_tok, rows.k_head),
+        opt("v", v, cfg.G, rows.v_tok, rows.v_head), opt("q", q, cfg.H, rows.q_tok, rows.q_head),
+        _tensor("block_table", block_table, torch.int32, (cfg.n_seq, cfg.table_width)),
+        _tensor("start", start, torch.int32, (cfg.n_seq,)), _tensor("cu_new", cu_new, torch.int32, (cfg.n_seq + 1,)),
+        None if pos is None else _tensor("pos", pos, torch.int32, (n,)), tab("rope_cos", rope_cos), tab("rope_sin", rope_sin),
+        _pages("K_pages", cfg, K_pages), _pages("V_pages", cfg, V_pages),
+        opt("q_out", q_out, cfg.H, rows.qout_tok, rows.qout_head), _stream(stream)), "cache_append")
+
+
+def paged_ws_bytes(cfg: PageConfig) -> int:
+    n = ctypes.c_size_t(0)
+    _ok(lib().gracekv_paged_ws_bytes(ctypes.byref(cfg), ctypes.byref(n)), "paged_ws_bytes")
+    return int(n.value)
+
+
+@dataclasses.dataclass
+class Prefix:
+    """Packed entries in front of the pages (gracekv_prefix): start, count [n_seq * G]
+    int64; K, V [rows][d]; logm [rows] fp32.  For one sequence these are slices of pack's
+    outputs: layer l takes offsets[l * G:l * G + G] and counts[l * G:l * G + G]."""
+    start: torch.Tensor
+    count: torch.Tensor
+    K: torch.Tensor
+    V: torch.Tensor
+    logm: torch.Tensor
+
+
+def paged_attention(cfg: PageConfig, q, K_pages, V_pages, block_table, seq_len, out, ws, lse=None, prefix: Optional[Prefix] = None,
+                    stream=None):
+    """Attention of one token of every sequence over its pages and packed entries
+    (gracekv_paged_attention): q [n_seq][H][d] (rows any distance apart), seq_len [n_seq]
+    int32, out [n_seq][H][d], lse [n_seq][H] fp32, ws: paged_ws_bytes(cfg) bytes."""
+    t, shape = _TORCH[cfg.dtype], (cfg.n_seq, cfg.H, cfg.d)
+    far = _strides(q)[0]
+    px = None
+    if prefix is not None:
+        R, rows = (cfg.n_seq * cfg.G,), prefix.K.shape[0]
+        px = ctypes.byref(PrefixArrays(
+            _tensor("prefix.start", prefix.start, torch.int64, R), _tensor("prefix.count", prefix.count, torch.int64, R),
+            _tensor("prefix.K", prefix.K, t, (rows, cfg.d)), _tensor("prefix.V", prefix.V, t, (rows, cfg.d)),
+            _tensor("prefix.logm", prefix.logm, torch.float32, (rows,)), rows))
+    _ok(lib().gracekv_paged_attention(
+        ctypes.byref(cfg), _strided("q", q, t, shape, far, cfg.d if cfg.H > 1 else 0), far, _pages("K_pages", cfg, K_pages),
+        _pages("V_pages", cfg, V_pages), _tensor("block_table", block_table, torch.int32, (cfg.n_seq, cfg.table_width)),
+        _tensor("seq_len", seq_len, torch.int32, (cfg.n_seq,)), px, _tensor("out", out, t, shape),
+        None if lse is None else _tensor("lse", lse, torch.float32, (cfg.n_seq, cfg.H)), *_workspace(ws), _stream(stream)),
+        "paged_attention")
 
 
 def selftest_mfma(which: int, stream=None) -> torch.Tensor:
