@@ -589,9 +589,10 @@ static gracekv_status prompt_dims(const gracekv_prompt_config* c, PromptDims* pd
     if (!stride_ok(c->dtype, s)) return GRACEKV_ERR_INVALID_ARG;
   if ((c->out_tok == 0 && c->n_q > 1) || (c->out_head == 0 && c->H > 1)) return GRACEKV_ERR_INVALID_ARG;   // rows on rows
   if (c->d != 64 && c->d != 128) return GRACEKV_ERR_UNSUPPORTED;
+  if (c->k_tok > PR_STRIDE || c->v_tok > PR_STRIDE) return GRACEKV_ERR_UNSUPPORTED;
   *pd = PromptDims{c->dtype, c->G, c->H, c->d, c->H / c->G, c->n_seq, c->n_q, c->n_k, c->q_tok, c->q_head,
                    c->k_tok, c->k_head, c->v_tok, c->v_head, c->out_tok, c->out_head};
-  if (prompt_items(*pd) > 0x7fffffff || c->H > 65535 * 8) return GRACEKV_ERR_UNSUPPORTED;   // one launch
+  if (c->n_q > 0x7fffffff / c->H || prompt_items(*pd) > 0x7fffffff) return GRACEKV_ERR_UNSUPPORTED;   // one launch
   return GRACEKV_OK;
 }
 

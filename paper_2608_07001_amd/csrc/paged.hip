@@ -30,8 +30,10 @@ namespace gkv {
 
 constexpr int PA_T = 256;
 constexpr int PA_W = PA_T / 64;
+constexpr int PA_OCC = 2;
 constexpr int PA_HEADS = 16;       // query heads of a workgroup
 constexpr int PA_MIN = PA_W;       // tiles of the shortest chunk: one a wave
+constexpr int PA_WHOLE = PA_W; // tiles up to which a row stays whole
 constexpr int PA_TARGET = 1024;    // chunks that the rows are cut into (beside one a row)
 
 static size_t al256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -60,35 +62,14 @@ static PagedWs paged_view(void* base, const PageDims& pg) {
 }
 size_t paged_ws_bytes(const PageDims& pg) { return paged_view(nullptr, pg).bytes; }
 
-// inclusive sum over the workgroup's threads; `total`: of all of them
-__device__ __forceinline__ int64_t scan_block(int64_t v, int64_t* sh, int64_t& total) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int64_t u = __shfl_up(v, o, 64);
-    if (lane >= o) v += u;
-  }
-  sync_after_lds_stores();
-  if (lane == 63) sh[w] = v;
-  sync_after_lds_stores();
-  int64_t before = 0;
-  total = 0;
-#pragma unroll
-  for (int i = 0; i < PA_W; ++i) {
-    if (i < w) before += sh[i];
-    total += sh[i];
-  }
-  return v + before;
-}
-
 // What a workgroup works on: tiles [t0, t1) of row (b, g); chunk `c` of `chunks`.
 struct Chunk {
   int b, g, c, chunks, t0, t1;
 };
 
 template <int TILE>
-__device__ __forceinline__ int64_t tiles_of(const PageDims& pg, int64_t len, int64_t count) {
-  const int64_t t = (len + TILE - 1) / TILE + (count + TILE - 1) / TILE;
+__device__ __forceinline__ int tiles_of(int64_t len, int64_t count) {
+  const int t = (int)((len + TILE - 1) / TILE) + (int)((count + TILE - 1) / TILE);
   return t > 0 ? t : 1;              // an empty row has a chunk, which writes its zeros
 }
 __device__ __forceinline__ int64_t held_count(const PrefixView& px, int64_t row, int64_t& start) {
@@ -99,56 +80,88 @@ __device__ __forceinline__ int64_t held_count(const PrefixView& px, int64_t row,
   return c;
 }
 
+// inclusive sum over the lanes of the wave
+__device__ __forceinline__ int scan_wave(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);     // row_shr 1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+  const int r = (threadIdx.x & 63) >> 4;
+  const int a = __builtin_amdgcn_readlane(v, 15), b = __builtin_amdgcn_readlane(v, 31), c = __builtin_amdgcn_readlane(v, 47);
+  return v + (r > 0 ? a : 0) + (r > 1 ? b : 0) + (r > 2 ? c : 0);
+}
+
+// Tiles of a chunk: all rows' tiles over the places that the grid leaves beside one a row
+// (every row may leave one chunk unfilled), and no fewer than the waves.
+__device__ __forceinline__ int chunk_tiles(uint64_t total, int room) {
+  const uint64_t size = total < 0x7fffffffu ? ((uint32_t)total + (uint32_t)room - 1) / (uint32_t)room : (total + room - 1) / room;
+  return size < (uint64_t)PA_MIN ? PA_MIN : (size > 0x7fffffffu ? 0x7fffffff : (int)size);
+}
+// ... and chunks of a row: short rows stay whole, which spares their joining
+__device__ __forceinline__ int chunks_of(int tiles, int size) {
+  return tiles <= PA_WHOLE ? 1 : (int)(((uint32_t)tiles + (uint32_t)size - 1) / (uint32_t)size);
+}
+
 // The chunk of workgroup blockIdx.x; false past the last.  Rows are looked at as units:
-// (b, g) where a prefix makes their lengths differ, b (G equal rows) otherwise.
+// (b, g) where a prefix makes their lengths differ, b (G equal rows) otherwise.  Every
+// wave finds it by itself, 64 units at a time; over few units that is one load and a
+// scan without a barrier.
 template <int TILE, bool PREFIX>
 __device__ __forceinline__ bool find_chunk(const PageDims& pg, const PrefixView& px, const int32_t* len, Chunk& out) {
-  __shared__ int64_t sh[PA_W];
-  __shared__ int64_t found[3];
-  const int tid = threadIdx.x;
+  const int lane = threadIdx.x & 63, bid = blockIdx.x;
   const int units = PREFIX ? pg.n_seq * pg.G : pg.n_seq, mult = PREFIX ? 1 : pg.G;
-  auto tiles = [&](int u) -> int64_t {
+  auto tiles = [&](int u) -> int {
+    if (u >= units) return 0;
     int64_t s = 0;
-    return tiles_of<TILE>(pg, held_len(pg, len[PREFIX ? u / pg.G : u]), PREFIX ? held_count(px, u, s) : 0);
+    return tiles_of<TILE>(held_len(pg, len[PREFIX ? u / pg.G : u]), PREFIX ? held_count(px, u, s) : 0);
   };
-  int64_t mine = 0, total;
-  for (int u = tid; u < units; u += PA_T) mine += tiles(u);
-  scan_block(mine, sh, total);
-  total *= mult;
-  const int64_t room = gridDim.x - (int64_t)pg.n_seq * pg.G;      // every row may leave one chunk unfilled
-  int64_t size = (total + room - 1) / room;
-  if (size < PA_MIN) size = PA_MIN;
-  if (tid == 0) found[0] = -1;
-  int64_t base = 0;
-  for (int u0 = 0; u0 < units; u0 += PA_T) {
-    const int u = u0 + tid;
-    const int64_t n = u < units ? tiles(u) : 0, c = (n + size - 1) / size;
-    const int64_t to = base + scan_block(c * mult, sh, total), from = to - c * mult;
-    if (u < units && (int64_t)blockIdx.x >= from && (int64_t)blockIdx.x < to) {
-      found[0] = u;
-      found[1] = blockIdx.x - from;
-      found[2] = n;
-    }
-    base += total;
-    if ((int64_t)blockIdx.x < base) break;
+  const int first = tiles(lane);
+  uint64_t total = 0;
+  if (units <= 64) {
+    int64_t sum = first;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+    total = (uint64_t)sum * mult;
+  } else {                             // the waves share the sum
+    __shared__ uint64_t part[PA_W];
+    uint64_t sum = 0;
+    for (int u = threadIdx.x; u < units; u += PA_T) sum += tiles(u);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+    if (lane == 0) part[threadIdx.x >> 6] = sum;
+    sync_after_lds_stores();
+#pragma unroll
+    for (int i = 0; i < PA_W; ++i) total += part[i];
+    total *= mult;
   }
-  sync_after_lds_stores();
-  // one value for the workgroup: kept in scalar registers
-  const int u = __builtin_amdgcn_readfirstlane((int)found[0]);
-  if (u < 0) return false;
-  const int local = __builtin_amdgcn_readfirstlane((int)found[1]), n = __builtin_amdgcn_readfirstlane((int)found[2]);
-  const int chunks = __builtin_amdgcn_readfirstlane((int)((n + size - 1) / size));
-  out.b = PREFIX ? u / pg.G : u;
-  out.g = PREFIX ? u % pg.G : local / chunks;
-  out.c = PREFIX ? local : local % chunks;
-  out.chunks = chunks;
-  out.t0 = (int)((int64_t)n * out.c / chunks);
-  out.t1 = (int)((int64_t)n * (out.c + 1) / chunks);
-  return true;
+  const int size = chunk_tiles(total, gridDim.x - pg.n_seq * pg.G);
+  int base = 0;
+  for (int u0 = 0; u0 < units; u0 += 64) {
+    const int n = u0 ? tiles(u0 + lane) : first;
+    const int c = n ? chunks_of(n, size) * mult : 0;
+    const int to = scan_wave(c);       // at most the grid: no overflow
+    const int all = base + __builtin_amdgcn_readlane(to, 63);
+    if (bid < all) {
+      const int at = __popcll(__ballot(base + to <= bid));       // the unit's lane
+      const int u = u0 + at;
+      const int tn = __builtin_amdgcn_readlane(n, at), chunks = chunks_of(tn, size);
+      const int local = bid - base - (__builtin_amdgcn_readlane(to, at) - chunks * mult);
+      out.b = PREFIX ? u / pg.G : u;
+      out.g = PREFIX ? u % pg.G : local / chunks;
+      out.c = PREFIX ? local : local % chunks;
+      out.chunks = chunks;
+      const int each = tn / chunks, more = tn % chunks;            // the first `more` take one more
+      out.t0 = out.c * each + min(out.c, more);
+      out.t1 = out.t0 + each + (out.c < more);
+      return true;
+    }
+    base = all;
+  }
+  return false;
 }
 
 template <typename T, int D, int NS, bool PREFIX>
-__global__ __launch_bounds__(PA_T, 2) void k_paged(PageDims pg, int64_t q_tok, const T* __restrict__ q,
+__global__ __launch_bounds__(PA_T, PA_OCC) void k_paged(PageDims pg, int64_t q_tok, const T* __restrict__ q,
                                                    const T* __restrict__ Kp, const T* __restrict__ Vp,
                                                    const int32_t* __restrict__ table, const int32_t* __restrict__ len,
                                                    PrefixView px, T* __restrict__ out, float* __restrict__ lse, PagedWs ws) {
@@ -160,7 +173,7 @@ __global__ __launch_bounds__(PA_T, 2) void k_paged(PageDims pg, int64_t q_tok, c
   constexpr int VB = BF ? 1 : D / 64;         // ... in so many places of the row
   constexpr int VW = VD * (int)sizeof(T) / 4; // words of one place
   __shared__ float sM[PA_W][PA_HEADS], sL[PA_W][PA_HEADS];
-  __shared__ float sO[PA_W][PA_HEADS][D];
+  __shared__ __align__(16) float sO[PA_W][PA_HEADS][D + 4];      // rows start in other banks
   Chunk ck;
   if (!find_chunk<TILE, PREFIX>(pg, px, len, ck)) return;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i16 = lane & 15, g4 = lane >> 4;
@@ -315,19 +328,26 @@ __global__ __launch_bounds__(PA_T, 2) void k_paged(PageDims pg, int64_t q_tok, c
         l += pr[h][r];
       }
     if constexpr (BF) {
-      static_assert(!BF || NS == 2, "two tiles of 16 make one product of 32");
-      const s16x8 pb = pk8(make_uint4(pack_bf16(pr[0][0], pr[0][1]), pack_bf16(pr[0][2], pr[0][3]),
-                                      pack_bf16(pr[1][0], pr[1][1]), pack_bf16(pr[1][2], pr[1][3])));
+      uint32_t pb[NS][2];
+#pragma unroll
+      for (int h = 0; h < NS; ++h) {
+        pb[h][0] = pack_bf16(pr[h][0], pr[h][1]);
+        pb[h][1] = pack_bf16(pr[h][2], pr[h][3]);
+      }
 #pragma unroll
       for (int j = 0; j < VD; ++j) {
         const uint32_t sel = (j & 1) ? 0x07060302u : 0x05040100u;
-        uint32_t a[4];
+        uint32_t a[NS][2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < NS; ++h)
 #pragma unroll
           for (int r = 0; r < 2; ++r)
-            a[2 * h + r] = __builtin_amdgcn_perm(t.v[h][2 * r + 1][0][j / 2], t.v[h][2 * r][0][j / 2], sel);
-        o[0][j] = mfma_bf16_16x16x32(pk8(make_uint4(a[0], a[1], a[2], a[3])), pb, o[0][j]);
+            a[h][r] = __builtin_amdgcn_perm(t.v[h][2 * r + 1][0][j / 2], t.v[h][2 * r][0][j / 2], sel);
+        if constexpr (NS == 2)
+          o[0][j] = mfma_bf16_16x16x32(pk8(make_uint4(a[0][0], a[0][1], a[1][0], a[1][1])),
+                                       pk8(make_uint4(pb[0][0], pb[0][1], pb[1][0], pb[1][1])), o[0][j]);
+        else
+          o[0][j] = mfma_bf16_16x16x16(pk4(a[0][0], a[0][1]), pk4(pb[0][0], pb[0][1]), o[0][j]);
       }
     } else {
 #pragma unroll
@@ -362,12 +382,15 @@ __global__ __launch_bounds__(PA_T, 2) void k_paged(PageDims pg, int64_t q_tok, c
   l = col_sum4(l);
   // row 4 g4 + r of product (p, j) is dimension 64 p + VD (4 g4 + r) + j, column i16 the head
   if (g4 == 0) { sM[w][i16] = m; sL[w][i16] = l; }
+  if (i16 < heads) {
 #pragma unroll
-  for (int p = 0; p < VB; ++p)
+    for (int p = 0; p < VB; ++p)
 #pragma unroll
-    for (int j = 0; j < VD; ++j)
+      for (int r = 0; r < 4; ++r)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) sO[w][i16][64 * p + VD * (4 * g4 + r) + j] = o[p][j][r];
+        for (int j = 0; j < VD; j += 4)
+          *(float4*)&sO[w][i16][64 * p + VD * (4 * g4 + r) + j] = make_float4(o[p][j][r], o[p][j + 1][r], o[p][j + 2][r], o[p][j + 3][r]);
+  }
   sync_after_lds_stores();
   const bool whole = ck.chunks == 1;
   if (tid == 0 && ck.c == 0 && blockIdx.y == 0) ws.rows[row] = make_int2((int)blockIdx.x, ck.chunks);
@@ -380,7 +403,8 @@ __global__ __launch_bounds__(PA_T, 2) void k_paged(PageDims pg, int64_t q_tok, c
 #pragma unroll
     for (int x = 0; x < PA_W; ++x) {
       const float c = sM[x][h] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((sM[x][h] - M) * LOG2E);
-      S += sL[x][h] * c;
+      const float lx = sL[x][h];
+      S += c == 0.f ? (lx == lx ? 0.f : lx) : lx * c;           // NaN stays
       O += c == 0.f ? 0.f : sO[x][h][dd] * c;
     }
     const int64_t hd = (int64_t)ck.g * pg.hpg + h0 + h;
@@ -395,44 +419,47 @@ __global__ __launch_bounds__(PA_T, 2) void k_paged(PageDims pg, int64_t q_tok, c
   }
 }
 
-// One workgroup per (row, head): the chunks' states, D lanes over the dims and the rest
-// over the chunks.
+// One workgroup per (row, head): the chunks' states in one pass, D lanes over the dims
+// and the rest over the chunks.
+constexpr int PC_T = 256;
 template <typename T, int D>
-__global__ __launch_bounds__(PA_T) void k_paged_combine(PageDims pg, PagedWs ws, T* __restrict__ out, float* __restrict__ lse) {
-  constexpr int GR = PA_T / D;
+__global__ __launch_bounds__(PC_T) void k_paged_combine(PageDims pg, PagedWs ws, T* __restrict__ out, float* __restrict__ lse) {
+  constexpr int GR = PC_T / D, UN = 4;
   constexpr float LOG2E = 1.44269504088896341f;
-  __shared__ float sS[GR], sO[GR][D], sW[PA_W];
+  __shared__ float sM[GR], sS[GR], sO[GR][D];
   const int64_t row = blockIdx.x;
   const int h = blockIdx.y, tid = threadIdx.x, gr = tid / D, dd = tid % D;
   const int2 ch = ws.rows[row];
   if (ch.y <= 1) return;
   const int64_t base = (int64_t)ch.x * pg.hpg + h;
-  float M = -INFINITY;
-  for (int c = tid; c < ch.y; c += PA_T) M = fmaxf(M, ws.ml[base + (int64_t)c * pg.hpg].x);
-  M = wave_max(M);
-  if ((tid & 63) == 0) sW[tid >> 6] = M;
-  sync_after_lds_stores();
+  float M = -INFINITY, S = 0.f, O = 0.f;
+  auto add = [&](float m, float s, float o) {
+    const float mn = fmaxf(M, m);
+    const float a = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((M - mn) * LOG2E);
+    const float c = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mn) * LOG2E);
+    S = (a == 0.f ? (S == S ? 0.f : S) : S * a) + (c == 0.f ? (s == s ? 0.f : s) : s * c);     // NaN stays
+    O = (a == 0.f ? 0.f : O * a) + (c == 0.f ? 0.f : o * c);
+    M = mn;
+  };
+  for (int c0 = gr; c0 < ch.y; c0 += GR * UN) {
+    float2 ml[UN];
+    float ov[UN];
 #pragma unroll
-  for (int x = 0; x < PA_W; ++x) M = fmaxf(M, sW[x]);
-  float S = 0.f, O = 0.f;
-#pragma unroll 4
-  for (int c = gr; c < ch.y; c += GR) {
-    const int64_t part = base + (int64_t)c * pg.hpg;
-    const float2 ml = ws.ml[part];
-    const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ml.x - M) * LOG2E);
-    const float ov = ws.o[part * D + dd];
-    S += ml.y * f;
-    O += f == 0.f ? 0.f : ov * f;
+    for (int i = 0; i < UN; ++i) {
+      const int64_t part = base + (int64_t)(c0 + i * GR < ch.y ? c0 + i * GR : c0) * pg.hpg;
+      ml[i] = ws.ml[part];
+      ov[i] = ws.o[part * D + dd];
+    }
+#pragma unroll
+    for (int i = 0; i < UN; ++i)
+      if (c0 + i * GR < ch.y) add(ml[i].x, ml[i].y, ov[i]);
   }
   sO[gr][dd] = O;
-  if (dd == 0) sS[gr] = S;
+  if (dd == 0) { sM[gr] = M; sS[gr] = S; }
   sync_after_lds_stores();
   if (gr == 0) {
 #pragma unroll
-    for (int x = 1; x < GR; ++x) {
-      S += sS[x];
-      O += sO[x][dd];
-    }
+    for (int x = 1; x < GR; ++x) add(sM[x], sS[x], sO[x][dd]);
     const int64_t b = row / pg.G, hd = (row % pg.G) * pg.hpg + h;
     stf(out, (b * pg.H + hd) * D + dd, S > 0.f ? O / S : S);
     if (lse && dd == 0) lse[b * pg.H + hd] = M + logf(S);
@@ -459,7 +486,7 @@ hipError_t launch_paged(const PageDims& pg, int64_t q_tok, const void* q, const 
                          len, px, (T*)out, lse, v);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((k_paged_combine<T, D>), dim3((unsigned)R, (unsigned)pg.hpg), dim3(PA_T), 0, st, pg, v, (T*)out, lse);
+    hipLaunchKernelGGL((k_paged_combine<T, D>), dim3((unsigned)R, (unsigned)pg.hpg), dim3(PC_T), 0, st, pg, v, (T*)out, lse);
     return hipGetLastError();
   };
   using std::integral_constant;

@@ -40,11 +40,10 @@ GKV_HD int64_t held_len(const PageDims& p, int64_t len) {
 // bounds of sequence b in packed rows (n of them), as given by the n_seq + 1 ascending
 // starts `cu`: held inside [0, n], and empty where they descend
 struct Span { int64_t a, n; };
+GKV_HD int64_t held(int64_t x, int64_t n) { return x < 0 ? 0 : (x > n ? n : x); }
 GKV_HD Span span_of(const int32_t* cu, int b, int64_t n) {
-  int64_t a = cu[b], e = cu[b + 1];
-  a = a < 0 ? 0 : (a > n ? n : a);
-  e = e < a ? a : (e > n ? n : e);
-  return {a, e - a};
+  const int64_t a = held(cu[b], n), e = held(cu[b + 1], n);
+  return {a, e < a ? 0 : e - a};
 }
 
 }  // namespace gkv

@@ -30,6 +30,9 @@ namespace gkv {
 
 constexpr int PR_T = 256;
 constexpr int PR_W = PR_T / 64;
+constexpr int PB_T = 256, PB_W = PB_T / 64, PB_OCC = 3, PB_KEYS = 32;     // bf16
+constexpr int PR_FILL = 512;       // workgroups that the keys of few rows are split into
+constexpr float PR_LAG = 8.f;      // base-2 units
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -43,23 +46,27 @@ __device__ __forceinline__ void mfma_done16(f32x16& x, f32x16& y) { asm volatile
 
 static size_t al256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-template <bool BF> constexpr int tile_rows() { return BF ? 32 * PR_W : 16 * PR_W; }
-template <bool BF> constexpr int tile_keys() { return BF ? 64 : 32; }
+template <bool BF> constexpr int tile_rows() { return BF ? 32 * PB_W : 16 * PR_W; }
+template <bool BF> constexpr int tile_keys() { return BF ? PB_KEYS : 32; }
 
-// row tiles of all sequences: sequence b's begin at cu_q[b] * hpg / rows + b, which
-// leaves each at least as many as it needs whatever the lengths are
-static int64_t row_tiles(const PromptDims& pd, int rows) { return pd.n_q * pd.hpg / rows + pd.n_seq; }
+// Row tiles of all sequences: sequence b's begin at cu_q[b] * hpg / rows + b, which
+// leaves each at least as many as it needs whatever the lengths are; one sequence alone
+// has as many as all rows need.
+GKV_HD int row_tiles(const PromptDims& pd, int rows) {
+  const uint32_t n = (uint32_t)(pd.n_q * pd.hpg);
+  return pd.n_seq > 1 ? (int)(n / rows) + pd.n_seq : (int)((n + rows - 1) / rows);
+}
 
 // Parts that every row tile's keys are cut into: one where the tiles fill the chip twice
 // over, more where they are few, each part holding at least 256 keys of the longest row.
 static int prompt_parts(const PromptDims& pd) {
   const int rows = pd.dtype == GRACEKV_BF16 ? tile_rows<true>() : tile_rows<false>();
-  const int64_t tiles = row_tiles(pd, rows) * pd.G;
-  const int64_t want = (512 + tiles - 1) / tiles, most = (pd.n_k + 255) / 256;
+  const int64_t tiles = (int64_t)row_tiles(pd, rows) * pd.G;
+  const int64_t want = tiles ? (PR_FILL + tiles - 1) / tiles : 1, most = (pd.n_k + 255) / 256;
   return (int)(want < 1 ? 1 : (want > most ? (most < 1 ? 1 : most) : want));
 }
 int64_t prompt_items(const PromptDims& pd) {
-  return row_tiles(pd, pd.dtype == GRACEKV_BF16 ? tile_rows<true>() : tile_rows<false>()) * prompt_parts(pd) * pd.G;
+  return (int64_t)row_tiles(pd, pd.dtype == GRACEKV_BF16 ? tile_rows<true>() : tile_rows<false>()) * prompt_parts(pd) * pd.G;
 }
 size_t prompt_ws_bytes(const PromptDims& pd) {
   const int P = prompt_parts(pd);
@@ -68,11 +75,11 @@ size_t prompt_ws_bytes(const PromptDims& pd) {
   return al256(n * 8) + n * pd.d * 4;
 }
 
-// what a workgroup works on
+// what a workgroup works on (rows of all heads of a group, and keys, are below 2^31)
 struct Item {
   int b, g, part;
-  int64_t q0, lq, k0, lk;      // the sequence's rows
-  int64_t r0, rows;            // first (token, head) row of the tile; rows of the sequence
+  int q0, lq, k0, lk;          // the sequence's rows
+  int r0, rows;                // first (token, head) row of the tile; rows of the sequence
   int t0, t1;                  // key tiles [t0, t1)
 };
 
@@ -81,33 +88,53 @@ struct Item {
 // L2; the tiles with the most keys come first.
 template <int ROWS, int KEYS>
 __device__ __forceinline__ bool find_item(const PromptDims& pd, const int32_t* cu_q, const int32_t* cu_k, int parts, Item& it) {
-  int64_t bid = blockIdx.x;
-  it.g = (int)(bid % pd.G);
-  bid /= pd.G;
-  it.part = (int)(bid % parts);
-  bid /= parts;
-  const int64_t slot = (int64_t)gridDim.x / pd.G / parts - 1 - bid;
-  auto first = [&](int b) { return span_of(cu_q, b, pd.n_q).a * pd.hpg / ROWS + b; };
-  it.b = find_last(pd.n_seq, [&](int b) { return first(b) <= slot; });
+  uint32_t bid = blockIdx.x;
+  it.g = (int)(bid % (uint32_t)pd.G);
+  bid /= (uint32_t)pd.G;
+  it.part = parts > 1 ? (int)(bid % (uint32_t)parts) : 0;
+  if (parts > 1) bid /= (uint32_t)parts;
+  const int slot = row_tiles(pd, ROWS) - 1 - (int)bid;
+  auto first = [&](int b) { return (int)((uint32_t)(held((int64_t)cu_q[b], pd.n_q) * pd.hpg) / ROWS) + b; };
+  it.b = pd.n_seq > 1 ? find_last(pd.n_seq, [&](int b) { return first(b) <= slot; }) : 0;
   const Span sq = span_of(cu_q, it.b, pd.n_q), sk = span_of(cu_k, it.b, pd.n_k);
-  it.q0 = sq.a; it.lq = sq.n; it.k0 = sk.a; it.lk = sk.n;
-  it.rows = sq.n * pd.hpg;
-  it.r0 = (slot - first(it.b)) * ROWS;
-  if (it.r0 < 0 || it.r0 >= it.rows) return false;
+  it.q0 = (int)sq.a; it.lq = (int)sq.n; it.k0 = (int)sk.a; it.lk = (int)sk.n;
+  it.rows = it.lq * pd.hpg;
+  const int tile = pd.n_seq > 1 ? slot - first(it.b) : slot;
+  if (tile < 0 || tile >= (int)(((uint32_t)it.rows + ROWS - 1) / ROWS)) return false;
+  it.r0 = tile * ROWS;
   // keys that the tile's last row sees
-  const int64_t last = (it.r0 + ROWS < it.rows ? it.r0 + ROWS : it.rows) - 1;
-  int64_t n = last / pd.hpg + 1 + sk.n - sq.n;
+  const uint32_t last = (uint32_t)(it.rows - it.r0 > ROWS ? it.r0 + ROWS : it.rows) - 1;
+  int n = (int)(last / (uint32_t)pd.hpg) + 1 + (it.lk - it.lq);
   n = n < 0 ? 0 : n;
-  const int64_t tiles = (n + KEYS - 1) / KEYS;
-  it.t0 = (int)(tiles * it.part / parts);
-  it.t1 = (int)(tiles * (it.part + 1) / parts);
+  const int tiles = n / KEYS + (n % KEYS != 0);
+  it.t0 = 0;
+  it.t1 = tiles;
+  if (parts > 1) {                     // the first tiles % parts of them take one more
+    const int each = tiles / parts, more = tiles % parts;
+    it.t0 = it.part * each + min(it.part, more);
+    it.t1 = it.t0 + each + (it.part < more);
+  }
   return true;
 }
 
-// the four 16-bit values of a lane after the transposing read: `p` is the lane's 8 bytes
-// of its group's 4 x 16 block (lanes 4 r .. 4 r + 3: row r), returned is column lane % 16
-__device__ __forceinline__ uint2 lds_read_tr(const uint16_t* p) {
-  auto q = (__attribute__((address_space(3))) s16x4*)p;
+// Orders a block's N products and their LDS reads (R a product): the reads AHEAD products early.
+template <int N, int R, int AHEAD> __device__ __forceinline__ void reads_ahead() {
+  constexpr int A = AHEAD < N ? AHEAD : N;
+  __builtin_amdgcn_sched_group_barrier(0x100, R * A, 0);        // LDS reads
+#pragma unroll
+  for (int i = 0; i < N - A; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);          // products
+    __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x008, A, 0);
+}
+
+// 16 bytes of a tile
+__device__ __forceinline__ uint4 lds_at(const uint4* tile, int byte) { return *(const uint4*)((const char*)tile + byte); }
+// the four 16-bit values of a lane after the transposing read: `byte` is where the lane's 8
+// bytes of its group's 4 x 16 block lie (lanes 4 r .. 4 r + 3: row r), returned is column lane % 16
+__device__ __forceinline__ uint2 lds_read_tr(const uint4* tile, int byte) {
+  auto q = (__attribute__((address_space(3))) s16x4*)((const char*)tile + byte);
   return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(q));
 }
 
@@ -127,6 +154,21 @@ template <bool BF> __device__ __forceinline__ uint4 finite(uint4 x, bool& any) {
   else return make_uint4(finite_f(x.x, any), finite_f(x.y, any), finite_f(x.z, any), finite_f(x.w, any));
 }
 
+// The rows of one key tile as a bounded buffer: `rows` rows of D elements, `tok` elements
+// apart; a load past the last row gives 0.  (tok is at most PR_STRIDE, so the bytes of a
+// tile fit 31 bits.)
+typedef __amdgpu_buffer_rsrc_t Buffer;
+template <typename T, int D>
+__device__ __forceinline__ Buffer tile_buffer(const T* base, int64_t tok, int rows) {
+  const int bytes = (int)(((int64_t)(rows - 1) * tok + D) * (int64_t)sizeof(T));
+  return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x00020000);
+}
+// 16 bytes a lane straight into LDS, lane l to dst + l (dst: the same for the wave); the
+// wave's vector memory counter says when they are there
+__device__ __forceinline__ void buffer_load_lds(Buffer b, uint4* dst, int off) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (__attribute__((address_space(3))) void*)dst, 16, off, 0, 0, 0);
+}
+
 // place of 16-byte piece c of key row t in a staged tile: neighbouring rows start in
 // other banks, for the reads along a row (16 rows, one piece) and the transposing ones
 // (8 rows, four pieces)
@@ -136,36 +178,40 @@ template <int D> __device__ __forceinline__ int swz(int t, int c) {
 }
 
 template <int D>
-__global__ __launch_bounds__(PR_T, 2) void k_prompt_bf(PromptDims pd, int parts, const uint16_t* __restrict__ q,
+__global__ __launch_bounds__(PB_T, PB_OCC) void k_prompt_bf(PromptDims pd, int parts, const uint16_t* __restrict__ q,
                                                        const uint16_t* __restrict__ k, const uint16_t* __restrict__ v,
                                                        const int32_t* __restrict__ cu_q, const int32_t* __restrict__ cu_k,
                                                        uint16_t* __restrict__ out, float* __restrict__ lse,
                                                        float2* __restrict__ pml, float* __restrict__ po) {
   constexpr int ROWS = tile_rows<true>(), KEYS = tile_keys<true>();
   constexpr int CH = D / 8;                     // 16-byte pieces of a row
-  constexpr int NL = KEYS * CH / PR_T;          // ... that a thread stages
+  constexpr int RI = 64 / CH;                   // rows that one load of a wave brings
+  constexpr int NI = KEYS / RI / PB_W;          // such loads of a wave and array
   constexpr int KS = D / 16;                    // product steps over the dims
   constexpr int DT = D / 32;                    // 32-dim tiles of the output
-  __shared__ uint4 sK[2][KEYS * CH], sV[2][KEYS * CH];
+  constexpr int NB = KEYS / 32;                 // 32-key blocks of a tile
+  // arrays of their own, so that loads into one tile and reads of the other are told apart
+  __shared__ uint4 sK0[KEYS * CH], sK1[KEYS * CH], sV0[KEYS * CH], sV1[KEYS * CH];
   __shared__ int bad;
   Item it;
   if (!find_item<ROWS, KEYS>(pd, cu_q, cu_k, parts, it)) return;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i32 = lane & 31, half = lane >> 5;
-  const int64_t off = it.lk - it.lq;            // query i sees the keys up to i + off
+  const int off = it.lk - it.lq;                // query i sees the keys up to i + off
   // the lane's row
-  const int64_t row = it.r0 + 32 * w + i32, rowc = row < it.rows ? row : it.rows - 1;
-  const int64_t tok = rowc / pd.hpg;
-  const int head = it.g * pd.hpg + (int)(rowc % pd.hpg);
-  const int64_t see = tok + off;                // its last key
+  const uint32_t hpg = (uint32_t)pd.hpg;
+  const int row = it.r0 + 32 * w + i32, rowc = row < it.rows ? row : it.rows - 1;
+  const int tok = (int)((uint32_t)rowc / hpg);
+  const int head = it.g * pd.hpg + (rowc - tok * pd.hpg);
+  const int see = tok + off;                    // its last key
   // what the wave's and the workgroup's rows see
-  const int64_t wr0 = it.r0 + 32 * w, wr1 = wr0 + 31;
-  const int64_t w_all = (wr0 < it.rows ? wr0 : it.rows - 1) / pd.hpg + off;
-  const int64_t w_any = wr0 < it.rows ? (wr1 < it.rows ? wr1 : it.rows - 1) / pd.hpg + off : -1;
-  const int64_t g_all = it.r0 / pd.hpg + off;
+  const int wr0 = it.r0 + 32 * w, wr1 = min(wr0 + 31, it.rows - 1);
+  const int w_all = (int)((uint32_t)min(wr0, it.rows - 1) / hpg) + off;
+  const int w_any = wr0 < it.rows ? (int)((uint32_t)wr1 / hpg) + off : -1;
+  const int g_all = (int)((uint32_t)it.r0 / hpg) + off;
 
   uint4 qv[KS];
   {
-    const uint16_t* qp = q + (it.q0 + tok) * pd.q_tok + head * pd.q_head;
+    const uint16_t* qp = q + (int64_t)(it.q0 + tok) * pd.q_tok + head * pd.q_head;
 #pragma unroll
     for (int s = 0; s < KS; ++s) qv[s] = *(const uint4*)(qp + 16 * s + 8 * half);
   }
@@ -179,116 +225,127 @@ __global__ __launch_bounds__(PR_T, 2) void k_prompt_bf(PromptDims pd, int parts,
 
   const uint16_t* kp = k + it.k0 * pd.k_tok + it.g * pd.k_head;
   const uint16_t* vp = v + it.k0 * pd.v_tok + it.g * pd.v_head;
-  uint4 rk[NL], rv[NL];
-  auto load = [&](int t) {
+  // Load i of a wave brings rows RI (w + PB_W i) .. + RI - 1 straight into LDS, lane l to
+  // the l-th 16 bytes: the piece that swz() puts there
+  const int lr = RI * w + lane / CH, lc = swz<D>(lr, lane % CH) - lr * CH;
+  const int k_off = (int)(lr * pd.k_tok * 2) + lc * 16, k_step = (int)(RI * PB_W * pd.k_tok * 2);
+  const int v_off = (int)(lr * pd.v_tok * 2) + lc * 16, v_step = (int)(RI * PB_W * pd.v_tok * 2);
+  auto load = [&](int t, uint4* dK, uint4* dV) {
+    const int64_t j0 = (int64_t)t * KEYS;
+    const int n = min(it.lk - t * KEYS, KEYS);   // at least one
+    const Buffer kb = tile_buffer<uint16_t, D>(kp + j0 * pd.k_tok, pd.k_tok, n);
+    const Buffer vb = tile_buffer<uint16_t, D>(vp + j0 * pd.v_tok, pd.v_tok, n);
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int e = tid + PR_T * i, c = e % CH;
-      const int64_t j = (int64_t)t * KEYS + e / CH;
-      const bool in = j < it.lk;
-      rk[i] = in ? *(const uint4*)(kp + j * pd.k_tok + 8 * c) : make_uint4(0, 0, 0, 0);
-      rv[i] = in ? *(const uint4*)(vp + j * pd.v_tok + 8 * c) : make_uint4(0, 0, 0, 0);
+    for (int i = 0; i < NI; ++i) {
+      buffer_load_lds(kb, dK + 64 * (w + PB_W * i), k_off + i * k_step);
+      buffer_load_lds(vb, dV + 64 * (w + PB_W * i), v_off + i * v_step);
     }
   };
-  auto store = [&](int buf, int t) {
-    if ((int64_t)t * KEYS + KEYS - 1 > g_all) {
+  // Where the lane reads in a tile, in bytes: piece 2 x + half of key row i32 lies at
+  // k_at ^ 32 x; row 4 half + (lane % 16) / 4 of the transposing read's 8 bytes at v_at,
+  // dim tile d at v_at ^ 64 d, the row 8 further at ^ 32 (swz()).
+  constexpr int RB = 2 * D;
+  int k_at = 16 * swz<D>(i32, half);
+  const int v_at = 16 * swz<D>(4 * half + ((lane & 15) >> 2), 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + 8 * (lane & 1);
+  auto step = [&](int t, const uint4* cK, uint4* cV, uint4* nK, uint4* nV) __attribute__((always_inline)) {
+    // the wave's own loads of tile t are there, then everyone's; and everyone is done with
+    // tile t - 1, which t + 1 replaces.  (A third tile in flight was slower for long prompts:
+    // 16K 1985 -> 2014 us, 8K 522 -> 536, though not for a ragged batch, 367 -> 360.)
+    wait_vm();
+    sync_after_lds_stores();
+    const int j0 = t * KEYS;
+    if (j0 + (KEYS - 1) > g_all) {              // values that are not finite: see above
       bool any = false;
 #pragma unroll
-      for (int i = 0; i < NL; ++i) rv[i] = finite<true>(rv[i], any);
+      for (int i = 0; i < KEYS * CH / PB_T; ++i) cV[tid + PB_T * i] = finite<true>(cV[tid + PB_T * i], any);
       if (any) bad = 1;
+      sync_after_lds_stores();
+    }
+    if (t + 1 < it.t1) load(t + 1, nK, nV);
+    if (j0 > w_any) return;
+    f32x16 s[NB];
+    asm volatile("" : "+v"(k_at));               // eight places: formed anew, not held in registers
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[b][r] = 0.f;
     }
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int e = tid + PR_T * i;
-      sK[buf][swz<D>(e / CH, e % CH)] = rk[i];
-      sV[buf][swz<D>(e / CH, e % CH)] = rv[i];
+    for (int x = 0; x < KS; ++x)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) s[b] = mfma_bf16_32x32x16(lds_at(cK, (k_at ^ (32 * x)) + 32 * b * RB), qv[x], s[b]);
+    // LDS reads four products ahead
+    reads_ahead<KS * NB, 1, 4>();
+#pragma unroll
+    for (int b = 0; b < NB; ++b) mfma_done16(s[b]);
+    // register r of block b: key 32 b + 8 (r / 4) + 4 half + r % 4
+    if (j0 + (KEYS - 1) > w_all) {
+      const int rel = see - j0 - 4 * half;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[b][r] = 32 * b + 8 * (r / 4) + r % 4 > rel ? -INFINITY : s[b][r];
     }
+    float mx = s[0][0];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[b][r]);
+    {
+      const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+      mx = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1])) * sc2;
+    }
+    // the maximum that is subtracted may lag behind by PR_LAG: weights up to 2^PR_LAG
+    // are as exact, and the outputs are rescaled seldom
+    if (__any(mx > m + PR_LAG)) {
+      const float mn = fmaxf(m, mx);
+      const float c = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= c;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[d] *= c;
+    }
+    const float ms = m == -INFINITY ? 0.f : m;
+    uint4 pr[2 * NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float e[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) e[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][8 * h + r], sc2, -ms));
+        l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+        pr[2 * b + h] = make_uint4(pack_bf16(e[0], e[1]), pack_bf16(e[2], e[3]), pack_bf16(e[4], e[5]), pack_bf16(e[6], e[7]));
+      }
+    // product step x: keys 16 x + 8 (j / 4) + 4 half + j % 4 in place 8 half + j
+#pragma unroll
+    for (int x = 0; x < 2 * NB; ++x)
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        const uint2 a = lds_read_tr(cV, (v_at ^ (64 * d)) + 16 * x * RB);
+        const uint2 b = lds_read_tr(cV, (v_at ^ (64 * d + 32)) + (16 * x + 8) * RB);
+        o[d] = mfma_bf16_32x32x16(make_uint4(a.x, a.y, b.x, b.y), pr[x], o[d]);
+      }
+    reads_ahead<2 * NB * DT, 2, 3>();
   };
   if (tid == 0) bad = 0;
-  if (it.t0 < it.t1) load(it.t0);
-  sync_after_lds_stores();
-  if (it.t0 < it.t1) store(0, it.t0);
-  for (int t = it.t0; t < it.t1; ++t) {
-    const int buf = (t - it.t0) & 1;
-    sync_after_lds_stores();
-    if (t + 1 < it.t1) load(t + 1);
-    const int64_t j0 = (int64_t)t * KEYS;
-    if (j0 <= w_any) {
-      f32x16 s[2];
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[b][r] = 0.f;
-#pragma unroll
-        for (int x = 0; x < KS; ++x) s[b] = mfma_bf16_32x32x16(sK[buf][swz<D>(32 * b + i32, 2 * x + half)], qv[x], s[b]);
-      }
-      mfma_done16(s[0], s[1]);
-      // register r of block b: key 32 b + 8 (r / 4) + 4 half + r % 4
-      if (j0 + KEYS - 1 > w_all) {
-        const int rel = (int)(see - j0 < KEYS ? (see - j0 < -1 ? -1 : see - j0) : KEYS) - 4 * half;
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (32 * b + 8 * (r / 4) + r % 4 > rel) s[b][r] = -INFINITY;
-      }
-      float mx = s[0][0];
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[b][r]);
-      {
-        const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-        mx = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1])) * sc2;
-      }
-      if (__any(mx > m)) {
-        const float mn = fmaxf(m, mx);
-        const float c = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
-        m = mn;
-        l *= c;
-#pragma unroll
-        for (int d = 0; d < DT; ++d) o[d] *= c;
-      }
-      const float ms = m == -INFINITY ? 0.f : m;
-      uint4 pr[4];
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float e[8];
-#pragma unroll
-          for (int r = 0; r < 8; ++r) e[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][8 * h + r], sc2, -ms));
-          l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
-          pr[2 * b + h] = make_uint4(pack_bf16(e[0], e[1]), pack_bf16(e[2], e[3]), pack_bf16(e[4], e[5]), pack_bf16(e[6], e[7]));
-        }
-      const uint16_t* sv = (const uint16_t*)sV[buf];
-      // product step x: keys 16 x + 8 (j / 4) + 4 half + j % 4 in place 8 half + j
-      const int tr = 4 * half + ((lane & 15) >> 2), tc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-#pragma unroll
-      for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const uint2 a = lds_read_tr(sv + 8 * swz<D>(16 * x + tr, 4 * d + tc) + 4 * (lane & 1));
-          const uint2 b = lds_read_tr(sv + 8 * swz<D>(16 * x + 8 + tr, 4 * d + tc) + 4 * (lane & 1));
-          o[d] = mfma_bf16_32x32x16(make_uint4(a.x, a.y, b.x, b.y), pr[x], o[d]);
-        }
-    }
-    if (t + 1 < it.t1) store(buf ^ 1, t + 1);
+  if (it.t0 < it.t1) load(it.t0, sK0, sV0);
+  for (int t = it.t0; t < it.t1; t += 2) {
+    step(t, sK0, sV0, sK1, sV1);
+    if (t + 1 < it.t1) step(t + 1, sK1, sV1, sK0, sV0);
   }
 #pragma unroll
   for (int d = 0; d < DT; ++d) mfma_done16(o[d]);
   sync_after_lds_stores();
   // values that are not finite in partly seen tiles, for the rows that see them
   if (bad) {
-    const int64_t from = (g_all + 1) / KEYS * KEYS > (int64_t)it.t0 * KEYS ? (g_all + 1) / KEYS * KEYS : (int64_t)it.t0 * KEYS;
-    const int64_t to = (int64_t)it.t1 * KEYS < it.lk ? (int64_t)it.t1 * KEYS : it.lk;
-    for (int64_t j = from > 0 ? from : 0; j < to; ++j)
+    for (int j = max(max(g_all + 1, 0) / KEYS, it.t0) * KEYS; j < min(it.t1 * KEYS, it.lk); ++j)
       if (j <= see) {
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            const float x = bf16_to_f32(vp[j * pd.v_tok + 32 * d + 8 * (r / 4) + 4 * half + r % 4]);
+            const float x = bf16_to_f32(vp[(int64_t)j * pd.v_tok + 32 * d + 8 * (r / 4) + 4 * half + r % 4]);
             if (!(fabsf(x) < INFINITY)) o[d][r] += x;
           }
       }
@@ -298,7 +355,7 @@ __global__ __launch_bounds__(PR_T, 2) void k_prompt_bf(PromptDims pd, int parts,
     l = __uint_as_float(p[0]) + __uint_as_float(p[1]);
   }
   if (row >= it.rows) return;
-  const int64_t qrow = it.q0 + tok;
+  const int64_t qrow = (int64_t)it.q0 + tok;
   if (parts > 1) {
     const int64_t part = ((int64_t)it.part * pd.n_q + qrow) * pd.H + head;
     if (half == 0) pml[part] = make_float2(m, l);
@@ -335,19 +392,19 @@ __global__ __launch_bounds__(PR_T, 2) void k_prompt_f32(PromptDims pd, int parts
   Item it;
   if (!find_item<ROWS, KEYS>(pd, cu_q, cu_k, parts, it)) return;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i16 = lane & 15, g4 = lane >> 4;
-  const int64_t off = it.lk - it.lq;
-  const int64_t row = it.r0 + 16 * w + i16, rowc = row < it.rows ? row : it.rows - 1;
-  const int64_t tok = rowc / pd.hpg;
-  const int head = it.g * pd.hpg + (int)(rowc % pd.hpg);
-  const int64_t see = tok + off;
-  const int64_t wr0 = it.r0 + 16 * w, wr1 = wr0 + 15;
-  const int64_t w_all = (wr0 < it.rows ? wr0 : it.rows - 1) / pd.hpg + off;
-  const int64_t w_any = wr0 < it.rows ? (wr1 < it.rows ? wr1 : it.rows - 1) / pd.hpg + off : -1;
-  const int64_t g_all = it.r0 / pd.hpg + off;
+  const uint32_t hpg = (uint32_t)pd.hpg;
+  const int off = it.lk - it.lq;
+  const int row = it.r0 + 16 * w + i16, rowc = row < it.rows ? row : it.rows - 1;
+  const int tok = (int)((uint32_t)rowc / hpg);
+  const int head = it.g * pd.hpg + (rowc - tok * pd.hpg);
+  const int see = tok + off;
+  const int wr0 = it.r0 + 16 * w, wr1 = min(wr0 + 15, it.rows - 1);
+  const int w_any = wr0 < it.rows ? (int)((uint32_t)wr1 / hpg) + off : -1;
+  const int g_all = (int)((uint32_t)it.r0 / hpg) + off;
 
   float4 qv[KC];                                // pieces g4, g4 + 4, ... of the row
   {
-    const float* qp = q + (it.q0 + tok) * pd.q_tok + head * pd.q_head;
+    const float* qp = q + (int64_t)(it.q0 + tok) * pd.q_tok + head * pd.q_head;
 #pragma unroll
     for (int s = 0; s < KC; ++s) qv[s] = *(const float4*)(qp + 16 * s + 4 * g4);
   }
@@ -375,7 +432,7 @@ __global__ __launch_bounds__(PR_T, 2) void k_prompt_f32(PromptDims pd, int parts
   if (it.t0 < it.t1) load(it.t0);
   for (int t = it.t0; t < it.t1; ++t) {
     sync_after_lds_stores();
-    if ((int64_t)t * KEYS + KEYS - 1 > g_all) {
+    if (t * KEYS + (KEYS - 1) > g_all) {
       bool any = false;
 #pragma unroll
       for (int i = 0; i < NL; ++i) rv[i] = finite<false>(rv[i], any);
@@ -389,7 +446,7 @@ __global__ __launch_bounds__(PR_T, 2) void k_prompt_f32(PromptDims pd, int parts
     }
     if (t + 1 < it.t1) load(t + 1);
     sync_after_lds_stores();
-    const int64_t j0 = (int64_t)t * KEYS;
+    const int j0 = t * KEYS;
     if (j0 > w_any) continue;
     float x[KEYS / 16][4];
 #pragma unroll
@@ -450,9 +507,7 @@ __global__ __launch_bounds__(PR_T, 2) void k_prompt_f32(PromptDims pd, int parts
   sync_after_lds_stores();
   // row 4 g4 + r of product (p, j) is dimension 64 p + 4 (4 g4 + r) + j
   if (bad) {
-    const int64_t from = (g_all + 1) / KEYS * KEYS > (int64_t)it.t0 * KEYS ? (g_all + 1) / KEYS * KEYS : (int64_t)it.t0 * KEYS;
-    const int64_t to = (int64_t)it.t1 * KEYS < it.lk ? (int64_t)it.t1 * KEYS : it.lk;
-    for (int64_t j = from > 0 ? from : 0; j < to; ++j)
+    for (int j = max(max(g_all + 1, 0) / KEYS, it.t0) * KEYS; j < min(it.t1 * KEYS, it.lk); ++j)
       if (j <= see) {
 #pragma unroll
         for (int p = 0; p < VB; ++p)
@@ -460,14 +515,14 @@ __global__ __launch_bounds__(PR_T, 2) void k_prompt_f32(PromptDims pd, int parts
           for (int r = 0; r < 4; ++r)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const float x = vp[j * pd.v_tok + 64 * p + 4 * (4 * g4 + r) + i];
+              const float x = vp[(int64_t)j * pd.v_tok + 64 * p + 4 * (4 * g4 + r) + i];
               if (!(fabsf(x) < INFINITY)) o[p][i][r] += x;
             }
       }
   }
   l = col_sum4(l);
   if (row >= it.rows) return;
-  const int64_t qrow = it.q0 + tok;
+  const int64_t qrow = (int64_t)it.q0 + tok;
   const int64_t part = ((int64_t)it.part * pd.n_q + qrow) * pd.H + head;
   const float inv = parts > 1 ? 1.f : (l > 0.f ? 1.f / l : l);
   float* op = parts > 1 ? po + part * D : out + qrow * pd.o_tok + head * pd.o_head;
@@ -481,30 +536,55 @@ __global__ __launch_bounds__(PR_T, 2) void k_prompt_f32(PromptDims pd, int parts
   else if (lse) lse[qrow * pd.H + head] = m == -INFINITY ? logf(l) : (m + log2f(l)) * LN2;
 }
 
-// the parts of every (token, head) of the sequences, a lane for four dims
+// The parts of (token, head) rows: a lane for four dims, `over` (a power of two) groups of
+// such lanes over the parts of a row, every lane's loads in flight together.
 template <typename T, int D>
-__global__ __launch_bounds__(PR_T) void k_prompt_combine(PromptDims pd, int parts, const int32_t* __restrict__ cu_q,
+__global__ __launch_bounds__(PR_T) void k_prompt_combine(PromptDims pd, int parts, int over, const int32_t* __restrict__ cu_q,
                                                          const float2* __restrict__ pml, const float* __restrict__ po,
                                                          T* __restrict__ out, float* __restrict__ lse) {
-  constexpr int LH = D / 4;                     // lanes of a head
-  const int64_t t = blockIdx.x;
-  const int b = find_span(cu_q, pd.n_seq, t);
+  constexpr int LH = D / 4, GR = PR_T / LH, UN = 4;
+  __shared__ float sM[GR], sS[GR];
+  __shared__ __align__(16) float sO[GR][D];
+  const int group = threadIdx.x / LH, gr = group & (over - 1), c = 4 * (threadIdx.x % LH);
+  const int64_t row = (int64_t)blockIdx.x * (GR / over) + group / over, rows = pd.n_q * pd.H;
+  const int64_t at = row < rows ? row : rows - 1;
+  const int t = (int)((uint32_t)at / (uint32_t)pd.H), head = (int)at - t * pd.H;
+  // is the token in a sequence?  (rows behind the last one are nobody's)
+  const int b = pd.n_seq > 1 ? span_with(cu_q, pd.n_seq, t) : 0;
   const Span sp = span_of(cu_q, b, pd.n_q);
-  if (t < sp.a || t >= sp.a + sp.n) return;     // behind the last sequence
-  const int head = blockIdx.y * (PR_T / LH) + threadIdx.x / LH, c = 4 * (threadIdx.x % LH);
-  if (head >= pd.H) return;
-  const int64_t step = pd.n_q * pd.H, at = t * pd.H + head;
-  float M = -INFINITY;
-  for (int p = 0; p < parts; ++p) M = fmaxf(M, pml[at + p * step].x);
-  float S = 0.f, O[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int p = 0; p < parts; ++p) {
-    const float2 ml = pml[at + p * step];
-    const float f = ml.x == -INFINITY ? (ml.y == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(ml.x - M);
-    const float4 x = *(const float4*)(po + (at + p * step) * D + c);
-    if (f == 0.f) continue;
-    S += ml.y * f;
-    O[0] += x.x * f; O[1] += x.y * f; O[2] += x.z * f; O[3] += x.w * f;
+  const bool on = row < rows && t >= sp.a && t < sp.a + sp.n;
+  const int64_t step = pd.n_q * pd.H;
+  float M = -INFINITY, S = 0.f, O[4] = {0.f, 0.f, 0.f, 0.f};
+  // a state of no key has the maximum -inf and adds nothing, unless its sum is no number
+  auto add = [&](float m, float s, const float4& x) {
+    const float mn = fmaxf(M, m);
+    const float f = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - mn), g = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+    S = (f == 0.f && S == S ? 0.f : S * f) + (g == 0.f && s == s ? 0.f : s * g);
+    const float v[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) O[i] = (f == 0.f ? 0.f : O[i] * f) + (g == 0.f ? 0.f : v[i] * g);
+    M = mn;
+  };
+  for (int p0 = gr; p0 < parts && on; p0 += over * UN) {
+    float2 ml[UN];
+    float4 x[UN];
+#pragma unroll
+    for (int i = 0; i < UN; ++i) {
+      const int64_t p = at + (p0 + i * over < parts ? p0 + i * over : p0) * step;
+      ml[i] = pml[p];
+      x[i] = *(const float4*)(po + p * D + c);
+    }
+#pragma unroll
+    for (int i = 0; i < UN; ++i)
+      if (p0 + i * over < parts) add(ml[i].x, ml[i].y, x[i]);
   }
+  if (over > 1) {
+    *(float4*)&sO[group][c] = make_float4(O[0], O[1], O[2], O[3]);
+    if (c == 0) { sM[group] = M; sS[group] = S; }
+    sync_after_lds_stores();
+  }
+  if (gr != 0 || !on) return;
+  for (int i = 1; i < over; ++i) add(sM[group + i], sS[group + i], *(const float4*)&sO[group + i][c]);
 #pragma unroll
   for (int i = 0; i < 4; ++i) stf(out, t * pd.o_tok + head * pd.o_head + c + i, S > 0.f ? O[i] / S : S);
   if (lse && c == 0) lse[at] = M == -INFINITY ? logf(S) : (M + log2f(S)) * LN2;
@@ -519,7 +599,7 @@ hipError_t launch_prompt(const PromptDims& pd, const void* q, const void* k, con
   const bool bf = pd.dtype == GRACEKV_BF16;
   const dim3 grid((unsigned)prompt_items(pd));
 #define GKV_PROMPT(KERNEL, TT)                                                                                            \
-  hipLaunchKernelGGL(KERNEL, grid, dim3(PR_T), 0, st, pd, P, (const TT*)q, (const TT*)k, (const TT*)v, cu_q, cu_k, (TT*)out, \
+  hipLaunchKernelGGL(KERNEL, grid, dim3(bf ? PB_T : PR_T), 0, st, pd, P, (const TT*)q, (const TT*)k, (const TT*)v, cu_q, cu_k, (TT*)out, \
                      lse, pml, po)
   if (bf) {
     if (pd.d == 128) GKV_PROMPT(k_prompt_bf<128>, uint16_t); else GKV_PROMPT(k_prompt_bf<64>, uint16_t);
@@ -531,9 +611,12 @@ hipError_t launch_prompt(const PromptDims& pd, const void* q, const void* k, con
   if (e != hipSuccess || P == 1) return e;
   auto join = [&](auto type, auto dim) {
     using T = decltype(type);
-    constexpr int D = decltype(dim)::value, HB = PR_T / (D / 4);
-    hipLaunchKernelGGL((k_prompt_combine<T, D>), dim3((unsigned)pd.n_q, (unsigned)((pd.H + HB - 1) / HB)), dim3(PR_T), 0, st, pd, P,
-                       cu_q, pml, po, (T*)out, lse);
+    constexpr int D = decltype(dim)::value, GR = PR_T / (D / 4);
+    int over = 1;                        // about four parts a lane, as it has loads in flight
+    while (over < GR && over * 4 < P) over *= 2;
+    const int64_t rows = pd.n_q * pd.H, each = GR / over;
+    hipLaunchKernelGGL((k_prompt_combine<T, D>), dim3((unsigned)((rows + each - 1) / each)), dim3(PR_T), 0, st, pd, P, over, cu_q,
+                       pml, po, (T*)out, lse);
   };
   using std::integral_constant;
   if (bf) {

@@ -20,6 +20,7 @@ struct PromptDims {
   int64_t n_q, n_k;
   int64_t q_tok, q_head, k_tok, k_head, v_tok, v_head, o_tok, o_head;
 };
+constexpr int64_t PR_STRIDE = 1 << 24;    // longest distance of two rows of a prompt's keys or values
 // the packed entries in front of the pages (all null: none)
 struct PrefixView {
   const int64_t* start;
@@ -69,6 +70,15 @@ __device__ __forceinline__ int find_last(int n, F at_most) {   // at_most(b): st
     if (step == 1) break;
   }
   return __builtin_amdgcn_readfirstlane(lo > 0 ? lo - 1 : 0);
+}
+// the same, each lane for a row of its own
+__device__ __forceinline__ int span_with(const int32_t* cu, int n, int64_t t) {
+  int lo = 0, hi = n;
+  while (lo < hi) {
+    const int mid = lo + (hi - lo) / 2;
+    if (cu[mid] <= t) lo = mid + 1; else hi = mid;
+  }
+  return lo > 0 ? lo - 1 : 0;
 }
 __device__ __forceinline__ int find_span(const int32_t* cu, int n, int64_t t) {
   return find_last(n, [&](int b) { return cu[b] <= t; });

@@ -168,8 +168,8 @@ def _ptr(t: Optional[torch.Tensor]):
 
 
 def _stream(stream=None):
-    if stream is None:
-        stream = torch.cuda.current_stream()
+    if stream is None:                     # the raw handle: a Stream object costs 3 us a call
+        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
     return ctypes.c_void_p(stream.cuda_stream)
 
 
@@ -276,26 +276,36 @@ def _same(what: str, got, want):
         raise ValueError(f"{what}: got {got}, need {want}")
 
 
-def _tensor(name: str, t: torch.Tensor, dtype: torch.dtype, shape) -> int:
-    """Address of a contiguous tensor of that type and shape on the current device."""
-    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"{name}: got {t.dtype} {tuple(t.shape)}{'' if t.is_contiguous() else ', not contiguous'}, "
-                         f"need {dtype} {tuple(shape)}, contiguous")
-    return _here(name, t)
+# These checks run in front of every generated token, so a good call costs one
+# comparison each and the words are found only for a bad one.
+
+def _refuse(name: str, t: torch.Tensor, dtype, shape, dev: int, strides=None):
+    raise ValueError(f"{name}: got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}, need {dtype} {tuple(shape)} "
+                     f"{'contiguous' if strides is None else f'with strides {strides}'} on the current device cuda:{dev}")
 
 
-def _strided(name: str, t: torch.Tensor, dtype: torch.dtype, shape, tok: int, head: int) -> int:
-    """Address of [rows][heads][d] rows with these strides on the current device."""
-    if t.dtype != dtype or t.shape != shape or t.stride(2) != 1 or _strides(t) != (tok, head):
-        raise ValueError(f"{name}: got {t.dtype} {tuple(t.shape)} with strides {t.stride()}, "
-                         f"need {dtype} {tuple(shape)} with strides {(tok, head, 1)}")
-    return _here(name, t)
-
-
-def _here(name: str, t: torch.Tensor) -> int:
-    if t.device.index != torch.cuda.current_device():      # None on the CPU
-        raise ValueError(f"{name}: on {t.device}, but the current device is cuda:{torch.cuda.current_device()}")
+def _tensor(name: str, t: torch.Tensor, dtype: torch.dtype, shape, dev: int) -> int:
+    """Address of a contiguous tensor of that type and shape on device ``dev``."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        _refuse(name, t, dtype, shape, dev)
     return t.data_ptr()
+
+
+def _rows(name: str, t: torch.Tensor, dtype: torch.dtype, shape, dev: int):
+    """Address and strides of [rows][heads][d] rows on device ``dev``: 0 for a length of one,
+    whatever the tensor says."""
+    tok, head, one = t.stride()
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or one != 1:
+        _refuse(name, t, dtype, shape, dev, "(any, any, 1)")
+    return t.data_ptr(), tok if shape[0] > 1 else 0, head if shape[1] > 1 else 0
+
+
+def _strided(name: str, t: torch.Tensor, dtype: torch.dtype, shape, tok: int, head: int, dev: int) -> int:
+    """Address of [rows][heads][d] rows that have these strides."""
+    p, a, b = _rows(name, t, dtype, shape, dev)
+    if a != tok or b != head:
+        _refuse(name, t, dtype, shape, dev, (tok, head, 1))
+    return p
 
 
 def _heads(name: str, t: torch.Tensor):
@@ -312,7 +322,8 @@ def _dtype_of(name: str, t: torch.Tensor) -> int:
 
 def _strides(t: torch.Tensor):
     """Strides of rows and heads; 0 where there is one, whatever the tensor says."""
-    return t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0
+    (n, h, _), (tok, head, _) = t.shape, t.stride()
+    return tok if n > 1 else 0, head if h > 1 else 0
 
 
 def prompt_config(q, k, v, out, n_seq: int) -> PromptConfig:
@@ -334,21 +345,22 @@ def prompt_ws_bytes(cfg: PromptConfig) -> int:
 def prompt_attention(cfg: PromptConfig, q, k, v, cu_q, cu_k, out, ws=None, lse=None, stream=None):
     """Causal attention over packed prompts (gracekv_prompt_attention): ``cfg`` from
     prompt_config; cu_q, cu_k [n_seq + 1] int32; lse [n_q][H] fp32; ws: prompt_ws_bytes(cfg) bytes."""
-    t, n = _TORCH[cfg.dtype], (cfg.n_seq + 1,)
+    dev, t, n, G, H, d, n_q, n_k = torch.cuda.current_device(), _TORCH[cfg.dtype], (cfg.n_seq + 1,), cfg.G, cfg.H, cfg.d, cfg.n_q, cfg.n_k
     _ok(lib().gracekv_prompt_attention(
-        ctypes.byref(cfg), _strided("q", q, t, (cfg.n_q, cfg.H, cfg.d), cfg.q_tok, cfg.q_head),
-        _strided("k", k, t, (cfg.n_k, cfg.G, cfg.d), cfg.k_tok, cfg.k_head),
-        _strided("v", v, t, (cfg.n_k, cfg.G, cfg.d), cfg.v_tok, cfg.v_head),
-        _tensor("cu_q", cu_q, torch.int32, n), _tensor("cu_k", cu_k, torch.int32, n),
-        _strided("out", out, t, (cfg.n_q, cfg.H, cfg.d), cfg.out_tok, cfg.out_head),
-        None if lse is None else _tensor("lse", lse, torch.float32, (cfg.n_q, cfg.H)),
-        *_workspace(ws), _stream(stream)), "prompt_attention")
+        ctypes.byref(cfg), _strided("q", q, t, (n_q, H, d), cfg.q_tok, cfg.q_head, dev),
+        _strided("k", k, t, (n_k, G, d), cfg.k_tok, cfg.k_head, dev), _strided("v", v, t, (n_k, G, d), cfg.v_tok, cfg.v_head, dev),
+        _tensor("cu_q", cu_q, torch.int32, n, dev), _tensor("cu_k", cu_k, torch.int32, n, dev),
+        _strided("out", out, t, (n_q, H, d), cfg.out_tok, cfg.out_head, dev),
+        None if lse is None else _tensor("lse", lse, torch.float32, (n_q, H), dev), *_workspace(ws, dev), _raw(stream, dev)),
+        "prompt_attention")
 
 
-def _workspace(ws):
+def _workspace(ws, dev: int):
     if ws is None:
         return None, 0
-    return _tensor("ws", ws, ws.dtype, ws.shape), ws.numel() * ws.element_size()
+    if not ws.is_contiguous() or ws.get_device() != dev:
+        _refuse("ws", ws, ws.dtype, ws.shape, dev)
+    return ws.data_ptr(), ws.nbytes
 
 
 def page_config(K_pages, H: int, block_table) -> PageConfig:
@@ -369,12 +381,20 @@ def _page_strides(name: str, cfg: PageConfig, t: torch.Tensor):
         raise ValueError(f"{name}: strides {t.stride()}, need {want}")
 
 
-def _pages(name: str, cfg: PageConfig, t: torch.Tensor) -> int:
-    want = (cfg.n_pages, cfg.G, cfg.page_size, cfg.d)
-    if t.dtype != _TORCH[cfg.dtype] or t.shape != want:
-        raise ValueError(f"{name}: got {t.dtype} {tuple(t.shape)}, need {_TORCH[cfg.dtype]} {want}")
-    _page_strides(name, cfg, t)
-    return _here(name, t)
+def _pages(cfg: PageConfig, K_pages, V_pages, dev: int):
+    """Addresses of both pools of a cache."""
+    t, G, page, d = _TORCH[cfg.dtype], cfg.G, cfg.page_size, cfg.d
+    shape, far = (cfg.n_pages, G, page, d), (cfg.page_stride, page * d, d, 1)
+    for name, x in (("K_pages", K_pages), ("V_pages", V_pages)):
+        if x.dtype is not t or x.shape != shape or x.get_device() != dev:
+            _refuse(name, x, t, shape, dev, far)
+        if x.stride() != far:
+            _page_strides(name, cfg, x)
+    return K_pages.data_ptr(), V_pages.data_ptr()
+
+
+def _raw(stream, dev: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
 def cache_append(cfg: PageConfig, k, v, K_pages, V_pages, block_table, start, cu_new, pos=None, rope_cos=None, rope_sin=None,
@@ -382,20 +402,20 @@ def cache_append(cfg: PageConfig, k, v, K_pages, V_pages, block_table, start, cu
     """New tokens into the pages (gracekv_cache_append): k, v [n_new][G][d] and q, q_out
     [n_new][H][d] with any strides of rows and heads; start [n_seq], cu_new [n_seq + 1],
     pos [n_new] int32; rope_cos, rope_sin [rope_rows][d/2] fp32."""
-    t = _TORCH[cfg.dtype]
-    n = k.shape[0]
-    rows = AppendConfig(n, 0 if rope_cos is None else rope_cos.shape[0], *_strides(k), *_strides(v),
-                        *(_strides(q) if q is not None else (0, 0)), *(_strides(q_out) if q_out is not None else (0, 0)))
-    opt = lambda name, x, heads, tok, head: None if x is None else _strided(name, x, t, (n, heads, cfg.d), tok, head)  # noqa: E731
-    tab = lambda name, x: None if x is None else _tensor(name, x, torch.float32, (rows.rope_rows, cfg.d // 2))  # noqa: E731
+    dev, t, i32 = torch.cuda.current_device(), _TORCH[cfg.dtype], torch.int32
+    n, n_seq, G, d = k.shape[0], cfg.n_seq, cfg.G, cfg.d
+    kp, k_tok, k_head = _rows("k", k, t, (n, G, d), dev)
+    vp, v_tok, v_head = _rows("v", v, t, (n, G, d), dev)
+    qp, q_tok, q_head = (None, 0, 0) if q is None else _rows("q", q, t, (n, cfg.H, d), dev)
+    op, o_tok, o_head = (None, 0, 0) if q_out is None else _rows("q_out", q_out, t, (n, cfg.H, d), dev)
+    r = 0 if rope_cos is None else rope_cos.shape[0]
     _ok(lib().gracekv_cache_append(
-        ctypes.byref(cfg), ctypes.byref(rows), opt("k", k, cfg.G, rows.k_tok, rows.k_head),
-        opt("v", v, cfg.G, rows.v_tok, rows.v_head), opt("q", q, cfg.H, rows.q_tok, rows.q_head),
-        _tensor("block_table", block_table, torch.int32, (cfg.n_seq, cfg.table_width)),
-        _tensor("start", start, torch.int32, (cfg.n_seq,)), _tensor("cu_new", cu_new, torch.int32, (cfg.n_seq + 1,)),
-        None if pos is None else _tensor("pos", pos, torch.int32, (n,)), tab("rope_cos", rope_cos), tab("rope_sin", rope_sin),
-        _pages("K_pages", cfg, K_pages), _pages("V_pages", cfg, V_pages),
-        opt("q_out", q_out, cfg.H, rows.qout_tok, rows.qout_head), _stream(stream)), "cache_append")
+        ctypes.byref(cfg), ctypes.byref(AppendConfig(n, r, k_tok, k_head, v_tok, v_head, q_tok, q_head, o_tok, o_head)), kp, vp, qp,
+        _tensor("block_table", block_table, i32, (n_seq, cfg.table_width), dev), _tensor("start", start, i32, (n_seq,), dev),
+        _tensor("cu_new", cu_new, i32, (n_seq + 1,), dev), None if pos is None else _tensor("pos", pos, i32, (n,), dev),
+        None if rope_cos is None else _tensor("rope_cos", rope_cos, torch.float32, (r, d // 2), dev),
+        None if rope_sin is None else _tensor("rope_sin", rope_sin, torch.float32, (r, d // 2), dev),
+        *_pages(cfg, K_pages, V_pages, dev), op, _raw(stream, dev)), "cache_append")
 
 
 def paged_ws_bytes(cfg: PageConfig) -> int:
@@ -421,20 +441,22 @@ def paged_attention(cfg: PageConfig, q, K_pages, V_pages, block_table, seq_len, 
     """Attention of one token of every sequence over its pages and packed entries
     (gracekv_paged_attention): q [n_seq][H][d] (rows any distance apart), seq_len [n_seq]
     int32, out [n_seq][H][d], lse [n_seq][H] fp32, ws: paged_ws_bytes(cfg) bytes."""
-    t, shape = _TORCH[cfg.dtype], (cfg.n_seq, cfg.H, cfg.d)
-    far = _strides(q)[0]
+    dev, t, n, G, H, d = torch.cuda.current_device(), _TORCH[cfg.dtype], cfg.n_seq, cfg.G, cfg.H, cfg.d
+    shape = (n, H, d)
+    qp, far, head = _rows("q", q, t, shape, dev)
+    if head != (d if H > 1 else 0):
+        _refuse("q", q, t, shape, dev, (far, d, 1))
     px = None
     if prefix is not None:
-        R, rows = (cfg.n_seq * cfg.G,), prefix.K.shape[0]
+        R, rows = (n * G,), prefix.K.shape[0]
         px = ctypes.byref(PrefixArrays(
-            _tensor("prefix.start", prefix.start, torch.int64, R), _tensor("prefix.count", prefix.count, torch.int64, R),
-            _tensor("prefix.K", prefix.K, t, (rows, cfg.d)), _tensor("prefix.V", prefix.V, t, (rows, cfg.d)),
-            _tensor("prefix.logm", prefix.logm, torch.float32, (rows,)), rows))
+            _tensor("prefix.start", prefix.start, torch.int64, R, dev), _tensor("prefix.count", prefix.count, torch.int64, R, dev),
+            _tensor("prefix.K", prefix.K, t, (rows, d), dev), _tensor("prefix.V", prefix.V, t, (rows, d), dev),
+            _tensor("prefix.logm", prefix.logm, torch.float32, (rows,), dev), rows))
     _ok(lib().gracekv_paged_attention(
-        ctypes.byref(cfg), _strided("q", q, t, shape, far, cfg.d if cfg.H > 1 else 0), far, _pages("K_pages", cfg, K_pages),
-        _pages("V_pages", cfg, V_pages), _tensor("block_table", block_table, torch.int32, (cfg.n_seq, cfg.table_width)),
-        _tensor("seq_len", seq_len, torch.int32, (cfg.n_seq,)), px, _tensor("out", out, t, shape),
-        None if lse is None else _tensor("lse", lse, torch.float32, (cfg.n_seq, cfg.H)), *_workspace(ws), _stream(stream)),
+        ctypes.byref(cfg), qp, far, *_pages(cfg, K_pages, V_pages, dev), _tensor("block_table", block_table, torch.int32, (n, cfg.table_width), dev),
+        _tensor("seq_len", seq_len, torch.int32, (n,), dev), px, _tensor("out", out, t, shape, dev),
+        None if lse is None else _tensor("lse", lse, torch.float32, (n, H), dev), *_workspace(ws, dev), _raw(stream, dev)),
         "paged_attention")
 
 
