@@ -631,8 +631,8 @@ static gracekv_status page_dims(const gracekv_page_config* c, PageDims* pg) {
   if (c->page_stride < page || !stride_ok(c->dtype, c->page_stride) || c->n_pages > INT64_MAX / 4 / c->page_stride)
     return GRACEKV_ERR_INVALID_ARG;
   *pg = PageDims{c->dtype, c->G, c->H, c->d, c->H / c->G, c->n_seq, shift, c->table_width, c->n_pages, c->page_stride};
-  // one launch: rows (sequence, KV head) in x, query heads in y; lengths are int32
-  if ((int64_t)c->n_seq * c->G > (1 << 24) || c->H > 65535 || ((int64_t)c->table_width << shift) > 0x7fffffff)
+  // groups of query heads in one launch; the tiles of 64 rows are counted in 31 bits
+  if ((int64_t)c->n_seq * c->G > (1 << 24) || c->H > 65535 || ((int64_t)c->table_width << shift) > PAGED_ROWS)
     return GRACEKV_ERR_UNSUPPORTED;
   return GRACEKV_OK;
 }
@@ -682,8 +682,9 @@ gracekv_status gracekv_paged_attention(const gracekv_page_config* c, const void*
   PrefixView px{nullptr, nullptr, nullptr, nullptr, nullptr, 0};
   if (prefix) {
     if (!prefix->start || !prefix->count || !prefix->K || !prefix->V || !prefix->logm || !aligned16(prefix->K) ||
-        !aligned16(prefix->V) || prefix->rows < 0 || prefix->rows > (int64_t)1 << 34)
+        !aligned16(prefix->V) || prefix->rows < 0)
       return GRACEKV_ERR_INVALID_ARG;
+    if (prefix->rows > PAGED_ROWS) return GRACEKV_ERR_UNSUPPORTED;
     px = PrefixView{prefix->start, prefix->count, prefix->K, prefix->V, prefix->logm, prefix->rows};
   }
   if (ws_bytes < paged_ws_bytes(pg)) return GRACEKV_ERR_WORKSPACE;

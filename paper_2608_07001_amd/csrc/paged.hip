@@ -9,10 +9,13 @@
 // The work is a stream over keys and values, each read once for all query heads of its
 // group: bound by HBM.  Sequences differ in length, and how long they are is known on
 // the device only, so the split is made there: every row (b, g) is cut into tiles of 16
-// or 32 entries, a chunk is so many tiles that the chunks of all rows fill the grid
-// once, and workgroup w finds its chunk by a scan over the rows' lengths.  A row of one
-// chunk is finished by its workgroup; the others leave a partial state each, merged by
-// k_paged_combine.
+// or 32 entries, a chunk is so many tiles that the chunks of all rows fill the chip
+// twice, and workgroup w finds its chunk by a scan over the rows' lengths.  A row of one
+// chunk is finished by its workgroup; the chunks of a longer one leave a partial state
+// each, and the workgroup that comes last joins them, in their order (Tickets).
+// (One line of all rows' tiles cut into equal pieces, rows beginning and ending anywhere
+// in them, was slower: 64 sequences of 1 to 8192 tokens 81 -> 114 us, for a workgroup then
+// has many short rows, one after the other.)
 //
 // A wave takes whole tiles.  Logits are formed transposed, S^T = K Q^T (entries x heads,
 // 16x16 matrix tiles, heads past the group's zero), keys straight from memory as the
@@ -30,19 +33,20 @@ namespace gkv {
 
 constexpr int PA_T = 256;
 constexpr int PA_W = PA_T / 64;
-constexpr int PA_OCC = 2;
+constexpr int PA_OCC = 2;          // waves a SIMD
 constexpr int PA_HEADS = 16;       // query heads of a workgroup
 constexpr int PA_MIN = PA_W;       // tiles of the shortest chunk: one a wave
-constexpr int PA_WHOLE = PA_W; // tiles up to which a row stays whole
-constexpr int PA_TARGET = 1024;    // chunks that the rows are cut into (beside one a row)
+// Chunks that the rows are cut into: as many as the chip holds for few rows, twice that
+// for many, whose own ends then even out.
+constexpr int PA_TARGET = 1024, PA_FEW = 256;
 
 static size_t al256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// workspace: per row (first chunk, chunks), then per chunk and head (max, sum), then the
-// partial outputs [chunk][hpg][d]
+// Workspace: a ticket word for every row and group of heads, then per chunk and head
+// (max, sum), then the partial sums [chunk][hpg][d].
 struct PagedWs {
-  int2* rows;
-  float2* ml;
+  long long* ticket;
+  unsigned long long* ml;
   float* o;
   size_t bytes;
 };
@@ -51,9 +55,9 @@ static PagedWs paged_view(void* base, const PageDims& pg) {
   char* p = (char*)base;
   PagedWs w;
   size_t o = 0;
-  w.rows = (int2*)(p + o);
-  o += al256(R * 8);
-  w.ml = (float2*)(p + o);
+  w.ticket = (long long*)(p + o);
+  o += al256(R * ((pg.hpg + PA_HEADS - 1) / PA_HEADS) * 8);
+  w.ml = (unsigned long long*)(p + o);
   o += al256(chunks * pg.hpg * 8);
   w.o = (float*)(p + o);
   o += chunks * pg.hpg * pg.d * 4;
@@ -62,16 +66,38 @@ static PagedWs paged_view(void* base, const PageDims& pg) {
 }
 size_t paged_ws_bytes(const PageDims& pg) { return paged_view(nullptr, pg).bytes; }
 
-// What a workgroup works on: tiles [t0, t1) of row (b, g); chunk `c` of `chunks`.
-struct Chunk {
-  int b, g, c, chunks, t0, t1;
-};
+// Tickets.  The chunks of a row count themselves in its word, from PA_BASE on; the one
+// that makes the count whole sets the word to 0 and joins.  Whatever a word holds before
+// is raised to PA_BASE first, so the workspace needs no clearing: every call leaves the
+// words it used at 0, and of other data only numbers above PA_BASE would count (as floats
+// or bf16 no numbers, of a pattern that arithmetic does not give; -1 and 0 are below).
+// States are written and read with device-coherent operations, and a wait for the writes
+// stands between them and the ticket, so no fence is needed, which on this chip would
+// write back and invalidate the L2 of the XCD.  (Counting by compare-and-swap took 40
+// chunks of a row 20 us, one after the other.)
+constexpr long long PA_BASE = 0x7fffffffffff0000ll;
+__device__ __forceinline__ bool last_of(long long* word, int parts) {
+  __hip_atomic_fetch_max(word, PA_BASE, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  const bool last = __hip_atomic_fetch_add(word, 1ll, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == PA_BASE + parts - 1;
+  if (last) __hip_atomic_store(word, 0ll, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return last;
+}
+__device__ __forceinline__ unsigned long long pair_bits(float a, float b) {
+  return (unsigned long long)__float_as_uint(a) | (unsigned long long)__float_as_uint(b) << 32;
+}
+__device__ __forceinline__ float2 pair_of(unsigned long long x) {
+  return make_float2(__uint_as_float((uint32_t)x), __uint_as_float((uint32_t)(x >> 32)));
+}
+__device__ __forceinline__ void put_agent(unsigned long long* p, unsigned long long x) {
+  __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
 
 template <int TILE>
 __device__ __forceinline__ int tiles_of(int64_t len, int64_t count) {
   const int t = (int)((len + TILE - 1) / TILE) + (int)((count + TILE - 1) / TILE);
   return t > 0 ? t : 1;              // an empty row has a chunk, which writes its zeros
 }
+// (a row has below 2^24 tiles, by the sizes that the entry point takes)
 __device__ __forceinline__ int64_t held_count(const PrefixView& px, int64_t row, int64_t& start) {
   int64_t s = px.start[row], c = px.count[row];
   s = s < 0 ? 0 : (s > px.rows ? px.rows : s);
@@ -91,15 +117,20 @@ __device__ __forceinline__ int scan_wave(int v) {
   return v + (r > 0 ? a : 0) + (r > 1 ? b : 0) + (r > 2 ? c : 0);
 }
 
+// What a workgroup works on: tiles [t0, t1) of row (b, g); chunk `c` of `chunks`.
+struct Chunk {
+  int b, g, c, chunks, t0, t1;
+};
+
 // Tiles of a chunk: all rows' tiles over the places that the grid leaves beside one a row
 // (every row may leave one chunk unfilled), and no fewer than the waves.
 __device__ __forceinline__ int chunk_tiles(uint64_t total, int room) {
   const uint64_t size = total < 0x7fffffffu ? ((uint32_t)total + (uint32_t)room - 1) / (uint32_t)room : (total + room - 1) / room;
   return size < (uint64_t)PA_MIN ? PA_MIN : (size > 0x7fffffffu ? 0x7fffffff : (int)size);
 }
-// ... and chunks of a row: short rows stay whole, which spares their joining
+// ... and chunks of a row
 __device__ __forceinline__ int chunks_of(int tiles, int size) {
-  return tiles <= PA_WHOLE ? 1 : (int)(((uint32_t)tiles + (uint32_t)size - 1) / (uint32_t)size);
+  return (int)(((uint32_t)tiles + (uint32_t)size - 1) / (uint32_t)size);
 }
 
 // The chunk of workgroup blockIdx.x; false past the last.  Rows are looked at as units:
@@ -118,10 +149,7 @@ __device__ __forceinline__ bool find_chunk(const PageDims& pg, const PrefixView&
   const int first = tiles(lane);
   uint64_t total = 0;
   if (units <= 64) {
-    int64_t sum = first;
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-    total = (uint64_t)sum * mult;
+    total = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(scan_wave(first), 63) * mult;
   } else {                             // the waves share the sum
     __shared__ uint64_t part[PA_W];
     uint64_t sum = 0;
@@ -174,71 +202,73 @@ __global__ __launch_bounds__(PA_T, PA_OCC) void k_paged(PageDims pg, int64_t q_t
   constexpr int VW = VD * (int)sizeof(T) / 4; // words of one place
   __shared__ float sM[PA_W][PA_HEADS], sL[PA_W][PA_HEADS];
   __shared__ __align__(16) float sO[PA_W][PA_HEADS][D + 4];      // rows start in other banks
+  __shared__ int joins;
   Chunk ck;
   if (!find_chunk<TILE, PREFIX>(pg, px, len, ck)) return;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i16 = lane & 15, g4 = lane >> 4;
   const int h0 = blockIdx.y * PA_HEADS, heads = min(PA_HEADS, pg.hpg - h0);
-  const int64_t row = (int64_t)ck.b * pg.G + ck.g;
-  const int64_t n_page = held_len(pg, len[ck.b]);
-  int64_t p_start = 0, n_pack = 0;
-  if constexpr (PREFIX) n_pack = held_count(px, row, p_start);
-  const int pack_tiles = (int)((n_pack + TILE - 1) / TILE);
   const T* PK = (const T*)px.K;
   const T* PV = (const T*)px.V;
   constexpr float LOG2E = 1.44269504088896341f;
   const float scale = 1.0f / sqrtf((float)D);
+  const int seq = ck.b, kv = ck.g;
+  const int64_t row = (int64_t)seq * pg.G + kv;
+  const int64_t n_page = held_len(pg, len[seq]);
+  int64_t p_start = 0, n_pack = 0;
+  if constexpr (PREFIX) n_pack = held_count(px, row, p_start);
+  const int pack_tiles = (int)((n_pack + TILE - 1) / TILE);
 
   // the group's queries: lane (head i16, quarter g4) holds pieces g4, g4 + 4, ... of the row
   uint4 qv[KC];
 #pragma unroll
   for (int s = 0; s < KC; ++s)
-    qv[s] = i16 < heads ? *(const uint4*)(q + ck.b * q_tok + ((int64_t)ck.g * pg.hpg + h0 + i16) * D + (4 * s + g4) * E)
+    qv[s] = i16 < heads ? *(const uint4*)(q + seq * q_tok + ((int64_t)kv * pg.hpg + h0 + i16) * D + (4 * s + g4) * E)
                         : make_uint4(0, 0, 0, 0);
 
   struct Tile {
     uint4 k[NS][KC];
     uint32_t v[NS][4][VB][VW];
-    float lm[NS][4];              // log m; -inf: no weight (absent, or masked by its log m)
-    bool all;                     // every entry there with log m = 0
+    float lm[PREFIX ? NS : 1][4]; // log m of packed entries
+    int n[NS];                    // entries there are
+    bool packed;
   };
-  const int32_t* tab = table + (int64_t)ck.b * pg.width;
-  auto fetch = [&](Tile& t, int ti) {
-    const bool packed = PREFIX && ti < pack_tiles;
-    t.all = !packed;
+  const int32_t* tab = table + (int64_t)seq * pg.width;
+  // 16 keys and values from kb, vb (the same for the wave): key row rk of the lane, value row rv(r)
+  auto rows16 = [&](Tile& t, int h, const char* kb, const char* vb, uint32_t rk, auto rv) __attribute__((always_inline)) {
+    constexpr uint32_t RB = D * sizeof(T);
+#pragma unroll
+    for (int s = 0; s < KC; ++s) t.k[h][s] = *(const uint4*)(kb + (rk * RB + 16 * g4) + 64 * s);
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int p = 0; p < VB; ++p) {
+        const char* x = vb + (rv(r) * RB + VD * sizeof(T) * i16) + 64 * sizeof(T) * p;
+        if constexpr (VW == 4) {
+          const uint4 u = *(const uint4*)x;
+          t.v[h][r][p][0] = u.x; t.v[h][r][p][1] = u.y; t.v[h][r][p][2] = u.z; t.v[h][r][p][3] = u.w;
+        } else {
+          const uint2 u = *(const uint2*)x;
+          t.v[h][r][p][0] = u.x; t.v[h][r][p][1] = u.y;
+        }
+      }
+  };
+  auto fetch = [&](Tile& t, int ti) __attribute__((always_inline)) {
+    t.packed = PREFIX && ti < pack_tiles;
 #pragma unroll
     for (int h = 0; h < NS; ++h) {
-      const int64_t e = (int64_t)(packed ? ti : ti - pack_tiles) * TILE + 16 * h;
-      int64_t left = (packed ? n_pack : n_page) - e, at = 0;
-      if (!packed && left > 0) {
-        at = page_row(pg, tab[e >> pg.shift], ck.g, (int)(e & (((int64_t)1 << pg.shift) - 1)));
+      const int64_t e = (int64_t)(t.packed ? ti : ti - pack_tiles) * TILE + 16 * h;
+      int64_t left = (t.packed ? n_pack : n_page) - e, at = 0;
+      if (!t.packed && left > 0) {
+        at = page_row(pg, tab[e >> pg.shift], kv, (int)(e & (((int64_t)1 << pg.shift) - 1)));
         if (at < 0) left = 0;
-      } else if (packed) {
+      } else if (t.packed) {
         at = (p_start + e) * D;
       }
       const int n = left > 16 ? 16 : (left < 0 ? 0 : (int)left);
-      t.all &= n == 16;
-      const T* kb = (packed ? PK : Kp) + at;
-      const T* vb = (packed ? PV : Vp) + at;
-      if (n > 0) {                // absent entries read the last one there
-        const T* kr = kb + (int64_t)min(i16, n - 1) * D;
-#pragma unroll
-        for (int s = 0; s < KC; ++s) t.k[h][s] = *(const uint4*)(kr + (4 * s + g4) * E);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const T* vr = vb + (int64_t)min(4 * g4 + r, n - 1) * D;
-#pragma unroll
-          for (int p = 0; p < VB; ++p) {
-            const uint32_t* x = (const uint32_t*)(vr + 64 * p + VD * i16);
-            if constexpr (VW == 4) {
-              const uint4 u = *(const uint4*)x;
-              t.v[h][r][p][0] = u.x; t.v[h][r][p][1] = u.y; t.v[h][r][p][2] = u.z; t.v[h][r][p][3] = u.w;
-            } else {
-              const uint2 u = *(const uint2*)x;
-              t.v[h][r][p][0] = u.x; t.v[h][r][p][1] = u.y;
-            }
-          }
-        }
-      } else {
+      t.n[h] = n;
+      const char* kb = (const char*)((t.packed ? PK : Kp) + at);
+      const char* vb = (const char*)((t.packed ? PV : Vp) + at);
+      if (n == 0) {
 #pragma unroll
         for (int s = 0; s < KC; ++s) t.k[h][s] = make_uint4(0, 0, 0, 0);
 #pragma unroll
@@ -247,11 +277,15 @@ __global__ __launch_bounds__(PA_T, PA_OCC) void k_paged(PageDims pg, int64_t q_t
           for (int p = 0; p < VB; ++p)
 #pragma unroll
             for (int x = 0; x < VW; ++x) t.v[h][r][p][x] = 0;
+      } else if (PREFIX && t.packed && n < 16) {       // the arrays may end here: absent entries read the last one
+        rows16(t, h, kb, vb, min(i16, n - 1), [&](int r) { return (uint32_t)min(4 * g4 + r, n - 1); });
+      } else {                    // a page holds all 16, written or not
+        rows16(t, h, kb, vb, i16, [&](int r) { return (uint32_t)(4 * g4 + r); });
       }
+      if constexpr (PREFIX) {
+        if (t.packed)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int i = 4 * g4 + r;
-        t.lm[h][r] = i >= n ? -INFINITY : (packed ? px.logm[p_start + e + i] : 0.f);
+          for (int r = 0; r < 4; ++r) t.lm[h][r] = 4 * g4 + r < n ? px.logm[p_start + e + 4 * g4 + r] : -INFINITY;
       }
     }
   };
@@ -263,7 +297,7 @@ __global__ __launch_bounds__(PA_T, PA_OCC) void k_paged(PageDims pg, int64_t q_t
     for (int j = 0; j < VD; ++j) o[p][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;               // of head i16; l: this lane's entries only
 
-  auto fold = [&](Tile& t) {
+  auto fold = [&](Tile& t) __attribute__((always_inline)) {
     float x[NS][4];
 #pragma unroll
     for (int h = 0; h < NS; ++h) {
@@ -282,14 +316,21 @@ __global__ __launch_bounds__(PA_T, PA_OCC) void k_paged(PageDims pg, int64_t q_t
 #pragma unroll
       for (int r = 0; r < 4; ++r) x[h][r] = acc[r] * scale;
     }
-    if (!t.all) {
+    bool all = !t.packed;
+#pragma unroll
+    for (int h = 0; h < NS; ++h) all &= t.n[h] == 16;
+    if (!all) {                   // absent entries and those masked by their log m
 #pragma unroll
       for (int h = 0; h < NS; ++h)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const bool none = t.lm[h][r] == -INFINITY;
-          x[h][r] = none ? -INFINITY : x[h][r] + t.lm[h][r];
+          bool none = 4 * g4 + r >= t.n[h];
+          if (PREFIX && t.packed) {
+            none = t.lm[h][r] == -INFINITY;
+            x[h][r] += t.lm[h][r];
+          }
           if (none) {             // 0 times an infinity is not 0
+            x[h][r] = -INFINITY;
 #pragma unroll
             for (int p = 0; p < VB; ++p)
 #pragma unroll
@@ -364,14 +405,15 @@ __global__ __launch_bounds__(PA_T, PA_OCC) void k_paged(PageDims pg, int64_t q_t
 
   // the next tile in flight while one is folded in; two places that take turns
   Tile ta, tb;
+  const int end = ck.t1;
   int ti = ck.t0 + w;
-  if (ti < ck.t1) fetch(ta, ti);
-  while (ti < ck.t1) {
-    if (ti + PA_W < ck.t1) fetch(tb, ti + PA_W);
+  if (ti < end) fetch(ta, ti);
+  while (ti < end) {
+    if (ti + PA_W < end) fetch(tb, ti + PA_W);
     fold(ta);
     ti += PA_W;
-    if (ti >= ck.t1) break;
-    if (ti + PA_W < ck.t1) fetch(ta, ti + PA_W);
+    if (ti >= end) break;
+    if (ti + PA_W < end) fetch(ta, ti + PA_W);
     fold(tb);
     ti += PA_W;
   }
@@ -392,77 +434,83 @@ __global__ __launch_bounds__(PA_T, PA_OCC) void k_paged(PageDims pg, int64_t q_t
           *(float4*)&sO[w][i16][64 * p + VD * (4 * g4 + r) + j] = make_float4(o[p][j][r], o[p][j + 1][r], o[p][j + 2][r], o[p][j + 3][r]);
   }
   sync_after_lds_stores();
-  const bool whole = ck.chunks == 1;
-  if (tid == 0 && ck.c == 0 && blockIdx.y == 0) ws.rows[row] = make_int2((int)blockIdx.x, ck.chunks);
-  for (int i = tid; i < heads * D; i += PA_T) {
-    const int h = i / D, dd = i % D;
-    float M = -INFINITY;
-#pragma unroll
-    for (int x = 0; x < PA_W; ++x) M = fmaxf(M, sM[x][h]);
-    float S = 0.f, O = 0.f;
-#pragma unroll
-    for (int x = 0; x < PA_W; ++x) {
-      const float c = sM[x][h] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((sM[x][h] - M) * LOG2E);
-      const float lx = sL[x][h];
-      S += c == 0.f ? (lx == lx ? 0.f : lx) : lx * c;           // NaN stays
-      O += c == 0.f ? 0.f : sO[x][h][dd] * c;
-    }
-    const int64_t hd = (int64_t)ck.g * pg.hpg + h0 + h;
-    if (whole) {
-      stf(out, ((int64_t)ck.b * pg.H + hd) * D + dd, S > 0.f ? O / S : S);     // nothing: 0; NaN stays
-      if (lse && dd == 0) lse[(int64_t)ck.b * pg.H + hd] = M + logf(S);
-    } else {
-      const int64_t part = (int64_t)blockIdx.x * pg.hpg + h0 + h;
-      ws.o[part * D + dd] = O;
-      if (dd == 0) ws.ml[part] = make_float2(M, S);
-    }
-  }
-}
-
-// One workgroup per (row, head): the chunks' states in one pass, D lanes over the dims
-// and the rest over the chunks.
-constexpr int PC_T = 256;
-template <typename T, int D>
-__global__ __launch_bounds__(PC_T) void k_paged_combine(PageDims pg, PagedWs ws, T* __restrict__ out, float* __restrict__ lse) {
-  constexpr int GR = PC_T / D, UN = 4;
-  constexpr float LOG2E = 1.44269504088896341f;
-  __shared__ float sM[GR], sS[GR], sO[GR][D];
-  const int64_t row = blockIdx.x;
-  const int h = blockIdx.y, tid = threadIdx.x, gr = tid / D, dd = tid % D;
-  const int2 ch = ws.rows[row];
-  if (ch.y <= 1) return;
-  const int64_t base = (int64_t)ch.x * pg.hpg + h;
-  float M = -INFINITY, S = 0.f, O = 0.f;
-  auto add = [&](float m, float s, float o) {
-    const float mn = fmaxf(M, m);
-    const float a = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((M - mn) * LOG2E);
-    const float c = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mn) * LOG2E);
-    S = (a == 0.f ? (S == S ? 0.f : S) : S * a) + (c == 0.f ? (s == s ? 0.f : s) : s * c);     // NaN stays
-    O = (a == 0.f ? 0.f : O * a) + (c == 0.f ? 0.f : o * c);
+  auto finish = [&](int h, int dd, float M, float S, float O0, float O1) {
+    const int64_t hd = (int64_t)seq * pg.H + (int64_t)kv * pg.hpg + h0 + h;
+    stf(out, hd * D + dd, S > 0.f ? O0 / S : S);                  // nothing: 0; NaN stays
+    stf(out, hd * D + dd + 1, S > 0.f ? O1 / S : S);
+    if (lse && dd == 0) lse[hd] = M + logf(S);
+  };
+  // state (m, s, o) onto (M, S, O): one of no entry has the maximum -inf and adds nothing,
+  // unless its sum is no number
+  auto add = [&](float& M, float& S, float& O0, float& O1, float m2, float s2, float a0, float a1) {
+    const float mn = fmaxf(M, m2);
+    const float f = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((M - mn) * LOG2E);
+    const float c = m2 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m2 - mn) * LOG2E);
+    S = (f == 0.f && S == S ? 0.f : S * f) + (c == 0.f && s2 == s2 ? 0.f : s2 * c);
+    O0 = (f == 0.f ? 0.f : O0 * f) + (c == 0.f ? 0.f : a0 * c);
+    O1 = (f == 0.f ? 0.f : O1 * f) + (c == 0.f ? 0.f : a1 * c);
     M = mn;
   };
-  for (int c0 = gr; c0 < ch.y; c0 += GR * UN) {
-    float2 ml[UN];
-    float ov[UN];
+  const int64_t place = (int64_t)blockIdx.x * pg.hpg + h0;
+  for (int i = tid; i < heads * (D / 2); i += PA_T) {
+    const int h = i / (D / 2), dd = 2 * (i % (D / 2));
+    float M = -INFINITY, S = 0.f, O0 = 0.f, O1 = 0.f;
 #pragma unroll
-    for (int i = 0; i < UN; ++i) {
-      const int64_t part = base + (int64_t)(c0 + i * GR < ch.y ? c0 + i * GR : c0) * pg.hpg;
-      ml[i] = ws.ml[part];
-      ov[i] = ws.o[part * D + dd];
+    for (int x = 0; x < PA_W; ++x) add(M, S, O0, O1, sM[x][h], sL[x][h], sO[x][h][dd], sO[x][h][dd + 1]);
+    if (ck.chunks == 1) {
+      finish(h, dd, M, S, O0, O1);
+    } else {
+      put_agent((unsigned long long*)(ws.o + (place + h) * D + dd), pair_bits(O0, O1));
+      if (dd == 0) put_agent(ws.ml + place + h, pair_bits(M, S));
     }
-#pragma unroll
-    for (int i = 0; i < UN; ++i)
-      if (c0 + i * GR < ch.y) add(ml[i].x, ml[i].y, ov[i]);
   }
-  sO[gr][dd] = O;
-  if (dd == 0) { sM[gr] = M; sS[gr] = S; }
+  if (ck.chunks == 1) return;
+  wait_vm();                                    // the thread's states are there
+  __syncthreads();
+  if (tid == 0) joins = last_of(ws.ticket + row * gridDim.y + blockIdx.y, ck.chunks);
   sync_after_lds_stores();
-  if (gr == 0) {
+  if (!joins) return;
+  // A head's pairs of dims lie on LH neighbouring lanes, which hold the (max, sum) of LH
+  // chunks at a time, one each, and pass the weights round.
+  constexpr int LH = D / 2;
+  const int64_t base = ((int64_t)blockIdx.x - ck.c) * pg.hpg + h0;              // the row's first chunk
+  for (int i = tid; i < (heads * LH + 63) / 64 * 64; i += PA_T) {               // whole waves
+    const int h = min(i / LH, heads - 1), sub = i % LH, dd = 2 * sub;
+    float M = -INFINITY, S = 0.f, O0 = 0.f, O1 = 0.f;
+    for (int b0 = 0; b0 < ck.chunks; b0 += LH) {
+      const int nb = min(ck.chunks - b0, LH);
+      const unsigned long long* src = (const unsigned long long*)(ws.o + (base + (int64_t)b0 * pg.hpg + h) * D + dd);
+      const int64_t step = (int64_t)pg.hpg * LH;
+      constexpr int UN = 8;
+      unsigned long long ov[UN];
+      auto load = [&](int c0) {                 // past the last: that one again
 #pragma unroll
-    for (int x = 1; x < GR; ++x) add(sM[x], sS[x], sO[x][dd]);
-    const int64_t b = row / pg.G, hd = (row % pg.G) * pg.hpg + h;
-    stf(out, (b * pg.H + hd) * D + dd, S > 0.f ? O / S : S);
-    if (lse && dd == 0) lse[b * pg.H + hd] = M + logf(S);
+        for (int c = 0; c < UN; ++c) ov[c] = ld_agent(src + min(c0 + c, nb - 1) * step);
+      };
+      float2 ml = make_float2(-INFINITY, 0.f);
+      if (sub < nb) ml = pair_of(ld_agent(ws.ml + base + (int64_t)(b0 + sub) * pg.hpg + h));
+      load(0);
+      float mb = ml.x;
+#pragma unroll
+      for (int o = LH / 2; o > 0; o >>= 1) mb = fmaxf(mb, __shfl_xor(mb, o, 64));
+      const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ml.x - mb) * LOG2E);
+      float sb = f == 0.f && ml.y == ml.y ? 0.f : ml.y * f;                     // NaN stays
+#pragma unroll
+      for (int o = LH / 2; o > 0; o >>= 1) sb += __shfl_xor(sb, o, 64);
+      float a0 = 0.f, a1 = 0.f;
+      for (int c0 = 0; c0 < nb; c0 += UN) {
+        if (c0) load(c0);
+#pragma unroll
+        for (int c = 0; c < UN; ++c) {
+          const float g = c0 + c < nb ? __shfl(f, (tid & 63 & ~(LH - 1)) + c0 + c, 64) : 0.f;
+          const float2 v = pair_of(ov[c]);
+          a0 += g == 0.f ? 0.f : v.x * g;
+          a1 += g == 0.f ? 0.f : v.y * g;
+        }
+      }
+      add(M, S, O0, O1, mb, sb, a0, a1);
+    }
+    if (i < heads * LH) finish(h, dd, M, S, O0, O1);
   }
 }
 
@@ -470,23 +518,24 @@ hipError_t launch_paged(const PageDims& pg, int64_t q_tok, const void* q, const 
                         const int32_t* table, const int32_t* len, const PrefixView& px, void* out, float* lse, void* ws,
                         hipStream_t st) {
   const PagedWs v = paged_view(ws, pg);
-  const int64_t R = (int64_t)pg.n_seq * pg.G;
+  const int64_t R = (int64_t)pg.n_seq * pg.G;                   // rows
   auto go = [&](auto type, auto dim, auto sub) {
     using T = decltype(type);
     constexpr int D = decltype(dim)::value, NS = decltype(sub)::value;
-    // chunks that the longest rows could make: no larger grid than that
+    // Places beside one a row: half the rows leave theirs unfilled, and no larger a grid than
+    // the shortest chunks of the longest rows could make.
     const int64_t tiles = R * ((((int64_t)pg.width << pg.shift) + 16 * NS - 1) / (16 * NS)) + (px.K ? px.rows / (16 * NS) + R : 0);
-    const int64_t most = (tiles + PA_MIN - 1) / PA_MIN;
-    const dim3 grid((unsigned)(R + (most < PA_TARGET ? (most > 0 ? most : 1) : PA_TARGET)), (unsigned)((pg.hpg + PA_HEADS - 1) / PA_HEADS));
+    int64_t room = (tiles + PA_MIN - 1) / PA_MIN;
+    const int64_t target = R < PA_FEW ? PA_TARGET / 2 : PA_TARGET;
+    const int64_t most = target - R / 2 > target / 4 ? target - R / 2 : target / 4;
+    room = room < 1 ? 1 : (room > most ? most : room);
+    const dim3 grid((unsigned)(R + room), (unsigned)((pg.hpg + PA_HEADS - 1) / PA_HEADS));
     if (px.K)
       hipLaunchKernelGGL((k_paged<T, D, NS, true>), grid, dim3(PA_T), 0, st, pg, q_tok, (const T*)q, (const T*)Kp, (const T*)Vp, table,
                          len, px, (T*)out, lse, v);
     else
       hipLaunchKernelGGL((k_paged<T, D, NS, false>), grid, dim3(PA_T), 0, st, pg, q_tok, (const T*)q, (const T*)Kp, (const T*)Vp, table,
                          len, px, (T*)out, lse, v);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((k_paged_combine<T, D>), dim3((unsigned)R, (unsigned)pg.hpg), dim3(PC_T), 0, st, pg, v, (T*)out, lse);
     return hipGetLastError();
   };
   using std::integral_constant;
