@@ -33,12 +33,12 @@ namespace gkv {
 
 constexpr int PA_T = 256;
 constexpr int PA_W = PA_T / 64;
-constexpr int PA_OCC = 2;          // waves a SIMD
+constexpr int PA_OCC = 3;          // waves a SIMD
 constexpr int PA_HEADS = 16;       // query heads of a workgroup
 constexpr int PA_MIN = PA_W;       // tiles of the shortest chunk: one a wave
 // Chunks that the rows are cut into: as many as the chip holds for few rows, twice that
 // for many, whose own ends then even out.
-constexpr int PA_TARGET = 1024, PA_FEW = 256;
+constexpr int PA_TARGET = 1536, PA_FEW = 256;
 
 static size_t al256(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -163,28 +163,32 @@ __device__ __forceinline__ bool find_chunk(const PageDims& pg, const PrefixView&
     total *= mult;
   }
   const int size = chunk_tiles(total, gridDim.x - pg.n_seq * pg.G);
+  // the rows of several chunks first, then the others, which even out the end
   int base = 0;
-  for (int u0 = 0; u0 < units; u0 += 64) {
-    const int n = u0 ? tiles(u0 + lane) : first;
-    const int c = n ? chunks_of(n, size) * mult : 0;
-    const int to = scan_wave(c);       // at most the grid: no overflow
-    const int all = base + __builtin_amdgcn_readlane(to, 63);
-    if (bid < all) {
-      const int at = __popcll(__ballot(base + to <= bid));       // the unit's lane
-      const int u = u0 + at;
-      const int tn = __builtin_amdgcn_readlane(n, at), chunks = chunks_of(tn, size);
-      const int local = bid - base - (__builtin_amdgcn_readlane(to, at) - chunks * mult);
-      out.b = PREFIX ? u / pg.G : u;
-      out.g = PREFIX ? u % pg.G : local / chunks;
-      out.c = PREFIX ? local : local % chunks;
-      out.chunks = chunks;
-      const int each = tn / chunks, more = tn % chunks;            // the first `more` take one more
-      out.t0 = out.c * each + min(out.c, more);
-      out.t1 = out.t0 + each + (out.c < more);
-      return true;
+#pragma unroll 1
+  for (int many = 1; many >= 0; --many)
+    for (int u0 = 0; u0 < units; u0 += 64) {
+      const int n = u0 ? tiles(u0 + lane) : first;
+      int c = n ? chunks_of(n, size) : 0;
+      c = (c > 1) == many ? c * mult : 0;
+      const int to = scan_wave(c);     // at most the grid: no overflow
+      const int all = base + __builtin_amdgcn_readlane(to, 63);
+      if (bid < all) {
+        const int at = __popcll(__ballot(base + to <= bid));       // the unit's lane
+        const int u = u0 + at;
+        const int tn = __builtin_amdgcn_readlane(n, at), chunks = chunks_of(tn, size);
+        const int local = bid - base - (__builtin_amdgcn_readlane(to, at) - chunks * mult);
+        out.b = PREFIX ? u / pg.G : u;
+        out.g = PREFIX ? u % pg.G : local / chunks;
+        out.c = PREFIX ? local : local % chunks;
+        out.chunks = chunks;
+        const int each = tn / chunks, more = tn % chunks;            // the first `more` take one more
+        out.t0 = out.c * each + min(out.c, more);
+        out.t1 = out.t0 + each + (out.c < more);
+        return true;
+      }
+      base = all;
     }
-    base = all;
-  }
   return false;
 }
 
@@ -225,67 +229,95 @@ __global__ __launch_bounds__(PA_T, PA_OCC) void k_paged(PageDims pg, int64_t q_t
     qv[s] = i16 < heads ? *(const uint4*)(q + seq * q_tok + ((int64_t)kv * pg.hpg + h0 + i16) * D + (4 * s + g4) * E)
                         : make_uint4(0, 0, 0, 0);
 
-  struct Tile {
-    uint4 k[NS][KC];
-    uint32_t v[NS][4][VB][VW];
-    float lm[PREFIX ? NS : 1][4]; // log m of packed entries
-    int n[NS];                    // entries there are
+  // One tile's keys and values: the next tile's keys are asked for when the products with
+  // the present ones are formed, the next values likewise, so the registers of one tile
+  // keep a tile's loads in flight nearly all the time and leave room for a third wave.
+  uint4 tk[NS][KC];
+  uint32_t tv[NS][4][VB][VW];
+  float lm[PREFIX ? NS : 1][4];   // log m of packed entries
+  struct Where {                  // of a tile, the same for the wave: elements, entries there are
+    int64_t at[NS], lm;
+    int n[NS];
     bool packed;
   };
   const int32_t* tab = table + (int64_t)seq * pg.width;
-  // 16 keys and values from kb, vb (the same for the wave): key row rk of the lane, value row rv(r)
-  auto rows16 = [&](Tile& t, int h, const char* kb, const char* vb, uint32_t rk, auto rv) __attribute__((always_inline)) {
-    constexpr uint32_t RB = D * sizeof(T);
-#pragma unroll
-    for (int s = 0; s < KC; ++s) t.k[h][s] = *(const uint4*)(kb + (rk * RB + 16 * g4) + 64 * s);
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-#pragma unroll
-      for (int p = 0; p < VB; ++p) {
-        const char* x = vb + (rv(r) * RB + VD * sizeof(T) * i16) + 64 * sizeof(T) * p;
-        if constexpr (VW == 4) {
-          const uint4 u = *(const uint4*)x;
-          t.v[h][r][p][0] = u.x; t.v[h][r][p][1] = u.y; t.v[h][r][p][2] = u.z; t.v[h][r][p][3] = u.w;
-        } else {
-          const uint2 u = *(const uint2*)x;
-          t.v[h][r][p][0] = u.x; t.v[h][r][p][1] = u.y;
-        }
-      }
-  };
-  auto fetch = [&](Tile& t, int ti) __attribute__((always_inline)) {
-    t.packed = PREFIX && ti < pack_tiles;
+  auto where = [&](int ti) __attribute__((always_inline)) {
+    Where r;
+    r.packed = PREFIX && ti < pack_tiles;
+    r.lm = 0;
 #pragma unroll
     for (int h = 0; h < NS; ++h) {
-      const int64_t e = (int64_t)(t.packed ? ti : ti - pack_tiles) * TILE + 16 * h;
-      int64_t left = (t.packed ? n_pack : n_page) - e, at = 0;
-      if (!t.packed && left > 0) {
+      const int64_t e = (int64_t)(r.packed ? ti : ti - pack_tiles) * TILE + 16 * h;
+      int64_t left = (r.packed ? n_pack : n_page) - e, at = 0;
+      if (!r.packed && left > 0) {
         at = page_row(pg, tab[e >> pg.shift], kv, (int)(e & (((int64_t)1 << pg.shift) - 1)));
         if (at < 0) left = 0;
-      } else if (t.packed) {
+      } else if (r.packed) {
         at = (p_start + e) * D;
+        if (h == 0) r.lm = p_start + e;
       }
-      const int n = left > 16 ? 16 : (left < 0 ? 0 : (int)left);
-      t.n[h] = n;
-      const char* kb = (const char*)((t.packed ? PK : Kp) + at);
-      const char* vb = (const char*)((t.packed ? PV : Vp) + at);
-      if (n == 0) {
+      r.n[h] = left > 16 ? 16 : (left < 0 ? 0 : (int)left);
+      r.at[h] = at;
+    }
+    return r;
+  };
+  // a page holds all 16 rows, written or not; the packed arrays may end behind the last
+  // entry, which absent ones read in place of their own
+  constexpr uint32_t RB = D * sizeof(T);
+  auto load_keys = [&](const Where& t) __attribute__((always_inline)) {
 #pragma unroll
-        for (int s = 0; s < KC; ++s) t.k[h][s] = make_uint4(0, 0, 0, 0);
+    for (int h = 0; h < NS; ++h) {
+      if (t.n[h] == 0) {
+#pragma unroll
+        for (int s = 0; s < KC; ++s) tk[h][s] = make_uint4(0, 0, 0, 0);
+        continue;
+      }
+      const char* base = (const char*)((t.packed ? PK : Kp) + t.at[h]);
+      const uint32_t r = PREFIX && t.packed ? min(i16, t.n[h] - 1) : i16;
+#pragma unroll
+      for (int s = 0; s < KC; ++s) tk[h][s] = *(const uint4*)(base + (r * RB + 16 * g4) + 64 * s);
+    }
+  };
+  auto load_values = [&](const Where& t) __attribute__((always_inline)) {
+#pragma unroll
+    for (int h = 0; h < NS; ++h) {
+      if (t.n[h] == 0) {
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
           for (int p = 0; p < VB; ++p)
 #pragma unroll
-            for (int x = 0; x < VW; ++x) t.v[h][r][p][x] = 0;
-      } else if (PREFIX && t.packed && n < 16) {       // the arrays may end here: absent entries read the last one
-        rows16(t, h, kb, vb, min(i16, n - 1), [&](int r) { return (uint32_t)min(4 * g4 + r, n - 1); });
-      } else {                    // a page holds all 16, written or not
-        rows16(t, h, kb, vb, i16, [&](int r) { return (uint32_t)(4 * g4 + r); });
+            for (int x = 0; x < VW; ++x) tv[h][r][p][x] = 0;
+      } else {
+        const char* base = (const char*)((t.packed ? PV : Vp) + t.at[h]);
+        auto rows = [&](auto row) __attribute__((always_inline)) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int p = 0; p < VB; ++p) {
+              const char* x = base + (row(r) * RB + VD * sizeof(T) * i16) + 64 * sizeof(T) * p;
+              if constexpr (VW == 4) {
+                const uint4 u = *(const uint4*)x;
+                tv[h][r][p][0] = u.x; tv[h][r][p][1] = u.y; tv[h][r][p][2] = u.z; tv[h][r][p][3] = u.w;
+              } else {
+                const uint2 u = *(const uint2*)x;
+                tv[h][r][p][0] = u.x; tv[h][r][p][1] = u.y;
+              }
+            }
+        };
+        if (PREFIX && t.packed && t.n[h] < 16) rows([&](int r) { return (uint32_t)min(4 * g4 + r, t.n[h] - 1); });
+        else rows([&](int r) { return (uint32_t)(4 * g4 + r); });
       }
       if constexpr (PREFIX) {
-        if (t.packed)
+        if (t.packed) {
+          const float* lp = px.logm + (t.lm + 16 * h) + 4 * g4;
+          if (t.n[h] == 16) {
+            __builtin_memcpy(lm[h], lp, 16);
+          } else {
 #pragma unroll
-          for (int r = 0; r < 4; ++r) t.lm[h][r] = 4 * g4 + r < n ? px.logm[p_start + e + 4 * g4 + r] : -INFINITY;
+            for (int r = 0; r < 4; ++r) lm[h][r] = 4 * g4 + r < t.n[h] ? lp[r] : -INFINITY;
+          }
+        }
       }
     }
   };
@@ -297,7 +329,16 @@ __global__ __launch_bounds__(PA_T, PA_OCC) void k_paged(PageDims pg, int64_t q_t
     for (int j = 0; j < VD; ++j) o[p][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;               // of head i16; l: this lane's entries only
 
-  auto fold = [&](Tile& t) __attribute__((always_inline)) {
+  int ti = ck.t0 + w;
+  Where now{}, next{};
+  if (ti < ck.t1) {
+    now = where(ti);
+    load_keys(now);
+    load_values(now);
+  }
+  for (; ti < ck.t1; ti += PA_W) {
+    const bool more = ti + PA_W < ck.t1;
+    if (more) next = where(ti + PA_W);
     float x[NS][4];
 #pragma unroll
     for (int h = 0; h < NS; ++h) {
@@ -305,9 +346,9 @@ __global__ __launch_bounds__(PA_T, PA_OCC) void k_paged(PageDims pg, int64_t q_t
 #pragma unroll
       for (int s = 0; s < KC; ++s) {
         if constexpr (BF) {
-          acc = mfma_bf16_16x16x32(pk8(t.k[h][s]), pk8(qv[s]), acc);
+          acc = mfma_bf16_16x16x32(pk8(tk[h][s]), pk8(qv[s]), acc);
         } else {
-          const uint32_t a[4] = {t.k[h][s].x, t.k[h][s].y, t.k[h][s].z, t.k[h][s].w};
+          const uint32_t a[4] = {tk[h][s].x, tk[h][s].y, tk[h][s].z, tk[h][s].w};
           const uint32_t b[4] = {qv[s].x, qv[s].y, qv[s].z, qv[s].w};
 #pragma unroll
           for (int i = 0; i < 4; ++i) acc = mfma_f32_16x16x4(__uint_as_float(a[i]), __uint_as_float(b[i]), acc);
@@ -316,27 +357,35 @@ __global__ __launch_bounds__(PA_T, PA_OCC) void k_paged(PageDims pg, int64_t q_t
 #pragma unroll
       for (int r = 0; r < 4; ++r) x[h][r] = acc[r] * scale;
     }
-    bool all = !t.packed;
+    if (more) load_keys(next);
+    bool all = !now.packed;
 #pragma unroll
-    for (int h = 0; h < NS; ++h) all &= t.n[h] == 16;
+    for (int h = 0; h < NS; ++h) all &= now.n[h] == 16;
     if (!all) {                   // absent entries and those masked by their log m
+      bool none[NS][4], any = false;
 #pragma unroll
       for (int h = 0; h < NS; ++h)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          bool none = 4 * g4 + r >= t.n[h];
-          if (PREFIX && t.packed) {
-            none = t.lm[h][r] == -INFINITY;
-            x[h][r] += t.lm[h][r];
+          none[h][r] = 4 * g4 + r >= now.n[h];
+          if (PREFIX && now.packed) {
+            none[h][r] = lm[h][r] == -INFINITY;
+            x[h][r] += lm[h][r];
           }
-          if (none) {             // 0 times an infinity is not 0
-            x[h][r] = -INFINITY;
+          any |= none[h][r];
+        }
+      if (__any(any)) {
+#pragma unroll
+        for (int h = 0; h < NS; ++h)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            x[h][r] = none[h][r] ? -INFINITY : x[h][r];
 #pragma unroll
             for (int p = 0; p < VB; ++p)
 #pragma unroll
-              for (int i = 0; i < VW; ++i) t.v[h][r][p][i] = 0;
+              for (int i = 0; i < VW; ++i) tv[h][r][p][i] = none[h][r] ? 0 : tv[h][r][p][i];     // 0 times an infinity is not 0
           }
-        }
+      }
     }
     float mx = x[0][0];
 #pragma unroll
@@ -383,7 +432,7 @@ __global__ __launch_bounds__(PA_T, PA_OCC) void k_paged(PageDims pg, int64_t q_t
         for (int h = 0; h < NS; ++h)
 #pragma unroll
           for (int r = 0; r < 2; ++r)
-            a[h][r] = __builtin_amdgcn_perm(t.v[h][2 * r + 1][0][j / 2], t.v[h][2 * r][0][j / 2], sel);
+            a[h][r] = __builtin_amdgcn_perm(tv[h][2 * r + 1][0][j / 2], tv[h][2 * r][0][j / 2], sel);
         if constexpr (NS == 2)
           o[0][j] = mfma_bf16_16x16x32(pk8(make_uint4(a[0][0], a[0][1], a[1][0], a[1][1])),
                                        pk8(make_uint4(pb[0][0], pb[0][1], pb[1][0], pb[1][1])), o[0][j]);
@@ -399,23 +448,12 @@ __global__ __launch_bounds__(PA_T, PA_OCC) void k_paged(PageDims pg, int64_t q_t
           for (int p = 0; p < VB; ++p)
 #pragma unroll
             for (int j = 0; j < VD; ++j)
-              o[p][j] = mfma_f32_16x16x4(__uint_as_float(t.v[h][r][p][j]), pr[h][r], o[p][j]);
+              o[p][j] = mfma_f32_16x16x4(__uint_as_float(tv[h][r][p][j]), pr[h][r], o[p][j]);
     }
-  };
-
-  // the next tile in flight while one is folded in; two places that take turns
-  Tile ta, tb;
-  const int end = ck.t1;
-  int ti = ck.t0 + w;
-  if (ti < end) fetch(ta, ti);
-  while (ti < end) {
-    if (ti + PA_W < end) fetch(tb, ti + PA_W);
-    fold(ta);
-    ti += PA_W;
-    if (ti >= end) break;
-    if (ti + PA_W < end) fetch(ta, ti + PA_W);
-    fold(tb);
-    ti += PA_W;
+    if (more) {
+      load_values(next);
+      now = next;
+    }
   }
 #pragma unroll
   for (int p = 0; p < VB; ++p)
