@@ -402,7 +402,7 @@ typedef struct {
   int32_t dtype, G, H, d;           /* gracekv_dtype, KV heads, query heads, head dim */
   int32_t n_seq;                    /* sequences */
   int32_t reserved;                 /* 0 */
-  int64_t n_q, n_k;                 /* rows of Q and out; rows of K and V (below 2^31) */
+  int64_t n_q, n_k;                 /* rows of Q and out; rows of K and V (at most 2^30) */
   int64_t q_tok, q_head, k_tok, k_head, v_tok, v_head, out_tok, out_head; /* strides */
 } gracekv_prompt_config;
 
@@ -487,7 +487,9 @@ typedef struct {
  *   seq_len    [n_seq] int32, held to [0, table_width * page_size]
  *   prefix     host structure, read by the call, or NULL
  *   out        [n_seq][H][d] (cfg->dtype); lse [n_seq][H] fp32 or NULL
- *   ws         gracekv_paged_ws_bytes bytes; calls that overlap on one workspace race */
+ *   ws         gracekv_paged_ws_bytes bytes, which need no initialisation; calls that
+ *              overlap on one workspace race, and what they leave in it has to be cleared
+ * Lengths, counts and tables must not change while the call runs. */
 gracekv_status gracekv_paged_attention(const gracekv_page_config* cfg, const void* q, int64_t q_tok, const void* K_pages,
                                        const void* V_pages, const int32_t* block_table, const int32_t* seq_len,
                                        const gracekv_prefix* prefix, void* out, float* lse, void* ws, size_t ws_bytes,

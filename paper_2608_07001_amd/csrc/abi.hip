@@ -584,7 +584,7 @@ static bool stride_ok(int dtype, int64_t s) { return s >= 0 && s % (dtype == GRA
 static gracekv_status prompt_dims(const gracekv_prompt_config* c, PromptDims* pd) {
   if (!c) return GRACEKV_ERR_INVALID_ARG;
   if (!heads_ok(c->dtype, c->G, c->H, c->n_seq) || c->reserved != 0) return GRACEKV_ERR_INVALID_ARG;
-  if (c->n_q < 0 || c->n_k < 0 || c->n_q > 0x7fffffff || c->n_k > 0x7fffffff) return GRACEKV_ERR_INVALID_ARG;
+  if (c->n_q < 0 || c->n_k < 0 || c->n_q > 1 << 30 || c->n_k > 1 << 30) return GRACEKV_ERR_INVALID_ARG;
   for (int64_t s : {c->q_tok, c->q_head, c->k_tok, c->k_head, c->v_tok, c->v_head, c->out_tok, c->out_head})
     if (!stride_ok(c->dtype, s)) return GRACEKV_ERR_INVALID_ARG;
   if ((c->out_tok == 0 && c->n_q > 1) || (c->out_head == 0 && c->H > 1)) return GRACEKV_ERR_INVALID_ARG;   // rows on rows

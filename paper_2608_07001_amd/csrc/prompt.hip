@@ -30,7 +30,6 @@ namespace gkv {
 
 constexpr int PR_T = 256;
 constexpr int PR_W = PR_T / 64;
-constexpr int PB_T = 256, PB_W = PB_T / 64, PB_OCC = 3, PB_KEYS = 32;     // bf16
 constexpr int PR_FILL = 512;       // workgroups that the keys of few rows are split into
 constexpr float PR_LAG = 8.f;      // base-2 units
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
@@ -46,8 +45,10 @@ __device__ __forceinline__ void mfma_done16(f32x16& x, f32x16& y) { asm volatile
 
 static size_t al256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-template <bool BF> constexpr int tile_rows() { return BF ? 32 * PB_W : 16 * PR_W; }
-template <bool BF> constexpr int tile_keys() { return BF ? PB_KEYS : 32; }
+// Rows and keys of a workgroup's tile: SPLIT of its waves have the same rows, with 32 keys
+// each of a key tile (bf16: 32 rows a wave; fp32: 16)
+template <bool BF, int SPLIT> constexpr int tile_rows() { return (BF ? 32 : 16) * PR_W / SPLIT; }
+template <int SPLIT> constexpr int tile_keys() { return 32 * SPLIT; }
 
 // Row tiles of all sequences: sequence b's begin at cu_q[b] * hpg / rows + b, which
 // leaves each at least as many as it needs whatever the lengths are; one sequence alone
@@ -57,19 +58,40 @@ GKV_HD int row_tiles(const PromptDims& pd, int rows) {
   return pd.n_seq > 1 ? (int)(n / rows) + pd.n_seq : (int)((n + rows - 1) / rows);
 }
 
-// Parts that every row tile's keys are cut into: one where the tiles fill the chip twice
-// over, more where they are few, each part holding at least 256 keys of the longest row.
-static int prompt_parts(const PromptDims& pd) {
-  const int rows = pd.dtype == GRACEKV_BF16 ? tile_rows<true>() : tile_rows<false>();
-  const int64_t tiles = (int64_t)row_tiles(pd, rows) * pd.G;
-  const int64_t want = tiles ? (PR_FILL + tiles - 1) / tiles : 1, most = (pd.n_k + 255) / 256;
-  return (int)(want < 1 ? 1 : (want > most ? (most < 1 ? 1 : most) : want));
+// The kernel and the parts that every row tile's keys are cut into.
+struct Plan {
+  bool split;                  // waves share rows
+  int rows, parts;
+};
+static Plan prompt_plan(const PromptDims& pd) {
+  const bool bf = pd.dtype == GRACEKV_BF16;
+  auto tiles = [&](int rows) { return (int64_t)row_tiles(pd, rows) * pd.G; };
+  constexpr int ROWS = tile_rows<true, 1>(), FEW = tile_rows<true, 2>();
+  Plan p;
+  // Short prompts that leave the chip part empty are bound by the way along the keys, which
+  // waves in pairs halve; the tiles of 64 rows have to fill the chip without further parts,
+  // and their keys be few, for a long way is walked faster by single waves.  One prompt of
+  // the 8B heads, single and paired: 1024 tokens 33.2 and 26.6 us, 1536 47.4 and 40.7, 2048
+  // 55.0 and 63.0 (d = 64: 41.5 and 31.4), 512 tokens, too few for either, 21.3 and 22.2;
+  // 64 queries over 32K keys 62.7 and 73.4.
+  p.split = bf && tiles(FEW) >= PR_FILL && tiles(ROWS) < (pd.d == 128 ? PR_FILL : 2 * PR_FILL) && pd.n_k <= 2048;
+  p.rows = bf ? (p.split ? FEW : ROWS) : tile_rows<false, 1>();
+  // One part where the tiles fill the chip (bf16: twice over; fp32, whose key tiles take
+  // four times as long: three times, 1056 tokens of the 8B heads 134 -> 111 us; the same in
+  // bf16 slows 1024 tokens down, 27 -> 39), more where they are few, each part holding at
+  // least so many keys of the longest row that joining it is worth it (bf16 with 128: 256
+  // tokens 12 -> 17 us; fp32 with 256: 300 tokens 27 -> 30).
+  const int64_t n = tiles(p.rows), fill = bf ? PR_FILL : PR_FILL + PR_FILL / 2, keys = bf ? 256 : 128;
+  const int64_t want = n ? (fill + n - 1) / n : 1, most = (pd.n_k + keys - 1) / keys;
+  p.parts = (int)(want < 1 ? 1 : (want > most ? (most < 1 ? 1 : most) : want));
+  return p;
 }
 int64_t prompt_items(const PromptDims& pd) {
-  return (int64_t)row_tiles(pd, pd.dtype == GRACEKV_BF16 ? tile_rows<true>() : tile_rows<false>()) * prompt_parts(pd) * pd.G;
+  const Plan p = prompt_plan(pd);
+  return (int64_t)row_tiles(pd, p.rows) * p.parts * pd.G;
 }
 size_t prompt_ws_bytes(const PromptDims& pd) {
-  const int P = prompt_parts(pd);
+  const int P = prompt_plan(pd).parts;
   if (P == 1) return 0;
   const size_t n = (size_t)P * pd.n_q * pd.H;
   return al256(n * 8) + n * pd.d * 4;
@@ -177,34 +199,34 @@ template <int D> __device__ __forceinline__ int swz(int t, int c) {
   else return t * 8 + (c ^ ((((t >> 1) & 1) << 2) | ((t >> 2) & 3)));
 }
 
-template <int D>
-__global__ __launch_bounds__(PB_T, PB_OCC) void k_prompt_bf(PromptDims pd, int parts, const uint16_t* __restrict__ q,
+template <int D, int SPLIT>
+__global__ __launch_bounds__(PR_T, 3) void k_prompt_bf(PromptDims pd, int parts, const uint16_t* __restrict__ q,
                                                        const uint16_t* __restrict__ k, const uint16_t* __restrict__ v,
                                                        const int32_t* __restrict__ cu_q, const int32_t* __restrict__ cu_k,
                                                        uint16_t* __restrict__ out, float* __restrict__ lse,
                                                        float2* __restrict__ pml, float* __restrict__ po) {
-  constexpr int ROWS = tile_rows<true>(), KEYS = tile_keys<true>();
+  constexpr int ROWS = tile_rows<true, SPLIT>(), KEYS = tile_keys<SPLIT>();
   constexpr int CH = D / 8;                     // 16-byte pieces of a row
   constexpr int RI = 64 / CH;                   // rows that one load of a wave brings
-  constexpr int NI = KEYS / RI / PB_W;          // such loads of a wave and array
+  constexpr int NI = KEYS / RI / PR_W;          // such loads of a wave and array
   constexpr int KS = D / 16;                    // product steps over the dims
   constexpr int DT = D / 32;                    // 32-dim tiles of the output
-  constexpr int NB = KEYS / 32;                 // 32-key blocks of a tile
   // arrays of their own, so that loads into one tile and reads of the other are told apart
-  __shared__ uint4 sK0[KEYS * CH], sK1[KEYS * CH], sV0[KEYS * CH], sV1[KEYS * CH];
+  __shared__ __align__(16) uint4 sK0[KEYS * CH], sK1[KEYS * CH], sV0[KEYS * CH], sV1[KEYS * CH];
   __shared__ int bad;
   Item it;
   if (!find_item<ROWS, KEYS>(pd, cu_q, cu_k, parts, it)) return;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i32 = lane & 31, half = lane >> 5;
+  const int rw = w / SPLIT, kw = w % SPLIT;     // the wave's 32 rows, its 32 keys of a tile
   const int off = it.lk - it.lq;                // query i sees the keys up to i + off
   // the lane's row
   const uint32_t hpg = (uint32_t)pd.hpg;
-  const int row = it.r0 + 32 * w + i32, rowc = row < it.rows ? row : it.rows - 1;
+  const int row = it.r0 + 32 * rw + i32, rowc = row < it.rows ? row : it.rows - 1;
   const int tok = (int)((uint32_t)rowc / hpg);
   const int head = it.g * pd.hpg + (rowc - tok * pd.hpg);
   const int see = tok + off;                    // its last key
   // what the wave's and the workgroup's rows see
-  const int wr0 = it.r0 + 32 * w, wr1 = min(wr0 + 31, it.rows - 1);
+  const int wr0 = it.r0 + 32 * rw, wr1 = min(wr0 + 31, it.rows - 1);
   const int w_all = (int)((uint32_t)min(wr0, it.rows - 1) / hpg) + off;
   const int w_any = wr0 < it.rows ? (int)((uint32_t)wr1 / hpg) + off : -1;
   const int g_all = (int)((uint32_t)it.r0 / hpg) + off;
@@ -225,11 +247,11 @@ __global__ __launch_bounds__(PB_T, PB_OCC) void k_prompt_bf(PromptDims pd, int p
 
   const uint16_t* kp = k + it.k0 * pd.k_tok + it.g * pd.k_head;
   const uint16_t* vp = v + it.k0 * pd.v_tok + it.g * pd.v_head;
-  // Load i of a wave brings rows RI (w + PB_W i) .. + RI - 1 straight into LDS, lane l to
+  // Load i of a wave brings rows RI (w + PR_W i) .. + RI - 1 straight into LDS, lane l to
   // the l-th 16 bytes: the piece that swz() puts there
   const int lr = RI * w + lane / CH, lc = swz<D>(lr, lane % CH) - lr * CH;
-  const int k_off = (int)(lr * pd.k_tok * 2) + lc * 16, k_step = (int)(RI * PB_W * pd.k_tok * 2);
-  const int v_off = (int)(lr * pd.v_tok * 2) + lc * 16, v_step = (int)(RI * PB_W * pd.v_tok * 2);
+  const int k_off = (int)(lr * pd.k_tok * 2) + lc * 16, k_step = (int)(RI * PR_W * pd.k_tok * 2);
+  const int v_off = (int)(lr * pd.v_tok * 2) + lc * 16, v_step = (int)(RI * PR_W * pd.v_tok * 2);
   auto load = [&](int t, uint4* dK, uint4* dV) {
     const int64_t j0 = (int64_t)t * KEYS;
     const int n = min(it.lk - t * KEYS, KEYS);   // at least one
@@ -237,8 +259,8 @@ __global__ __launch_bounds__(PB_T, PB_OCC) void k_prompt_bf(PromptDims pd, int p
     const Buffer vb = tile_buffer<uint16_t, D>(vp + j0 * pd.v_tok, pd.v_tok, n);
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-      buffer_load_lds(kb, dK + 64 * (w + PB_W * i), k_off + i * k_step);
-      buffer_load_lds(vb, dV + 64 * (w + PB_W * i), v_off + i * v_step);
+      buffer_load_lds(kb, dK + 64 * (w + PR_W * i), k_off + i * k_step);
+      buffer_load_lds(vb, dV + 64 * (w + PR_W * i), v_off + i * v_step);
     }
   };
   // Where the lane reads in a tile, in bytes: piece 2 x + half of key row i32 lies at
@@ -257,40 +279,30 @@ __global__ __launch_bounds__(PB_T, PB_OCC) void k_prompt_bf(PromptDims pd, int p
     if (j0 + (KEYS - 1) > g_all) {              // values that are not finite: see above
       bool any = false;
 #pragma unroll
-      for (int i = 0; i < KEYS * CH / PB_T; ++i) cV[tid + PB_T * i] = finite<true>(cV[tid + PB_T * i], any);
+      for (int i = 0; i < KEYS * CH / PR_T; ++i) cV[tid + PR_T * i] = finite<true>(cV[tid + PR_T * i], any);
       if (any) bad = 1;
       sync_after_lds_stores();
     }
     if (t + 1 < it.t1) load(t + 1, nK, nV);
-    if (j0 > w_any) return;
-    f32x16 s[NB];
+    const int k0 = j0 + 32 * kw;                 // the wave's keys
+    if (k0 > w_any) return;
+    f32x16 s;
     asm volatile("" : "+v"(k_at));               // eight places: formed anew, not held in registers
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
+    for (int r = 0; r < 16; ++r) s[r] = 0.f;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[b][r] = 0.f;
+    for (int x = 0; x < KS; ++x) s = mfma_bf16_32x32x16(lds_at(cK, (k_at ^ (32 * x)) + 32 * kw * RB), qv[x], s);
+    reads_ahead<KS, 1, 4>();
+    mfma_done16(s);
+    // register r: key 8 (r / 4) + 4 half + r % 4
+    if (k0 + 31 > w_all) {
+      const int rel = see - k0 - 4 * half;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = 8 * (r / 4) + r % 4 > rel ? -INFINITY : s[r];
     }
+    float mx = s[0];
 #pragma unroll
-    for (int x = 0; x < KS; ++x)
-#pragma unroll
-      for (int b = 0; b < NB; ++b) s[b] = mfma_bf16_32x32x16(lds_at(cK, (k_at ^ (32 * x)) + 32 * b * RB), qv[x], s[b]);
-    // LDS reads four products ahead
-    reads_ahead<KS * NB, 1, 4>();
-#pragma unroll
-    for (int b = 0; b < NB; ++b) mfma_done16(s[b]);
-    // register r of block b: key 32 b + 8 (r / 4) + 4 half + r % 4
-    if (j0 + (KEYS - 1) > w_all) {
-      const int rel = see - j0 - 4 * half;
-#pragma unroll
-      for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[b][r] = 32 * b + 8 * (r / 4) + r % 4 > rel ? -INFINITY : s[b][r];
-    }
-    float mx = s[0][0];
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[b][r]);
+    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
     {
       const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
       mx = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1])) * sc2;
@@ -306,27 +318,25 @@ __global__ __launch_bounds__(PB_T, PB_OCC) void k_prompt_bf(PromptDims pd, int p
       for (int d = 0; d < DT; ++d) o[d] *= c;
     }
     const float ms = m == -INFINITY ? 0.f : m;
-    uint4 pr[2 * NB];
+    uint4 pr[2];
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
+    for (int h = 0; h < 2; ++h) {
+      float e[8];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        float e[8];
-#pragma unroll
-        for (int r = 0; r < 8; ++r) e[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][8 * h + r], sc2, -ms));
-        l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
-        pr[2 * b + h] = make_uint4(pack_bf16(e[0], e[1]), pack_bf16(e[2], e[3]), pack_bf16(e[4], e[5]), pack_bf16(e[6], e[7]));
-      }
+      for (int r = 0; r < 8; ++r) e[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * h + r], sc2, -ms));
+      l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+      pr[h] = make_uint4(pack_bf16(e[0], e[1]), pack_bf16(e[2], e[3]), pack_bf16(e[4], e[5]), pack_bf16(e[6], e[7]));
+    }
     // product step x: keys 16 x + 8 (j / 4) + 4 half + j % 4 in place 8 half + j
 #pragma unroll
-    for (int x = 0; x < 2 * NB; ++x)
+    for (int x = 0; x < 2; ++x)
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
-        const uint2 a = lds_read_tr(cV, (v_at ^ (64 * d)) + 16 * x * RB);
-        const uint2 b = lds_read_tr(cV, (v_at ^ (64 * d + 32)) + (16 * x + 8) * RB);
+        const uint2 a = lds_read_tr(cV, (v_at ^ (64 * d)) + (32 * kw + 16 * x) * RB);
+        const uint2 b = lds_read_tr(cV, (v_at ^ (64 * d + 32)) + (32 * kw + 16 * x + 8) * RB);
         o[d] = mfma_bf16_32x32x16(make_uint4(a.x, a.y, b.x, b.y), pr[x], o[d]);
       }
-    reads_ahead<2 * NB * DT, 2, 3>();
+    reads_ahead<2 * DT, 2, 3>();
   };
   if (tid == 0) bad = 0;
   if (it.t0 < it.t1) load(it.t0, sK0, sV0);
@@ -337,6 +347,32 @@ __global__ __launch_bounds__(PB_T, PB_OCC) void k_prompt_bf(PromptDims pd, int p
 #pragma unroll
   for (int d = 0; d < DT; ++d) mfma_done16(o[d]);
   sync_after_lds_stores();
+  if constexpr (SPLIT == 2) {                   // the second wave of a pair to the first, through the tiles' LDS
+    static_assert(PR_W / SPLIT == 2 && KEYS * CH * 16 >= 64 * 4 * 16 * DT, "an array for each pair");
+    __shared__ float2 sml[PR_W / SPLIT][64];
+    float* so = (float*)(rw == 0 ? sK0 : sK1);
+    if (kw == 1) {
+      sml[rw][lane] = make_float2(m, l);
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) so[64 * (16 * d + r) + lane] = o[d][r];
+    }
+    sync_after_lds_stores();
+    if (kw == 1) return;
+    const float2 x = sml[rw][lane];
+    const float mn = fmaxf(m, x.x);
+    const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn), g = x.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x.x - mn);
+    l = (f == 0.f && l == l ? 0.f : l * f) + (g == 0.f && x.y == x.y ? 0.f : x.y * g);       // NaN stays
+    m = mn;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float y = so[64 * (16 * d + r) + lane];
+        o[d][r] = (f == 0.f ? 0.f : o[d][r] * f) + (g == 0.f ? 0.f : y * g);
+      }
+  }
   // values that are not finite in partly seen tiles, for the rows that see them
   if (bad) {
     for (int j = max(max(g_all + 1, 0) / KEYS, it.t0) * KEYS; j < min(it.t1 * KEYS, it.lk); ++j)
@@ -384,7 +420,7 @@ __global__ __launch_bounds__(PR_T, 2) void k_prompt_f32(PromptDims pd, int parts
                                                         const int32_t* __restrict__ cu_q, const int32_t* __restrict__ cu_k,
                                                         float* __restrict__ out, float* __restrict__ lse,
                                                         float2* __restrict__ pml, float* __restrict__ po) {
-  constexpr int ROWS = tile_rows<false>(), KEYS = tile_keys<false>();
+  constexpr int ROWS = tile_rows<false, 1>(), KEYS = tile_keys<1>();
   constexpr int CH = D / 4, NL = KEYS * CH / PR_T, LD = D + 4;
   constexpr int KC = D / 16, VB = D / 64;
   __shared__ __align__(16) float sK[KEYS * LD], sV[KEYS * LD];
@@ -593,18 +629,23 @@ __global__ __launch_bounds__(PR_T) void k_prompt_combine(PromptDims pd, int part
 hipError_t launch_prompt(const PromptDims& pd, const void* q, const void* k, const void* v, const int32_t* cu_q,
                          const int32_t* cu_k, void* out, float* lse, void* ws, hipStream_t st) {
   if (pd.n_q == 0) return hipSuccess;
-  const int P = prompt_parts(pd);
+  const Plan plan = prompt_plan(pd);
+  const int P = plan.parts;
   float2* pml = P > 1 ? (float2*)ws : nullptr;
   float* po = P > 1 ? (float*)((char*)ws + al256((size_t)P * pd.n_q * pd.H * 8)) : nullptr;
   const bool bf = pd.dtype == GRACEKV_BF16;
   const dim3 grid((unsigned)prompt_items(pd));
-#define GKV_PROMPT(KERNEL, TT)                                                                                            \
-  hipLaunchKernelGGL(KERNEL, grid, dim3(bf ? PB_T : PR_T), 0, st, pd, P, (const TT*)q, (const TT*)k, (const TT*)v, cu_q, cu_k, (TT*)out, \
+#define GKV_PROMPT(TT, ...)                                                                                                  \
+  hipLaunchKernelGGL((__VA_ARGS__), grid, dim3(PR_T), 0, st, pd, P, (const TT*)q, (const TT*)k, (const TT*)v, cu_q, cu_k, (TT*)out, \
                      lse, pml, po)
   if (bf) {
-    if (pd.d == 128) GKV_PROMPT(k_prompt_bf<128>, uint16_t); else GKV_PROMPT(k_prompt_bf<64>, uint16_t);
+    if (plan.split) {
+      if (pd.d == 128) GKV_PROMPT(uint16_t, k_prompt_bf<128, 2>); else GKV_PROMPT(uint16_t, k_prompt_bf<64, 2>);
+    } else {
+      if (pd.d == 128) GKV_PROMPT(uint16_t, k_prompt_bf<128, 1>); else GKV_PROMPT(uint16_t, k_prompt_bf<64, 1>);
+    }
   } else {
-    if (pd.d == 128) GKV_PROMPT(k_prompt_f32<128>, float); else GKV_PROMPT(k_prompt_f32<64>, float);
+    if (pd.d == 128) GKV_PROMPT(float, k_prompt_f32<128>); else GKV_PROMPT(float, k_prompt_f32<64>);
   }
 #undef GKV_PROMPT
   const hipError_t e = hipGetLastError();

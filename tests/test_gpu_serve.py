@@ -96,6 +96,17 @@ def test_prompt_long(dtype, d):
     assert not _check_prompt(dtype, d, 8, 32, [1030, 1030], [1030, 1030], seed=10) or dtype == "f32"
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_prompt_waves_in_pairs(d):
+    # few short prompts of many heads: two waves to the same rows; odd ends, a row with no key, infinities
+    assert not _check_prompt("bf16", d, 8, 32, [700, 0, 3, 321, 1], [700, 0, 3, 321, 1], behind=2, seed=20)
+    assert not _check_prompt("bf16", d, 8, 40, [33, 500, 330], [1, 530, 330], "head", seed=21)
+
+    def edit(q, k, v):
+        v[417, 3, 5], v[40, 0, 1], v[-1, 7] = math.inf, math.nan, -math.inf
+    assert not _check_prompt("bf16", d, 8, 32, [418, 607], [418, 607], seed=22, edit=edit)
+
+
 @pytest.mark.parametrize("dtype,d", TYPES)
 @pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
 def test_prompt_masked_places_reach_nothing(dtype, d, bad):
@@ -439,6 +450,16 @@ def test_paged_malformed_inputs_stay_inside():
     c.pre["count"].clamp_(min=0)
     c.pre["count"] = torch.minimum(c.pre["count"], n - c.pre["start"])
     c.check((out, lse))
+
+
+@pytest.mark.parametrize("fill", [0, 1, 127, 255])
+def test_paged_workspace_needs_no_clearing(fill):
+    # whatever a workspace holds, also what calls of other shapes left in it; the same twice
+    a = Cache("bf16", 128, 2, 8, [4001, 3, 0, 900], 16, seed=20)
+    b = Cache("f32", 64, 1, 20, [60] * 40 + [3000], 16, [5] * 41, seed=21)
+    ws = torch.full((8 << 20,), fill, dtype=torch.uint8, device="cuda")
+    for c in (a, b, a, a, b):
+        c.check(c.call(ws=ws))
 
 
 def test_paged_every_batch_size():
