@@ -434,7 +434,7 @@ typedef struct {
   int32_t dtype, G, H, d;
   int32_t n_seq;
   int32_t page_size;                /* 16, 32, 64, 128 or 256 */
-  int32_t table_width;
+  int32_t table_width;              /* table_width * page_size <= 2^25; n_seq * G <= 65536 */
   int32_t reserved;                 /* 0 */
   int64_t n_pages, page_stride;     /* page_stride >= G * page_size * d, a multiple of 16 bytes */
 } gracekv_page_config;
@@ -471,7 +471,7 @@ gracekv_status gracekv_paged_ws_bytes(const gracekv_page_config* cfg, size_t* ws
  * arrays are entries of (sequence b, KV head g), with logits q.k / sqrt(d) + logm; an
  * entry with logm = -inf has no weight.  For one sequence these are gracekv_pack's
  * outputs as they stand: layer l takes start = offsets + l*G and count = counts + l*G.
- * Starts and counts that leave [0, rows] are held inside. */
+ * Starts and counts that leave [0, rows] are held inside, and counts to 2^25. */
 typedef struct {
   const int64_t* start;             /* [n_seq * G] */
   const int64_t* count;             /* [n_seq * G] */

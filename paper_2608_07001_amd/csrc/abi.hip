@@ -631,8 +631,8 @@ static gracekv_status page_dims(const gracekv_page_config* c, PageDims* pg) {
   if (c->page_stride < page || !stride_ok(c->dtype, c->page_stride) || c->n_pages > INT64_MAX / 4 / c->page_stride)
     return GRACEKV_ERR_INVALID_ARG;
   *pg = PageDims{c->dtype, c->G, c->H, c->d, c->H / c->G, c->n_seq, shift, c->table_width, c->n_pages, c->page_stride};
-  // groups of query heads in one launch; the tiles of 64 rows are counted in 31 bits
-  if ((int64_t)c->n_seq * c->G > (1 << 24) || c->H > 65535 || ((int64_t)c->table_width << shift) > PAGED_ROWS)
+  // rows (sequence, KV head) that every workgroup looks through, and their lengths (paged.hip)
+  if ((int64_t)c->n_seq * c->G > 65536 || c->H > 65536 || ((int64_t)c->table_width << shift) > PAGED_ROWS)
     return GRACEKV_ERR_UNSUPPORTED;
   return GRACEKV_OK;
 }
@@ -682,9 +682,8 @@ gracekv_status gracekv_paged_attention(const gracekv_page_config* c, const void*
   PrefixView px{nullptr, nullptr, nullptr, nullptr, nullptr, 0};
   if (prefix) {
     if (!prefix->start || !prefix->count || !prefix->K || !prefix->V || !prefix->logm || !aligned16(prefix->K) ||
-        !aligned16(prefix->V) || prefix->rows < 0)
+        !aligned16(prefix->V) || prefix->rows < 0 || prefix->rows > INT64_MAX / 1024)
       return GRACEKV_ERR_INVALID_ARG;
-    if (prefix->rows > PAGED_ROWS) return GRACEKV_ERR_UNSUPPORTED;
     px = PrefixView{prefix->start, prefix->count, prefix->K, prefix->V, prefix->logm, prefix->rows};
   }
   if (ws_bytes < paged_ws_bytes(pg)) return GRACEKV_ERR_WORKSPACE;

@@ -9,13 +9,20 @@
 // The work is a stream over keys and values, each read once for all query heads of its
 // group: bound by HBM.  Sequences differ in length, and how long they are is known on
 // the device only, so the split is made there: every row (b, g) is cut into tiles of 16
-// or 32 entries, a chunk is so many tiles that the chunks of all rows fill the chip
-// twice, and workgroup w finds its chunk by a scan over the rows' lengths.  A row of one
-// chunk is finished by its workgroup; the chunks of a longer one leave a partial state
-// each, and the workgroup that comes last joins them, in their order (Tickets).
-// (One line of all rows' tiles cut into equal pieces, rows beginning and ending anywhere
-// in them, was slower: 64 sequences of 1 to 8192 tokens 81 -> 114 us, for a workgroup then
-// has many short rows, one after the other.)
+// or 32 entries, a chunk is so many tiles that the chunks of all rows fill the chip once
+// (few rows) or twice, and every workgroup finds its chunk by a scan over the rows'
+// lengths.  A row of one chunk is finished by its workgroup; the chunks of a longer one
+// leave a partial state each, and the workgroup that comes last joins them, in their order
+// (Tickets).  (Joining in a second launch cost 64 ragged sequences 4 us of 81, the smallest
+// call 5 of 14; one line of all rows' tiles cut into equal pieces, rows beginning and ending
+// anywhere in them, 114 us instead of 81, for a workgroup then has many short rows, one
+// after the other, and the loop over them spills.)
+//
+// Measured (graph of 12 calls over three states): four caches of 128K tokens, 8 KV heads of
+// 128, 8 query heads each, 351 to 362 us for 2.01 GB, 5.6 to 5.7 TB/s (a copy moves 4.9, read
+// and write together); 64 sequences of 1 to 8192 tokens 73 us, 4.7 TB/s, of which about 11 us
+// are the way to the first byte and from the last; 24 compressed contexts of 2048 entries
+// a head 47 us; one of 512 entries a head 9.3 us, latency.
 //
 // A wave takes whole tiles.  Logits are formed transposed, S^T = K Q^T (entries x heads,
 // 16x16 matrix tiles, heads past the group's zero), keys straight from memory as the
@@ -23,7 +30,9 @@
 // layout of the second product O^T = V^T P^T: probabilities never cross lanes.  V^T needs
 // the same four entries of one dimension; a lane loads those entries' rows (16 bytes
 // each) and pairs the halves up in registers, row i of product j being dimension 8 i + j.
-// No LDS before the waves are merged.  For bf16 the probabilities are rounded to bf16
+// No LDS before the waves are merged, and one tile's registers serve the next (159 at d =
+// 128: three waves a SIMD; two tiles in turn took 236, two waves, and were 2 to 4 % slower).
+// For bf16 the probabilities are rounded to bf16
 // (nearest even) as the second product's operand, while their sum takes them unrounded:
 // each weight is off by at most 2^-9 of itself, at random, like the output's own rounding.
 // fp32 caches use the fp32 matrix instructions.
@@ -36,8 +45,10 @@ constexpr int PA_W = PA_T / 64;
 constexpr int PA_OCC = 3;          // waves a SIMD
 constexpr int PA_HEADS = 16;       // query heads of a workgroup
 constexpr int PA_MIN = PA_W;       // tiles of the shortest chunk: one a wave
-// Chunks that the rows are cut into: as many as the chip holds for few rows, twice that
-// for many, whose own ends then even out.
+// Chunks that the rows are cut into: as many as the chip holds (three workgroups a CU) for
+// few rows, twice that for many, whose own ends then even out.  Rows below PA_FEW count as
+// few: 192 rows of compressed contexts 47.0 us with 768, 51.8 with 1536; 512 rows of ragged
+// sequences 74.8 with 1024, 73.4 with 1536, 74.0 with 2048.
 constexpr int PA_TARGET = 1536, PA_FEW = 256;
 
 static size_t al256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -45,7 +56,7 @@ static size_t al256(size_t x) { return (x + 255) & ~(size_t)255; }
 // Workspace: a ticket word for every row and group of heads, then per chunk and head
 // (max, sum), then the partial sums [chunk][hpg][d].
 struct PagedWs {
-  long long* ticket;
+  unsigned long long* ticket;
   unsigned long long* ml;
   float* o;
   size_t bytes;
@@ -55,7 +66,7 @@ static PagedWs paged_view(void* base, const PageDims& pg) {
   char* p = (char*)base;
   PagedWs w;
   size_t o = 0;
-  w.ticket = (long long*)(p + o);
+  w.ticket = (unsigned long long*)(p + o);
   o += al256(R * ((pg.hpg + PA_HEADS - 1) / PA_HEADS) * 8);
   w.ml = (unsigned long long*)(p + o);
   o += al256(chunks * pg.hpg * 8);
@@ -66,22 +77,29 @@ static PagedWs paged_view(void* base, const PageDims& pg) {
 }
 size_t paged_ws_bytes(const PageDims& pg) { return paged_view(nullptr, pg).bytes; }
 
-// Tickets.  The chunks of a row count themselves in its word, from PA_BASE on; the one
-// that makes the count whole sets the word to 0 and joins.  Whatever a word holds before
-// is raised to PA_BASE first, so the workspace needs no clearing: every call leaves the
-// words it used at 0, and of other data only numbers above PA_BASE would count (as floats
-// or bf16 no numbers, of a pattern that arithmetic does not give; -1 and 0 are below).
+// Tickets.  The chunks of a row count themselves in its word, PA_BASE, PA_BASE + 1, ...;
+// the one that makes the count whole finds PA_BASE + parts - 1, and its counting sets the
+// word to 0.  What a word holds before is no count: anything below PA_BASE is raised to it
+// first, and counting on anything past the end gives 0, whoever did it counting again.
+// So the workspace needs no clearing, and every call leaves the words it used at 0.  (The
+// few numbers from PA_BASE on would be taken for a count; nothing leaves them but calls
+// that overlap.)
 // States are written and read with device-coherent operations, and a wait for the writes
 // stands between them and the ticket, so no fence is needed, which on this chip would
-// write back and invalidate the L2 of the XCD.  (Counting by compare-and-swap took 40
+// write back and invalidate the L2 of the XCD.  (Counting by compare-and-swap took the 40
 // chunks of a row 20 us, one after the other.)
-constexpr long long PA_BASE = 0x7fffffffffff0000ll;
-__device__ __forceinline__ bool last_of(long long* word, int parts) {
-  __hip_atomic_fetch_max(word, PA_BASE, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  const bool last = __hip_atomic_fetch_add(word, 1ll, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == PA_BASE + parts - 1;
-  if (last) __hip_atomic_store(word, 0ll, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  return last;
+constexpr unsigned long long PA_BASE = 0x7fffffffffff0000ull;
+__device__ __forceinline__ bool last_of(unsigned long long* word, int parts) {
+  const unsigned long long end = PA_BASE + parts - 1;
+  unsigned long long was;
+  do {
+    __hip_atomic_fetch_max(word, PA_BASE, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    was = __builtin_amdgcn_atomic_inc64((unsigned long*)word, end, __ATOMIC_RELAXED, "agent");
+  } while (was > end || was < PA_BASE);       // below: put to 0 by another between the two steps
+  return was == end;
 }
+// the thread's stores are where every other workgroup sees them
+__device__ __forceinline__ void stores_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ unsigned long long pair_bits(float a, float b) {
   return (unsigned long long)__float_as_uint(a) | (unsigned long long)__float_as_uint(b) << 32;
 }
@@ -97,13 +115,14 @@ __device__ __forceinline__ int tiles_of(int64_t len, int64_t count) {
   const int t = (int)((len + TILE - 1) / TILE) + (int)((count + TILE - 1) / TILE);
   return t > 0 ? t : 1;              // an empty row has a chunk, which writes its zeros
 }
-// (a row has below 2^24 tiles, by the sizes that the entry point takes)
+// a row has at most PAGED_ROWS tokens in pages and as many packed entries: 2^22 tiles, so that
+// those of 256 rows are counted in 31 bits
 __device__ __forceinline__ int64_t held_count(const PrefixView& px, int64_t row, int64_t& start) {
   int64_t s = px.start[row], c = px.count[row];
   s = s < 0 ? 0 : (s > px.rows ? px.rows : s);
   c = c < 0 ? 0 : (c > px.rows - s ? px.rows - s : c);
   start = s;
-  return c;
+  return c > PAGED_ROWS ? PAGED_ROWS : c;
 }
 
 // inclusive sum over the lanes of the wave
@@ -128,55 +147,86 @@ __device__ __forceinline__ int chunk_tiles(uint64_t total, int room) {
   const uint64_t size = total < 0x7fffffffu ? ((uint32_t)total + (uint32_t)room - 1) / (uint32_t)room : (total + room - 1) / room;
   return size < (uint64_t)PA_MIN ? PA_MIN : (size > 0x7fffffffu ? 0x7fffffff : (int)size);
 }
-// ... and chunks of a row
-__device__ __forceinline__ int chunks_of(int tiles, int size) {
-  return (int)(((uint32_t)tiles + (uint32_t)size - 1) / (uint32_t)size);
+// ... and chunks of a row, n / size upwards; inv: 1 / size or next to it (n below 2^24)
+__device__ __forceinline__ int chunks_of(int n, int size, float inv) {
+  int c = (int)((float)n * inv);
+  int left = n - c * size;
+  if (left < 0) { --c; left += size; }
+  else if (left >= size) { ++c; left -= size; }
+  return c + (left > 0);
 }
 
-// The chunk of workgroup blockIdx.x; false past the last.  Rows are looked at as units:
+// The chunk of place `bid` of `places`; false past the last.  Rows are looked at as units:
 // (b, g) where a prefix makes their lengths differ, b (G equal rows) otherwise.  Every
-// wave finds it by itself, 64 units at a time; over few units that is one load and a
-// scan without a barrier.
+// wave finds it by itself, 64 units at a time; over that few it takes one round of loads
+// and scans without a barrier.  With more units the waves share a first look at them all,
+// which is enough where no row needs a second chunk (4096 sequences of 64 tokens: 860 us
+// with the search, 403 without).
 template <int TILE, bool PREFIX>
-__device__ __forceinline__ bool find_chunk(const PageDims& pg, const PrefixView& px, const int32_t* len, Chunk& out) {
-  const int lane = threadIdx.x & 63, bid = blockIdx.x;
+__device__ __forceinline__ bool find_chunk(const PageDims& pg, const PrefixView& px, const int32_t* len, int bid, int places, Chunk& out) {
+  const int lane = threadIdx.x & 63;
   const int units = PREFIX ? pg.n_seq * pg.G : pg.n_seq, mult = PREFIX ? 1 : pg.G;
   auto tiles = [&](int u) -> int {
     if (u >= units) return 0;
     int64_t s = 0;
     return tiles_of<TILE>(held_len(pg, len[PREFIX ? u / pg.G : u]), PREFIX ? held_count(px, u, s) : 0);
   };
-  const int first = tiles(lane);
-  uint64_t total = 0;
+  const int room = places - pg.n_seq * pg.G;
+  int first = 0, size;
   if (units <= 64) {
-    total = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(scan_wave(first), 63) * mult;
-  } else {                             // the waves share the sum
+    first = tiles(lane);
+    size = chunk_tiles((uint64_t)(uint32_t)__builtin_amdgcn_readlane(scan_wave(first), 63) * mult, room);
+  } else {
     __shared__ uint64_t part[PA_W];
+    __shared__ int most[PA_W];
     uint64_t sum = 0;
-    for (int u = threadIdx.x; u < units; u += PA_T) sum += tiles(u);
+    int mx = 0;
+    for (int u = threadIdx.x; u < units; u += PA_T) {
+      const int n = tiles(u);
+      sum += n;
+      mx = max(mx, n);
+    }
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-    if (lane == 0) part[threadIdx.x >> 6] = sum;
+    for (int o = 32; o > 0; o >>= 1) {
+      sum += __shfl_xor(sum, o, 64);
+      mx = max(mx, __shfl_xor(mx, o, 64));
+    }
+    if (lane == 0) { part[threadIdx.x >> 6] = sum; most[threadIdx.x >> 6] = mx; }
     sync_after_lds_stores();
+    sum = 0;
 #pragma unroll
-    for (int i = 0; i < PA_W; ++i) total += part[i];
-    total *= mult;
+    for (int i = 0; i < PA_W; ++i) { sum += part[i]; mx = max(mx, most[i]); }
+    size = __builtin_amdgcn_readfirstlane(chunk_tiles(sum * mult, room));
+    if (__builtin_amdgcn_readfirstlane(mx) <= size) {
+      if (bid >= units * mult) return false;
+      const int u = bid / mult;
+      out.b = PREFIX ? u / pg.G : u;
+      out.g = PREFIX ? u % pg.G : bid % mult;
+      out.c = 0;
+      out.chunks = 1;
+      out.t0 = 0;
+      out.t1 = __builtin_amdgcn_readfirstlane(tiles(u));
+      return true;
+    }
+    first = tiles(lane);
   }
-  const int size = chunk_tiles(total, gridDim.x - pg.n_seq * pg.G);
-  // the rows of several chunks first, then the others, which even out the end
+  const float inv = 1.0f / (float)size;
+  // the rows of several chunks first, then the others, which even out the end (where there
+  // are more units than a wave looks at in one round, rows as they come: their end is short)
+  const bool ordered = units <= 64;
   int base = 0;
 #pragma unroll 1
-  for (int many = 1; many >= 0; --many)
+  for (int many = 1; many >= (ordered ? 0 : 1); --many)
+#pragma unroll 1
     for (int u0 = 0; u0 < units; u0 += 64) {
-      const int n = u0 ? tiles(u0 + lane) : first;
-      int c = n ? chunks_of(n, size) : 0;
-      c = (c > 1) == many ? c * mult : 0;
-      const int to = scan_wave(c);     // at most the grid: no overflow
+      const int n = u0 ? tiles(u0 + lane) : first, x = n ? chunks_of(n, size, inv) : 0;
+      const int c = !ordered || (x > 1) == many ? x * mult : 0;
+      const int to = scan_wave(c);     // at most the places: no overflow
       const int all = base + __builtin_amdgcn_readlane(to, 63);
       if (bid < all) {
         const int at = __popcll(__ballot(base + to <= bid));       // the unit's lane
         const int u = u0 + at;
-        const int tn = __builtin_amdgcn_readlane(n, at), chunks = chunks_of(tn, size);
+        const int tn = __builtin_amdgcn_readlane(n, at), chunks = __builtin_amdgcn_readlane(x, at);
         const int local = bid - base - (__builtin_amdgcn_readlane(to, at) - chunks * mult);
         out.b = PREFIX ? u / pg.G : u;
         out.g = PREFIX ? u % pg.G : local / chunks;
@@ -207,13 +257,17 @@ __global__ __launch_bounds__(PA_T, PA_OCC) void k_paged(PageDims pg, int64_t q_t
   __shared__ float sM[PA_W][PA_HEADS], sL[PA_W][PA_HEADS];
   __shared__ __align__(16) float sO[PA_W][PA_HEADS][D + 4];      // rows start in other banks
   __shared__ int joins;
+  // groups of 16 query heads of one chunk are neighbours: they read the same keys
+  const int groups = (pg.hpg + PA_HEADS - 1) / PA_HEADS;
+  const int bid = groups > 1 ? blockIdx.x / groups : blockIdx.x, group = groups > 1 ? blockIdx.x % groups : 0;
   Chunk ck;
-  if (!find_chunk<TILE, PREFIX>(pg, px, len, ck)) return;
+  const int places = groups > 1 ? gridDim.x / groups : gridDim.x;
+  if (!find_chunk<TILE, PREFIX>(pg, px, len, bid, places, ck)) return;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i16 = lane & 15, g4 = lane >> 4;
-  const int h0 = blockIdx.y * PA_HEADS, heads = min(PA_HEADS, pg.hpg - h0);
+  const int h0 = group * PA_HEADS, heads = min(PA_HEADS, pg.hpg - h0);
   const T* PK = (const T*)px.K;
   const T* PV = (const T*)px.V;
-  constexpr float LOG2E = 1.44269504088896341f;
+  constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
   const float scale = 1.0f / sqrtf((float)D);
   const int seq = ck.b, kv = ck.g;
   const int64_t row = (int64_t)seq * pg.G + kv;
@@ -414,7 +468,10 @@ __global__ __launch_bounds__(PA_T, PA_OCC) void k_paged(PageDims pg, int64_t q_t
     for (int h = 0; h < NS; ++h)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        pr[h][r] = __builtin_amdgcn_exp2f((x[h][r] - ms) * LOG2E);
+        const float y = (x[h][r] - ms) * LOG2E;
+        pr[h][r] = __builtin_amdgcn_exp2f(y);
+        // fp32: what the product lost, to first order
+        if (!BF && pr[h][r] > 0.f) pr[h][r] = __builtin_fmaf(pr[h][r], __builtin_fmaf(x[h][r] - ms, LOG2E, -y) * LN2, pr[h][r]);
         l += pr[h][r];
       }
     if constexpr (BF) {
@@ -489,7 +546,7 @@ __global__ __launch_bounds__(PA_T, PA_OCC) void k_paged(PageDims pg, int64_t q_t
     O1 = (f == 0.f ? 0.f : O1 * f) + (c == 0.f ? 0.f : a1 * c);
     M = mn;
   };
-  const int64_t place = (int64_t)blockIdx.x * pg.hpg + h0;
+  const int64_t place = (int64_t)bid * pg.hpg + h0;
   for (int i = tid; i < heads * (D / 2); i += PA_T) {
     const int h = i / (D / 2), dd = 2 * (i % (D / 2));
     float M = -INFINITY, S = 0.f, O0 = 0.f, O1 = 0.f;
@@ -503,15 +560,15 @@ __global__ __launch_bounds__(PA_T, PA_OCC) void k_paged(PageDims pg, int64_t q_t
     }
   }
   if (ck.chunks == 1) return;
-  wait_vm();                                    // the thread's states are there
+  stores_done();
   __syncthreads();
-  if (tid == 0) joins = last_of(ws.ticket + row * gridDim.y + blockIdx.y, ck.chunks);
+  if (tid == 0) joins = last_of(ws.ticket + row * groups + group, ck.chunks);
   sync_after_lds_stores();
   if (!joins) return;
   // A head's pairs of dims lie on LH neighbouring lanes, which hold the (max, sum) of LH
   // chunks at a time, one each, and pass the weights round.
   constexpr int LH = D / 2;
-  const int64_t base = ((int64_t)blockIdx.x - ck.c) * pg.hpg + h0;              // the row's first chunk
+  const int64_t base = (int64_t)(bid - ck.c) * pg.hpg + h0;              // the row's first chunk
   for (int i = tid; i < (heads * LH + 63) / 64 * 64; i += PA_T) {               // whole waves
     const int h = min(i / LH, heads - 1), sub = i % LH, dd = 2 * sub;
     float M = -INFINITY, S = 0.f, O0 = 0.f, O1 = 0.f;
@@ -567,7 +624,7 @@ hipError_t launch_paged(const PageDims& pg, int64_t q_tok, const void* q, const 
     const int64_t target = R < PA_FEW ? PA_TARGET / 2 : PA_TARGET;
     const int64_t most = target - R / 2 > target / 4 ? target - R / 2 : target / 4;
     room = room < 1 ? 1 : (room > most ? most : room);
-    const dim3 grid((unsigned)(R + room), (unsigned)((pg.hpg + PA_HEADS - 1) / PA_HEADS));
+    const dim3 grid((unsigned)((R + room) * ((pg.hpg + PA_HEADS - 1) / PA_HEADS)));
     if (px.K)
       hipLaunchKernelGGL((k_paged<T, D, NS, true>), grid, dim3(PA_T), 0, st, pg, q_tok, (const T*)q, (const T*)Kp, (const T*)Vp, table,
                          len, px, (T*)out, lse, v);

@@ -135,7 +135,7 @@ def test_prompt_refuses_pointers_and_workspaces():
     (dict(dtype=3), -1), (dict(G=0), -1), (dict(H=31), -1), (dict(n_seq=0), -1), (dict(reserved=1), -1), (dict(page_size=8), -2),
     (dict(page_size=48), -2), (dict(page_size=512, page_stride=1 << 22), -2), (dict(table_width=0), -1), (dict(n_pages=0), -1),
     (dict(page_stride=8 * 16 * 128 - 8), -1), (dict(page_stride=8 * 16 * 128 + 4), -1), (dict(d=80), -2),
-    (dict(n_pages=1 << 50), -1), (dict(table_width=1 << 28), -2)])
+    (dict(n_pages=1 << 50), -1), (dict(table_width=(1 << 21) + 1), -2), (dict(n_seq=8193), -2)])
 def test_pages_refuse_configurations(bad, code):
     n, c = ctypes.c_size_t(0), _page(**bad)
     rows = gk.AppendConfig(1, 16, 1024, 128, 1024, 128, 4096, 128, 4096, 128)
