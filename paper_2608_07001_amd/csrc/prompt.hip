@@ -19,11 +19,24 @@
 //
 // A tile that some row of the workgroup sees in part (its diagonal, its end) is staged
 // with values that are not finite replaced by 0, since 0 times an infinity is not 0; rows
-// that do see such a value get it at the end (poison()).
+// that do see such a value get it at the end.
 //
 // bf16 probabilities are rounded to bf16 (nearest even) as operands, their sum takes them
-// unrounded: each weight is off by at most 2^-9 of itself, at random, like the output's
+// unrounded: each weight is off by at most 2^-8 of itself, at random, like the output's
 // own rounding.  fp32 uses the fp32 matrix instructions.
+//
+// What bounds it: long prompts by the products and what goes on beside them.  16K tokens of
+// the 8B heads take 1.97 to 2.03 ms on different devices, 1.09 to 1.13 PFLOP/s of the pairs
+// that are seen (a library product of 8192^3 reaches 1.32): the matrix pipes are busy in
+// 64 % of the cycles, LDS in 32 %, without a bank conflict, and the chip runs at 1.7 GHz of
+// its 2.4; without the softmax, for timing, the same loop reached 1.26, without loads as
+// well 1.36.  What was tried and left: tiles of
+// 64 keys with two waves a SIMD (2.00 ms), through registers instead of straight into LDS
+// (2.34), the two waves of a SIMD held in opposite phases by barriers (2.11 to 2.34), other
+// orders and priorities of reads and products (within 1 %).  Short prompts and pieces are
+// bound by the way along the keys, about 0.9 us a tile for a workgroup with few beside it
+// (Plan), and by the parts' states, 33 MB of them for 64 queries over 32K keys: 50 us of
+// products, 10 of joining.  fp32: 2048 tokens of the 8B heads 325 us, 106 TFLOP/s of 153.
 #include "serve.h"
 
 namespace gkv {
@@ -41,7 +54,6 @@ __device__ __forceinline__ f32x16 mfma_bf16_32x32x16(uint4 a, uint4 b, f32x16 c)
 
 // the stated wait for the matrix pipeline (mfma_done) for these accumulators
 __device__ __forceinline__ void mfma_done16(f32x16& x) { asm volatile("s_nop 15\n\ts_nop 4" : "+v"(x)); }
-__device__ __forceinline__ void mfma_done16(f32x16& x, f32x16& y) { asm volatile("s_nop 15\n\ts_nop 4" : "+v"(x), "+v"(y)); }
 
 static size_t al256(size_t x) { return (x + 255) & ~(size_t)255; }
 
