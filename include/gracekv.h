@@ -395,7 +395,8 @@ gracekv_status gracekv_decode_attention_noalloc(const gracekv_config* cfg, const
  * the inputs' type, lse = log sum exp of the logits is fp32 (natural logarithm;
  * NULL: not wanted).  A query with no key has the output 0 and lse -inf; a masked or
  * absent key and its value never reach an output, whatever they hold.  Every call may
- * be captured in a HIP graph; lengths and tables are read when it runs. */
+ * be captured in a HIP graph; lengths and tables are read when it runs.  Shapes that one
+ * launch does not hold (2^24 workgroups) are GRACEKV_ERR_UNSUPPORTED. */
 
 /* Causal attention over packed prompts. */
 typedef struct {
@@ -441,7 +442,7 @@ typedef struct {
 
 /* New tokens of gracekv_cache_append. */
 typedef struct {
-  int64_t n_new;                    /* rows of k, v (and q, q_out), below 2^31 */
+  int64_t n_new;                    /* rows of k, v (and q, q_out), below 2^24 */
   int64_t rope_rows;                /* rows of rope_cos, rope_sin */
   int64_t k_tok, k_head, v_tok, v_head, q_tok, q_head, qout_tok, qout_head; /* strides */
 } gracekv_append_config;
@@ -478,7 +479,7 @@ typedef struct {
   const void* K;                    /* [rows][d] (cfg->dtype) */
   const void* V;
   const float* logm;                /* [rows] */
-  int64_t rows;
+  int64_t rows;                     /* 0: no entries, and K, V, logm may be NULL */
 } gracekv_prefix;
 
 /* Attention of one token of every sequence over the first seq_len[b] tokens of its
@@ -486,7 +487,7 @@ typedef struct {
  *   q          [n_seq] rows x [H][d], rows q_tok elements apart, rotated already
  *   seq_len    [n_seq] int32, held to [0, table_width * page_size]
  *   prefix     host structure, read by the call, or NULL
- *   out        [n_seq][H][d] (cfg->dtype); lse [n_seq][H] fp32 or NULL
+ *   out        [n_seq][H][d] (cfg->dtype), not an input's memory; lse [n_seq][H] fp32 or NULL
  *   ws         gracekv_paged_ws_bytes bytes, which need no initialisation; calls that
  *              overlap on one workspace race, and what they leave in it has to be cleared
  * Lengths, counts and tables must not change while the call runs. */

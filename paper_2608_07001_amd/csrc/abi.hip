@@ -578,6 +578,8 @@ gracekv_status gracekv_decode_attention_noalloc(const gracekv_config* c, const v
 static bool heads_ok(int dtype, int G, int H, int n_seq) {
   return (dtype == GRACEKV_F32 || dtype == GRACEKV_BF16) && G >= 1 && H >= 1 && H % G == 0 && n_seq >= 1;
 }
+// workgroups of 256 that one launch holds: it counts its work items in 32 bits
+constexpr int64_t MOST_GROUPS = (1 << 24) - 1;
 // a stride: rows stay 16-byte aligned and go upwards
 static bool stride_ok(int dtype, int64_t s) { return s >= 0 && s % (dtype == GRACEKV_BF16 ? 8 : 4) == 0; }
 
@@ -592,7 +594,7 @@ static gracekv_status prompt_dims(const gracekv_prompt_config* c, PromptDims* pd
   if (c->k_tok > PR_STRIDE || c->v_tok > PR_STRIDE) return GRACEKV_ERR_UNSUPPORTED;
   *pd = PromptDims{c->dtype, c->G, c->H, c->d, c->H / c->G, c->n_seq, c->n_q, c->n_k, c->q_tok, c->q_head,
                    c->k_tok, c->k_head, c->v_tok, c->v_head, c->out_tok, c->out_head};
-  if (c->n_q > 0x7fffffff / c->H || prompt_items(*pd) > 0x7fffffff) return GRACEKV_ERR_UNSUPPORTED;   // one launch
+  if (c->n_q > 0x7fffffff / c->H || c->n_seq > MOST_GROUPS || prompt_items(*pd) > MOST_GROUPS) return GRACEKV_ERR_UNSUPPORTED;
   return GRACEKV_OK;
 }
 
@@ -632,7 +634,8 @@ static gracekv_status page_dims(const gracekv_page_config* c, PageDims* pg) {
     return GRACEKV_ERR_INVALID_ARG;
   *pg = PageDims{c->dtype, c->G, c->H, c->d, c->H / c->G, c->n_seq, shift, c->table_width, c->n_pages, c->page_stride};
   // rows (sequence, KV head) that every workgroup looks through, and their lengths (paged.hip)
-  if ((int64_t)c->n_seq * c->G > 65536 || c->H > 65536 || ((int64_t)c->table_width << shift) > PAGED_ROWS)
+  if ((int64_t)c->n_seq * c->G > 65536 || c->H > 65536 || ((int64_t)c->table_width << shift) > PAGED_ROWS ||
+      paged_items(*pg) > MOST_GROUPS)
     return GRACEKV_ERR_UNSUPPORTED;
   return GRACEKV_OK;
 }
@@ -650,10 +653,11 @@ gracekv_status gracekv_cache_append(const gracekv_page_config* c, const gracekv_
   if (!aligned16(k) || !aligned16(v) || !aligned16(q) || !aligned16(K_pages) || !aligned16(V_pages) || !aligned16(q_out) ||
       !aligned16(rope_cos) || !aligned16(rope_sin))
     return GRACEKV_ERR_INVALID_ARG;
-  if (r->n_new < 0 || r->n_new > 0x7fffffff || r->rope_rows < 0) return GRACEKV_ERR_INVALID_ARG;
+  if (r->n_new < 0 || r->rope_rows < 0) return GRACEKV_ERR_INVALID_ARG;
   for (int64_t x : {r->k_tok, r->k_head, r->v_tok, r->v_head, r->q_tok, r->q_head, r->qout_tok, r->qout_head})
     if (!stride_ok(c->dtype, x)) return GRACEKV_ERR_INVALID_ARG;
   if (q && ((r->qout_tok == 0 && r->n_new > 1) || (r->qout_head == 0 && c->H > 1))) return GRACEKV_ERR_INVALID_ARG;
+  if (r->n_new > MOST_GROUPS) return GRACEKV_ERR_UNSUPPORTED;
   const AppendDims ap{r->n_new, r->rope_rows, r->k_tok, r->k_head, r->v_tok, r->v_head, r->q_tok, r->q_head, r->qout_tok, r->qout_head};
   return hip_status(launch_append(pg, ap, k, v, q, block_table, start, cu_new, pos, rope_cos, rope_sin, K_pages, V_pages, q_out,
                                   (hipStream_t)stream));
@@ -681,10 +685,11 @@ gracekv_status gracekv_paged_attention(const gracekv_page_config* c, const void*
   if (!stride_ok(c->dtype, q_tok)) return GRACEKV_ERR_INVALID_ARG;
   PrefixView px{nullptr, nullptr, nullptr, nullptr, nullptr, 0};
   if (prefix) {
-    if (!prefix->start || !prefix->count || !prefix->K || !prefix->V || !prefix->logm || !aligned16(prefix->K) ||
+    const bool some = prefix->rows != 0;          // none: the arrays may be NULL
+    if (!prefix->start || !prefix->count || (some && (!prefix->K || !prefix->V || !prefix->logm)) || !aligned16(prefix->K) ||
         !aligned16(prefix->V) || prefix->rows < 0 || prefix->rows > INT64_MAX / 1024)
       return GRACEKV_ERR_INVALID_ARG;
-    px = PrefixView{prefix->start, prefix->count, prefix->K, prefix->V, prefix->logm, prefix->rows};
+    if (some) px = PrefixView{prefix->start, prefix->count, prefix->K, prefix->V, prefix->logm, prefix->rows};
   }
   if (ws_bytes < paged_ws_bytes(pg)) return GRACEKV_ERR_WORKSPACE;
   return hip_status(launch_paged(pg, q_tok, q, K_pages, V_pages, block_table, seq_len, px, out, lse, ws, (hipStream_t)stream));

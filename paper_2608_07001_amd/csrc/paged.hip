@@ -34,7 +34,7 @@
 // 128: three waves a SIMD; two tiles in turn took 236, two waves, and were 2 to 4 % slower).
 // For bf16 the probabilities are rounded to bf16
 // (nearest even) as the second product's operand, while their sum takes them unrounded:
-// each weight is off by at most 2^-9 of itself, at random, like the output's own rounding.
+// each weight is off by at most 2^-8 of itself, at random, like the output's own rounding.
 // fp32 caches use the fp32 matrix instructions.
 #include "serve.h"
 
@@ -76,6 +76,9 @@ static PagedWs paged_view(void* base, const PageDims& pg) {
   return w;
 }
 size_t paged_ws_bytes(const PageDims& pg) { return paged_view(nullptr, pg).bytes; }
+int64_t paged_items(const PageDims& pg) {
+  return ((int64_t)pg.n_seq * pg.G + PA_TARGET) * ((pg.hpg + PA_HEADS - 1) / PA_HEADS);
+}
 
 // Tickets.  The chunks of a row count themselves in its word, PA_BASE, PA_BASE + 1, ...;
 // the one that makes the count whole finds PA_BASE + parts - 1, and its counting sets the

@@ -40,6 +40,7 @@ int64_t prompt_items(const PromptDims& pd);      // workgroups of its launch
 hipError_t launch_prompt(const PromptDims& pd, const void* q, const void* k, const void* v, const int32_t* cu_q,
                          const int32_t* cu_k, void* out, float* lse, void* ws, hipStream_t st);
 size_t paged_ws_bytes(const PageDims& pg);
+int64_t paged_items(const PageDims& pg);         // at most so many workgroups
 hipError_t launch_paged(const PageDims& pg, int64_t q_tok, const void* q, const void* Kp, const void* Vp,
                         const int32_t* table, const int32_t* len, const PrefixView& px, void* out, float* lse, void* ws,
                         hipStream_t st);

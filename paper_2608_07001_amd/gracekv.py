@@ -394,7 +394,11 @@ def _pages(cfg: PageConfig, K_pages, V_pages, dev: int):
 
 
 def _raw(stream, dev: int) -> int:
-    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(dev)
+    if stream.device_index != dev:
+        raise ValueError(f"stream: got one of device {stream.device_index}, need the current device cuda:{dev}")
+    return stream.cuda_stream
 
 
 def cache_append(cfg: PageConfig, k, v, K_pages, V_pages, block_table, start, cu_new, pos=None, rope_cos=None, rope_sin=None,

@@ -317,7 +317,7 @@ class Cache:
             self.pre = dict(start=start, count=c, K=_rand(gen, n, d, dtype=dtype), V=_rand(gen, n, d, dtype=dtype),
                             logm=torch.rand(n, generator=gen) * 4)
 
-    def call(self, out=None, ws=None, width=None):
+    def call(self, out=None, ws=None):
         g = lambda x: x.cuda()                                   # noqa: E731
         table = g(self.table)
         K, V = g(self.K), g(self.V)
@@ -468,6 +468,13 @@ def test_paged_every_batch_size():
         lens = torch.randint(0, 60, (B,), generator=gen).tolist()
         c = Cache("bf16", 64, 1, 2, lens, 16, torch.randint(0, 40, (B,), generator=gen).tolist() if B % 2 else None, seed=B)
         c.check()
+
+
+def test_paged_prefix_of_no_rows():
+    c = Cache("bf16", 64, 2, 6, [70, 0], 16, [0] * 4, seed=22)
+    for name in ("K", "V", "logm"):
+        c.pre[name] = c.pre[name][:0]
+    c.check()
 
 
 def test_paged_shared_pages_and_packed_rows():
@@ -623,3 +630,35 @@ def test_prompt_captured_and_replayed():
         out.zero_()
         gk.prompt_attention(cfg, q, k, v, cu_q, cu_k, out, ws, lse=lse)
         assert torch.equal(got[0], out) and torch.equal(got[1], lse)
+
+
+def test_calls_at_once_on_two_streams():
+    """Prompts and a batch's next tokens on two streams at the same time, a workspace each:
+    bit for bit what one after the other gives."""
+    gen = torch.Generator().manual_seed(5)
+    c = Cache("bf16", 128, 2, 16, [9000, 40, 3000, 0, 1, 700], 64, seed=30)
+    dev = {n: getattr(c, n).cuda() for n in ("K", "V", "table", "len", "q")}
+    page = gk.page_config(dev["K"], c.H, dev["table"])
+    q, k, v = _rand(gen, 100, 16, 128).cuda(), _rand(gen, 4000, 2, 128).cuda(), _rand(gen, 4000, 2, 128).cuda()
+    cu_q, cu_k = _cu([100]).cuda(), _cu([4000]).cuda()
+    prompt = gk.prompt_config(q, k, v, q, 1)
+    sides = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = []
+    for _ in sides + [None]:
+        got.append(dict(po=torch.zeros_like(q), pl=torch.zeros(100, 16, device="cuda"), do=torch.zeros_like(dev["q"]),
+                        dl=torch.zeros(6, 16, device="cuda"), pw=torch.empty(gk.prompt_ws_bytes(prompt), dtype=torch.uint8, device="cuda"),
+                        dw=torch.empty(gk.paged_ws_bytes(page), dtype=torch.uint8, device="cuda")))
+
+    def run(b, stream):
+        gk.prompt_attention(prompt, q, k, v, cu_q, cu_k, b["po"], b["pw"], lse=b["pl"], stream=stream)
+        gk.paged_attention(page, dev["q"], dev["K"], dev["V"], dev["table"], dev["len"], b["do"], b["dw"], lse=b["dl"], stream=stream)
+    run(got[2], None)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for b, stream in zip(got, sides):
+            run(b, stream)
+    torch.cuda.synchronize()
+    for b in got[:2]:
+        for name in ("po", "pl", "do", "dl"):
+            assert torch.equal(b[name], got[2][name]), name
+    c.check((got[2]["do"].cpu(), got[2]["dl"].cpu()))

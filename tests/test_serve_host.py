@@ -109,7 +109,9 @@ def _prompt_call(cfg, drop=None, odd=None, ws=FAKE, ws_bytes=1 << 40):
 @pytest.mark.parametrize("bad,code", [
     (dict(dtype=2), -1), (dict(G=0), -1), (dict(H=30), -1), (dict(n_seq=0), -1), (dict(reserved=1), -1), (dict(n_q=-1), -1),
     (dict(n_k=-1), -1), (dict(n_q=1 << 31), -1), (dict(d=96), -2), (dict(q_tok=4), -1), (dict(k_head=-128), -1), (dict(v_tok=12), -1),
-    (dict(out_tok=0), -1), (dict(out_head=0), -1), (dict(out_head=4), -1)])
+    (dict(out_tok=0), -1), (dict(out_head=0), -1), (dict(out_head=4), -1), (dict(k_tok=(1 << 24) + 8), -2),
+    (dict(n_seq=1 << 24), -2), (dict(n_seq=(1 << 31) - 1), -2), (dict(n_seq=1 << 22), -2), (dict(n_q=1 << 26), -2),
+    (dict(n_q=1 << 30, G=1, H=1, dtype=gk.F32), -2), (dict(n_q=1 << 24, H=128), -2)])
 def test_prompt_refuses_configurations(bad, code):
     n = ctypes.c_size_t(0)
     assert _status(gk.lib().gracekv_prompt_ws_bytes, _prompt(**bad), ctypes.byref(n)) == code
@@ -135,7 +137,8 @@ def test_prompt_refuses_pointers_and_workspaces():
     (dict(dtype=3), -1), (dict(G=0), -1), (dict(H=31), -1), (dict(n_seq=0), -1), (dict(reserved=1), -1), (dict(page_size=8), -2),
     (dict(page_size=48), -2), (dict(page_size=512, page_stride=1 << 22), -2), (dict(table_width=0), -1), (dict(n_pages=0), -1),
     (dict(page_stride=8 * 16 * 128 - 8), -1), (dict(page_stride=8 * 16 * 128 + 4), -1), (dict(d=80), -2),
-    (dict(n_pages=1 << 50), -1), (dict(table_width=(1 << 21) + 1), -2), (dict(n_seq=8193), -2)])
+    (dict(n_pages=1 << 50), -1), (dict(table_width=(1 << 21) + 1), -2), (dict(n_seq=8193), -2),
+    (dict(n_seq=65536, G=1, H=65536), -2)])
 def test_pages_refuse_configurations(bad, code):
     n, c = ctypes.c_size_t(0), _page(**bad)
     rows = gk.AppendConfig(1, 16, 1024, 128, 1024, 128, 4096, 128, 4096, 128)
@@ -162,6 +165,9 @@ def test_paged_refuses_pointers_and_workspaces():
     assert call(prefix=gk.PrefixArrays(**dict(good, K=ODD)), n=0) == -1
     assert call(prefix=gk.PrefixArrays(**dict(good, rows=-1)), n=0) == -1
     assert call(prefix=gk.PrefixArrays(**good), n=0) == -4
+    none = dict(good, K=None, V=None, logm=None, rows=0)
+    assert call(prefix=gk.PrefixArrays(**none), n=0) == -4
+    assert call(prefix=gk.PrefixArrays(**dict(none, start=None)), n=0) == -1
 
 
 def test_append_refuses_pointers_and_strides():
@@ -179,7 +185,7 @@ def test_append_refuses_pointers_and_strides():
         assert call(**{name: ODD}) == -1, name
     for bad in (dict(k_tok=4), dict(v_head=-8), dict(q_tok=12), dict(qout_tok=0), dict(qout_head=0), dict(rope_rows=-1)):
         assert call(row=bad) == -1, bad
-    assert call(n_new=-1) == -1 and call(n_new=1 << 31) == -1
+    assert call(n_new=-1) == -1 and call(n_new=1 << 24) == -2 and call(n_new=1 << 31) == -2
     assert gk.lib().gracekv_cache_append(ctypes.byref(c), None, *[FAKE] * 12, None) == -1
 
 
@@ -205,6 +211,10 @@ def test_binding_refuses_other_tensors(monkeypatch):
         gk.prompt_attention(cfg, q.bfloat16(), k, k, cu, cu, q)
     with pytest.raises(ValueError, match="strides"):
         gk.prompt_attention(cfg, q.transpose(0, 1).contiguous().transpose(0, 1), k, k, cu, cu, q)
+    class Other:
+        device_index, cuda_stream = 1, 1 << 20
+    with pytest.raises(ValueError, match="device 1"):
+        gk._raw(Other(), 0)
     # a length of one has no stride that matters
     one = torch.zeros(1, 8, 64).as_strided((1, 8, 64), (3, 64, 1))
     assert gk.prompt_config(one, k, k, one, 1).q_tok == 0
