@@ -50,6 +50,13 @@ constexpr int PA_MIN = PA_W;       // tiles of the shortest chunk: one a wave
 // few: 192 rows of compressed contexts 47.0 us with 768, 51.8 with 1536; 512 rows of ragged
 // sequences 74.8 with 1024, 73.4 with 1536, 74.0 with 2048.
 constexpr int PA_TARGET = 1536, PA_FEW = 256;
+// The last chunk of a row joins PA_JOIN states at a time; PA_COST weighs that against a tile's
+// step (chunks_of; half or twice as much is up to a fifth slower, and so are 32 states at a
+// time, 16 the same).  Without that limit on the chunks of a row one sequence of 128K tokens
+// and one KV head took 240 us with 16 query heads of 128 and 77 with one of 64; now 55 and
+// 24.  (Four dims a lane instead of two joins 16 heads faster, 48, and the others slower.)
+constexpr int PA_JOIN = 8;
+constexpr float PA_COST = 0.6f;
 
 static size_t al256(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -150,9 +157,13 @@ __device__ __forceinline__ int chunk_tiles(uint64_t total, int room) {
   const uint64_t size = total < 0x7fffffffu ? ((uint32_t)total + (uint32_t)room - 1) / (uint32_t)room : (total + room - 1) / room;
   return size < (uint64_t)PA_MIN ? PA_MIN : (size > 0x7fffffffu ? 0x7fffffff : (int)size);
 }
-// ... and chunks of a row, n / size upwards; inv: 1 / size or next to it (n below 2^24)
-__device__ __forceinline__ int chunks_of(int n, int size, float inv) {
-  int c = (int)((float)n * inv);
+// ... and chunks of a row of n tiles (below 2^24), n / size upwards, where size is also no less
+// than sqrt(join n), in whole steps of the waves.  A workgroup walks size / PA_W tiles a wave, one after the other, and the
+// last of a row's joins n / size states, PA_JOIN at a time, in join's passes over the heads:
+// the longer of few rows are bound by the sum of both.
+__device__ __forceinline__ int chunks_of(int n, int size, float join) {
+  size = max(size, ((int)sqrtf(join * (float)n) + PA_W / 2) & ~(PA_W - 1));
+  int c = (int)((float)n * (1.0f / (float)size));      // or next to it
   int left = n - c * size;
   if (left < 0) { --c; left += size; }
   else if (left >= size) { ++c; left -= size; }
@@ -166,7 +177,8 @@ __device__ __forceinline__ int chunks_of(int n, int size, float inv) {
 // which is enough where no row needs a second chunk (4096 sequences of 64 tokens: 860 us
 // with the search, 403 without).
 template <int TILE, bool PREFIX>
-__device__ __forceinline__ bool find_chunk(const PageDims& pg, const PrefixView& px, const int32_t* len, int bid, int places, Chunk& out) {
+__device__ __forceinline__ bool find_chunk(const PageDims& pg, const PrefixView& px, const int32_t* len, int bid, int places, float join,
+                                           Chunk& out) {
   const int lane = threadIdx.x & 63;
   const int units = PREFIX ? pg.n_seq * pg.G : pg.n_seq, mult = PREFIX ? 1 : pg.G;
   auto tiles = [&](int u) -> int {
@@ -213,7 +225,6 @@ __device__ __forceinline__ bool find_chunk(const PageDims& pg, const PrefixView&
     }
     first = tiles(lane);
   }
-  const float inv = 1.0f / (float)size;
   // the rows of several chunks first, then the others, which even out the end (where there
   // are more units than a wave looks at in one round, rows as they come: their end is short)
   const bool ordered = units <= 64;
@@ -222,7 +233,7 @@ __device__ __forceinline__ bool find_chunk(const PageDims& pg, const PrefixView&
   for (int many = 1; many >= (ordered ? 0 : 1); --many)
 #pragma unroll 1
     for (int u0 = 0; u0 < units; u0 += 64) {
-      const int n = u0 ? tiles(u0 + lane) : first, x = n ? chunks_of(n, size, inv) : 0;
+      const int n = u0 ? tiles(u0 + lane) : first, x = n ? chunks_of(n, size, join) : 0;
       const int c = !ordered || (x > 1) == many ? x * mult : 0;
       const int to = scan_wave(c);     // at most the places: no overflow
       const int all = base + __builtin_amdgcn_readlane(to, 63);
@@ -265,7 +276,8 @@ __global__ __launch_bounds__(PA_T, PA_OCC) void k_paged(PageDims pg, int64_t q_t
   const int bid = groups > 1 ? blockIdx.x / groups : blockIdx.x, group = groups > 1 ? blockIdx.x % groups : 0;
   Chunk ck;
   const int places = groups > 1 ? gridDim.x / groups : gridDim.x;
-  if (!find_chunk<TILE, PREFIX>(pg, px, len, bid, places, ck)) return;
+  const int passes = (min(PA_HEADS, pg.hpg) * (D / 2) + PA_T - 1) / PA_T;
+  if (!find_chunk<TILE, PREFIX>(pg, px, len, bid, places, PA_COST * passes, ck)) return;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i16 = lane & 15, g4 = lane >> 4;
   const int h0 = group * PA_HEADS, heads = min(PA_HEADS, pg.hpg - h0);
   const T* PK = (const T*)px.K;
@@ -579,11 +591,10 @@ __global__ __launch_bounds__(PA_T, PA_OCC) void k_paged(PageDims pg, int64_t q_t
       const int nb = min(ck.chunks - b0, LH);
       const unsigned long long* src = (const unsigned long long*)(ws.o + (base + (int64_t)b0 * pg.hpg + h) * D + dd);
       const int64_t step = (int64_t)pg.hpg * LH;
-      constexpr int UN = 8;
-      unsigned long long ov[UN];
+      unsigned long long ov[PA_JOIN];
       auto load = [&](int c0) {                 // past the last: that one again
 #pragma unroll
-        for (int c = 0; c < UN; ++c) ov[c] = ld_agent(src + min(c0 + c, nb - 1) * step);
+        for (int c = 0; c < PA_JOIN; ++c) ov[c] = ld_agent(src + min(c0 + c, nb - 1) * step);
       };
       float2 ml = make_float2(-INFINITY, 0.f);
       if (sub < nb) ml = pair_of(ld_agent(ws.ml + base + (int64_t)(b0 + sub) * pg.hpg + h));
@@ -596,10 +607,10 @@ __global__ __launch_bounds__(PA_T, PA_OCC) void k_paged(PageDims pg, int64_t q_t
 #pragma unroll
       for (int o = LH / 2; o > 0; o >>= 1) sb += __shfl_xor(sb, o, 64);
       float a0 = 0.f, a1 = 0.f;
-      for (int c0 = 0; c0 < nb; c0 += UN) {
+      for (int c0 = 0; c0 < nb; c0 += PA_JOIN) {
         if (c0) load(c0);
 #pragma unroll
-        for (int c = 0; c < UN; ++c) {
+        for (int c = 0; c < PA_JOIN; ++c) {
           const float g = c0 + c < nb ? __shfl(f, (tid & 63 & ~(LH - 1)) + c0 + c, 64) : 0.f;
           const float2 v = pair_of(ov[c]);
           a0 += g == 0.f ? 0.f : v.x * g;
