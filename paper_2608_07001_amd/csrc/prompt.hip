@@ -44,6 +44,7 @@ namespace gkv {
 constexpr int PR_T = 256;
 constexpr int PR_W = PR_T / 64;
 constexpr int PR_FILL = 512;       // workgroups that the keys of few rows are split into
+constexpr int CUS = 256;
 constexpr float PR_LAG = 8.f;      // base-2 units
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 
@@ -84,7 +85,7 @@ static Plan prompt_plan(const PromptDims& pd) {
   // waves in pairs halve; the tiles of 64 rows have to fill the chip without further parts,
   // and their keys be few, for a long way is walked faster by single waves.  One prompt of
   // the 8B heads, single and paired: 1024 tokens 33.2 and 26.6 us, 1536 47.4 and 40.7, 2048
-  // 55.0 and 63.0 (d = 64: 41.5 and 31.4), 512 tokens, too few for either, 21.3 and 22.2;
+  // 55.0 and 63.0 (d = 64: 41.5 and 31.4), 512 tokens, too few for pairs, 18.6 and 22.2;
   // 64 queries over 32K keys 62.7 and 73.4.
   p.split = bf && tiles(FEW) >= PR_FILL && tiles(ROWS) < (pd.d == 128 ? PR_FILL : 2 * PR_FILL) && pd.n_k <= 2048;
   p.rows = bf ? (p.split ? FEW : ROWS) : tile_rows<false, 1>();
@@ -95,7 +96,20 @@ static Plan prompt_plan(const PromptDims& pd) {
   // tokens 12 -> 17 us; fp32 with 256: 300 tokens 27 -> 30).
   const int64_t n = tiles(p.rows), fill = bf ? PR_FILL : PR_FILL + PR_FILL / 2, keys = bf ? 256 : 128;
   const int64_t want = n ? (fill + n - 1) / n : 1, most = (pd.n_k + keys - 1) / keys;
-  p.parts = (int)(want < 1 ? 1 : (want > most ? (most < 1 ? 1 : most) : want));
+  const int64_t cap = want > most ? (most < 1 ? 1 : most) : want;
+  // ... and only where that pays, by what was measured, in us: a key tile's step on the longest
+  // way (longer where workgroups share a CU), the second kernel, and the states, written and
+  // read.  The 8B heads: 512 tokens 26 -> 19, 700 31 -> 23 (two and three parts before, one
+  // now), 128 queries over 4096 keys 31 -> 27 (16, 8).
+  const double join = 5, state = 2.0 * pd.n_q * pd.H * (4 * pd.d + 8) / 3.5e6;
+  auto cost = [&](int64_t parts) {
+    const double step = bf ? (n * parts > CUS ? 0.9 : 0.75) : (pd.d == 128 ? 2.2 : 1.2);
+    return pd.n_k / 32.0 / parts * step + (parts > 1 ? state * parts + join : 0);
+  };
+  const int64_t even = (int64_t)sqrt(pd.n_k / 32.0 * (bf ? 0.9 : pd.d == 128 ? 2.2 : 1.2) / (state > 0 ? state : 1e-9) + 0.5);
+  p.parts = 1;
+  for (const int64_t x : {cap, even, even + 1, n ? CUS / n : 1, n ? 2 * CUS / n : 1})
+    if (x > 1 && x <= cap && cost(x) < cost(p.parts)) p.parts = (int)x;
   return p;
 }
 int64_t prompt_items(const PromptDims& pd) {
