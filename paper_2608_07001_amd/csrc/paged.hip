@@ -411,7 +411,7 @@ __global__ __launch_bounds__(PA_T, PA_OCC) void k_paged(PageDims pg, int64_t q_t
     float x[NS][4];
 #pragma unroll
     for (int h = 0; h < NS; ++h) {
-      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f}, odd = acc;       // fp32: two chains, which round half as often
 #pragma unroll
       for (int s = 0; s < KC; ++s) {
         if constexpr (BF) {
@@ -420,9 +420,13 @@ __global__ __launch_bounds__(PA_T, PA_OCC) void k_paged(PageDims pg, int64_t q_t
           const uint32_t a[4] = {tk[h][s].x, tk[h][s].y, tk[h][s].z, tk[h][s].w};
           const uint32_t b[4] = {qv[s].x, qv[s].y, qv[s].z, qv[s].w};
 #pragma unroll
-          for (int i = 0; i < 4; ++i) acc = mfma_f32_16x16x4(__uint_as_float(a[i]), __uint_as_float(b[i]), acc);
+          for (int i = 0; i < 4; i += 2) {
+            acc = mfma_f32_16x16x4(__uint_as_float(a[i]), __uint_as_float(b[i]), acc);
+            odd = mfma_f32_16x16x4(__uint_as_float(a[i + 1]), __uint_as_float(b[i + 1]), odd);
+          }
         }
       }
+      if constexpr (!BF) acc += odd;
 #pragma unroll
       for (int r = 0; r < 4; ++r) x[h][r] = acc[r] * scale;
     }
