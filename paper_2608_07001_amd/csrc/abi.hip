@@ -1,5 +1,5 @@
 // Host side of the C ABI: defaults, size planning, argument validation and
-// the five entry points.  Every entry point validates on the host and only
+// the entry points.  Every entry point validates on the host and only
 // enqueues kernels on the caller's stream.
 #include <math.h>
 #include <string.h>

@@ -22,7 +22,7 @@
 // 128, 8 query heads each, 351 to 362 us for 2.01 GB, 5.6 to 5.7 TB/s (a copy moves 4.9, read
 // and write together); 64 sequences of 1 to 8192 tokens 73 us, 4.7 TB/s, of which about 11 us
 // are the way to the first byte and from the last; 24 compressed contexts of 2048 entries
-// a head 47 us; one of 512 entries a head 9.3 us, latency.
+// a head 47 us; one of 512 entries a head 9.6 us, latency.
 //
 // A wave takes whole tiles.  Logits are formed transposed, S^T = K Q^T (entries x heads,
 // 16x16 matrix tiles, heads past the group's zero), keys straight from memory as the
