@@ -81,13 +81,19 @@ static Plan prompt_plan(const PromptDims& pd) {
   auto tiles = [&](int rows) { return (int64_t)row_tiles(pd, rows) * pd.G; };
   constexpr int ROWS = tile_rows<true, 1>(), FEW = tile_rows<true, 2>();
   Plan p;
-  // Short prompts that leave the chip part empty are bound by the way along the keys, which
-  // waves in pairs halve; the tiles of 64 rows have to fill the chip without further parts,
-  // and their keys be few, for a long way is walked faster by single waves.  One prompt of
-  // the 8B heads, single and paired: 1024 tokens 33.2 and 26.6 us, 1536 47.4 and 40.7, 2048
-  // 55.0 and 63.0 (d = 64: 41.5 and 31.4), 512 tokens, too few for pairs, 18.6 and 22.2;
-  // 64 queries over 32K keys 62.7 and 73.4.
-  p.split = bf && tiles(FEW) >= PR_FILL && tiles(ROWS) < (pd.d == 128 ? PR_FILL : 2 * PR_FILL) && pd.n_k <= 2048;
+  // Prompts that leave the chip part empty are bound by the way along the keys, which waves
+  // in pairs halve, as long as the tiles of 64 rows are not too few to be cut no further, and
+  // the keys of the longest sequence (of n_seq, taken as twice the mean or all there are) not
+  // so many that a long way is walked faster in parts.  The 8B heads, single (in parts) and
+  // paired: 256 tokens 12.4 and 11.5 us, 512 18.6 and 15.9, 1024 28.1 and 25.9, 1536 44.8 and
+  // 41.8, 2048 55 and 63; one KV head with 8 heads of 128, 3000 tokens 47.9 and 51.2, with 16
+  // heads of 64, 3500 tokens 56 and 43; 2 with 8 of 128, three sequences of 3300 tokens 41.9
+  // and 33.1; 64 queries over 32K keys 62.7 and 73.4; fewer tiles than PR_FILL / 2: 16 heads
+  // of 128 on 4, 700 tokens 22.2 and 18.1, 64 heads of 64 on 8, 128 queries over 4000 keys
+  // 24.7 and 42.0.
+  const int64_t longest = 2 * pd.n_k / (pd.n_seq + 1);
+  p.split = bf && tiles(FEW) >= (longest <= 1024 ? PR_FILL / 4 : PR_FILL / 2) && tiles(ROWS) < (pd.d == 128 ? PR_FILL : 2 * PR_FILL) &&
+            longest <= (pd.d == 128 ? 2048 : 4096);
   p.rows = bf ? (p.split ? FEW : ROWS) : tile_rows<false, 1>();
   // One part where the tiles fill the chip (bf16: twice over; fp32, whose key tiles take
   // four times as long: three times, 1056 tokens of the 8B heads 134 -> 111 us; the same in
@@ -95,12 +101,11 @@ static Plan prompt_plan(const PromptDims& pd) {
   // least so many keys of the longest row that joining it is worth it (bf16 with 128: 256
   // tokens 12 -> 17 us; fp32 with 256: 300 tokens 27 -> 30).
   const int64_t n = tiles(p.rows), fill = bf ? PR_FILL : PR_FILL + PR_FILL / 2, keys = bf ? 256 : 128;
-  const int64_t want = n ? (fill + n - 1) / n : 1, most = (pd.n_k + keys - 1) / keys;
+  const int64_t want = n && !p.split ? (fill + n - 1) / n : 1, most = (pd.n_k + keys - 1) / keys;
   const int64_t cap = want > most ? (most < 1 ? 1 : most) : want;
   // ... and only where that pays, by what was measured, in us: a key tile's step on the longest
   // way (longer where workgroups share a CU), the second kernel, and the states, written and
-  // read.  The 8B heads: 512 tokens 26 -> 19, 700 31 -> 23 (two and three parts before, one
-  // now), 128 queries over 4096 keys 31 -> 27 (16, 8).
+  // read.  The 8B heads: 512 tokens 26 in two parts, 19 in one, 128 queries over 4096 keys 31 in 16, 27 in eight.
   const double join = 5, state = 2.0 * pd.n_q * pd.H * (4 * pd.d + 8) / 3.5e6;
   auto cost = [&](int64_t parts) {
     const double step = bf ? (n * parts > CUS ? 0.9 : 0.75) : (pd.d == 128 ? 2.2 : 1.2);
@@ -226,12 +231,17 @@ template <int D> __device__ __forceinline__ int swz(int t, int c) {
 }
 
 template <int D, int SPLIT>
-__global__ __launch_bounds__(PR_T, 3) void k_prompt_bf(PromptDims pd, int parts, const uint16_t* __restrict__ q,
+__global__ __launch_bounds__(PR_T, SPLIT == 2 && D == 128 ? 2 : 3) void k_prompt_bf(PromptDims pd, int parts, const uint16_t* __restrict__ q,
                                                        const uint16_t* __restrict__ k, const uint16_t* __restrict__ v,
                                                        const int32_t* __restrict__ cu_q, const int32_t* __restrict__ cu_k,
                                                        uint16_t* __restrict__ out, float* __restrict__ lse,
                                                        float2* __restrict__ pml, float* __restrict__ po) {
   constexpr int ROWS = tile_rows<true, SPLIT>(), KEYS = tile_keys<SPLIT>();
+  // Pairs form the next tile's logits beside the present one's softmax, which their LDS, two
+  // workgroups a CU, leaves registers for: 1024 tokens of the 8B heads 27.6 -> 25.6 us, 1536
+  // 44.8 -> 41.5.  Single waves gain nothing (2048 tokens 57.4 -> 60.8) and lose the third (16K
+  // 2.08 -> 2.22 ms).
+  constexpr bool AHEAD = SPLIT == 2 && D == 128;
   constexpr int CH = D / 8;                     // 16-byte pieces of a row
   constexpr int RI = 64 / CH;                   // rows that one load of a wave brings
   constexpr int NI = KEYS / RI / PR_W;          // such loads of a wave and array
@@ -278,24 +288,31 @@ __global__ __launch_bounds__(PR_T, 3) void k_prompt_bf(PromptDims pd, int parts,
   const int lr = RI * w + lane / CH, lc = swz<D>(lr, lane % CH) - lr * CH;
   const int k_off = (int)(lr * pd.k_tok * 2) + lc * 16, k_step = (int)(RI * PR_W * pd.k_tok * 2);
   const int v_off = (int)(lr * pd.v_tok * 2) + lc * 16, v_step = (int)(RI * PR_W * pd.v_tok * 2);
-  auto load = [&](int t, uint4* dK, uint4* dV) {
-    const int64_t j0 = (int64_t)t * KEYS;
+  auto load = [&](const uint16_t* rows, int64_t stride, int off, int by, int t, uint4* to) {
     const int n = min(it.lk - t * KEYS, KEYS);   // at least one
-    const Buffer kb = tile_buffer<uint16_t, D>(kp + j0 * pd.k_tok, pd.k_tok, n);
-    const Buffer vb = tile_buffer<uint16_t, D>(vp + j0 * pd.v_tok, pd.v_tok, n);
+    const Buffer b = tile_buffer<uint16_t, D>(rows + (int64_t)t * KEYS * stride, stride, n);
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      buffer_load_lds(kb, dK + 64 * (w + PR_W * i), k_off + i * k_step);
-      buffer_load_lds(vb, dV + 64 * (w + PR_W * i), v_off + i * v_step);
-    }
+    for (int i = 0; i < NI; ++i) buffer_load_lds(b, to + 64 * (w + PR_W * i), off + i * by);
   };
+  auto load_keys = [&](int t, uint4* to) { load(kp, pd.k_tok, k_off, k_step, t, to); };
+  auto load_values = [&](int t, uint4* to) { load(vp, pd.v_tok, v_off, v_step, t, to); };
   // Where the lane reads in a tile, in bytes: piece 2 x + half of key row i32 lies at
   // k_at ^ 32 x; row 4 half + (lane % 16) / 4 of the transposing read's 8 bytes at v_at,
   // dim tile d at v_at ^ 64 d, the row 8 further at ^ 32 (swz()).
   constexpr int RB = 2 * D;
   int k_at = 16 * swz<D>(i32, half);
   const int v_at = 16 * swz<D>(4 * half + ((lane & 15) >> 2), 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + 8 * (lane & 1);
-  auto step = [&](int t, const uint4* cK, uint4* cV, uint4* nK, uint4* nV) __attribute__((always_inline)) {
+  auto logits = [&](const uint4* cK) __attribute__((always_inline)) {
+    f32x16 s;
+    asm volatile("" : "+v"(k_at));               // eight places: formed anew, not held in registers
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = 0.f;
+#pragma unroll
+    for (int x = 0; x < KS; ++x) s = mfma_bf16_32x32x16(lds_at(cK, (k_at ^ (32 * x)) + 32 * kw * RB), qv[x], s);
+    return s;
+  };
+  f32x16 s;                                      // AHEAD: the logits of the tile whose turn it is
+  auto step = [&](int t, uint4* cK, uint4* cV, uint4* nK, uint4* nV) __attribute__((always_inline)) {
     // the wave's own loads of tile t are there, then everyone's; and everyone is done with
     // tile t - 1, which t + 1 replaces.  (A third tile in flight was slower for long prompts:
     // 16K 1985 -> 2014 us, 8K 522 -> 536, though not for a ragged batch, 367 -> 360.)
@@ -309,16 +326,19 @@ __global__ __launch_bounds__(PR_T, 3) void k_prompt_bf(PromptDims pd, int parts,
       if (any) bad = 1;
       sync_after_lds_stores();
     }
-    if (t + 1 < it.t1) load(t + 1, nK, nV);
+    if constexpr (AHEAD) {
+      if (t + 2 < it.t1) load_keys(t + 2, cK);   // whose keys are logits already
+      if (t + 1 < it.t1) load_values(t + 1, nV);
+    } else if (t + 1 < it.t1) {
+      load_keys(t + 1, nK);
+      load_values(t + 1, nV);
+    }
     const int k0 = j0 + 32 * kw;                 // the wave's keys
     if (k0 > w_any) return;
-    f32x16 s;
-    asm volatile("" : "+v"(k_at));               // eight places: formed anew, not held in registers
-#pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] = 0.f;
-#pragma unroll
-    for (int x = 0; x < KS; ++x) s = mfma_bf16_32x32x16(lds_at(cK, (k_at ^ (32 * x)) + 32 * kw * RB), qv[x], s);
-    reads_ahead<KS, 1, 4>();
+    if constexpr (!AHEAD) {
+      s = logits(cK);
+      reads_ahead<KS, 1, 4>();
+    }
     mfma_done16(s);
     // register r: key 8 (r / 4) + 4 half + r % 4
     if (k0 + 31 > w_all) {
@@ -344,6 +364,17 @@ __global__ __launch_bounds__(PR_T, 3) void k_prompt_bf(PromptDims pd, int parts,
       for (int d = 0; d < DT; ++d) o[d] *= c;
     }
     const float ms = m == -INFINITY ? 0.f : m;
+    f32x16 sn;
+    if constexpr (AHEAD) {                       // past the last tile: of what is there, and not used
+      sn = logits(nK);
+      __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+      for (int x = 0; x < KS; ++x) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if (x + 4 < KS) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 72 / KS, 0);      // vector instructions
+      }
+    }
     uint4 pr[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -363,9 +394,19 @@ __global__ __launch_bounds__(PR_T, 3) void k_prompt_bf(PromptDims pd, int parts,
         o[d] = mfma_bf16_32x32x16(make_uint4(a.x, a.y, b.x, b.y), pr[x], o[d]);
       }
     reads_ahead<2 * DT, 2, 3>();
+    if constexpr (AHEAD) s = sn;
   };
   if (tid == 0) bad = 0;
-  if (it.t0 < it.t1) load(it.t0, sK0, sV0);
+  if (it.t0 < it.t1) {
+    load_keys(it.t0, sK0);
+    load_values(it.t0, sV0);
+    if constexpr (AHEAD) {
+      if (it.t0 + 1 < it.t1) load_keys(it.t0 + 1, sK1);
+      wait_vm();
+      sync_after_lds_stores();
+      s = logits(sK0);
+    }
+  }
   for (int t = it.t0; t < it.t1; t += 2) {
     step(t, sK0, sV0, sK1, sV1);
     if (t + 1 < it.t1) step(t + 1, sK1, sV1, sK0, sV0);

@@ -107,6 +107,15 @@ def test_prompt_waves_in_pairs(d):
     assert not _check_prompt("bf16", d, 8, 32, [418, 607], [418, 607], seed=22, edit=edit)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_prompt_between_pairs_and_parts(d):
+    # lengths and head counts on both sides of every rule that chooses the kernel and the parts
+    for i, (G, Hq, lq, lk) in enumerate([(8, 32, [127], None), (8, 32, [256], None), (8, 32, [511, 2], None), (4, 16, [700], None),
+                                         (4, 16, [200], [1000]), (4, 32, [256], [1400]), (8, 32, [3, 60, 0, 300, 20], None),
+                                         (1, 8, [1000, 900, 700], None), (2, 16, [5, 700], [2100, 705])]):
+        _check_prompt("bf16", d, G, Hq, lq, lk or lq, seed=40 + i)
+
+
 @pytest.mark.parametrize("dtype,d", TYPES)
 @pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
 def test_prompt_masked_places_reach_nothing(dtype, d, bad):
