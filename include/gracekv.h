@@ -415,8 +415,10 @@ gracekv_status gracekv_prompt_ws_bytes(const gracekv_prompt_config* cfg, size_t*
  * j <= i + Lk - Lq, so Lq = Lk is a whole prompt, Lq < Lk a later piece of one (the
  * question's window, a chunk), and with Lq > Lk the first queries see nothing.
  *   Q          [n_q] rows x H heads (strides q_tok, q_head); K, V [n_k] x G
- *   cu_q, cu_k [n_seq + 1] int32, ascending; places outside [0, n_q] and [0, n_k]
- *              are held inside, a descending pair is an empty sequence
+ *   cu_q, cu_k [n_seq + 1] int32, ascending (two equal ones: an empty sequence);
+ *              places outside [0, n_q] and [0, n_k] are held inside.  Where they descend,
+ *              the call ends and stays inside the arrays and the sequences' rows of out and
+ *              lse, but what these hold then is not specified
  *   out        [n_q] x H (strides out_tok, out_head); not an input's memory
  *   lse        [n_q][H] fp32 or NULL
  *   ws         gracekv_prompt_ws_bytes bytes (NULL where that is 0); calls that
@@ -453,7 +455,8 @@ typedef struct {
  *   k, v       [n_new] x G;  q, q_out [n_new] x H, or both NULL (q_out may be q itself,
  *              with the same strides)
  *   start      [n_seq] int32: tokens that sequence b holds already
- *   cu_new     [n_seq + 1] int32, as cu_q above
+ *   cu_new     [n_seq + 1] int32, ascending, as cu_q above: where it descends, which tokens
+ *              are written is not specified, each to its own place of a sequence or left out
  *   pos        [n_new] int32: row of rope_cos, rope_sin ([rope_rows][d/2] fp32, as
  *              above) that turns the token's key and query; all three NULL: nothing is
  *              turned (keys that are rotated already)

@@ -38,7 +38,8 @@ GKV_HD int64_t held_len(const PageDims& p, int64_t len) {
 }
 
 // bounds of sequence b in packed rows (n of them), as given by the n_seq + 1 ascending
-// starts `cu`: held inside [0, n], and empty where they descend
+// starts `cu`: held inside [0, n], and empty where this pair descends (which of several
+// sequences a row belongs to is then not told: find_last, span_with)
 struct Span { int64_t a, n; };
 GKV_HD int64_t held(int64_t x, int64_t n) { return x < 0 ? 0 : (x > n ? n : x); }
 GKV_HD Span span_of(const int32_t* cu, int b, int64_t n) {

@@ -55,7 +55,9 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 
 // the sequence b in [0, n) whose span could hold row t: the last with cu[b] <= t (0 if
 // none has).  A wave asks 64 places at a time, so up to 64 sequences take one load.
-// Every lane of the wave calls it with the same arguments.
+// Every lane of the wave calls it with the same arguments.  The starts have to ascend: the
+// places that hold are counted.  Otherwise it gives some b in [0, n), and its caller leaves
+// out a row that is not in the span of that one.
 template <typename F>
 __device__ __forceinline__ int find_last(int n, F at_most) {   // at_most(b): start of b <= what is looked for; falling
   const int lane = threadIdx.x & 63;

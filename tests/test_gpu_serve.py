@@ -166,6 +166,46 @@ def test_prompt_malformed_starts_stay_inside():
         S.check_rows(out[:n, 0], lse[:n, 0], want, n, 64, True, cu)
 
 
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_prompt_descending_starts_stay_inside(dtype, d):
+    """A descending pair between sequences of several tiles, alone and among more sequences than one
+    look of the search: the call ends and writes to rows of its sequences only."""
+    gen = torch.Generator().manual_seed(16)
+    for lead in (0, 100):
+        cu = torch.tensor([10] * lead + [10, 500, 200, 900], dtype=torch.int32)
+        q, k, v = _rand(gen, 1000, 2, d, dtype=dtype), _rand(gen, 1000, 1, d, dtype=dtype), _rand(gen, 1000, 1, d, dtype=dtype)
+        wide = torch.full((1000, 4, d + 16), 7.0, dtype=DT[dtype], device="cuda")
+        out, lse = wide[:, 1:3, 8:-8], torch.full((1000, 2), 7.0, device="cuda")
+        cfg = gk.prompt_config(q, k, v, out, cu.numel() - 1)
+        ws = torch.full((max(gk.prompt_ws_bytes(cfg), 1),), 0, dtype=torch.uint8, device="cuda")
+        gk.prompt_attention(cfg, q.cuda(), k.cuda(), v.cuda(), cu.cuda(), cu.cuda(), out, ws, lse=lse)
+        torch.cuda.synchronize()
+        out[10:900], lse[10:900] = 7.0, 7.0
+        assert (wide == 7).all() and (lse == 7).all()
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_prompt_many_sequences(dtype, d):
+    # more sequences than one look of the search (64), and than two (64 * 64), empty ones among them
+    for B, most, seed in ((65, 40, 1), (200, 9, 2), (4200, 3, 3)):
+        lens = torch.randint(0, most, (B,), generator=torch.Generator().manual_seed(seed)).tolist()
+        lens[-1] = 150
+        gen = torch.Generator().manual_seed(seed)
+        n = sum(lens) + 2
+        q, k, v = _rand(gen, n, 2, d, dtype=dtype, scale=1.5), _rand(gen, n, 1, d, dtype=dtype), _rand(gen, n, 1, d, dtype=dtype)
+        out, lse, _ = _prompt(q, k, v, _cu(lens), _cu(lens))
+        looked = set(range(B)) if B < 300 else set(range(0, B, 97)) | {B - 2, B - 1}
+        a = 0
+        for b, m in enumerate(lens):
+            if b in looked and m:
+                for h in range(2):
+                    ref = S.attend64(q[a:a + m, h].double(), k[a:a + m, 0].double(), v[a:a + m, 0].double(), seen=torch.ones(m, m).tril().bool())
+                    S.check_rows(out[a:a + m, h], lse[a:a + m, h], ref, m, d, dtype == "bf16", (B, b, h))
+            a += m
+        assert torch.isfinite(lse).all() and (out[a:] == 7).all() and (lse[a:] == 7).all()
+        assert not (lse[:a] == 7).any()
+
+
 def test_prompt_nothing_to_do():
     q, k = torch.empty(0, 4, 64, dtype=torch.bfloat16, device="cuda"), torch.empty(0, 2, 64, dtype=torch.bfloat16, device="cuda")
     cu = torch.zeros(4, dtype=torch.int32, device="cuda")
@@ -302,6 +342,26 @@ def test_append_many_sequences():
     on = place < 2 * page
     want[table.long()[b[on], place[on] // page], 0, place[on] % page] = k[on, 0]
     assert torch.equal(K.cpu(), want) and torch.equal(V.cpu(), want)
+
+
+def test_append_descending_starts_stay_inside():
+    # a token lands in its own place of a sequence that could hold it, or nowhere
+    gen = torch.Generator().manual_seed(17)
+    d, page, n = 64, 16, 70
+    cu = [0, 40, 20, 60]                                       # the middle sequence is none, the others overlap
+    table = torch.randperm(9, generator=gen).to(torch.int32).view(3, 3)
+    k = _rand(gen, n, 1, d)
+    K = torch.full((12, 1, page, d), 5.0, dtype=torch.bfloat16, device="cuda")
+    V = K.clone()
+    gk.cache_append(gk.page_config(K, 1, table), k.cuda(), k.cuda(), K, V, table.cuda(), torch.zeros(3, dtype=torch.int32).cuda(),
+                    torch.tensor(cu, dtype=torch.int32).cuda())
+    assert torch.equal(K, V)
+    K = K.cpu()
+    for b in range(3):
+        for place in range(3 * page):
+            row, t = K[table[b, place // page], 0, place % page], cu[b] + place
+            assert (row == 5).all() or (b != 1 and place < 40 and torch.equal(row, k[t, 0])), (b, place)
+    assert (K[9:] == 5).all()
 
 
 # ---------------------------------------------------------------------------
