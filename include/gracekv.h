@@ -393,7 +393,9 @@ gracekv_status gracekv_decode_attention_noalloc(const gracekv_config* cfg, const
  * contiguous.  Logits are q.k / sqrt(d), softmax statistics are fp32; bf16
  * probabilities are rounded to bf16 in the product with the values.  The outputs are of
  * the inputs' type, lse = log sum exp of the logits is fp32 (natural logarithm;
- * NULL: not wanted).  A query with no key has the output 0 and lse -inf; a masked or
+ * NULL: not wanted).  Values are summed under weights of at most 1 and then divided by the
+ * weights' sum: |v| times the keys of a row has to stay below 2^127, and what is below
+ * 2^-118 in size may lose bits.  A query with no key has the output 0 and lse -inf; a masked or
  * absent key and its value never reach an output, whatever they hold.  Every call may
  * be captured in a HIP graph; lengths and tables are read when it runs.  Shapes that one
  * launch does not hold (2^24 workgroups) are GRACEKV_ERR_UNSUPPORTED. */

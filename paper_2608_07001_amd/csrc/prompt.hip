@@ -45,7 +45,8 @@ constexpr int PR_T = 256;
 constexpr int PR_W = PR_T / 64;
 constexpr int PR_FILL = 512;       // workgroups that the keys of few rows are split into
 constexpr int CUS = 256;
-constexpr float PR_LAG = 8.f;      // base-2 units
+constexpr float PR_LAG = 8.f;      // base-2 units, and as a factor
+constexpr float PR_TOP = 256.f;
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -278,7 +279,7 @@ __global__ __launch_bounds__(PR_T, SPLIT == 2 && D == 128 ? 2 : 3) void k_prompt
   for (int t = 0; t < DT; ++t)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[t][r] = 0.f;
-  float m = -INFINITY, l = 0.f;                 // base-2 units; l: this lane's keys only
+  float m = -INFINITY, l = 0.f;                 // what is subtracted, base-2 units; l: this lane's keys only
   const float sc2 = LOG2E / sqrtf((float)D);
 
   const uint16_t* kp = k + it.k0 * pd.k_tok + it.g * pd.k_head;
@@ -353,10 +354,11 @@ __global__ __launch_bounds__(PR_T, SPLIT == 2 && D == 128 ? 2 : 3) void k_prompt
       const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
       mx = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1])) * sc2;
     }
-    // the maximum that is subtracted may lag behind by PR_LAG: weights up to 2^PR_LAG
-    // are as exact, and the outputs are rescaled seldom
-    if (__any(mx > m + PR_LAG)) {
-      const float mn = fmaxf(m, mx);
+    // What is subtracted stands PR_LAG above a maximum that may lag behind by as much: the outputs
+    // are rescaled seldom, no weight is above 1 (sums of large values stay in range as under the
+    // maximum itself), the row's largest at least 2^-PR_LAG, and all are as exact
+    if (__any(mx > m)) {
+      const float mn = fmaxf(m, mx + PR_LAG);
       const float c = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
       m = mn;
       l *= c;
@@ -477,7 +479,8 @@ __global__ __launch_bounds__(PR_T, SPLIT == 2 && D == 128 ? 2 : 3) void k_prompt
     for (int r = 0; r < 4; ++r)
       *(uint2*)(op + 32 * d + 8 * r + 4 * half) =
           make_uint2(pack_bf16(o[d][4 * r] * inv, o[d][4 * r + 1] * inv), pack_bf16(o[d][4 * r + 2] * inv, o[d][4 * r + 3] * inv));
-  if (lse && half == 0) lse[qrow * pd.H + head] = m == -INFINITY ? logf(l) : (m + log2f(l)) * LN2;
+  // (with the sum in units of its largest weight, whose logarithm is small)
+  if (lse && half == 0) lse[qrow * pd.H + head] = m == -INFINITY ? logf(l) : ((m - PR_LAG) + log2f(l * PR_TOP)) * LN2;
 }
 
 // fp32: 16 rows a wave, 32 keys a tile, fp32 matrix instructions

@@ -154,6 +154,20 @@ def test_prompt_large_logits(dtype, d):
     _check_prompt(dtype, d, 1, 2, [300], [300], seed=15, edit=fall)
 
 
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_prompt_large_values_stay_finite(dtype, d):
+    """Values of 5e34 at keys whose logits rise and fall by 5 from block to block: averages of up to 2000
+    of them at weights up to 1 stay below 1.1e38, so no sum on the way passes fp32's range (weights of
+    e^5 beside a first block of weight 1 would, from 64 keys on).  One part, pairs, several parts."""
+    def edit(q, k, v):
+        q[:] = 1.0
+        k[:] = ((torch.arange(k.shape[0]) // 64 % 2) * 5.0 / math.sqrt(d))[:, None, None]
+        v.abs_().add_(0.5).mul_(5e34)
+    _check_prompt(dtype, d, 1, 1, [200], [200], seed=18, edit=edit)
+    _check_prompt(dtype, d, 8, 32, [1024], [1024], seed=19, edit=edit)
+    assert _check_prompt(dtype, d, 2, 4, [5], [4000], seed=20, edit=edit)
+
+
 def test_prompt_malformed_starts_stay_inside():
     # starts outside the rows, and descending: held inside, the call ends, rows before stay right
     gen = torch.Generator().manual_seed(1)
