@@ -493,8 +493,11 @@ typedef struct {
  *   seq_len    [n_seq] int32, held to [0, table_width * page_size]
  *   prefix     host structure, read by the call, or NULL
  *   out        [n_seq][H][d] (cfg->dtype), not an input's memory; lse [n_seq][H] fp32 or NULL
- *   ws         gracekv_paged_ws_bytes bytes, which need no initialisation; calls that
- *              overlap on one workspace race, and what they leave in it has to be cleared
+ *   ws         gracekv_paged_ws_bytes bytes, which need no initialisation unless an aligned
+ *              64-bit word of them lies between 0x7fffffffffff0001 and 0x7fffffffffff0fff: it
+ *              would be taken for a count of parts (neither floating-point numbers nor calls
+ *              that ran to their end leave one); calls that overlap on one workspace race, and
+ *              what they leave in it has to be cleared
  * Lengths, counts and tables must not change while the call runs. */
 gracekv_status gracekv_paged_attention(const gracekv_page_config* cfg, const void* q, int64_t q_tok, const void* K_pages,
                                        const void* V_pages, const int32_t* block_table, const int32_t* seq_len,

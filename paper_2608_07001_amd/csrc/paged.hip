@@ -92,13 +92,15 @@ int64_t paged_items(const PageDims& pg) {
 // word to 0.  What a word holds before is no count: anything below PA_BASE is raised to it
 // first, and counting on anything past the end gives 0, whoever did it counting again.
 // So the workspace needs no clearing, and every call leaves the words it used at 0.  (The
-// few numbers from PA_BASE on would be taken for a count; nothing leaves them but calls
-// that overlap.)
+// numbers from PA_BASE + 1 to PA_BASE + parts - 1, at most PA_BASE + PA_TARGET, would be taken
+// for a count, and nothing here can tell them from one: the header excludes them.  Calls that
+// overlap leave them, and nothing else does.)
 // States are written and read with device-coherent operations, and a wait for the writes
 // stands between them and the ticket, so no fence is needed, which on this chip would
 // write back and invalidate the L2 of the XCD.  (Counting by compare-and-swap took the 40
 // chunks of a row 20 us, one after the other.)
 constexpr unsigned long long PA_BASE = 0x7fffffffffff0000ull;
+static_assert(PA_TARGET <= 0xfff, "the words that the header excludes");
 __device__ __forceinline__ bool last_of(unsigned long long* word, int parts) {
   const unsigned long long end = PA_BASE + parts - 1;
   unsigned long long was;

@@ -545,6 +545,15 @@ def test_paged_workspace_needs_no_clearing(fill):
         c.check(c.call(ws=ws))
 
 
+@pytest.mark.parametrize("word", [0x7fffffffffff0000, 0x7fffffffffff1000, 0x7fffffffffffffff, -1, -2 ** 63, 1, 0x7fffffff7fffffff])
+def test_paged_workspace_words_around_a_count(word):
+    # any word that is not between the first and the last number of a count; the same workspace again afterwards
+    c = Cache("bf16", 64, 2, 8, [4001, 3, 900], 16, seed=23)
+    ws = torch.full((1 << 19,), word, dtype=torch.int64, device="cuda")
+    for _ in range(2):
+        c.check(c.call(ws=ws))
+
+
 def test_paged_every_batch_size():
     for B in (1, 2, 63, 64, 65, 257, 700):
         gen = torch.Generator().manual_seed(B)
