@@ -40,23 +40,11 @@
 
 namespace gkv {
 
-constexpr int PA_T = 256;
-constexpr int PA_W = PA_T / 64;
 constexpr int PA_OCC = 3;          // waves a SIMD
-constexpr int PA_HEADS = 16;       // query heads of a workgroup
-constexpr int PA_MIN = PA_W;       // tiles of the shortest chunk: one a wave
-// Chunks that the rows are cut into: as many as the chip holds (three workgroups a CU) for
-// few rows, twice that for many, whose own ends then even out.  Rows below PA_FEW count as
-// few: 192 rows of compressed contexts 47.0 us with 768, 51.8 with 1536; 512 rows of ragged
-// sequences 74.8 with 1024, 73.4 with 1536, 74.0 with 2048.
-constexpr int PA_TARGET = 1536, PA_FEW = 256;
-// The last chunk of a row joins PA_JOIN states at a time; PA_COST weighs that against a tile's
-// step (chunks_of; half or twice as much is up to a fifth slower, and so are 32 states at a
-// time, 16 the same).  Without that limit on the chunks of a row one sequence of 128K tokens
-// and one KV head took 240 us with 16 query heads of 128 and 77 with one of 64; now 55 and
-// 24.  (Four dims a lane instead of two joins 16 heads faster, 48, and the others slower.)
+// The last chunk of a row joins PA_JOIN states at a time (32 are up to a fifth slower, 16 the
+// same; four dims a lane instead of two joins 16 heads faster, 128K tokens of one KV head 48 us
+// instead of 55, and the others slower).
 constexpr int PA_JOIN = 8;
-constexpr float PA_COST = 0.6f;
 
 static size_t al256(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -122,13 +110,6 @@ __device__ __forceinline__ void put_agent(unsigned long long* p, unsigned long l
   __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-template <int TILE>
-__device__ __forceinline__ int tiles_of(int64_t len, int64_t count) {
-  const int t = (int)((len + TILE - 1) / TILE) + (int)((count + TILE - 1) / TILE);
-  return t > 0 ? t : 1;              // an empty row has a chunk, which writes its zeros
-}
-// a row has at most PAGED_ROWS tokens in pages and as many packed entries: 2^22 tiles, so that
-// those of 256 rows are counted in 31 bits
 __device__ __forceinline__ int64_t held_count(const PrefixView& px, int64_t row, int64_t& start) {
   int64_t s = px.start[row], c = px.count[row];
   s = s < 0 ? 0 : (s > px.rows ? px.rows : s);
@@ -152,25 +133,6 @@ __device__ __forceinline__ int scan_wave(int v) {
 struct Chunk {
   int b, g, c, chunks, t0, t1;
 };
-
-// Tiles of a chunk: all rows' tiles over the places that the grid leaves beside one a row
-// (every row may leave one chunk unfilled), and no fewer than the waves.
-__device__ __forceinline__ int chunk_tiles(uint64_t total, int room) {
-  const uint64_t size = total < 0x7fffffffu ? ((uint32_t)total + (uint32_t)room - 1) / (uint32_t)room : (total + room - 1) / room;
-  return size < (uint64_t)PA_MIN ? PA_MIN : (size > 0x7fffffffu ? 0x7fffffff : (int)size);
-}
-// ... and chunks of a row of n tiles (below 2^24), n / size upwards, where size is also no less
-// than sqrt(join n), in whole steps of the waves.  A workgroup walks size / PA_W tiles a wave, one after the other, and the
-// last of a row's joins n / size states, PA_JOIN at a time, in join's passes over the heads:
-// the longer of few rows are bound by the sum of both.
-__device__ __forceinline__ int chunks_of(int n, int size, float join) {
-  size = max(size, ((int)sqrtf(join * (float)n) + PA_W / 2) & ~(PA_W - 1));
-  int c = (int)((float)n * (1.0f / (float)size));      // or next to it
-  int left = n - c * size;
-  if (left < 0) { --c; left += size; }
-  else if (left >= size) { ++c; left -= size; }
-  return c + (left > 0);
-}
 
 // The chunk of place `bid` of `places`; false past the last.  Rows are looked at as units:
 // (b, g) where a prefix makes their lengths differ, b (G equal rows) otherwise.  Every
@@ -278,8 +240,7 @@ __global__ __launch_bounds__(PA_T, PA_OCC) void k_paged(PageDims pg, int64_t q_t
   const int bid = groups > 1 ? blockIdx.x / groups : blockIdx.x, group = groups > 1 ? blockIdx.x % groups : 0;
   Chunk ck;
   const int places = groups > 1 ? gridDim.x / groups : gridDim.x;
-  const int passes = (min(PA_HEADS, pg.hpg) * (D / 2) + PA_T - 1) / PA_T;
-  if (!find_chunk<TILE, PREFIX>(pg, px, len, bid, places, PA_COST * passes, ck)) return;
+  if (!find_chunk<TILE, PREFIX>(pg, px, len, bid, places, join_cost(pg.hpg, D), ck)) return;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i16 = lane & 15, g4 = lane >> 4;
   const int h0 = group * PA_HEADS, heads = min(PA_HEADS, pg.hpg - h0);
   const T* PK = (const T*)px.K;
@@ -637,13 +598,7 @@ hipError_t launch_paged(const PageDims& pg, int64_t q_tok, const void* q, const 
   auto go = [&](auto type, auto dim, auto sub) {
     using T = decltype(type);
     constexpr int D = decltype(dim)::value, NS = decltype(sub)::value;
-    // Places beside one a row: half the rows leave theirs unfilled, and no larger a grid than
-    // the shortest chunks of the longest rows could make.
-    const int64_t tiles = R * ((((int64_t)pg.width << pg.shift) + 16 * NS - 1) / (16 * NS)) + (px.K ? px.rows / (16 * NS) + R : 0);
-    int64_t room = (tiles + PA_MIN - 1) / PA_MIN;
-    const int64_t target = R < PA_FEW ? PA_TARGET / 2 : PA_TARGET;
-    const int64_t most = target - R / 2 > target / 4 ? target - R / 2 : target / 4;
-    room = room < 1 ? 1 : (room > most ? most : room);
+    const int64_t room = chunk_room(pg, px.K ? px.rows : 0, 16 * NS);
     const dim3 grid((unsigned)((R + room) * ((pg.hpg + PA_HEADS - 1) / PA_HEADS)));
     if (px.K)
       hipLaunchKernelGGL((k_paged<T, D, NS, true>), grid, dim3(PA_T), 0, st, pg, q_tok, (const T*)q, (const T*)Kp, (const T*)Vp, table,

@@ -21,7 +21,6 @@ struct PromptDims {
   int64_t q_tok, q_head, k_tok, k_head, v_tok, v_head, o_tok, o_head;
 };
 constexpr int64_t PR_STRIDE = 1 << 24;    // longest distance of two rows of a prompt's keys or values
-constexpr int64_t PAGED_ROWS = 1 << 25;  // most tokens of a sequence's pages, and most packed entries of a row
 // the packed entries in front of the pages (all null: none)
 struct PrefixView {
   const int64_t* start;

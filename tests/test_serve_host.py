@@ -2,6 +2,7 @@
 checks (no GPU call is made), and the index arithmetic of the pages, compiled for the CPU."""
 import ctypes
 import os
+import random
 import subprocess
 
 import pytest
@@ -78,6 +79,94 @@ def test_page_arithmetic(tmp_path):
     subprocess.run(["g++", "-std=c++17", "-Wall", "-Werror", "-I", os.path.join(ROOT, "paper_2608_07001_amd", "csrc"),
                     str(tmp_path / "p.cpp"), "-o", str(tmp_path / "p")], check=True)
     assert subprocess.run([str(tmp_path / "p")], capture_output=True, text=True, check=True).stdout.strip() == "0"
+
+
+CHUNKS = r"""
+#include <stdio.h>
+#include <algorithm>
+#include <vector>
+#include "pages.h"
+using namespace gkv;
+// how a call's rows are cut: what launch_paged and find_chunk work out, printed for every shape read
+template <int TILE> void replay(const PageDims& p, int64_t px_rows, const std::vector<long>& len, const std::vector<long>& count) {
+  const int R = p.n_seq * p.G, units = px_rows ? R : p.n_seq, mult = px_rows ? 1 : p.G;
+  const int room = (int)chunk_room(p, px_rows, TILE);
+  std::vector<int> n;
+  uint64_t total = 0;
+  for (int u = 0; u < units; ++u) {
+    n.push_back(tiles_of<TILE>(held_len(p, len[px_rows ? u / p.G : u]), px_rows ? count[u] : 0));
+    total += (uint64_t)n[u] * mult;
+  }
+  const int size = chunk_tiles(total, room);
+  int64_t sum = 0;
+  int most = 0;
+  for (int x : n) {
+    const int c = chunks_of(x, size, join_cost(p.hpg, p.d));
+    sum += (int64_t)c * mult;
+    most = std::max(most, c);
+    if (c < 1 || (int64_t)(c - 1) * size >= x) most = 1 << 30;          // no chunk is empty
+  }
+  printf("%d %d %d %d %llu %lld %d\n", units, room, size, *std::max_element(n.begin(), n.end()), (unsigned long long)total,
+         (long long)sum, most);
+}
+int main() {
+  int bf, G, H, d, B, shift, width;
+  long px;
+  while (scanf("%d %d %d %d %d %d %d %ld", &bf, &G, &H, &d, &B, &shift, &width, &px) == 8) {
+    PageDims p{bf, G, H, d, H / G, B, shift, width, 1, 1};
+    std::vector<long> len(B), count(px ? B * G : 0);
+    for (long& x : len) if (scanf("%ld", &x) != 1) return 1;
+    for (long& x : count) if (scanf("%ld", &x) != 1) return 1;
+    if (!bf && d == 128) replay<16>(p, px, len, count); else replay<32>(p, px, len, count);
+  }
+  return 0;
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def chunks(tmp_path_factory):
+    """chunks(shapes): for each (dtype, d, G, H, lens, page, counts, rows) the units looked through, places beside
+    one a row, tiles of a chunk, of the longest row and of all, chunks of all and of the row with the most."""
+    at = tmp_path_factory.mktemp("chunks")
+    (at / "c.cpp").write_text(CHUNKS)
+    subprocess.run(["g++", "-O1", "-std=c++17", "-Wall", "-Werror", "-I", os.path.join(ROOT, "paper_2608_07001_amd", "csrc"),
+                    str(at / "c.cpp"), "-o", str(at / "c")], check=True)
+
+    def run(shapes):
+        text = []
+        for dtype, d, G, Hq, lens, page, counts, rows in shapes:
+            width = max(max(-(-n // page) for n in lens), 1)
+            text.append(" ".join(map(str, [int(dtype == "bf16"), G, Hq, d, len(lens), page.bit_length() - 1, width, rows] + lens
+                                     + (counts or []))))
+        out = subprocess.run([str(at / "c")], input="\n".join(text), capture_output=True, text=True, check=True).stdout
+        return [[int(x) for x in line.split()] for line in out.splitlines()]
+    return run
+
+
+def test_chunks_fit_the_grid(chunks):
+    """Every row's chunks have a place whatever the lengths are, none is empty, and the grid is as large
+    as rows with entries of their own could use."""
+    r = random.Random(1)
+    shapes = []
+    for i in range(3000):
+        G = r.choice([1, 2, 3, 8])
+        B = int(2 ** r.uniform(0, 9))
+        page = r.choice([16, 64, 256])
+        top = int(2 ** r.uniform(0, 17))
+        lens = [r.randint(0, top) if r.random() < 0.8 else r.choice([0, 1, 15, 33]) for _ in range(B)]
+        counts, rows = None, 0
+        if i % 2:                                              # entries of their own, or shared
+            few = int(2 ** r.uniform(0, 15))
+            counts = [r.randint(0, few) for _ in range(B * G)]
+            rows = sum(counts) + 1 if i % 4 == 1 else few
+        shapes.append((r.choice(["bf16", "f32"]), r.choice([64, 128]), G, G * r.choice([1, 4, 8, 20]), lens, page, counts, rows))
+    for shape, (units, room, size, longest, total, all_chunks, most) in zip(shapes, chunks(shapes)):
+        R = len(shape[4]) * shape[2]
+        assert most < 1 << 30 and all_chunks <= R + room, shape
+        target = 768 if R < 256 else 1536
+        if not shape[7] or shape[7] > sum(shape[6]):
+            assert room >= min(max(target - R // 2, target // 4), -(-total // 4) - R), shape
 
 
 def _prompt(**kw):
