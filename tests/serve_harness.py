@@ -11,6 +11,7 @@ logits of a row, X = max sum_i |q_i k_i| / sqrt(d) over its keys and A = sum_j p
 So |out - ref| <= A (w + 2 (n + n / 16 + 8) u [+ b]) + |ref| (u [or b]), and
 |lse - ref| <= w / 2 + (n + n / 16 + 8) u + 4 u |ref|."""
 import math
+import random
 
 import torch
 
@@ -93,3 +94,17 @@ def rotate64(x, cos, sin):
     a, e = x[..., :h], x[..., h:]
     c, s = cos[:, None], sin[:, None]
     return torch.cat([a * c - e * s, e * c + a * s], -1)
+
+
+def paged_shapes():
+    """Shapes that take paged attention down its rarer ways, name: (G, H, lens, page, counts of packed
+    entries or None).  `searched`: more units than a wave looks at in one round (64), rows of several
+    chunks among them, first, last and between; `long`: rows of more chunks than the join takes at once (d / 2)."""
+    r = random.Random(7)
+    ragged = [0 if i % 5 == 0 else r.randint(20, 60) for i in range(130)]
+    ragged[0], ragged[64], ragged[129] = 9000, 3001, 5003
+    few = [r.randint(0, 40) for _ in range(24)]
+    packed = [r.randint(0, 3000) if r.random() < 0.7 else r.choice([0, 1, 64]) for _ in range(24 * 8)]
+    packed[0], packed[63], packed[64], packed[191] = 3000, 2999, 0, 2800
+    return {"searched pages": (2, 4, ragged, 16, None), "searched entries": (8, 16, few, 16, packed),
+            "long pages": (1, 4, [131072], 64, None), "long entries": (1, 4, [100], 64, [131073])}

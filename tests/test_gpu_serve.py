@@ -562,6 +562,20 @@ def test_paged_every_batch_size():
         c.check()
 
 
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("name", list(S.paged_shapes()))
+def test_paged_rarer_ways(dtype, d, name):
+    # rows of several chunks among more units than one round of the search; rows of more chunks than the
+    # join takes at once (values that rise along the row: a part that is lost or taken twice shows)
+    G, Hq, lens, page, counts = S.paged_shapes()[name]
+    c = Cache(dtype, d, G, Hq, lens, page, counts, seed=24)
+    if name == "long pages":
+        c.V[c.table[0].long()] += torch.linspace(0, 4, lens[0]).view(-1, 1, page, 1).to(c.V.dtype)
+    if name == "long entries":
+        c.pre["V"][:counts[0]] += torch.linspace(0, 4, counts[0])[:, None].to(c.V.dtype)
+    c.check()
+
+
 def test_paged_prefix_of_no_rows():
     c = Cache("bf16", 64, 2, 6, [70, 0], 16, [0] * 4, seed=22)
     for name in ("K", "V", "logm"):

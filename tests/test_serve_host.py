@@ -8,6 +8,7 @@ import subprocess
 import pytest
 import torch
 
+import serve_harness as S
 from paper_2608_07001_amd import gracekv as gk
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -167,6 +168,20 @@ def test_chunks_fit_the_grid(chunks):
         target = 768 if R < 256 else 1536
         if not shape[7] or shape[7] > sum(shape[6]):
             assert room >= min(max(target - R // 2, target // 4), -(-total // 4) - R), shape
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 64), ("f32", 128)])
+def test_shapes_of_the_rarer_ways_take_them(chunks, dtype, d):
+    """The shapes that tests/test_gpu_serve.py runs for the search past its first round and for the join's
+    second block do reach them."""
+    shapes = S.paged_shapes()
+    cut = chunks([(dtype, d, G, Hq, lens, page, counts, sum(counts) + 3 if counts else 0)
+                  for G, Hq, lens, page, counts in shapes.values()])
+    for name, (units, room, size, longest, total, all_chunks, most) in zip(shapes, cut):
+        if name.startswith("searched"):
+            assert units > 64 and longest > size and most > 1, name
+        else:
+            assert most > d // 2, name
 
 
 def _prompt(**kw):
