@@ -96,6 +96,66 @@ def test_prompt_long(dtype, d):
     assert not _check_prompt(dtype, d, 8, 32, [1030, 1030], [1030, 1030], seed=10) or dtype == "f32"
 
 
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_prompt_piece_over_the_longest_contexts(dtype, d):
+    # a few queries over 128K keys, alone and beside short ones; values that rise along the keys
+    def edit(q, k, v):
+        v += torch.linspace(0, 4, v.shape[0])[:, None, None].to(v.dtype)
+    assert _check_prompt(dtype, d, 1, 4, [5], [131072 + 5], seed=25, edit=edit)
+    assert _check_prompt(dtype, d, 2, 4, [3, 1, 9], [40, 131072, 9], "head", seed=26, edit=edit)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_prompt_whole_context(d):
+    # a prefill of 128K tokens: rows from all over it against float64
+    n = 131072 + 33
+    gen = torch.Generator().manual_seed(27)
+    q, k, v = _rand(gen, n, 2, d, scale=1.5), _rand(gen, n, 1, d), _rand(gen, n, 1, d)
+    v += torch.linspace(0, 4, n)[:, None, None].to(v.dtype)
+    out, lse, _ = _prompt(q, k, v, _cu([n]), _cu([n]))
+    rows = torch.cat([torch.tensor([0, 1, 63, 64, 4095, 65535, 65536, n - 33, n - 1]), torch.randint(0, n, (40,), generator=gen)])
+    k64, v64 = k[:, 0].double(), v[:, 0].double()
+    for i in rows.tolist():
+        S.check_rows(out[i], lse[i], S.attend64(q[i].double(), k64[:i + 1], v64[:i + 1]), i + 1, d, True, i)
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("G,Hq,lq,lk", [(1, 32, 259, 259), (1, 2, 259, 259), (1, 2, 6, 259)])
+def test_prompt_far_rows(dtype, G, Hq, lq, lk):
+    """Rows 2^24 elements apart, the longest distance of keys and values: the last lie past 32 bits of elements,
+    in pairs (bf16, 32 heads), single waves and parts (fp32); then heads 2^32 elements apart.  Appending likewise."""
+    d, far = 128, 1 << 24
+    gen = torch.Generator().manual_seed(28)
+    q, k, v = (_rand(gen, n, x, d, dtype=dtype) for n, x in ((lq, Hq), (lk, G), (lk, G)))
+    pool = torch.empty((lk + 1) * far, dtype=DT[dtype], device="cuda")
+
+    def place(x, at):                                          # rows of all heads, `far` apart
+        y = pool[at:].as_strided(x.shape, (far, d, 1))
+        return y.copy_(x)
+    room = 32 * d + 8
+    qd, kd, vd, out = place(q, 0), place(k, room), place(v, 2 * room), place(torch.full_like(q, 7), 3 * room)
+    lse = torch.empty(lq, Hq, device="cuda")
+
+    def run(qd, kd, vd, out):
+        cfg = gk.prompt_config(qd, kd, vd, out, 1)
+        ws = torch.full((max(gk.prompt_ws_bytes(cfg), 1),), 255, dtype=torch.uint8, device="cuda")
+        gk.prompt_attention(cfg, qd, kd, vd, _cu([lq]).cuda(), _cu([lk]).cuda(), out, ws, lse=lse)
+        got, got_lse = out.cpu(), lse.cpu()
+        S.prompt64(q.double(), k.double(), v.double(), [lq], [lk],
+                   lambda rows, h, ref, m: S.check_rows(got[rows, h], got_lse[rows, h], ref, m, d, dtype == "bf16", (dtype, Hq, h)))
+    run(qd, kd, vd, out)
+    table = torch.arange(17, dtype=torch.int32, device="cuda")[None]
+    K = torch.zeros(17, G, 16, d, dtype=DT[dtype], device="cuda")
+    V = torch.zeros_like(K)
+    gk.cache_append(gk.page_config(K, Hq, table), kd, vd, K, V, table, torch.zeros(1, dtype=torch.int32, device="cuda"), _cu([lk]).cuda())
+    for got, want in ((K, k), (V, v)):
+        assert torch.equal(got.transpose(1, 2).reshape(-1, G, d)[:lk].cpu(), want)
+    if Hq == 2:                                                # the second head past 32 bits
+        two = lambda x, at: pool[at:].as_strided(x.shape, (d, 1 << 32, 1)).copy_(x)      # noqa: E731
+        run(two(q, 0), place(k, room << 4), place(v, room << 5), two(torch.full_like(q, 7), 1 << 20))
+
+
 @pytest.mark.parametrize("d", [64, 128])
 def test_prompt_waves_in_pairs(d):
     # few short prompts of many heads: two waves to the same rows; odd ends, a row with no key, infinities
