@@ -390,9 +390,9 @@ gracekv_status gracekv_decode_attention_noalloc(const gracekv_config* cfg, const
  * anything is enqueued) and take no gracekv_config: their shapes come in the
  * structures below.  Types: GRACEKV_BF16 and GRACEKV_F32; d: 64 or 128; any H / G.
  * Strides are in elements and multiples of 16 bytes; the elements of a head are
- * contiguous.  Logits are q.k / sqrt(d), softmax statistics are fp32; bf16
- * probabilities are rounded to bf16 in the product with the values.  The outputs are of
- * the inputs' type, lse = log sum exp of the logits is fp32 (natural logarithm;
+ * contiguous.  Logits are q.k / sqrt(d), softmax statistics are fp32.  In the product with
+ * bf16 values the probabilities of a prompt are rounded to bf16 (each off by at most 2^-8 of
+ * itself), those over pages are held in two bf16 parts (2^-15).  The outputs are of the inputs' type, lse = log sum exp of the logits is fp32 (natural logarithm;
  * NULL: not wanted).  Values are summed under weights of at most 1 and then divided by the
  * weights' sum: |v| times the keys of a row has to stay below 2^127, and what is below
  * 2^-118 in size may lose bits.  A query with no key has the output 0 and lse -inf; a masked or

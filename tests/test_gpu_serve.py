@@ -581,6 +581,45 @@ def test_paged_infinite_values_stay_in_their_dimension(dtype, d, bad):
     c.check()
 
 
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_paged_infinite_values_at_the_smallest_weights(dtype, d):
+    # infinities at weights from 1 down to e^-84, among them some that bf16 holds exactly
+    c = Cache(dtype, d, 1, 4, [20], 16, [60], seed=25)
+    c.q[:] = 0.0
+    c.pre["logm"][:] = 0.0
+    for i, (dim, lm) in enumerate([(1, 0.0), (2, -math.log(2.0)), (3, -1.0), (4, -20.0), (5, -60.0), (6, -78.0), (7, -80.0), (8, -84.0)]):
+        c.pre["logm"][3 * i + 1] = lm
+        c.pre["V"][3 * i + 1, dim] = math.inf if i % 2 else -math.inf
+    c.check()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_paged_weights_keep_more_than_bf16(d):
+    """Values that nearly cancel under weights that bf16 does not hold: the output is far below the
+    weighted values, and so are the weights' errors, 2^-15 of themselves (two bf16 parts), where weights
+    rounded to bf16 would leave up to 2^-8."""
+    gen = torch.Generator().manual_seed(26)
+    for lens, counts in (([700], None), ([0], [900]), ([3000], [40])):
+        c = Cache("bf16", d, 1, 16, lens, 16, counts, seed=27)
+        amp = (torch.rand(d, generator=gen) + 0.5).bfloat16()
+        c.q[:] = torch.linspace(0.05, 0.3, 16)[None, :, None].bfloat16()
+        for K, V in [(c.K, c.V)] + ([] if counts is None else [(c.pre["K"], c.pre["V"])]):
+            odd = torch.arange(K.shape[-2]) % 2 == 1
+            K[:] = 0.0
+            K[..., odd, :] = -1.0 / math.sqrt(d)
+            V[:] = amp
+            V[..., odd, :] = -amp
+        if counts is not None:
+            c.pre["logm"][:] = 0.0
+        out, lse = c.call()
+        k, v, lm = c.entries(0, 0)
+        ref, ref_lse, A, X = S.attend64(c.q[0].double(), k, v, bias=lm)
+        n = len(k)
+        w = 2 * ((d + 3) * X + 4 * X + 4) * S.U + 2.0 ** -15
+        tol = A * (w + 2 * (n + n / 16 + 8) * S.U)[:, None] + ref.abs() * S.B16
+        assert ((out[0].double() - ref).abs() <= tol).all(), (d, lens, float(((out[0].double() - ref).abs() / tol).max()))
+
+
 def test_paged_malformed_inputs_stay_inside():
     # lengths past the table, negative ones, pages that are none, packed rows outside the arrays
     c = Cache("bf16", 64, 2, 4, [40, 20, 33], 16, [10, 20, 5, 6, 7, 8], seed=9)
