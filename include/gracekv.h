@@ -403,7 +403,7 @@ gracekv_status gracekv_decode_attention_noalloc(const gracekv_config* cfg, const
 /* Causal attention over packed prompts. */
 typedef struct {
   int32_t dtype, G, H, d;           /* gracekv_dtype, KV heads, query heads, head dim */
-  int32_t n_seq;                    /* sequences */
+  int32_t n_seq;                    /* sequences, at least 1 */
   int32_t reserved;                 /* 0 */
   int64_t n_q, n_k;                 /* rows of Q and out; rows of K and V (at most 2^30) */
   int64_t q_tok, q_head, k_tok, k_head, v_tok, v_head, out_tok, out_head; /* strides */
@@ -437,7 +437,7 @@ gracekv_status gracekv_prompt_attention(const gracekv_prompt_config* cfg, const 
  * no page: nothing is written there, and its tokens do not take part in attention. */
 typedef struct {
   int32_t dtype, G, H, d;
-  int32_t n_seq;
+  int32_t n_seq;                    /* at least 1 */
   int32_t page_size;                /* 16, 32, 64, 128 or 256 */
   int32_t table_width;              /* table_width * page_size <= 2^25; n_seq * G <= 65536 */
   int32_t reserved;                 /* 0 */
@@ -462,6 +462,7 @@ typedef struct {
  *   pos        [n_new] int32: row of rope_cos, rope_sin ([rope_rows][d/2] fp32, as
  *              above) that turns the token's key and query; all three NULL: nothing is
  *              turned (keys that are rotated already)
+ * With n_new = 0 k, v, q, q_out, pos and the tables may each be NULL.
  * A token whose place has no page, or whose position is outside the tables, is left out:
  * neither its key and value nor its rotated query is written.  Two tokens with one place race.
  * Products and sums of the rotation are fp32, rounded once. */

@@ -647,9 +647,8 @@ gracekv_status gracekv_cache_append(const gracekv_page_config* c, const gracekv_
   PageDims pg;
   const gracekv_status s = page_dims(c, &pg);
   if (s != GRACEKV_OK) return s;
-  if (!r || (r->n_new > 0 && (!k || !v)) || !block_table || !start || !cu_new || !K_pages || !V_pages) return GRACEKV_ERR_INVALID_ARG;
-  if (!q != !q_out) return GRACEKV_ERR_INVALID_ARG;
-  if (!pos != !rope_cos || !pos != !rope_sin) return GRACEKV_ERR_INVALID_ARG;
+  if (!r || !block_table || !start || !cu_new || !K_pages || !V_pages) return GRACEKV_ERR_INVALID_ARG;
+  if (r->n_new > 0 && (!k || !v || !q != !q_out || !pos != !rope_cos || !pos != !rope_sin)) return GRACEKV_ERR_INVALID_ARG;
   if (!aligned16(k) || !aligned16(v) || !aligned16(q) || !aligned16(K_pages) || !aligned16(V_pages) || !aligned16(q_out) ||
       !aligned16(rope_cos) || !aligned16(rope_sin))
     return GRACEKV_ERR_INVALID_ARG;

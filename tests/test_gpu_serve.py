@@ -418,6 +418,22 @@ def test_append_many_sequences():
     assert torch.equal(K.cpu(), want) and torch.equal(V.cpu(), want)
 
 
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_append_nothing(dtype, d):
+    # a step in which no sequence has a new token, with and without queries and rotation
+    table = torch.arange(4, dtype=torch.int32, device="cuda").view(2, 2)
+    K = torch.full((4, 2, 16, d), 5.0, dtype=DT[dtype], device="cuda")
+    V, start, cu = K.clone(), torch.tensor([3, 20], dtype=torch.int32, device="cuda"), _cu([0, 0]).cuda()
+    cfg = gk.page_config(K, 4, table)
+    cos, sin = (x.cuda() for x in _rope(50, d))
+    k, q = torch.ones(0, 2, d, dtype=DT[dtype], device="cuda"), torch.ones(0, 4, d, dtype=DT[dtype], device="cuda")
+    pos = torch.zeros(0, dtype=torch.int32, device="cuda")
+    gk.cache_append(cfg, k, k, K, V, table, start, cu, pos, cos, sin, q, q.clone())
+    gk.cache_append(cfg, k, k, K, V, table, start, cu, pos, cos, sin)
+    gk.cache_append(cfg, k, k, K, V, table, start, cu)
+    assert (K == 5).all() and (V == 5).all()
+
+
 def test_append_descending_starts_stay_inside():
     # a token lands in its own place of a sequence that could hold it, or nowhere
     gen = torch.Generator().manual_seed(17)

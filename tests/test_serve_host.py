@@ -293,6 +293,26 @@ def test_append_refuses_pointers_and_strides():
     assert gk.lib().gracekv_cache_append(ctypes.byref(c), None, *[FAKE] * 12, None) == -1
 
 
+def test_nothing_to_append_is_no_error():
+    # a call of no tokens: tensors without elements have no address, tables and pools do
+    c = _page()
+    names = ["k", "v", "q", "table", "start", "cu", "pos", "cos", "sin", "K", "V", "q_out"]
+
+    def call(n_new=0, rope_rows=16, **kw):
+        r = gk.AppendConfig(n_new, rope_rows, 1024, 128, 1024, 128, 4096, 128, 4096, 128)
+        return gk.lib().gracekv_cache_append(ctypes.byref(c), ctypes.byref(r), *[kw.get(n, FAKE) for n in names], None)
+    assert call() == 0
+    assert call(k=None, v=None, q=None, q_out=None, pos=None) == 0
+    assert call(k=None, v=None, q=None, pos=None) == 0         # the output's buffer may be there all the same
+    assert call(rope_rows=0, cos=None, sin=None) == 0 and call(pos=None, cos=None, sin=None) == 0
+    for name in ("table", "start", "cu", "K", "V"):
+        assert call(**{name: None}) == -1, name
+    for name in ("k", "cos", "K", "q_out"):
+        assert call(**{name: ODD}) == -1, name
+    for kw in (dict(pos=None), dict(q=None), dict(cos=None), dict(cos=None, sin=None, rope_rows=0), dict(k=None)):
+        assert call(n_new=3, **kw) == -1, kw
+
+
 def test_binding_refuses_other_tensors(monkeypatch):
     q, k = torch.zeros(4, 8, 64), torch.zeros(4, 2, 64)
     with pytest.raises(ValueError, match="k: got 32"):
