@@ -156,6 +156,30 @@ def test_prompt_far_rows(dtype, G, Hq, lq, lk):
         run(two(q, 0), place(k, room << 4), place(v, room << 5), two(torch.full_like(q, 7), 1 << 20))
 
 
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_prompt_broadcast_rows_and_heads(dtype, d):
+    # strides of 0: one query, key or value for all tokens, or for all heads
+    gen = torch.Generator().manual_seed(29)
+    for G, Hq, lq, lk in ((2, 8, [70, 1, 33], [70, 40, 33]), (8, 32, [600], [600]), (2, 4, [3], [2500])):
+        n, m = sum(lq), sum(lk)
+        for which in range(3):
+            q = _rand(gen, n if which else 1, Hq, d, dtype=dtype).expand(n, Hq, d)
+            k = _rand(gen, m, 1 if which else G, d, dtype=dtype).expand(m, G, d)
+            v = _rand(gen, 1 if which == 2 else m, G, d, dtype=dtype).expand(m, G, d)
+            if which == 0:
+                k = k[:1].expand(m, G, d)
+            out, lse = torch.full((n, Hq, d), 7.0, dtype=DT[dtype], device="cuda"), torch.full((n, Hq), 7.0, device="cuda")
+            dev = [x.cuda() if 0 not in x.stride() else x[:1 if x.stride(0) == 0 else None, :1 if x.stride(1) == 0 else None].cuda().expand(x.shape)
+                   for x in (q, k, v)]
+            assert [x.stride() for x in dev] != [x.contiguous().stride() for x in dev]
+            cfg = gk.prompt_config(*dev, out, len(lq))
+            ws = torch.full((max(gk.prompt_ws_bytes(cfg), 1),), 255, dtype=torch.uint8, device="cuda")
+            gk.prompt_attention(cfg, *dev, _cu(lq).cuda(), _cu(lk).cuda(), out, ws, lse=lse)
+            got, got_lse = out.cpu(), lse.cpu()
+            S.prompt64(q.double(), k.double(), v.double(), lq, lk,
+                       lambda rows, h, ref, mm: S.check_rows(got[rows, h], got_lse[rows, h], ref, mm, d, dtype == "bf16", (which, h)))
+
+
 @pytest.mark.parametrize("d", [64, 128])
 def test_prompt_waves_in_pairs(d):
     # few short prompts of many heads: two waves to the same rows; odd ends, a row with no key, infinities
@@ -825,6 +849,32 @@ def test_step_captured_and_replayed_on_a_stream():
         side.synchronize()
         assert torch.equal(K2, dev["K"]) and torch.equal(V2, dev["V"])
         assert torch.equal(got[0], out) and torch.equal(got[1], lse) and torch.equal(got[2], qr)
+
+
+def test_two_graphs_in_turn_on_one_workspace():
+    """Two captured batches of different shapes and types, one workspace, replayed one after the other."""
+    a = Cache("bf16", 128, 2, 8, [4001, 3, 0, 900], 16, [5] * 8, seed=31)
+    b = Cache("f32", 64, 1, 20, [60] * 20 + [3000], 16, seed=32)
+    size = max(gk.paged_ws_bytes(gk.page_config(c.K, c.H, c.table)) for c in (a, b))
+    ws = torch.full((size,), 255, dtype=torch.uint8, device="cuda")
+    side, runs = torch.cuda.Stream(), []
+    for c in (a, b):
+        dev = {n: getattr(c, n).cuda() for n in ("K", "V", "table", "len", "q")}
+        pre = None if c.pre is None else gk.Prefix(**{n: x.cuda() for n, x in c.pre.items()})
+        out, lse = torch.empty_like(dev["q"]), torch.empty(c.q.shape[:2], device="cuda")
+        graph = torch.cuda.CUDAGraph()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.graph(graph, stream=side):
+            gk.paged_attention(gk.page_config(dev["K"], c.H, dev["table"]), dev["q"], dev["K"], dev["V"], dev["table"], dev["len"], out, ws,
+                               lse=lse, prefix=pre)
+        runs.append((c, graph, out, lse, dev, pre))
+    for _ in range(4):
+        for c, graph, out, lse, _, _ in runs:
+            out.fill_(7.0)
+            graph.replay()
+        torch.cuda.synchronize()
+        for c, _, out, lse, _, _ in runs:
+            c.check((out.cpu(), lse.cpu()))
 
 
 def test_prompt_captured_and_replayed():
