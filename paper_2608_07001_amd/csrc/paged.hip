@@ -35,7 +35,7 @@
 // bf16 probabilities go into the second product as two bf16 parts, off by at most 2^-15 of
 // themselves, so what remains is the output's own rounding.  The matrix pipes wait for memory
 // in any case: the second half costs 64 ragged sequences nothing (74.1 us), 24 compressed
-// contexts 48.1 -> 48.5, the smallest call 10.2 -> 10.3.  fp32 caches use the fp32 matrix
+// contexts 48.1 -> 48.5, the smallest call 9.7 -> 9.8.  fp32 caches use the fp32 matrix
 // instructions.
 #include "serve.h"
 

@@ -23,12 +23,14 @@
 //
 // bf16 probabilities are rounded to bf16 (nearest even) as operands, their sum takes them
 // unrounded: each weight is off by at most 2^-8 of itself, at random, like the output's
-// own rounding.  fp32 uses the fp32 matrix instructions.
+// own rounding, and the error against 64 bits is 0.5 to 3 % larger than that rounding's
+// alone.  (A second part of the weights, as over pages, would add half of the products, which
+// are what bounds long prompts.)  fp32 uses the fp32 matrix instructions.
 //
 // What bounds it: long prompts by the products and what goes on beside them.  16K tokens of
 // the 8B heads take 1.97 to 2.03 ms on different devices, 1.09 to 1.13 PFLOP/s of the pairs
 // that are seen (a library product of 8192^3 reaches 1.32): the matrix pipes are busy in
-// 64 % of the cycles, LDS in 32 %, without a bank conflict, and the chip runs at 1.7 GHz of
+// 63 % of the cycles, LDS in 32 %, without a bank conflict, and the chip runs at 1.7 GHz of
 // its 2.4; without the softmax, for timing, the same loop reached 1.26, without loads as
 // well 1.36.  What was tried and left: tiles of
 // 64 keys with two waves a SIMD (2.00 ms), through registers instead of straight into LDS
@@ -100,7 +102,15 @@ static Plan prompt_plan(const PromptDims& pd) {
   // four times as long: three times, 1056 tokens of the 8B heads 134 -> 111 us; the same in
   // bf16 slows 1024 tokens down, 27 -> 39), more where they are few, each part holding at
   // least so many keys of the longest row that joining it is worth it (bf16 with 128: 256
-  // tokens 12 -> 17 us; fp32 with 256: 300 tokens 27 -> 30).
+  // tokens 12 -> 17 us; fp32 with 256: 300 tokens 27 -> 30).  The lengths lie on the device, so
+  // one number of parts serves all sequences, and the longest row is taken to see all n_k keys,
+  // as it does where one sequence holds most of them.  Batches of pieces as long as each other
+  // are cut a little more often than they need: 31 x 16 queries over 256 keys (2 KV heads, 16
+  // heads) 12.7 us and 12.8 uncut, 8 x 100 over 700 (4, 16) 26.0 and 24.5, 20 x 30 over 1000
+  // (2, 8) 23.3 and 30.8, fp32 16 x 64 over 512 (8, 32) 118 and 120; with the longest estimated
+  // as above the same.  Batches of very different ones are cut too little, since the row tiles
+  // of the short count too: one query over 30000 keys of the 8B heads 32 us alone, 179 beside 15
+  // over 50 (676 uncut); 64 over 32K 65 alone, 269 beside 7 x 64 over 200.
   const int64_t n = tiles(p.rows), fill = bf ? PR_FILL : PR_FILL + PR_FILL / 2, keys = bf ? 256 : 128;
   const int64_t want = n && !p.split ? (fill + n - 1) / n : 1, most = (pd.n_k + keys - 1) / keys;
   const int64_t cap = want > most ? (most < 1 ? 1 : most) : want;
@@ -139,7 +149,12 @@ struct Item {
 
 // The item of workgroup blockIdx.x; false where there is none.  Pairs of one KV head and
 // part are neighbours modulo G, so with G a multiple of 8 a KV head stays on one XCD's
-// L2; the tiles with the most keys come first.
+// L2.  Row tiles are taken from the last to the first, so a sequence's tiles with the most
+// keys come first, and the last sequence's before the others'.  Where the tiles are few, a long
+// sequence at the batch's beginning ends later for that: 4000 tokens and 11 x 200 of the 8B
+// heads 168 us with the long one first, 150 with it last (the 70B heads' eight sequences of 1 to
+// 4099 tokens take 354 to 357 in any order).  Sequences ordered by their lengths on the device
+// gained 10 % there and cost 64 sequences of 64 tokens 26 -> 34 us.
 template <int ROWS, int KEYS>
 __device__ __forceinline__ bool find_item(const PromptDims& pd, const int32_t* cu_q, const int32_t* cu_k, int parts, Item& it) {
   uint32_t bid = blockIdx.x;
