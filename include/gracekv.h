@@ -67,7 +67,7 @@ typedef enum { GRACEKV_F32 = 0, GRACEKV_BF16 = 1 } gracekv_dtype;
 /* Version of this interface (structures and signatures).  A binding must
  * refuse a library whose gracekv_abi_version() differs from the value it was
  * written for: argument lists shift silently across versions. */
-#define GRACEKV_ABI_VERSION 12
+#define GRACEKV_ABI_VERSION 13
 
 /* Shapes and hyperparameters.  gracekv_default_config fills the paper's
  * defaults (App. A and B); the caller then sets the shape fields. */
@@ -504,6 +504,109 @@ gracekv_status gracekv_paged_attention(const gracekv_page_config* cfg, const voi
                                        const void* V_pages, const int32_t* block_table, const int32_t* seq_len,
                                        const gracekv_prefix* prefix, void* out, float* lse, void* ws, size_t ws_bytes,
                                        void* stream);
+
+/* An attention of the same queries over other entries, to be joined to one over pages: out
+ * and lse become those over both.  gracekv_shared_attention writes one. */
+typedef struct {
+  float* o;                         /* [n_seq][H][d] fp32: the mean of the values; not out */
+  float* lse;                       /* [n_seq][H] fp32; -inf: over no entry, whatever its row of o holds */
+} gracekv_part;
+
+/* gracekv_paged_attention, joined to `part` (host structure, read by the call; NULL: none). */
+gracekv_status gracekv_paged_attention_part(const gracekv_page_config* cfg, const void* q, int64_t q_tok,
+                                            const void* K_pages, const void* V_pages, const int32_t* block_table,
+                                            const int32_t* seq_len, const gracekv_prefix* prefix, const gracekv_part* part,
+                                            void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Quantised pages.  Keys and values lie in blocks of 32 neighbouring dims of one token and
+ * KV head: a code for each value and a scale byte s for the block, value = code * 2^(s - 127);
+ * s = 255: the block stands for NaN.  GRACEKV_E4M3 (8 bits, largest code 448): a byte a
+ * value; GRACEKV_E2M1 (4 bits, largest 6): dim 2 i in the low half of byte i, 2 i + 1 in its
+ * upper half.  A block is written with the least s for which its largest size is at most 464
+ * (E4M3) or 7 (E2M1) times 2^(s - 127), and at least 10: every value is the nearest code's
+ * (the even one in the middle), off by at most 2^-4 (E4M3) or 2^-2 (E2M1) of the block's
+ * largest size, or, where s is held at 10, by 2^-127 or 2^-119.  A block with a size of 2^127 or
+ * more, an infinity or a NaN is written with s = 255.
+ *
+ * The gracekv_page_config of such a cache has the type of the rows around it (k, v, q, out)
+ * as dtype; page i begins at code i * page_stride, a multiple of 16 bytes of codes. */
+typedef enum { GRACEKV_E4M3 = 0, GRACEKV_E2M1 = 1 } gracekv_format;
+
+typedef struct {                    /* host structure, read by the calls */
+  int32_t format;                   /* gracekv_format */
+  int32_t reserved;                 /* 0 */
+  int64_t scale_stride;             /* bytes from page to page of the scales, a multiple of 16 */
+  void* K;                          /* codes: each page [G][page_size][d] */
+  void* V;
+  uint8_t* K_scale;                 /* scales: each page [G][page_size][d / 32] */
+  uint8_t* V_scale;
+} gracekv_quant_pages;
+
+/* gracekv_cache_append into quantised pages: the same arguments, conditions and tokens left
+ * out.  A key is quantised from fp32, where the products of its rotation and their sum are each
+ * rounded; a rotated query is rounded to cfg->dtype from the same. */
+gracekv_status gracekv_quant_append(const gracekv_page_config* cfg, const gracekv_append_config* rows,
+                                    const gracekv_quant_pages* pages, const void* k, const void* v, const void* q,
+                                    const int32_t* block_table, const int32_t* start, const int32_t* cu_new,
+                                    const int32_t* pos, const float* rope_cos, const float* rope_sin, void* q_out,
+                                    void* stream);
+
+/* Rows of gracekv_quant_read. */
+typedef struct {
+  int64_t n_rows;                   /* rows of k and v, below 2^24 */
+  int64_t k_tok, k_head, v_tok, v_head; /* strides */
+} gracekv_read_config;
+
+/* Keys and values back from quantised pages: row cu_rows[b] + i of k and v becomes what
+ * place start[b] + i of sequence b stands for, exactly (fp32; bf16 holds it too; past their
+ * range, where no append leaves a value, infinite).
+ *   k, v       [n_rows] x G (cfg->dtype), written; either may be NULL: not wanted
+ *   start      [n_seq] int32: the first place of each sequence
+ *   cu_rows    [n_seq + 1] int32, ascending, as cu_new above
+ * A place that has no page gives zeros; rows outside every sequence are left as they are. */
+gracekv_status gracekv_quant_read(const gracekv_page_config* cfg, const gracekv_read_config* rows,
+                                  const gracekv_quant_pages* pages, const int32_t* block_table, const int32_t* start,
+                                  const int32_t* cu_rows, void* k, void* v, void* stream);
+
+/* gracekv_paged_attention_part over quantised pages, without packed entries of its own
+ * (those of a compressed context come as a part: gracekv_shared_attention).  Codes
+ * and scales are taken exactly; queries and weights in bf16 parts, one and two (bf16 rows:
+ * weights off by at most 2^-15) or three (fp32 rows).  ws: gracekv_paged_ws_bytes(cfg) bytes, as there. */
+gracekv_status gracekv_quant_attention(const gracekv_page_config* cfg, const gracekv_quant_pages* pages, const void* q,
+                                       int64_t q_tok, const int32_t* block_table, const int32_t* seq_len,
+                                       const gracekv_part* part, void* out, float* lse, void* ws, size_t ws_bytes,
+                                       void* stream);
+
+/* Attention of one token of every sequence over packed entries that groups of sequences
+ * share (many questions on one compressed context), each gone through once for its group. */
+typedef struct {
+  int32_t dtype, G, H, d;
+  int32_t n_seq, n_group;           /* at least 1; n_group * G <= 65536 */
+  int64_t q_tok;                    /* stride of q's rows */
+} gracekv_shared_config;
+
+/* Workspace of gracekv_shared_attention (bytes). */
+gracekv_status gracekv_shared_ws_bytes(const gracekv_shared_config* cfg, size_t* ws_bytes);
+
+/* Group s has the sequences cu_group[s] .. cu_group[s+1] - 1, and of KV head g the entries
+ * that prefix->start and ->count [n_group * G] give, with logits q.k / sqrt(d) + logm; an entry
+ * with logm = -inf has no weight.  For one group these are gracekv_pack's outputs as they stand.
+ *   q          [n_seq] rows x [H][d], rows q_tok elements apart, rotated already
+ *   cu_group   [n_group + 1] int32, ascending; places outside [0, n_seq] are held inside.  Where
+ *              they descend, the call stays inside the arrays, but what it writes there is
+ *              not specified
+ *   prefix     host structure, read by the call
+ *   part       host structure, read by the call: its arrays are written, o 16-byte aligned;
+ *              sequences outside every group are left as they are (one without entries belongs to
+ *              a group of count 0 and gets 0 and -inf)
+ *   ws         gracekv_shared_ws_bytes bytes, which need no initialisation; calls that overlap
+ *              on one workspace race
+ * bf16: weights are rounded to bf16 for the product with the values, as a prompt's are.
+ * Starts, counts and groups must not change while the call runs. */
+gracekv_status gracekv_shared_attention(const gracekv_shared_config* cfg, const void* q, const int32_t* cu_group,
+                                        const gracekv_prefix* prefix, const gracekv_part* part, void* ws,
+                                        size_t ws_bytes, void* stream);
 
 /* Layout check of the cross-lane instructions used by the kernels: computes
  * a 16x16 product from fixed inputs with the fp32 16x16x4 (which = 0), the

@@ -640,24 +640,35 @@ static gracekv_status page_dims(const gracekv_page_config* c, PageDims* pg) {
   return GRACEKV_OK;
 }
 
-gracekv_status gracekv_cache_append(const gracekv_page_config* c, const gracekv_append_config* r, const void* k,
-                                    const void* v, const void* q, const int32_t* block_table, const int32_t* start,
-                                    const int32_t* cu_new, const int32_t* pos, const float* rope_cos,
-                                    const float* rope_sin, void* K_pages, void* V_pages, void* q_out, void* stream) {
-  PageDims pg;
-  const gracekv_status s = page_dims(c, &pg);
-  if (s != GRACEKV_OK) return s;
-  if (!r || !block_table || !start || !cu_new || !K_pages || !V_pages) return GRACEKV_ERR_INVALID_ARG;
+// what both forms of an append ask of its rows
+static gracekv_status append_dims(const gracekv_page_config* c, const gracekv_append_config* r, const void* k, const void* v,
+                                  const void* q, const int32_t* block_table, const int32_t* start, const int32_t* cu_new,
+                                  const int32_t* pos, const float* rope_cos, const float* rope_sin, const void* q_out,
+                                  AppendDims* ap) {
+  if (!r || !block_table || !start || !cu_new) return GRACEKV_ERR_INVALID_ARG;
   if (r->n_new > 0 && (!k || !v || !q != !q_out || !pos != !rope_cos || !pos != !rope_sin)) return GRACEKV_ERR_INVALID_ARG;
-  if (!aligned16(k) || !aligned16(v) || !aligned16(q) || !aligned16(K_pages) || !aligned16(V_pages) || !aligned16(q_out) ||
-      !aligned16(rope_cos) || !aligned16(rope_sin))
+  if (!aligned16(k) || !aligned16(v) || !aligned16(q) || !aligned16(q_out) || !aligned16(rope_cos) || !aligned16(rope_sin))
     return GRACEKV_ERR_INVALID_ARG;
   if (r->n_new < 0 || r->rope_rows < 0) return GRACEKV_ERR_INVALID_ARG;
   for (int64_t x : {r->k_tok, r->k_head, r->v_tok, r->v_head, r->q_tok, r->q_head, r->qout_tok, r->qout_head})
     if (!stride_ok(c->dtype, x)) return GRACEKV_ERR_INVALID_ARG;
   if (q && ((r->qout_tok == 0 && r->n_new > 1) || (r->qout_head == 0 && c->H > 1))) return GRACEKV_ERR_INVALID_ARG;
   if (r->n_new > MOST_GROUPS) return GRACEKV_ERR_UNSUPPORTED;
-  const AppendDims ap{r->n_new, r->rope_rows, r->k_tok, r->k_head, r->v_tok, r->v_head, r->q_tok, r->q_head, r->qout_tok, r->qout_head};
+  *ap = AppendDims{r->n_new, r->rope_rows, r->k_tok, r->k_head, r->v_tok, r->v_head, r->q_tok, r->q_head, r->qout_tok, r->qout_head};
+  return GRACEKV_OK;
+}
+
+gracekv_status gracekv_cache_append(const gracekv_page_config* c, const gracekv_append_config* r, const void* k,
+                                    const void* v, const void* q, const int32_t* block_table, const int32_t* start,
+                                    const int32_t* cu_new, const int32_t* pos, const float* rope_cos,
+                                    const float* rope_sin, void* K_pages, void* V_pages, void* q_out, void* stream) {
+  PageDims pg;
+  gracekv_status s = page_dims(c, &pg);
+  if (s != GRACEKV_OK) return s;
+  if (!K_pages || !V_pages || !aligned16(K_pages) || !aligned16(V_pages)) return GRACEKV_ERR_INVALID_ARG;
+  AppendDims ap;
+  s = append_dims(c, r, k, v, q, block_table, start, cu_new, pos, rope_cos, rope_sin, q_out, &ap);
+  if (s != GRACEKV_OK) return s;
   return hip_status(launch_append(pg, ap, k, v, q, block_table, start, cu_new, pos, rope_cos, rope_sin, K_pages, V_pages, q_out,
                                   (hipStream_t)stream));
 }
@@ -671,10 +682,36 @@ gracekv_status gracekv_paged_ws_bytes(const gracekv_page_config* c, size_t* ws_b
   return GRACEKV_OK;
 }
 
+// a part that is read: null, or both of its arrays
+static bool part_view(const gracekv_part* part, PartView* v) {
+  *v = PartView{nullptr, nullptr};
+  if (!part) return true;
+  if (!part->o || !part->lse || !aligned16(part->o) || !aligned16(part->lse)) return false;
+  *v = PartView{part->o, part->lse};
+  return true;
+}
+static bool prefix_view(const gracekv_prefix* prefix, PrefixView* px) {
+  const bool some = prefix->rows != 0;            // none: the arrays may be NULL
+  if (!prefix->start || !prefix->count || (some && (!prefix->K || !prefix->V || !prefix->logm)) || !aligned16(prefix->K) ||
+      !aligned16(prefix->V) || prefix->rows < 0 || prefix->rows > INT64_MAX / 1024)
+    return false;
+  *px = PrefixView{nullptr, nullptr, nullptr, nullptr, nullptr, 0};
+  if (some) *px = PrefixView{prefix->start, prefix->count, prefix->K, prefix->V, prefix->logm, prefix->rows};
+  return true;
+}
+
 gracekv_status gracekv_paged_attention(const gracekv_page_config* c, const void* q, int64_t q_tok, const void* K_pages,
                                        const void* V_pages, const int32_t* block_table, const int32_t* seq_len,
                                        const gracekv_prefix* prefix, void* out, float* lse, void* ws, size_t ws_bytes,
                                        void* stream) {
+  return gracekv_paged_attention_part(c, q, q_tok, K_pages, V_pages, block_table, seq_len, prefix, nullptr, out, lse, ws, ws_bytes,
+                                      stream);
+}
+
+gracekv_status gracekv_paged_attention_part(const gracekv_page_config* c, const void* q, int64_t q_tok, const void* K_pages,
+                                            const void* V_pages, const int32_t* block_table, const int32_t* seq_len,
+                                            const gracekv_prefix* prefix, const gracekv_part* part, void* out, float* lse,
+                                            void* ws, size_t ws_bytes, void* stream) {
   PageDims pg;
   const gracekv_status s = page_dims(c, &pg);
   if (s != GRACEKV_OK) return s;
@@ -683,15 +720,113 @@ gracekv_status gracekv_paged_attention(const gracekv_page_config* c, const void*
     return GRACEKV_ERR_INVALID_ARG;
   if (!stride_ok(c->dtype, q_tok)) return GRACEKV_ERR_INVALID_ARG;
   PrefixView px{nullptr, nullptr, nullptr, nullptr, nullptr, 0};
-  if (prefix) {
-    const bool some = prefix->rows != 0;          // none: the arrays may be NULL
-    if (!prefix->start || !prefix->count || (some && (!prefix->K || !prefix->V || !prefix->logm)) || !aligned16(prefix->K) ||
-        !aligned16(prefix->V) || prefix->rows < 0 || prefix->rows > INT64_MAX / 1024)
-      return GRACEKV_ERR_INVALID_ARG;
-    if (some) px = PrefixView{prefix->start, prefix->count, prefix->K, prefix->V, prefix->logm, prefix->rows};
-  }
+  if (prefix && !prefix_view(prefix, &px)) return GRACEKV_ERR_INVALID_ARG;
+  PartView pv;
+  if (!part_view(part, &pv)) return GRACEKV_ERR_INVALID_ARG;
   if (ws_bytes < paged_ws_bytes(pg)) return GRACEKV_ERR_WORKSPACE;
-  return hip_status(launch_paged(pg, q_tok, q, K_pages, V_pages, block_table, seq_len, px, out, lse, ws, (hipStream_t)stream));
+  return hip_status(launch_paged(pg, q_tok, q, K_pages, V_pages, block_table, seq_len, px, pv, out, lse, ws, (hipStream_t)stream));
+}
+
+// ---- quantised pages ----
+static gracekv_status quant_dims(const gracekv_page_config* c, const gracekv_quant_pages* p, PageDims* pg, QuantDims* qd) {
+  const gracekv_status s = page_dims(c, pg);
+  if (s != GRACEKV_OK) return s;
+  if (!p || (p->format != GRACEKV_E4M3 && p->format != GRACEKV_E2M1) || p->reserved != 0) return GRACEKV_ERR_INVALID_ARG;
+  if (!p->K || !p->V || !p->K_scale || !p->V_scale || !aligned16(p->K) || !aligned16(p->V) || !aligned16(p->K_scale) ||
+      !aligned16(p->V_scale))
+    return GRACEKV_ERR_INVALID_ARG;
+  const int bits = p->format == GRACEKV_E4M3 ? 8 : 4;
+  const int64_t scales = (int64_t)c->G * c->page_size * (c->d / 32);
+  if (c->page_stride % (128 / bits) != 0 || p->scale_stride < scales || p->scale_stride % 16 != 0 ||
+      c->n_pages > INT64_MAX / 4 / p->scale_stride)
+    return GRACEKV_ERR_INVALID_ARG;
+  *qd = QuantDims{c->page_stride * bits / 8, p->scale_stride, (uint8_t*)p->K, (uint8_t*)p->V, p->K_scale, p->V_scale};
+  return GRACEKV_OK;
+}
+
+gracekv_status gracekv_quant_append(const gracekv_page_config* c, const gracekv_append_config* r, const gracekv_quant_pages* pages,
+                                    const void* k, const void* v, const void* q, const int32_t* block_table, const int32_t* start,
+                                    const int32_t* cu_new, const int32_t* pos, const float* rope_cos, const float* rope_sin,
+                                    void* q_out, void* stream) {
+  PageDims pg;
+  QuantDims qd;
+  gracekv_status s = quant_dims(c, pages, &pg, &qd);
+  if (s != GRACEKV_OK) return s;
+  AppendDims ap;
+  s = append_dims(c, r, k, v, q, block_table, start, cu_new, pos, rope_cos, rope_sin, q_out, &ap);
+  if (s != GRACEKV_OK) return s;
+  return hip_status(launch_quant_append(pg, pages->format, qd, ap, k, v, q, block_table, start, cu_new, pos, rope_cos, rope_sin, q_out,
+                                        (hipStream_t)stream));
+}
+
+gracekv_status gracekv_quant_read(const gracekv_page_config* c, const gracekv_read_config* r, const gracekv_quant_pages* pages,
+                                  const int32_t* block_table, const int32_t* start, const int32_t* cu_rows, void* k, void* v,
+                                  void* stream) {
+  PageDims pg;
+  QuantDims qd;
+  const gracekv_status s = quant_dims(c, pages, &pg, &qd);
+  if (s != GRACEKV_OK) return s;
+  if (!r || !block_table || !start || !cu_rows || !aligned16(k) || !aligned16(v) || r->n_rows < 0) return GRACEKV_ERR_INVALID_ARG;
+  for (int64_t x : {r->k_tok, r->k_head, r->v_tok, r->v_head})
+    if (!stride_ok(c->dtype, x)) return GRACEKV_ERR_INVALID_ARG;
+  if ((k && ((r->k_tok == 0 && r->n_rows > 1) || (r->k_head == 0 && c->G > 1))) ||
+      (v && ((r->v_tok == 0 && r->n_rows > 1) || (r->v_head == 0 && c->G > 1))))
+    return GRACEKV_ERR_INVALID_ARG;                        // rows on rows
+  if (r->n_rows > MOST_GROUPS) return GRACEKV_ERR_UNSUPPORTED;
+  if (!k && !v) return GRACEKV_OK;
+  const ReadDims rd{r->n_rows, r->k_tok, r->k_head, r->v_tok, r->v_head};
+  return hip_status(launch_quant_read(pg, pages->format, qd, rd, block_table, start, cu_rows, k, v, (hipStream_t)stream));
+}
+
+gracekv_status gracekv_quant_attention(const gracekv_page_config* c, const gracekv_quant_pages* pages, const void* q, int64_t q_tok,
+                                       const int32_t* block_table, const int32_t* seq_len, const gracekv_part* part, void* out,
+                                       float* lse, void* ws, size_t ws_bytes, void* stream) {
+  PageDims pg;
+  QuantDims qd;
+  const gracekv_status s = quant_dims(c, pages, &pg, &qd);
+  if (s != GRACEKV_OK) return s;
+  if (!q || !block_table || !seq_len || !out || !ws) return GRACEKV_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(out) || !aligned16(ws) || !stride_ok(c->dtype, q_tok)) return GRACEKV_ERR_INVALID_ARG;
+  PartView pv;
+  if (!part_view(part, &pv)) return GRACEKV_ERR_INVALID_ARG;
+  if (ws_bytes < paged_ws_bytes(pg)) return GRACEKV_ERR_WORKSPACE;
+  return hip_status(launch_quant_paged(pg, pages->format, qd, q_tok, q, block_table, seq_len, pv, out, lse, ws, (hipStream_t)stream));
+}
+
+// ---- shared entries ----
+static gracekv_status shared_dims(const gracekv_shared_config* c, SharedDims* sd) {
+  if (!c) return GRACEKV_ERR_INVALID_ARG;
+  if (!heads_ok(c->dtype, c->G, c->H, c->n_seq) || c->n_group < 1 || !stride_ok(c->dtype, c->q_tok)) return GRACEKV_ERR_INVALID_ARG;
+  if (c->d != 64 && c->d != 128) return GRACEKV_ERR_UNSUPPORTED;
+  *sd = SharedDims{c->dtype, c->G, c->H, c->d, c->H / c->G, c->n_seq, c->n_group, c->q_tok};
+  // units (group, KV head) that every workgroup looks through, and rows of one launch
+  if ((int64_t)c->n_group * c->G > 65536 || c->H > 65536 || (int64_t)c->n_seq * c->H > 1 << 26 || shared_items(*sd) > MOST_GROUPS)
+    return GRACEKV_ERR_UNSUPPORTED;
+  return GRACEKV_OK;
+}
+
+gracekv_status gracekv_shared_ws_bytes(const gracekv_shared_config* c, size_t* ws_bytes) {
+  SharedDims sd;
+  const gracekv_status s = shared_dims(c, &sd);
+  if (s != GRACEKV_OK) return s;
+  if (!ws_bytes) return GRACEKV_ERR_INVALID_ARG;
+  *ws_bytes = shared_ws_bytes(sd);
+  return GRACEKV_OK;
+}
+
+gracekv_status gracekv_shared_attention(const gracekv_shared_config* c, const void* q, const int32_t* cu_group,
+                                        const gracekv_prefix* prefix, const gracekv_part* part, void* ws, size_t ws_bytes,
+                                        void* stream) {
+  SharedDims sd;
+  const gracekv_status s = shared_dims(c, &sd);
+  if (s != GRACEKV_OK) return s;
+  if (!q || !cu_group || !prefix || !part || !ws || !aligned16(q) || !aligned16(ws)) return GRACEKV_ERR_INVALID_ARG;
+  PrefixView px;
+  PartView pv;
+  if (!prefix_view(prefix, &px) || !part_view(part, &pv)) return GRACEKV_ERR_INVALID_ARG;
+  if (prefix->rows == 0) px = PrefixView{prefix->start, prefix->count, nullptr, nullptr, nullptr, 0};       // every count is held to 0
+  if (ws_bytes < shared_ws_bytes(sd)) return GRACEKV_ERR_WORKSPACE;
+  return hip_status(launch_shared(sd, q, cu_group, px, part->o, part->lse, ws, (hipStream_t)stream));
 }
 
 gracekv_status gracekv_selftest_mfma(int32_t which, float* out, void* stream) {

@@ -1,0 +1,57 @@
+// How the rows of groups of sequences that share entries are tiled, and how their entries are
+// cut into chunks: index arithmetic of shared.hip, plain C++ so that the host can run it as
+// well.  Nothing here reads memory except through `cu`.
+//
+// A group's rows (sequence, query head of a KV head), row = sequence * hpg + head, fill row
+// tiles of R rows; the group's entries of that KV head, n key tiles of them, are cut into
+// chunks, and a workgroup takes one chunk for one row tile.
+#pragma once
+
+#include "pages.h"
+
+namespace gkv {
+
+struct SharedDims {
+  int dtype, G, H, d, hpg, n_seq, n_group;
+  int64_t q_tok;
+};
+
+// Row tiles of every KV head: group b's begin at cu[b] * hpg / R + b, which leaves each
+// at least as many as it needs whatever the groups are.
+GKV_HD int first_tile(const SharedDims& sd, const int32_t* cu, int b, int R) {
+  return (int)((uint32_t)(held(cu[b], sd.n_seq) * sd.hpg) / (uint32_t)R) + b;
+}
+GKV_HD int64_t most_tiles(const SharedDims& sd, int R) { return (int64_t)sd.n_seq * sd.hpg / R + sd.n_group; }
+GKV_HD int tiles_of_group(const SharedDims& sd, int64_t n, int R) { return (int)((n * sd.hpg + R - 1) / R); }
+
+// Key tiles of a chunk: all row tiles' key tiles over the places that the grid has beside
+// one a row tile (each may leave a chunk unfilled), and no fewer than `least`.
+GKV_HD int shared_chunk(uint64_t total, int room, int least) {
+  const uint64_t size = (total + (uint64_t)room - 1) / (uint64_t)room;
+  return size < (uint64_t)least ? least : (size > 0x7fffffff ? 0x7fffffff : (int)size);
+}
+
+// Rows and keys of a workgroup's tile: SPLIT of its waves have the same rows, and parts of a key tile
+constexpr int SH_T = 256;
+constexpr int SH_W = SH_T / 64;
+template <bool BF, int SPLIT> constexpr int shared_rows() { return (BF ? 32 : 16) * SH_W / SPLIT; }
+template <bool BF, int SPLIT> constexpr int shared_keys() { return BF ? 32 * SPLIT : (SPLIT == 4 ? 64 : 32); }
+
+struct SharedPlan {
+  int split, rows, places;     // waves to the same rows; rows of a tile; workgroups, a multiple of 8
+  int64_t tiles;               // row tiles of all KV heads, at most
+};
+inline SharedPlan shared_plan(const SharedDims& sd) {
+  const bool bf = sd.dtype == 1;               // GRACEKV_BF16
+  const int64_t mean = ((int64_t)sd.n_seq * sd.hpg + sd.n_group - 1) / sd.n_group;
+  SharedPlan p;
+  p.split = bf ? (mean > 64 ? 1 : mean > 32 ? 2 : 4) : (mean > 16 ? 1 : 4);
+  p.rows = (bf ? 32 : 16) * SH_W / p.split;
+  p.tiles = most_tiles(sd, p.rows) * sd.G;
+  const int64_t target = 512;
+  const int64_t room = target - p.tiles / 2 > target / 4 ? target - p.tiles / 2 : target / 4;
+  p.places = (int)((p.tiles + room + 7) & ~(int64_t)7);
+  return p;
+}
+
+}  // namespace gkv

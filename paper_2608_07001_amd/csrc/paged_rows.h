@@ -1,0 +1,283 @@
+// How the rows (sequence, KV head) of attention over pages are cut into chunks on the device,
+// and how the states of a chunk's waves, of a row's chunks and of another attention over
+// further entries become one result: what the kernels over plain (paged.hip) and quantised
+// pages (quant_paged.hip) have in common.
+#pragma once
+
+#include "serve.h"
+
+namespace gkv {
+
+// The last chunk of a row joins PA_JOIN states at a time (32 are up to a fifth slower, 16 the
+// same; four dims a lane instead of two joins 16 heads faster, 128K tokens of one KV head 48 us
+// instead of 55, and the others slower).
+constexpr int PA_JOIN = 8;
+
+static inline size_t al256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// Workspace: a ticket word for every row and group of heads, then per chunk and head
+// (max, sum), then the partial sums [chunk][hpg][d].
+struct PagedWs {
+  unsigned long long* ticket;
+  unsigned long long* ml;
+  float* o;
+  size_t bytes;
+};
+static inline PagedWs paged_view(void* base, const PageDims& pg) {
+  const size_t R = (size_t)pg.n_seq * pg.G, chunks = R + PA_TARGET;
+  char* p = (char*)base;
+  PagedWs w;
+  size_t o = 0;
+  w.ticket = (unsigned long long*)(p + o);
+  o += al256(R * ((pg.hpg + PA_HEADS - 1) / PA_HEADS) * 8);
+  w.ml = (unsigned long long*)(p + o);
+  o += al256(chunks * pg.hpg * 8);
+  w.o = (float*)(p + o);
+  o += chunks * pg.hpg * pg.d * 4;
+  w.bytes = o;
+  return w;
+}
+
+// Tickets.  The chunks of a row count themselves in its word, PA_BASE, PA_BASE + 1, ...;
+// the one that makes the count whole finds PA_BASE + parts - 1, and its counting sets the
+// word to 0.  What a word holds before is no count: anything below PA_BASE is raised to it
+// first, and counting on anything past the end gives 0, whoever did it counting again.
+// So the workspace needs no clearing, and every call leaves the words it used at 0.  (The
+// numbers from PA_BASE + 1 to PA_BASE + parts - 1, at most PA_BASE + PA_TARGET, would be taken
+// for a count, and nothing here can tell them from one: the header excludes them.  Calls that
+// overlap leave them, and nothing else does.)
+// States are written and read with device-coherent operations, and a wait for the writes
+// stands between them and the ticket, so no fence is needed, which on this chip would
+// write back and invalidate the L2 of the XCD.  (Counting by compare-and-swap took the 40
+// chunks of a row 20 us, one after the other.)
+constexpr unsigned long long PA_BASE = 0x7fffffffffff0000ull;
+static_assert(PA_TARGET <= 0xfff, "the words that the header excludes");
+__device__ __forceinline__ bool last_of(unsigned long long* word, int parts) {
+  const unsigned long long end = PA_BASE + parts - 1;
+  unsigned long long was;
+  do {
+    __hip_atomic_fetch_max(word, PA_BASE, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    was = __builtin_amdgcn_atomic_inc64((unsigned long*)word, end, __ATOMIC_RELAXED, "agent");
+  } while (was > end || was < PA_BASE);       // below: put to 0 by another between the two steps
+  return was == end;
+}
+// the thread's stores are where every other workgroup sees them
+__device__ __forceinline__ void stores_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ unsigned long long pair_bits(float a, float b) {
+  return (unsigned long long)__float_as_uint(a) | (unsigned long long)__float_as_uint(b) << 32;
+}
+__device__ __forceinline__ float2 pair_of(unsigned long long x) {
+  return make_float2(__uint_as_float((uint32_t)x), __uint_as_float((uint32_t)(x >> 32)));
+}
+__device__ __forceinline__ void put_agent(unsigned long long* p, unsigned long long x) {
+  __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+__device__ __forceinline__ int64_t held_count(const PrefixView& px, int64_t row, int64_t& start) {
+  int64_t s = px.start[row], c = px.count[row];
+  s = s < 0 ? 0 : (s > px.rows ? px.rows : s);
+  c = c < 0 ? 0 : (c > px.rows - s ? px.rows - s : c);
+  start = s;
+  return c > PAGED_ROWS ? PAGED_ROWS : c;
+}
+
+// inclusive sum over the lanes of the wave
+__device__ __forceinline__ int scan_wave(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);     // row_shr 1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+  const int r = (threadIdx.x & 63) >> 4;
+  const int a = __builtin_amdgcn_readlane(v, 15), b = __builtin_amdgcn_readlane(v, 31), c = __builtin_amdgcn_readlane(v, 47);
+  return v + (r > 0 ? a : 0) + (r > 1 ? b : 0) + (r > 2 ? c : 0);
+}
+
+// What a workgroup works on: tiles [t0, t1) of row (b, g); chunk `c` of `chunks`.
+struct Chunk {
+  int b, g, c, chunks, t0, t1;
+};
+
+// The chunk of place `bid` of `places`; false past the last.  Rows are looked at as units:
+// (b, g) where a prefix makes their lengths differ, b (G equal rows) otherwise.  Every
+// wave finds it by itself, 64 units at a time; over that few it takes one round of loads
+// and scans without a barrier.  With more units the waves share a first look at them all,
+// which is enough where no row needs a second chunk (4096 sequences of 64 tokens: 860 us
+// with the search, 403 without).
+template <int TILE, bool PREFIX>
+__device__ __forceinline__ bool find_chunk(const PageDims& pg, const PrefixView& px, const int32_t* len, int bid, int places, float join,
+                                           Chunk& out) {
+  const int lane = threadIdx.x & 63;
+  const int units = PREFIX ? pg.n_seq * pg.G : pg.n_seq, mult = PREFIX ? 1 : pg.G;
+  auto tiles = [&](int u) -> int {
+    if (u >= units) return 0;
+    int64_t s = 0;
+    return tiles_of<TILE>(held_len(pg, len[PREFIX ? u / pg.G : u]), PREFIX ? held_count(px, u, s) : 0);
+  };
+  const int room = places - pg.n_seq * pg.G;
+  int first = 0, size;
+  if (units <= 64) {
+    first = tiles(lane);
+    size = chunk_tiles((uint64_t)(uint32_t)__builtin_amdgcn_readlane(scan_wave(first), 63) * mult, room);
+  } else {
+    __shared__ uint64_t part[PA_W];
+    __shared__ int most[PA_W];
+    uint64_t sum = 0;
+    int mx = 0;
+    for (int u = threadIdx.x; u < units; u += PA_T) {
+      const int n = tiles(u);
+      sum += n;
+      mx = max(mx, n);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      sum += __shfl_xor(sum, o, 64);
+      mx = max(mx, __shfl_xor(mx, o, 64));
+    }
+    if (lane == 0) { part[threadIdx.x >> 6] = sum; most[threadIdx.x >> 6] = mx; }
+    sync_after_lds_stores();
+    sum = 0;
+#pragma unroll
+    for (int i = 0; i < PA_W; ++i) { sum += part[i]; mx = max(mx, most[i]); }
+    size = __builtin_amdgcn_readfirstlane(chunk_tiles(sum * mult, room));
+    if (__builtin_amdgcn_readfirstlane(mx) <= size) {
+      if (bid >= units * mult) return false;
+      const int u = bid / mult;
+      out.b = PREFIX ? u / pg.G : u;
+      out.g = PREFIX ? u % pg.G : bid % mult;
+      out.c = 0;
+      out.chunks = 1;
+      out.t0 = 0;
+      out.t1 = __builtin_amdgcn_readfirstlane(tiles(u));
+      return true;
+    }
+    first = tiles(lane);
+  }
+  // the rows of several chunks first, then the others, which even out the end (where there
+  // are more units than a wave looks at in one round, rows as they come: their end is short)
+  const bool ordered = units <= 64;
+  int base = 0;
+#pragma unroll 1
+  for (int many = 1; many >= (ordered ? 0 : 1); --many)
+#pragma unroll 1
+    for (int u0 = 0; u0 < units; u0 += 64) {
+      const int n = u0 ? tiles(u0 + lane) : first, x = n ? chunks_of(n, size, join) : 0;
+      const int c = !ordered || (x > 1) == many ? x * mult : 0;
+      const int to = scan_wave(c);     // at most the places: no overflow
+      const int all = base + __builtin_amdgcn_readlane(to, 63);
+      if (bid < all) {
+        const int at = __popcll(__ballot(base + to <= bid));       // the unit's lane
+        const int u = u0 + at;
+        const int tn = __builtin_amdgcn_readlane(n, at), chunks = __builtin_amdgcn_readlane(x, at);
+        const int local = bid - base - (__builtin_amdgcn_readlane(to, at) - chunks * mult);
+        out.b = PREFIX ? u / pg.G : u;
+        out.g = PREFIX ? u % pg.G : local / chunks;
+        out.c = PREFIX ? local : local % chunks;
+        out.chunks = chunks;
+        const int each = tn / chunks, more = tn % chunks;            // the first `more` take one more
+        out.t0 = out.c * each + min(out.c, more);
+        out.t1 = out.t0 + each + (out.c < more);
+        return true;
+      }
+      base = all;
+    }
+  return false;
+}
+
+// What the waves of a workgroup have of chunk `ck` (sM, sL, sO: maximum, sum and weighted
+// values of every wave and head; written, with a barrier behind): merged, written as the row's
+// result where the chunk is all of it, else left in the workspace, for the last of the row's
+// chunks to join.  `part` (o not null): an attention of the same queries over other entries,
+// joined to the row's as a state of its own, maximum lse, sum 1 and its mean.
+template <typename T, int D>
+__device__ __forceinline__ void finish_row(const PageDims& pg, const Chunk& ck, const PagedWs& ws, const PartView& part, int bid,
+                                           int group, int groups, const float (*sM)[PA_HEADS], const float (*sL)[PA_HEADS],
+                                           const float (*sO)[PA_HEADS][D + 4], T* __restrict__ out, float* __restrict__ lse) {
+  __shared__ int joins;
+  constexpr float LOG2E = 1.44269504088896341f;
+  const int tid = threadIdx.x;
+  const int h0 = group * PA_HEADS, heads = min(PA_HEADS, pg.hpg - h0);
+  const int64_t row = (int64_t)ck.b * pg.G + ck.g;
+  // state (m, s, o) onto (M, S, O): one of no entry has the maximum -inf and adds nothing,
+  // unless its sum is no number
+  auto add = [&](float& M, float& S, float& O0, float& O1, float m2, float s2, float a0, float a1) {
+    const float mn = fmaxf(M, m2);
+    const float f = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((M - mn) * LOG2E);
+    const float c = m2 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m2 - mn) * LOG2E);
+    S = (f == 0.f && S == S ? 0.f : S * f) + (c == 0.f && s2 == s2 ? 0.f : s2 * c);
+    O0 = (f == 0.f ? 0.f : O0 * f) + (c == 0.f ? 0.f : a0 * c);
+    O1 = (f == 0.f ? 0.f : O1 * f) + (c == 0.f ? 0.f : a1 * c);
+    M = mn;
+  };
+  auto finish = [&](int h, int dd, float M, float S, float O0, float O1) {
+    const int64_t hd = (int64_t)ck.b * pg.H + (int64_t)ck.g * pg.hpg + h0 + h;
+    if (part.o) {
+      const float2 x = *(const float2*)(part.o + hd * D + dd);
+      add(M, S, O0, O1, part.lse[hd], 1.f, x.x, x.y);
+    }
+    stf(out, hd * D + dd, S > 0.f ? O0 / S : S);                  // nothing: 0; NaN stays
+    stf(out, hd * D + dd + 1, S > 0.f ? O1 / S : S);
+    if (lse && dd == 0) lse[hd] = M + logf(S);
+  };
+  const int64_t place = (int64_t)bid * pg.hpg + h0;
+  for (int i = tid; i < heads * (D / 2); i += PA_T) {
+    const int h = i / (D / 2), dd = 2 * (i % (D / 2));
+    float M = -INFINITY, S = 0.f, O0 = 0.f, O1 = 0.f;
+#pragma unroll
+    for (int x = 0; x < PA_W; ++x) add(M, S, O0, O1, sM[x][h], sL[x][h], sO[x][h][dd], sO[x][h][dd + 1]);
+    if (ck.chunks == 1) {
+      finish(h, dd, M, S, O0, O1);
+    } else {
+      put_agent((unsigned long long*)(ws.o + (place + h) * D + dd), pair_bits(O0, O1));
+      if (dd == 0) put_agent(ws.ml + place + h, pair_bits(M, S));
+    }
+  }
+  if (ck.chunks == 1) return;
+  stores_done();
+  __syncthreads();
+  if (tid == 0) joins = last_of(ws.ticket + row * groups + group, ck.chunks);
+  sync_after_lds_stores();
+  if (!joins) return;
+  // A head's pairs of dims lie on LH neighbouring lanes, which hold the (max, sum) of LH
+  // chunks at a time, one each, and pass the weights round.
+  constexpr int LH = D / 2;
+  const int64_t base = (int64_t)(bid - ck.c) * pg.hpg + h0;              // the row's first chunk
+  for (int i = tid; i < (heads * LH + 63) / 64 * 64; i += PA_T) {               // whole waves
+    const int h = min(i / LH, heads - 1), sub = i % LH, dd = 2 * sub;
+    float M = -INFINITY, S = 0.f, O0 = 0.f, O1 = 0.f;
+    for (int b0 = 0; b0 < ck.chunks; b0 += LH) {
+      const int nb = min(ck.chunks - b0, LH);
+      const unsigned long long* src = (const unsigned long long*)(ws.o + (base + (int64_t)b0 * pg.hpg + h) * D + dd);
+      const int64_t step = (int64_t)pg.hpg * LH;
+      unsigned long long ov[PA_JOIN];
+      auto load = [&](int c0) {                 // past the last: that one again
+#pragma unroll
+        for (int c = 0; c < PA_JOIN; ++c) ov[c] = ld_agent(src + min(c0 + c, nb - 1) * step);
+      };
+      float2 ml = make_float2(-INFINITY, 0.f);
+      if (sub < nb) ml = pair_of(ld_agent(ws.ml + base + (int64_t)(b0 + sub) * pg.hpg + h));
+      load(0);
+      float mb = ml.x;
+#pragma unroll
+      for (int o = LH / 2; o > 0; o >>= 1) mb = fmaxf(mb, __shfl_xor(mb, o, 64));
+      const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ml.x - mb) * LOG2E);
+      float sb = f == 0.f && ml.y == ml.y ? 0.f : ml.y * f;                     // NaN stays
+#pragma unroll
+      for (int o = LH / 2; o > 0; o >>= 1) sb += __shfl_xor(sb, o, 64);
+      float a0 = 0.f, a1 = 0.f;
+      for (int c0 = 0; c0 < nb; c0 += PA_JOIN) {
+        if (c0) load(c0);
+#pragma unroll
+        for (int c = 0; c < PA_JOIN; ++c) {
+          const float g = c0 + c < nb ? __shfl(f, (tid & 63 & ~(LH - 1)) + c0 + c, 64) : 0.f;
+          const float2 v = pair_of(ov[c]);
+          a0 += g == 0.f ? 0.f : v.x * g;
+          a1 += g == 0.f ? 0.f : v.y * g;
+        }
+      }
+      add(M, S, O0, O1, mb, sb, a0, a1);
+    }
+    if (i < heads * LH) finish(h, dd, M, S, O0, O1);
+  }
+}
+
+}  // namespace gkv

@@ -39,7 +39,7 @@
 // bound by the way along the keys, about 0.9 us a tile for a workgroup with few beside it
 // (Plan), and by the parts' states, 33 MB of them for 64 queries over 32K keys: 50 us of
 // products, 10 of joining.  fp32: 2048 tokens of the 8B heads 325 us, 106 TFLOP/s of 153.
-#include "serve.h"
+#include "tiles.h"
 
 namespace gkv {
 
@@ -50,14 +50,6 @@ constexpr int CUS = 256;
 constexpr float PR_LAG = 8.f;      // base-2 units, and as a factor
 constexpr float PR_TOP = 256.f;
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
-
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-__device__ __forceinline__ f32x16 mfma_bf16_32x32x16(uint4 a, uint4 b, f32x16 c) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-
-// the stated wait for the matrix pipeline (mfma_done) for these accumulators
-__device__ __forceinline__ void mfma_done16(f32x16& x) { asm volatile("s_nop 15\n\ts_nop 4" : "+v"(x)); }
 
 static size_t al256(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -186,27 +178,6 @@ __device__ __forceinline__ bool find_item(const PromptDims& pd, const int32_t* c
   return true;
 }
 
-// Orders a block's N products and their LDS reads (R a product): the reads AHEAD products early.
-template <int N, int R, int AHEAD> __device__ __forceinline__ void reads_ahead() {
-  constexpr int A = AHEAD < N ? AHEAD : N;
-  __builtin_amdgcn_sched_group_barrier(0x100, R * A, 0);        // LDS reads
-#pragma unroll
-  for (int i = 0; i < N - A; ++i) {
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);          // products
-    __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
-  }
-  __builtin_amdgcn_sched_group_barrier(0x008, A, 0);
-}
-
-// 16 bytes of a tile
-__device__ __forceinline__ uint4 lds_at(const uint4* tile, int byte) { return *(const uint4*)((const char*)tile + byte); }
-// the four 16-bit values of a lane after the transposing read: `byte` is where the lane's 8
-// bytes of its group's 4 x 16 block lie (lanes 4 r .. 4 r + 3: row r), returned is column lane % 16
-__device__ __forceinline__ uint2 lds_read_tr(const uint4* tile, int byte) {
-  auto q = (__attribute__((address_space(3))) s16x4*)((const char*)tile + byte);
-  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(q));
-}
-
 // bf16 pairs / floats with what is not finite replaced by 0; `any` says whether there was
 __device__ __forceinline__ uint32_t finite_bf(uint32_t x, bool& any) {
   const bool h = (x & 0x7f800000u) == 0x7f800000u, l = (x & 0x7f80u) == 0x7f80u;
@@ -221,29 +192,6 @@ __device__ __forceinline__ uint32_t finite_f(uint32_t x, bool& any) {
 template <bool BF> __device__ __forceinline__ uint4 finite(uint4 x, bool& any) {
   if constexpr (BF) return make_uint4(finite_bf(x.x, any), finite_bf(x.y, any), finite_bf(x.z, any), finite_bf(x.w, any));
   else return make_uint4(finite_f(x.x, any), finite_f(x.y, any), finite_f(x.z, any), finite_f(x.w, any));
-}
-
-// The rows of one key tile as a bounded buffer: `rows` rows of D elements, `tok` elements
-// apart; a load past the last row gives 0.  (tok is at most PR_STRIDE, so the bytes of a
-// tile fit 31 bits.)
-typedef __amdgpu_buffer_rsrc_t Buffer;
-template <typename T, int D>
-__device__ __forceinline__ Buffer tile_buffer(const T* base, int64_t tok, int rows) {
-  const int bytes = (int)(((int64_t)(rows - 1) * tok + D) * (int64_t)sizeof(T));
-  return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x00020000);
-}
-// 16 bytes a lane straight into LDS, lane l to dst + l (dst: the same for the wave); the
-// wave's vector memory counter says when they are there
-__device__ __forceinline__ void buffer_load_lds(Buffer b, uint4* dst, int off) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (__attribute__((address_space(3))) void*)dst, 16, off, 0, 0, 0);
-}
-
-// place of 16-byte piece c of key row t in a staged tile: neighbouring rows start in
-// other banks, for the reads along a row (16 rows, one piece) and the transposing ones
-// (8 rows, four pieces)
-template <int D> __device__ __forceinline__ int swz(int t, int c) {
-  if constexpr (D == 128) return t * 16 + (c ^ (((t & 3) << 2) | ((t >> 2) & 3)));
-  else return t * 8 + (c ^ ((((t >> 1) & 1) << 2) | ((t >> 2) & 3)));
 }
 
 template <int D, int SPLIT>

@@ -6,6 +6,7 @@
 #include <type_traits>
 
 #include "common.h"
+#include "groups.h"
 #include "pages.h"
 
 namespace gkv {
@@ -14,6 +15,9 @@ namespace gkv {
 struct AppendDims {
   int64_t n_new, rope_rows;
   int64_t k_tok, k_head, v_tok, v_head, q_tok, q_head, o_tok, o_head;
+};
+struct ReadDims {
+  int64_t n_rows, k_tok, k_head, v_tok, v_head;
 };
 struct PromptDims {
   int dtype, G, H, d, hpg, n_seq;
@@ -31,6 +35,20 @@ struct PrefixView {
   int64_t rows;
 };
 
+// the pages of a quantised cache: bytes from page to page, of the codes and of their scales
+struct QuantDims {
+  int64_t code_stride, scale_stride;
+  uint8_t* K;
+  uint8_t* V;
+  uint8_t* Ks;
+  uint8_t* Vs;
+};
+// an attention of the same queries over other entries (o null: none): its mean and log sum exp, fp32
+struct PartView {
+  const float* o;
+  const float* lse;
+};
+
 hipError_t launch_append(const PageDims& pg, const AppendDims& ap, const void* k, const void* v, const void* q,
                          const int32_t* table, const int32_t* start, const int32_t* cu, const int32_t* pos,
                          const float* cosT, const float* sinT, void* Kp, void* Vp, void* q_out, hipStream_t st);
@@ -41,8 +59,19 @@ hipError_t launch_prompt(const PromptDims& pd, const void* q, const void* k, con
 size_t paged_ws_bytes(const PageDims& pg);
 int64_t paged_items(const PageDims& pg);         // at most so many workgroups
 hipError_t launch_paged(const PageDims& pg, int64_t q_tok, const void* q, const void* Kp, const void* Vp,
-                        const int32_t* table, const int32_t* len, const PrefixView& px, void* out, float* lse, void* ws,
-                        hipStream_t st);
+                        const int32_t* table, const int32_t* len, const PrefixView& px, const PartView& part, void* out, float* lse,
+                        void* ws, hipStream_t st);
+hipError_t launch_quant_append(const PageDims& pg, int format, const QuantDims& qd, const AppendDims& ap, const void* k, const void* v,
+                               const void* q, const int32_t* table, const int32_t* start, const int32_t* cu, const int32_t* pos,
+                               const float* cosT, const float* sinT, void* q_out, hipStream_t st);
+hipError_t launch_quant_read(const PageDims& pg, int format, const QuantDims& qd, const ReadDims& rd, const int32_t* table,
+                             const int32_t* start, const int32_t* cu, void* k, void* v, hipStream_t st);
+hipError_t launch_quant_paged(const PageDims& pg, int format, const QuantDims& qd, int64_t q_tok, const void* q, const int32_t* table,
+                              const int32_t* len, const PartView& part, void* out, float* lse, void* ws, hipStream_t st);
+size_t shared_ws_bytes(const SharedDims& sd);
+int64_t shared_items(const SharedDims& sd);      // at most so many workgroups
+hipError_t launch_shared(const SharedDims& sd, const void* q, const int32_t* cu, const PrefixView& px, float* out, float* lse, void* ws,
+                         hipStream_t st);
 
 // two floats to bf16, nearest even, low half first
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));

@@ -1,0 +1,679 @@
+// Attention of one token of every sequence over packed entries that groups of sequences share.
+//
+// Group s has the sequences [cu[s], cu[s+1]) and, of KV head g, the entries [start, start + count) of
+// (s, g): every query head of g of every sequence of the group attends to all of them,
+//   o = sum_j softmax_j(q.k_j / sqrt(d) + log m_j) v_j,  lse = log sum_j exp(...)
+// (no entry: 0 and -inf).  Both are fp32: a state that another attention joins to its own.
+//
+// The rows that share keys, hpg of every sequence of the group, fill the tiles of a matrix product, so
+// the entries are gone through once a row tile instead of once a sequence.  One pass with a running maximum and
+// sum, products transposed and tiles in LDS as in prompt.hip; there is no diagonal here, but
+// every entry has a log m, and one of -inf has no weight: its value is replaced by 0 in
+// LDS, since 0 times an infinity is not 0.
+//
+// Few sequences leave few row tiles, so a tile's entries are cut into chunks, as many as fill
+// the chip, found on the device by a scan over the groups' lengths; each leaves a state, and a second
+// kernel joins them, in their order.  Row tiles of one chunk are neighbours on one XCD, whose L2 then holds the chunk.
+//
+// bf16 weights are rounded to bf16 (nearest even) for the second product, their sum takes them
+// unrounded, as in prompts: each is off by at most 2^-8 of itself, at random.  fp32 uses the
+// fp32 matrix instructions.
+#include "tiles.h"
+
+namespace gkv {
+
+constexpr float SH_LAG = 8.f, SH_TOP = 256.f;  // as in prompt.hip: base-2 units, and as a factor
+constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
+
+static inline size_t al256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+int64_t shared_items(const SharedDims& sd) { return most_tiles(sd, 16) * sd.G + 1024; }   // no plan has more workgroups
+
+// Workspace: (first chunk's place, chunks) of every row tile, then per place and row (max, sum) and
+// the weighted values.
+struct SharedWs {
+  int2* info;
+  float2* ml;
+  float* o;
+  size_t bytes;
+};
+static SharedWs shared_view(void* base, const SharedDims& sd, const SharedPlan& p) {
+  SharedWs w;
+  size_t o = 0;
+  w.info = (int2*)base;
+  o += al256((size_t)p.tiles * 8);
+  w.ml = (float2*)((char*)base + o);
+  o += al256((size_t)p.places * p.rows * 8);
+  w.o = (float*)((char*)base + o);
+  o += (size_t)p.places * p.rows * sd.d * 4;
+  w.bytes = o;
+  return w;
+}
+size_t shared_ws_bytes(const SharedDims& sd) { return shared_view(nullptr, sd, shared_plan(sd)).bytes; }
+
+__device__ __forceinline__ int64_t held_entries(const PrefixView& px, int64_t row, int64_t& start) {
+  int64_t s = px.start[row], c = px.count[row];
+  s = s < 0 ? 0 : (s > px.rows ? px.rows : s);
+  c = c < 0 ? 0 : (c > px.rows - s ? px.rows - s : c);
+  start = s;
+  return c > PAGED_ROWS ? PAGED_ROWS : c;
+}
+
+// What a workgroup works on: key tiles [t0, t1), chunk c of `chunks`, of row tile `tile` of (group b, KV head g)
+struct Item {
+  int b, g, tile, tiles, c, chunks, t0, t1, id;
+};
+
+// The item of workgroup blockIdx.x; false where there is none.  Units are (group, KV head);
+// every wave looks at 64 of them at a time.
+template <int ROWS, int KEYS, int LEAST>
+__device__ __forceinline__ bool find_item(const SharedDims& sd, const int32_t* cu, const PrefixView& px, int room, Item& it) {
+  const int lane = threadIdx.x & 63, units = sd.n_group * sd.G;
+  // row tiles of unit u, and key tiles of each
+  auto shape = [&](int u, int& mt, int& n) {
+    mt = n = 0;
+    if (u >= units) return;
+    const Span sp = span_of(cu, u / sd.G, sd.n_seq);
+    mt = tiles_of_group(sd, sp.n, ROWS);
+    int64_t s = 0;
+    n = (int)((held_entries(px, u, s) + KEYS - 1) / KEYS);
+    if (n == 0) n = 1;                 // its zeros are written too
+  };
+  auto sum64 = [&](uint64_t v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    return v;
+  };
+  int mt, n;
+  uint64_t total = 0;
+  if (units <= 64) {
+    shape(lane, mt, n);
+    total = sum64((uint64_t)mt * n);
+  } else {
+    __shared__ uint64_t part[SH_W];
+    for (int u = threadIdx.x; u < units; u += SH_T) {
+      shape(u, mt, n);
+      total += (uint64_t)mt * n;
+    }
+    total = sum64(total);
+    if (lane == 0) part[threadIdx.x >> 6] = total;
+    sync_after_lds_stores();
+    total = 0;
+#pragma unroll
+    for (int i = 0; i < SH_W; ++i) total += part[i];
+    shape(lane, mt, n);
+  }
+  const int size = __builtin_amdgcn_readfirstlane(shared_chunk(total, room, LEAST));
+  int id = blockIdx.x, base = 0;
+#pragma unroll 1
+  for (int u0 = 0; u0 < units; u0 += 64) {
+    if (u0) shape(u0 + lane, mt, n);
+    const int ch = n / size + (n % size != 0);
+    const int64_t all64 = (int64_t)mt * ch;
+    const int x = all64 > (1 << 24) ? 1 << 24 : (int)all64;
+    int to = x;                          // inclusive sum over the lanes: at most 2^30
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(to, o, 64);
+      if (lane >= o) to += y;
+    }
+    const int all = base + __builtin_amdgcn_readlane(to, 63);
+    if (units <= 64) {                   // neighbouring items to one XCD, workgroups going round the eight
+      const int per = (all + 7) / 8, at = id >> 3;
+      id = (id & 7) * per + at;
+      if (at >= per || id >= all) return false;
+    }
+    if (id < all) {
+      const int at = __popcll(__ballot(base + to <= id));       // the unit's lane
+      const int u = u0 + at;
+      it.tiles = __builtin_amdgcn_readlane(mt, at);
+      it.chunks = __builtin_amdgcn_readlane(ch, at);
+      const int tn = __builtin_amdgcn_readlane(n, at);
+      const int local = id - base - (__builtin_amdgcn_readlane(to, at) - __builtin_amdgcn_readlane(x, at));
+      it.b = u / sd.G;
+      it.g = u % sd.G;
+      it.c = local / it.tiles;
+      it.tile = local % it.tiles;
+      const int each = tn / it.chunks, more = tn % it.chunks;     // the first `more` take one more
+      it.t0 = it.c * each + min(it.c, more);
+      it.t1 = it.t0 + each + (it.c < more);
+      it.id = id;
+      return true;
+    }
+    base = all;
+  }
+  return false;
+}
+
+// the rows of an item's tile: the lane's row, and where its query and its result lie
+struct Row {
+  int row, rows;               // of the group
+  int64_t hd;                  // sequence * H + head
+};
+__device__ __forceinline__ Row row_of(const SharedDims& sd, const int32_t* cu, const Item& it, int R, int r, int64_t& seq) {
+  const Span sp = span_of(cu, it.b, sd.n_seq);
+  Row x;
+  x.rows = (int)(sp.n * sd.hpg);
+  x.row = it.tile * R + r;
+  const int c = min(x.row, x.rows - 1), tok = (int)((uint32_t)c / (uint32_t)sd.hpg);
+  seq = sp.a + tok;
+  x.hd = seq * sd.H + (int64_t)it.g * sd.hpg + (c - tok * sd.hpg);
+  return x;
+}
+
+template <int D, int SPLIT>
+__global__ __launch_bounds__(SH_T, SPLIT == 4 ? 1 : SPLIT == 2 ? 2 : 3) void k_shared_bf(SharedDims sd, int room, const uint16_t* __restrict__ q,
+                                                                           const int32_t* __restrict__ cu, PrefixView px,
+                                                                           float* __restrict__ out, float* __restrict__ lse, SharedWs ws) {
+  constexpr int ROWS = shared_rows<true, SPLIT>(), KEYS = shared_keys<true, SPLIT>();
+  constexpr int CH = D / 8;                     // 16-byte pieces of a row
+  constexpr int RI = 64 / CH;                   // rows that one load of a wave brings
+  constexpr int NI = KEYS / RI / SH_W;          // such loads of a wave and array
+  constexpr int KS = D / 16;                    // product steps over the dims
+  constexpr int DT = D / 32;                    // 32-dim tiles of the output
+  constexpr int LN = KEYS < 64 ? 64 : KEYS;
+  __shared__ __align__(16) uint4 sK0[KEYS * CH], sK1[KEYS * CH], sV0[KEYS * CH], sV1[KEYS * CH];
+  __shared__ __align__(16) float sL0[LN], sL1[LN];
+  Item it;
+  if (!find_item<ROWS, KEYS, SPLIT == 1 ? 2 : 1>(sd, cu, px, room, it)) return;
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i32 = lane & 31, half = lane >> 5;
+  const int rw = w / SPLIT, kw = w % SPLIT;     // the wave's 32 rows, its 32 keys of a tile
+  int64_t seq, p_start;
+  const Row me = row_of(sd, cu, it, ROWS, 32 * rw + i32, seq);
+  const int n_keys = (int)held_entries(px, (int64_t)it.b * sd.G + it.g, p_start);
+  if (it.c == 0 && tid == 0) ws.info[(int64_t)(first_tile(sd, cu, it.b, ROWS) + it.tile) * sd.G + it.g] = make_int2(it.id, it.chunks);
+
+  uint4 qv[KS];
+  {
+    const uint16_t* qp = q + seq * sd.q_tok + (me.hd - seq * sd.H) * D;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) qv[s] = *(const uint4*)(qp + 16 * s + 8 * half);
+  }
+  f32x16 o[DT];
+#pragma unroll
+  for (int t = 0; t < DT; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[t][r] = 0.f;
+  float m = -INFINITY, l = 0.f;                 // what is subtracted, base-2 units; l: this lane's keys only
+  const float sc2 = LOG2E / sqrtf((float)D);
+
+  const uint16_t* kp = (const uint16_t*)px.K + p_start * D;
+  const uint16_t* vp = (const uint16_t*)px.V + p_start * D;
+  const float* lp = px.logm + p_start;
+  // Load i of a wave brings rows RI (w + SH_W i) .. + RI - 1 straight into LDS (prompt.hip)
+  const int lr = RI * w + lane / CH, lc = swz<D>(lr, lane % CH) - lr * CH;
+  const int off = lr * D * 2 + lc * 16;
+  constexpr int STEP = RI * SH_W * D * 2;
+  auto load = [&](const uint16_t* rows, int t, uint4* to) {
+    const Buffer b = tile_buffer<uint16_t, D>(rows + (int64_t)t * KEYS * D, D, min(n_keys - t * KEYS, KEYS));
+#pragma unroll
+    for (int i = 0; i < NI; ++i) buffer_load_lds(b, to + 64 * (w + SH_W * i), off + i * STEP);
+  };
+  auto load_logm = [&](int t, float* to) {      // the first LN / 64 waves, 64 a wave; past the last: 0
+    if (w < LN / 64) {
+      const int n = min(n_keys - t * KEYS, KEYS);
+      const Buffer b = __builtin_amdgcn_make_buffer_rsrc((void*)(lp + (int64_t)t * KEYS), 0, n * 4, 0x00020000);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (__attribute__((address_space(3))) void*)(to + 64 * w), 4, 256 * w + 4 * lane, 0, 0, 0);
+    }
+  };
+  auto load_tile = [&](int t, uint4* K, uint4* V, float* L) {
+    load(kp, t, K);
+    load(vp, t, V);
+    load_logm(t, L);
+  };
+  constexpr int RB = 2 * D;
+  int k_at = 16 * swz<D>(i32, half);
+  const int v_at = 16 * swz<D>(4 * half + ((lane & 15) >> 2), 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + 8 * (lane & 1);
+  auto step = [&](int t, uint4* cK, uint4* cV, float* cL, uint4* nK, uint4* nV, float* nL) __attribute__((always_inline)) {
+    // the wave's own loads of tile t are there, then everyone's; and everyone is done with tile t - 1
+    wait_vm();
+    sync_after_lds_stores();
+    const int left = n_keys - t * KEYS;          // entries from this tile on
+    // entries without weight: their values have to be 0
+    bool none = false;
+#pragma unroll
+    for (int i = 0; i < KEYS; i += 64)
+      if (i + lane < KEYS && i + lane < left) none |= cL[i + lane] == -INFINITY;
+    const bool masked = __any(none);             // the same for every wave
+    if (masked) {
+      for (int i = tid; i < KEYS * CH; i += SH_T)
+        if (cL[i / CH] == -INFINITY) cV[i] = make_uint4(0, 0, 0, 0);       // a row's pieces stay in its places
+      sync_after_lds_stores();
+    }
+    if (t + 1 < it.t1) load_tile(t + 1, nK, nV, nL);
+    f32x16 s;
+    asm volatile("" : "+v"(k_at));               // eight places: formed anew, not held in registers
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = 0.f;
+#pragma unroll
+    for (int x = 0; x < KS; ++x) s = mfma_bf16_32x32x16(lds_at(cK, (k_at ^ (32 * x)) + 32 * kw * RB), qv[x], s);
+    reads_ahead<KS, 1, 4>();
+    mfma_done16(s);
+    // register r: key 8 (r / 4) + 4 half + r % 4 of the wave's
+    const float* lw = cL + 32 * kw + 4 * half;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      const float4 g = *(const float4*)(lw + 8 * b);
+      s[4 * b] = __builtin_fmaf(s[4 * b], sc2, g.x * LOG2E);
+      s[4 * b + 1] = __builtin_fmaf(s[4 * b + 1], sc2, g.y * LOG2E);
+      s[4 * b + 2] = __builtin_fmaf(s[4 * b + 2], sc2, g.z * LOG2E);
+      s[4 * b + 3] = __builtin_fmaf(s[4 * b + 3], sc2, g.w * LOG2E);
+    }
+    if (masked) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = lw[8 * (r / 4) + r % 4] == -INFINITY ? -INFINITY : s[r];
+    }
+    if (left < KEYS) {
+      const int rel = left - 32 * kw - 4 * half;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = 8 * (r / 4) + r % 4 >= rel ? -INFINITY : s[r];
+    }
+    float mx = s[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+    {
+      const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+      mx = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+    }
+    if (__any(mx > m)) {                         // (prompt.hip on what is subtracted)
+      const float mn = fmaxf(m, mx + SH_LAG);
+      const float c = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= c;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[d] *= c;
+    }
+    const float ms = m == -INFINITY ? 0.f : m;
+    uint4 pr[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float e[8];
+#pragma unroll
+      for (int r = 0; r < 8; ++r) e[r] = __builtin_amdgcn_exp2f(s[8 * h + r] - ms);
+      l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+      pr[h] = make_uint4(pack_bf16(e[0], e[1]), pack_bf16(e[2], e[3]), pack_bf16(e[4], e[5]), pack_bf16(e[6], e[7]));
+    }
+    // product step x: keys 16 x + 8 (j / 4) + 4 half + j % 4 in place 8 half + j
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        const uint2 a = lds_read_tr(cV, (v_at ^ (64 * d)) + (32 * kw + 16 * x) * RB);
+        const uint2 b = lds_read_tr(cV, (v_at ^ (64 * d + 32)) + (32 * kw + 16 * x + 8) * RB);
+        o[d] = mfma_bf16_32x32x16(make_uint4(a.x, a.y, b.x, b.y), pr[x], o[d]);
+      }
+    reads_ahead<2 * DT, 2, 3>();
+  };
+  const int t1 = n_keys > 0 ? it.t1 : it.t0;     // an empty row: its zeros only
+  if (it.t0 < t1) load_tile(it.t0, sK0, sV0, sL0);
+  for (int t = it.t0; t < t1; t += 2) {
+    step(t, sK0, sV0, sL0, sK1, sV1, sL1);
+    if (t + 1 < t1) step(t + 1, sK1, sV1, sL1, sK0, sV0, sL0);
+  }
+#pragma unroll
+  for (int d = 0; d < DT; ++d) mfma_done16(o[d]);
+  {
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+    l = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+  }
+  const bool mine = me.row < me.rows;
+  // where dim tile d goes: the result, or the place's state
+  const int64_t place = (int64_t)it.id * ROWS + 32 * rw + i32;
+  float* to = it.chunks > 1 ? ws.o + place * D : out + me.hd * D;
+  const float M = m, S = l;
+  auto put = [&](int d, const f32x16& x, float mm, float ll) __attribute__((always_inline)) {
+    const float inv = it.chunks > 1 ? 1.f : (ll > 0.f ? 1.f / ll : ll);    // no entry: the sums are 0; NaN stays
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      *(float4*)(to + 32 * d + 8 * r + 4 * half) = make_float4(x[4 * r] * inv, x[4 * r + 1] * inv, x[4 * r + 2] * inv, x[4 * r + 3] * inv);
+    if (d == 0 && half == 0) {
+      if (it.chunks > 1) ws.ml[place] = make_float2(mm, ll);
+      // (with the sum in units of its largest weight, whose logarithm is small)
+      else lse[me.hd] = mm == -INFINITY ? logf(ll) : ((mm - SH_LAG) + log2f(ll * SH_TOP)) * LN2;
+    }
+  };
+  if constexpr (SPLIT == 1) {
+    if (!mine) return;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) put(d, o[d], M, S);
+  } else {
+    // the waves of the same rows join their states, each a share of the dims, through the tiles' LDS
+    static_assert(KEYS * CH * 16 >= 64 * 4 * 16 * DT, "an array for each wave");
+    __shared__ float2 sml[SH_W][32];
+    sync_after_lds_stores();
+    auto sums = [&](int x) { return (float*)(x == 0 ? sK0 : x == 1 ? sK1 : x == 2 ? sV0 : sV1); };
+    float* so = sums(w);
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) so[64 * (16 * d + r) + lane] = o[d][r];
+    if (half == 0) sml[w][i32] = make_float2(M, S);
+    sync_after_lds_stores();
+    float mm = -INFINITY, ll = 0.f, f[SPLIT];
+#pragma unroll
+    for (int x = 0; x < SPLIT; ++x) mm = fmaxf(mm, sml[SPLIT * rw + x][i32].x);
+#pragma unroll
+    for (int x = 0; x < SPLIT; ++x) {
+      const float2 y = sml[SPLIT * rw + x][i32];
+      f[x] = y.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(y.x - mm);
+      ll += f[x] == 0.f && y.y == y.y ? 0.f : y.y * f[x];        // NaN stays
+    }
+    if (!mine) return;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+      if (d % SPLIT == kw) {
+        f32x16 a;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) a[r] = 0.f;
+#pragma unroll
+        for (int x = 0; x < SPLIT; ++x) {
+          const float* src = sums(SPLIT * rw + x);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const float y = src[64 * (16 * d + r) + lane];
+            a[r] += f[x] == 0.f ? 0.f : y * f[x];
+          }
+        }
+        put(d, a, mm, ll);
+      }
+  }
+}
+
+// fp32: 16 rows a wave, fp32 matrix instructions; SPLIT = 4: the four waves have the same rows and
+// a quarter of a tile's keys each
+template <int D, int SPLIT>
+__global__ __launch_bounds__(SH_T, 2) void k_shared_f32(SharedDims sd, int room, const float* __restrict__ q, const int32_t* __restrict__ cu,
+                                                        PrefixView px, float* __restrict__ out, float* __restrict__ lse, SharedWs ws) {
+  constexpr int ROWS = shared_rows<false, SPLIT>(), KEYS = shared_keys<false, SPLIT>(), WK = KEYS / SPLIT;    // a wave's keys
+  constexpr int CH = D / 4, NL = KEYS * CH / SH_T, LD = D + 4;
+  constexpr int KC = D / 16, VB = D / 64;
+  __shared__ __align__(16) float sK[KEYS * LD], sV[KEYS * LD], sL[KEYS];
+  Item it;
+  if (!find_item<ROWS, KEYS, 1>(sd, cu, px, room, it)) return;
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i16 = lane & 15, g4 = lane >> 4;
+  const int rw = SPLIT == 1 ? w : 0, kw = SPLIT == 1 ? 0 : w;
+  int64_t seq, p_start;
+  const Row me = row_of(sd, cu, it, ROWS, 16 * rw + i16, seq);
+  const int n_keys = (int)held_entries(px, (int64_t)it.b * sd.G + it.g, p_start);
+  if (it.c == 0 && tid == 0) ws.info[(int64_t)(first_tile(sd, cu, it.b, ROWS) + it.tile) * sd.G + it.g] = make_int2(it.id, it.chunks);
+
+  float4 qv[KC];                                // pieces g4, g4 + 4, ... of the row
+  {
+    const float* qp = q + seq * sd.q_tok + (me.hd - seq * sd.H) * D;
+#pragma unroll
+    for (int s = 0; s < KC; ++s) qv[s] = *(const float4*)(qp + 16 * s + 4 * g4);
+  }
+  f32x4 o[VB][4];
+#pragma unroll
+  for (int p = 0; p < VB; ++p)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[p][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;                 // natural units; l: this lane's keys only
+  const float scale = 1.f / sqrtf((float)D);
+  const float* kp = (const float*)px.K + p_start * D;
+  const float* vp = (const float*)px.V + p_start * D;
+  const float* lp = px.logm + p_start;
+  uint4 rk[NL], rv[NL];
+  float rl = 0.f;
+  // entries that are absent or have no weight: log m = -inf, and a value of 0
+  auto load = [&](int t) {
+    const int left = n_keys - t * KEYS;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int e = tid + SH_T * i, c = e % CH, j = e / CH;
+      const int64_t at = ((int64_t)t * KEYS + j) * D + 4 * c;
+      rk[i] = j < left ? *(const uint4*)(kp + at) : make_uint4(0, 0, 0, 0);
+      rv[i] = j < left ? *(const uint4*)(vp + at) : make_uint4(0, 0, 0, 0);
+    }
+    if (tid < KEYS) rl = tid < left ? lp[(int64_t)t * KEYS + tid] : -INFINITY;
+  };
+  const int t1 = n_keys > 0 ? it.t1 : it.t0;
+  if (it.t0 < t1) load(it.t0);
+  for (int t = it.t0; t < t1; ++t) {
+    sync_after_lds_stores();
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int e = tid + SH_T * i;
+      *(uint4*)(sK + e / CH * LD + 4 * (e % CH)) = rk[i];
+      *(uint4*)(sV + e / CH * LD + 4 * (e % CH)) = rv[i];
+    }
+    if (tid < KEYS) sL[tid] = rl;
+    if (t + 1 < t1) load(t + 1);
+    sync_after_lds_stores();
+    bool none = false;
+    if (lane < KEYS) none = sL[lane] == -INFINITY;
+    if (__any(none)) {                          // the same for every wave
+      for (int i = tid; i < KEYS * CH; i += SH_T)
+        if (sL[i / CH] == -INFINITY) *(uint4*)(sV + i / CH * LD + 4 * (i % CH)) = make_uint4(0, 0, 0, 0);
+      sync_after_lds_stores();
+    }
+    float x[WK / 16][4];
+#pragma unroll
+    for (int b = 0; b < WK / 16; ++b) {
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f}, odd = acc;       // two chains, which round half as often
+#pragma unroll
+      for (int s = 0; s < KC; ++s) {
+        const float4 a = *(const float4*)(sK + (WK * kw + 16 * b + i16) * LD + 16 * s + 4 * g4);
+        acc = mfma_f32_16x16x4(a.x, qv[s].x, acc);
+        odd = mfma_f32_16x16x4(a.y, qv[s].y, odd);
+        acc = mfma_f32_16x16x4(a.z, qv[s].z, acc);
+        odd = mfma_f32_16x16x4(a.w, qv[s].w, odd);
+      }
+      mfma_done(acc);
+      mfma_done(odd);
+      acc += odd;
+      const float4 g = *(const float4*)(sL + WK * kw + 16 * b + 4 * g4);
+      const float lg[4] = {g.x, g.y, g.z, g.w};
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[b][r] = lg[r] == -INFINITY ? -INFINITY : acc[r] * scale + lg[r];
+    }
+    float mx = x[0][0];
+#pragma unroll
+    for (int b = 0; b < WK / 16; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) mx = fmaxf(mx, x[b][r]);
+    {
+      const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+      mx = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+      const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+      mx = fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+    }
+    if (__any(mx > m)) {
+      const float mn = fmaxf(m, mx);
+      const float c = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - mn) * LOG2E);
+      m = mn;
+      l *= c;
+#pragma unroll
+      for (int p = 0; p < VB; ++p)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[p][j] *= c;
+    }
+    const float ms = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int b = 0; b < WK / 16; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float y = (x[b][r] - ms) * LOG2E;
+        float e = __builtin_amdgcn_exp2f(y);
+        // what the product lost, to first order
+        if (e > 0.f) e = __builtin_fmaf(e, __builtin_fmaf(x[b][r] - ms, LOG2E, -y) * LN2, e);
+        l += e;
+#pragma unroll
+        for (int p = 0; p < VB; ++p) {
+          const float4 a = *(const float4*)(sV + (WK * kw + 16 * b + 4 * g4 + r) * LD + 64 * p + 4 * i16);
+          o[p][0] = mfma_f32_16x16x4(a.x, e, o[p][0]);
+          o[p][1] = mfma_f32_16x16x4(a.y, e, o[p][1]);
+          o[p][2] = mfma_f32_16x16x4(a.z, e, o[p][2]);
+          o[p][3] = mfma_f32_16x16x4(a.w, e, o[p][3]);
+        }
+      }
+#pragma unroll
+    for (int p = 0; p < VB; ++p) mfma_done(o[p]);
+  }
+  l = col_sum4(l);
+  const bool mine = me.row < me.rows;
+  const int64_t place = (int64_t)it.id * ROWS + 16 * rw + i16;
+  float* to = it.chunks > 1 ? ws.o + place * D : out + me.hd * D;
+  // states of chunks are left in natural units, the bf16 kernel's in base-2 units
+  auto sums = [&](float mm, float ll) {
+    if (it.chunks > 1) ws.ml[place] = make_float2(mm, ll);
+    else lse[me.hd] = mm == -INFINITY ? logf(ll) : mm + logf(ll);
+  };
+  // row 4 g4 + r of product (p, j) is dimension 64 p + 4 (4 g4 + r) + j
+  if constexpr (SPLIT == 1) {
+    if (!mine) return;
+    const float inv = it.chunks > 1 ? 1.f : (l > 0.f ? 1.f / l : l);
+#pragma unroll
+    for (int p = 0; p < VB; ++p)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        *(float4*)(to + 64 * p + 4 * (4 * g4 + r)) = make_float4(o[p][0][r] * inv, o[p][1][r] * inv, o[p][2][r] * inv, o[p][3][r] * inv);
+    if (g4 == 0) sums(m, l);
+  } else {
+    static_assert(KEYS * LD >= SH_W * 16 * LD, "a wave's sums in its share of a tile");
+    __shared__ float2 sml[SH_W][16];
+    sync_after_lds_stores();
+    if (g4 == 0) sml[w][i16] = make_float2(m, l);
+#pragma unroll
+    for (int p = 0; p < VB; ++p)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        *(float4*)(sK + (16 * w + i16) * LD + 64 * p + 4 * (4 * g4 + r)) = make_float4(o[p][0][r], o[p][1][r], o[p][2][r], o[p][3][r]);
+    sync_after_lds_stores();
+    float mm = -INFINITY, ll = 0.f, f[SH_W];
+#pragma unroll
+    for (int x = 0; x < SH_W; ++x) mm = fmaxf(mm, sml[x][i16].x);
+#pragma unroll
+    for (int x = 0; x < SH_W; ++x) {
+      const float2 y = sml[x][i16];
+      f[x] = y.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((y.x - mm) * LOG2E);
+      ll += f[x] == 0.f && y.y == y.y ? 0.f : y.y * f[x];
+    }
+    if (!mine) return;
+    const float inv = it.chunks > 1 ? 1.f : (ll > 0.f ? 1.f / ll : ll);
+    // 16 lanes have a row's pieces in turn
+    for (int c = 4 * (4 * w + g4); c < D; c += 64) {
+      float a[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int x = 0; x < SH_W; ++x) {
+        const float4 y = *(const float4*)(sK + (16 * x + i16) * LD + c);
+        const float v[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] += f[x] == 0.f ? 0.f : v[i] * f[x];
+      }
+      *(float4*)(to + c) = make_float4(a[0] * inv, a[1] * inv, a[2] * inv, a[3] * inv);
+    }
+    if (w == 0 && g4 == 0) sums(mm, ll);
+  }
+}
+
+// The chunks' states of (sequence, head) rows: a lane for four dims, `over` (a power of two) groups
+// of such lanes over the chunks of a row, every lane's loads in flight together.
+template <int D, bool BF>
+__global__ __launch_bounds__(SH_T) void k_shared_join(SharedDims sd, int R, int places, int over, const int32_t* __restrict__ cu,
+                                                      SharedWs ws, float* __restrict__ out, float* __restrict__ lse) {
+  constexpr int LH = D / 4, GR = SH_T / LH, UN = 4;
+  __shared__ float sM[GR], sS[GR];
+  __shared__ __align__(16) float sO[GR][D];
+  const int group = threadIdx.x / LH, gr = group & (over - 1), c = 4 * (threadIdx.x % LH);
+  const int64_t hd = (int64_t)blockIdx.x * (GR / over) + group / over, rows = (int64_t)sd.n_seq * sd.H;
+  const int64_t at = hd < rows ? hd : rows - 1;
+  const int seq = (int)((uint32_t)at / (uint32_t)sd.H), head = (int)at - seq * sd.H, g = head / sd.hpg;
+  const int b = sd.n_group > 1 ? span_with(cu, sd.n_group, seq) : 0;
+  const Span sp = span_of(cu, b, sd.n_seq);
+  bool on = hd < rows && seq >= sp.a && seq < sp.a + sp.n;      // in a group?
+  int first = 0, chunks = 0, tiles = 1, r = 0;
+  if (on) {
+    r = (int)(seq - sp.a) * sd.hpg + (head - g * sd.hpg);
+    tiles = tiles_of_group(sd, sp.n, R);
+    const int2 x = ws.info[(int64_t)(first_tile(sd, cu, b, R) + r / R) * sd.G + g];
+    first = x.x;
+    chunks = x.y < places ? x.y : places;
+    on = chunks > 1;                                             // one: written already
+  }
+  if (!on) chunks = 0;
+  constexpr float UNIT = BF ? 1.f : LOG2E;                       // of the maxima
+  float M = -INFINITY, S = 0.f, O[4] = {0.f, 0.f, 0.f, 0.f};
+  // a state of no entry has the maximum -inf and adds nothing, unless its sum is no number
+  auto add = [&](float m, float s, const float4& x) {
+    const float mn = fmaxf(M, m);
+    const float f = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((M - mn) * UNIT);
+    const float h = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mn) * UNIT);
+    S = (f == 0.f && S == S ? 0.f : S * f) + (h == 0.f && s == s ? 0.f : s * h);
+    const float v[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) O[i] = (f == 0.f ? 0.f : O[i] * f) + (h == 0.f ? 0.f : v[i] * h);
+    M = mn;
+  };
+  // chunk p of the row's tile left its state at place first + p * tiles (where groups descend, that may be none)
+  for (int p0 = gr; p0 < chunks; p0 += over * UN) {
+    float2 ml[UN];
+    float4 x[UN];
+#pragma unroll
+    for (int i = 0; i < UN; ++i) {
+      const int p = p0 + i * over < chunks ? p0 + i * over : p0;
+      int64_t id = first + (int64_t)p * tiles;
+      id = id < 0 ? 0 : (id >= places ? places - 1 : id);
+      ml[i] = ws.ml[id * R + r % R];
+      x[i] = *(const float4*)(ws.o + (id * R + r % R) * D + c);
+    }
+#pragma unroll
+    for (int i = 0; i < UN; ++i)
+      if (p0 + i * over < chunks) add(ml[i].x, ml[i].y, x[i]);
+  }
+  if (over > 1) {
+    *(float4*)&sO[group][c] = make_float4(O[0], O[1], O[2], O[3]);
+    if (c == 0) { sM[group] = M; sS[group] = S; }
+    sync_after_lds_stores();
+  }
+  if (gr != 0 || !on) return;
+  for (int i = 1; i < over; ++i) add(sM[group + i], sS[group + i], *(const float4*)&sO[group + i][c]);
+  const float inv = S > 0.f ? 1.f / S : S;
+  *(float4*)(out + at * D + c) = make_float4(O[0] * inv, O[1] * inv, O[2] * inv, O[3] * inv);
+  if (c == 0) lse[at] = M == -INFINITY ? logf(S) : BF ? ((M - SH_LAG) + log2f(S * SH_TOP)) * LN2 : M + logf(S);
+}
+
+hipError_t launch_shared(const SharedDims& sd, const void* q, const int32_t* cu, const PrefixView& px, float* out, float* lse, void* base,
+                         hipStream_t st) {
+  const SharedPlan p = shared_plan(sd);
+  const SharedWs ws = shared_view(base, sd, p);
+  const int room = p.places - (int)p.tiles;
+  const dim3 grid((unsigned)p.places);
+  const bool bf = sd.dtype == GRACEKV_BF16;
+#define GKV_SHARED(TT, ...) hipLaunchKernelGGL((__VA_ARGS__), grid, dim3(SH_T), 0, st, sd, room, (const TT*)q, cu, px, out, lse, ws)
+  if (bf) {
+    if (sd.d == 128) {
+      if (p.split == 1) GKV_SHARED(uint16_t, k_shared_bf<128, 1>);
+      else if (p.split == 2) GKV_SHARED(uint16_t, k_shared_bf<128, 2>);
+      else GKV_SHARED(uint16_t, k_shared_bf<128, 4>);
+    } else {
+      if (p.split == 1) GKV_SHARED(uint16_t, k_shared_bf<64, 1>);
+      else if (p.split == 2) GKV_SHARED(uint16_t, k_shared_bf<64, 2>);
+      else GKV_SHARED(uint16_t, k_shared_bf<64, 4>);
+    }
+  } else {
+    if (sd.d == 128) { if (p.split == 1) GKV_SHARED(float, k_shared_f32<128, 1>); else GKV_SHARED(float, k_shared_f32<128, 4>); }
+    else { if (p.split == 1) GKV_SHARED(float, k_shared_f32<64, 1>); else GKV_SHARED(float, k_shared_f32<64, 4>); }
+  }
+#undef GKV_SHARED
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  auto join = [&](auto dim, auto bf16) {
+    constexpr int D = decltype(dim)::value, GR = SH_T / (D / 4);
+    const int chunks = room / (int)p.tiles;
+    int over = 1;                        // about four chunks a lane, as it has loads in flight
+    while (over < GR && over * 4 < chunks) over *= 2;
+    const int64_t rows = (int64_t)sd.n_seq * sd.H, each = GR / over;
+    hipLaunchKernelGGL((k_shared_join<D, decltype(bf16)::value>), dim3((unsigned)((rows + each - 1) / each)), dim3(SH_T), 0, st, sd, p.rows,
+                       p.places, over, cu, ws, out, lse);
+  };
+  using std::integral_constant;
+  if (bf) {
+    if (sd.d == 128) join(integral_constant<int, 128>{}, std::true_type{}); else join(integral_constant<int, 64>{}, std::true_type{});
+  } else {
+    if (sd.d == 128) join(integral_constant<int, 128>{}, std::false_type{}); else join(integral_constant<int, 64>{}, std::false_type{});
+  }
+  return hipGetLastError();
+}
+
+}  // namespace gkv

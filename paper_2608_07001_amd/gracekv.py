@@ -16,7 +16,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libgracekv.so")
 
 F32, BF16 = 0, 1
-ABI_VERSION = 12         # GRACEKV_ABI_VERSION this binding is written for
+E4M3, E2M1 = 0, 1        # formats of quantised pages
+ABI_VERSION = 13         # GRACEKV_ABI_VERSION this binding is written for
 _STATUS = {0: "ok", -1: "invalid argument", -2: "unsupported configuration", -3: "budget",
            -4: "workspace too small", -5: "HIP error", -6: "numeric fault on the device",
            -7: "the tree buffer holds no build", -8: "malformed slot partition on the device",
@@ -95,11 +96,34 @@ class PrefixArrays(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("start", "count", "K", "V", "logm")] + [("rows", ctypes.c_int64)]
 
 
+class PartArrays(ctypes.Structure):
+    """gracekv_part."""
+    _fields_ = [("o", ctypes.c_void_p), ("lse", ctypes.c_void_p)]
+
+
+class QuantArrays(ctypes.Structure):
+    """gracekv_quant_pages."""
+    _fields_ = ([("format", ctypes.c_int32), ("reserved", ctypes.c_int32), ("scale_stride", ctypes.c_int64)]
+                + [(n, ctypes.c_void_p) for n in ("K", "V", "K_scale", "V_scale")])
+
+
+class ReadConfig(ctypes.Structure):
+    """gracekv_read_config."""
+    _fields_ = [(n, ctypes.c_int64) for n in ("n_rows", "k_tok", "k_head", "v_tok", "v_head")]
+
+
+class SharedConfig(ctypes.Structure):
+    """gracekv_shared_config."""
+    _fields_ = ([(n, ctypes.c_int32) for n in ("dtype", "G", "H", "d", "n_seq", "n_group")] + [("q_tok", ctypes.c_int64)])
+
+
 SYMBOLS = ["gracekv_abi_version", "gracekv_default_config", "gracekv_plan_sizes", "gracekv_status_string", "gracekv_check",
            "gracekv_segment", "gracekv_build_trees", "gracekv_score", "gracekv_select", "gracekv_pack",
            "gracekv_selftest_mfma", "gracekv_decode_ws_bytes", "gracekv_decode_attention", "gracekv_relevance_stats",
            "gracekv_decode_attention_noalloc", "gracekv_stage_times", "gracekv_prompt_ws_bytes", "gracekv_prompt_attention",
-           "gracekv_cache_append", "gracekv_paged_ws_bytes", "gracekv_paged_attention"]
+           "gracekv_cache_append", "gracekv_paged_ws_bytes", "gracekv_paged_attention", "gracekv_paged_attention_part",
+           "gracekv_quant_append", "gracekv_quant_read", "gracekv_quant_attention", "gracekv_shared_ws_bytes",
+           "gracekv_shared_attention"]
 
 _lib = None
 
@@ -143,6 +167,15 @@ def lib() -> ctypes.CDLL:
         "gracekv_paged_ws_bytes": [ctypes.POINTER(PageConfig), ctypes.POINTER(S)],
         "gracekv_paged_attention": [ctypes.POINTER(PageConfig), P, ctypes.c_int64, P, P, P, P, ctypes.POINTER(PrefixArrays),
                                     P, P, P, S, P],
+        "gracekv_paged_attention_part": [ctypes.POINTER(PageConfig), P, ctypes.c_int64, P, P, P, P, ctypes.POINTER(PrefixArrays),
+                                         ctypes.POINTER(PartArrays), P, P, P, S, P],
+        "gracekv_quant_append": [ctypes.POINTER(PageConfig), ctypes.POINTER(AppendConfig), ctypes.POINTER(QuantArrays),
+                                 P, P, P, P, P, P, P, P, P, P, P],
+        "gracekv_quant_read": [ctypes.POINTER(PageConfig), ctypes.POINTER(ReadConfig), ctypes.POINTER(QuantArrays), P, P, P, P, P, P],
+        "gracekv_quant_attention": [ctypes.POINTER(PageConfig), ctypes.POINTER(QuantArrays), P, ctypes.c_int64, P, P,
+                                    ctypes.POINTER(PartArrays), P, P, P, S, P],
+        "gracekv_shared_ws_bytes": [ctypes.POINTER(SharedConfig), ctypes.POINTER(S)],
+        "gracekv_shared_attention": [ctypes.POINTER(SharedConfig), P, P, ctypes.POINTER(PrefixArrays), ctypes.POINTER(PartArrays), P, S, P],
     }
     for name, args in sig.items():
         f = getattr(L, name)
@@ -440,28 +473,172 @@ class Prefix:
     logm: torch.Tensor
 
 
+@dataclasses.dataclass
+class Part:
+    """An attention of the same queries over other entries (gracekv_part), as shared_attention
+    writes it: o [n_seq][H][d] and lse [n_seq][H], fp32."""
+    o: torch.Tensor
+    lse: torch.Tensor
+
+
+def _part(part: Optional[Part], n: int, H: int, d: int, dev: int):
+    if part is None:
+        return None
+    return ctypes.byref(PartArrays(_tensor("part.o", part.o, torch.float32, (n, H, d), dev),
+                                   _tensor("part.lse", part.lse, torch.float32, (n, H), dev)))
+
+
+def _packed(prefix: Prefix, n: int, dtype: torch.dtype, d: int, dev: int):
+    """The packed entries of n rows (sequences or groups, KV heads)."""
+    rows = prefix.K.shape[0]
+    return ctypes.byref(PrefixArrays(
+        _tensor("prefix.start", prefix.start, torch.int64, (n,), dev), _tensor("prefix.count", prefix.count, torch.int64, (n,), dev),
+        _tensor("prefix.K", prefix.K, dtype, (rows, d), dev), _tensor("prefix.V", prefix.V, dtype, (rows, d), dev),
+        _tensor("prefix.logm", prefix.logm, torch.float32, (rows,), dev), rows))
+
+
+def _tokens(q, dtype: torch.dtype, n: int, H: int, d: int, dev: int):
+    """Address of one token's query of every sequence, and the distance of two."""
+    qp, far, head = _rows("q", q, dtype, (n, H, d), dev)
+    if head != (d if H > 1 else 0):
+        _refuse("q", q, dtype, (n, H, d), dev, (far, d, 1))
+    return qp, far
+
+
 def paged_attention(cfg: PageConfig, q, K_pages, V_pages, block_table, seq_len, out, ws, lse=None, prefix: Optional[Prefix] = None,
-                    stream=None):
+                    part: Optional[Part] = None, stream=None):
     """Attention of one token of every sequence over its pages and packed entries
     (gracekv_paged_attention): q [n_seq][H][d] (rows any distance apart), seq_len [n_seq]
-    int32, out [n_seq][H][d], lse [n_seq][H] fp32, ws: paged_ws_bytes(cfg) bytes."""
+    int32, out [n_seq][H][d], lse [n_seq][H] fp32, ws: paged_ws_bytes(cfg) bytes.  ``part``:
+    joined to it (gracekv_paged_attention_part)."""
     dev, t, n, G, H, d = torch.cuda.current_device(), _TORCH[cfg.dtype], cfg.n_seq, cfg.G, cfg.H, cfg.d
-    shape = (n, H, d)
-    qp, far, head = _rows("q", q, t, shape, dev)
-    if head != (d if H > 1 else 0):
-        _refuse("q", q, t, shape, dev, (far, d, 1))
-    px = None
-    if prefix is not None:
-        R, rows = (n * G,), prefix.K.shape[0]
-        px = ctypes.byref(PrefixArrays(
-            _tensor("prefix.start", prefix.start, torch.int64, R, dev), _tensor("prefix.count", prefix.count, torch.int64, R, dev),
-            _tensor("prefix.K", prefix.K, t, (rows, d), dev), _tensor("prefix.V", prefix.V, t, (rows, d), dev),
-            _tensor("prefix.logm", prefix.logm, torch.float32, (rows,), dev), rows))
-    _ok(lib().gracekv_paged_attention(
+    qp, far = _tokens(q, t, n, H, d, dev)
+    px = None if prefix is None else _packed(prefix, n * G, t, d, dev)
+    _ok(lib().gracekv_paged_attention_part(
         ctypes.byref(cfg), qp, far, *_pages(cfg, K_pages, V_pages, dev), _tensor("block_table", block_table, torch.int32, (n, cfg.table_width), dev),
-        _tensor("seq_len", seq_len, torch.int32, (n,), dev), px, _tensor("out", out, t, shape, dev),
+        _tensor("seq_len", seq_len, torch.int32, (n,), dev), px, _part(part, n, H, d, dev), _tensor("out", out, t, (n, H, d), dev),
         None if lse is None else _tensor("lse", lse, torch.float32, (n, H), dev), *_workspace(ws, dev), _raw(stream, dev)),
         "paged_attention")
+
+
+@dataclasses.dataclass
+class QuantPages:
+    """Quantised pages of one layer (gracekv_quant_pages): codes K, V uint8 [n_pages][G][page_size][d]
+    (E4M3) or [..][d / 2] (E2M1), scales K_scale, V_scale uint8 [n_pages][G][page_size][d / 32]; pages
+    any distance apart, the same for K and V, each contiguous."""
+    format: int
+    K: torch.Tensor
+    V: torch.Tensor
+    K_scale: torch.Tensor
+    V_scale: torch.Tensor
+
+
+def quant_config(pages: QuantPages, dtype: torch.dtype, H: int, block_table) -> PageConfig:
+    """The shapes of a quantised paged cache with rows of ``dtype`` around it (torch.bfloat16 or
+    torch.float32), block_table [n_seq][table_width] int32, H query heads."""
+    K = pages.K
+    if pages.format not in (E4M3, E2M1):
+        raise ValueError(f"format: got {pages.format}, need E4M3 or E2M1")
+    if K.dim() != 4 or block_table.dim() != 2:
+        raise ValueError(f"need [n_pages][G][page_size][bytes] and [n_seq][table_width], got {tuple(K.shape)}, {tuple(block_table.shape)}")
+    if dtype not in _DTYPE:
+        raise ValueError(f"dtype: got {dtype}, need one of {list(_DTYPE)}")
+    n, G, page, row = K.shape
+    each = 1 if pages.format == E4M3 else 2             # codes of a byte
+    far = (K.stride(0) if n > 1 else G * page * row) * each
+    return PageConfig(_DTYPE[dtype], G, H, row * each, block_table.shape[0], page, block_table.shape[1], 0, n, far)
+
+
+def _quantised(cfg: PageConfig, p: QuantPages, dev: int):
+    """The pools of a quantised cache, all four alike."""
+    each = 1 if p.format == E4M3 else 2
+    n, G, page, d, u8 = cfg.n_pages, cfg.G, cfg.page_size, cfg.d, torch.uint8
+    scale_far = p.K_scale.stride(0) if n > 1 else G * page * (d // 32)
+    for names, row, far in ((("K", "V"), d // each, cfg.page_stride // each), (("K_scale", "V_scale"), d // 32, scale_far)):
+        shape, strides = (n, G, page, row), (far, page * row, row, 1)
+        for name in names:
+            x = getattr(p, name)
+            if x.dtype is not u8 or x.shape != shape or x.get_device() != dev:
+                _refuse(name, x, u8, shape, dev, strides)
+            if x.stride() != strides and any(k > 1 and a != b for k, a, b in zip(shape, x.stride(), strides)):
+                raise ValueError(f"{name}: strides {x.stride()}, need {strides}")
+    return ctypes.byref(QuantArrays(p.format, 0, scale_far, p.K.data_ptr(), p.V.data_ptr(), p.K_scale.data_ptr(), p.V_scale.data_ptr()))
+
+
+def quant_append(cfg: PageConfig, pages: QuantPages, k, v, block_table, start, cu_new, pos=None, rope_cos=None, rope_sin=None,
+                 q=None, q_out=None, stream=None):
+    """New tokens quantised into the pages (gracekv_quant_append); ``cfg`` from quant_config,
+    the other arguments as cache_append's."""
+    dev, t, i32 = torch.cuda.current_device(), _TORCH[cfg.dtype], torch.int32
+    n, n_seq, G, d = k.shape[0], cfg.n_seq, cfg.G, cfg.d
+    kp, k_tok, k_head = _rows("k", k, t, (n, G, d), dev)
+    vp, v_tok, v_head = _rows("v", v, t, (n, G, d), dev)
+    qp, q_tok, q_head = (None, 0, 0) if q is None else _rows("q", q, t, (n, cfg.H, d), dev)
+    op, o_tok, o_head = (None, 0, 0) if q_out is None else _rows("q_out", q_out, t, (n, cfg.H, d), dev)
+    r = 0 if rope_cos is None else rope_cos.shape[0]
+    _ok(lib().gracekv_quant_append(
+        ctypes.byref(cfg), ctypes.byref(AppendConfig(n, r, k_tok, k_head, v_tok, v_head, q_tok, q_head, o_tok, o_head)),
+        _quantised(cfg, pages, dev), kp, vp, qp,
+        _tensor("block_table", block_table, i32, (n_seq, cfg.table_width), dev), _tensor("start", start, i32, (n_seq,), dev),
+        _tensor("cu_new", cu_new, i32, (n_seq + 1,), dev), None if pos is None else _tensor("pos", pos, i32, (n,), dev),
+        None if rope_cos is None else _tensor("rope_cos", rope_cos, torch.float32, (r, d // 2), dev),
+        None if rope_sin is None else _tensor("rope_sin", rope_sin, torch.float32, (r, d // 2), dev),
+        op, _raw(stream, dev)), "quant_append")
+
+
+def quant_read(cfg: PageConfig, pages: QuantPages, block_table, start, cu_rows, k=None, v=None, stream=None):
+    """Rows back from quantised pages (gracekv_quant_read): row cu_rows[b] + i of k and v
+    [n_rows][G][d] (any strides of rows and heads; either may be None) becomes what place
+    start[b] + i of sequence b stands for."""
+    dev, t, n_seq, G, d = torch.cuda.current_device(), _TORCH[cfg.dtype], cfg.n_seq, cfg.G, cfg.d
+    n = k.shape[0] if k is not None else (v.shape[0] if v is not None else 0)
+    kp, k_tok, k_head = (None, 0, 0) if k is None else _rows("k", k, t, (n, G, d), dev)
+    vp, v_tok, v_head = (None, 0, 0) if v is None else _rows("v", v, t, (n, G, d), dev)
+    _ok(lib().gracekv_quant_read(
+        ctypes.byref(cfg), ctypes.byref(ReadConfig(n, k_tok, k_head, v_tok, v_head)), _quantised(cfg, pages, dev),
+        _tensor("block_table", block_table, torch.int32, (n_seq, cfg.table_width), dev),
+        _tensor("start", start, torch.int32, (n_seq,), dev), _tensor("cu_rows", cu_rows, torch.int32, (n_seq + 1,), dev),
+        kp, vp, _raw(stream, dev)), "quant_read")
+
+
+def quant_attention(cfg: PageConfig, pages: QuantPages, q, block_table, seq_len, out, ws, lse=None, part: Optional[Part] = None,
+                    stream=None):
+    """Attention of one token of every sequence over its quantised pages, joined to ``part``
+    (gracekv_quant_attention); ``cfg`` from quant_config, the other arguments as paged_attention's."""
+    dev, t, n, H, d = torch.cuda.current_device(), _TORCH[cfg.dtype], cfg.n_seq, cfg.H, cfg.d
+    qp, far = _tokens(q, t, n, H, d, dev)
+    _ok(lib().gracekv_quant_attention(
+        ctypes.byref(cfg), _quantised(cfg, pages, dev), qp, far, _tensor("block_table", block_table, torch.int32, (n, cfg.table_width), dev),
+        _tensor("seq_len", seq_len, torch.int32, (n,), dev), _part(part, n, H, d, dev), _tensor("out", out, t, (n, H, d), dev),
+        None if lse is None else _tensor("lse", lse, torch.float32, (n, H), dev), *_workspace(ws, dev), _raw(stream, dev)),
+        "quant_attention")
+
+
+def shared_config(q, G: int, n_group: int) -> SharedConfig:
+    """The shapes of n_group groups of the sequences whose queries these are (q [n_seq][H][d], rows
+    any distance apart), with G KV heads, for shared_attention."""
+    n, H, d = _heads("q", q)
+    return SharedConfig(_dtype_of("q", q), G, H, d, n, n_group, q.stride(0) if n > 1 else 0)
+
+
+def shared_ws_bytes(cfg: SharedConfig) -> int:
+    n = ctypes.c_size_t(0)
+    _ok(lib().gracekv_shared_ws_bytes(ctypes.byref(cfg), ctypes.byref(n)), "shared_ws_bytes")
+    return int(n.value)
+
+
+def shared_attention(cfg: SharedConfig, q, cu_group, prefix: Prefix, part: Part, ws, stream=None):
+    """Attention of one token of every sequence over packed entries that its group shares
+    (gracekv_shared_attention), written to ``part``: cu_group [n_group + 1] int32, prefix.start and
+    .count [n_group * G], ws: shared_ws_bytes(cfg) bytes."""
+    dev, t, n, H, d = torch.cuda.current_device(), _TORCH[cfg.dtype], cfg.n_seq, cfg.H, cfg.d
+    qp, far = _tokens(q, t, n, H, d, dev)
+    if far != cfg.q_tok:
+        _refuse("q", q, t, (n, H, d), dev, (cfg.q_tok, d, 1))
+    _ok(lib().gracekv_shared_attention(
+        ctypes.byref(cfg), qp, _tensor("cu_group", cu_group, torch.int32, (cfg.n_group + 1,), dev),
+        _packed(prefix, cfg.n_group * cfg.G, t, d, dev), _part(part, n, H, d, dev), *_workspace(ws, dev), _raw(stream, dev)),
+        "shared_attention")
 
 
 def selftest_mfma(which: int, stream=None) -> torch.Tensor:

@@ -1,0 +1,836 @@
+"""Quantised pages (writing, reading back, attention) and entries that groups of sequences share, on the
+GPU, against their definitions in float64; tolerances count roundings (serve_harness, quant_harness)."""
+import itertools
+import math
+
+import pytest
+import torch
+
+import gpu_harness as H
+import quant_harness as Q
+import serve_harness as S
+from paper_2608_07001_amd import gracekv as gk
+from synth.workloads import make_case, small_shape
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+HEADS = [(2, 8), (1, 1), (3, 15), (2, 34), (1, 7)]
+TYPES = [("bf16", 128), ("bf16", 64), ("f32", 64), ("f32", 128)]
+FORMATS = [gk.E4M3, gk.E2M1]
+
+
+def _rand(gen, *shape, dtype="bf16", scale=1.0):
+    return (torch.randn(*shape, generator=gen) * scale).to(DT[dtype])
+
+
+def _i32(*x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def _cu(lens):
+    return torch.tensor([0] + list(lens), dtype=torch.int32).cumsum(0).to(torch.int32)
+
+
+def _tables(gen, need, page, extra=2):
+    """Page ids in no order, -1 where a row of the table has no page, and the number of pages."""
+    n = [-(-x // page) for x in need]
+    total, width = sum(n) + extra, max(max(n), 1)
+    ids = torch.randperm(total, generator=gen).to(torch.int32)
+    table = torch.full((len(need), width), -1, dtype=torch.int32)
+    at = 0
+    for b, x in enumerate(n):
+        table[b, :x] = ids[at:at + x]
+        at += x
+    return table, total
+
+
+def _rope(rows, d):
+    ang = torch.arange(rows, dtype=torch.float64)[:, None] * 1e4 ** (-torch.arange(0, d, 2, dtype=torch.float64) / d)
+    return ang.cos().float(), ang.sin().float()
+
+
+def _pools(gen, n_pages, G, page, d, fmt, layers=0):
+    """Random codes and scales (CPU), of several layers a page if asked."""
+    shape = (n_pages,) + ((layers,) if layers else ()) + (G, page)
+    code = lambda: torch.randint(0, 256, shape + (d * Q.BITS[fmt] // 8,), generator=gen).to(torch.uint8)      # noqa: E731
+    scale = lambda: torch.randint(120, 126, shape + (d // 32,), generator=gen).to(torch.uint8)               # noqa: E731
+    K, V = code(), code()
+    if fmt == gk.E4M3:                                          # no NaN unless it is meant
+        K[K & 127 == 127], V[V & 127 == 127] = 0, 0
+        Ks, Vs = (x - 4 for x in (scale(), scale()))
+    else:
+        Ks, Vs = scale(), scale()
+    return K, V, Ks, Vs
+
+
+# ---------------------------------------------------------------------------
+# writing and reading back
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("G,Hq", [(2, 8), (1, 1), (3, 15)])
+@pytest.mark.parametrize("page,layout", [(16, "token"), (32, "head"), (256, "wide")])
+def test_append(dtype, d, fmt, G, Hq, page, layout):
+    gen = torch.Generator().manual_seed(page + Hq)
+    start, new = [0, 15, 16, 33, 250, 5], [1, 2, 40, 0, 17, 1]
+    n = sum(new) + 2                                           # two rows behind the last sequence
+    table, n_pages = _tables(gen, [a + b for a, b in zip(start, new)], page)
+    k, v, q = (_rand(gen, n, x, d, dtype=dtype) for x in (G, G, Hq))
+    pos = torch.randint(0, 400, (n,), generator=gen).to(torch.int32)
+    cos, sin = _rope(400, d)
+    pools = _pools(gen, n_pages, G, page, d, fmt, layers=3)    # the middle layer of a pool of three
+    dev = [x.cuda() for x in pools]
+    pages = gk.QuantPages(fmt, *[x[:, 1] for x in dev])
+    q_out = S.laid(torch.full((n, Hq, d), 7.0, dtype=DT[dtype], device="cuda"), layout)
+    cfg = gk.quant_config(pages, DT[dtype], Hq, table)
+    gk.quant_append(cfg, pages, S.laid(k.cuda(), layout), S.laid(v.cuda(), layout), table.cuda(), _i32(*start), _cu(new).cuda(),
+                    pos.cuda(), cos.cuda(), sin.cuda(), S.laid(q.cuda(), layout), q_out)
+    torch.cuda.synchronize()
+    kr, qr = (Q.rotated32(x, cos[pos.long()], sin[pos.long()]) for x in (k, q))
+    want = [x.clone() for x in pools]
+    i = 0
+    (kc, ks), (vc, vs) = Q.quantise(kr.double(), fmt), Q.quantise(v.double(), fmt)
+    for b, (a, m) in enumerate(zip(start, new)):
+        for j in range(m):
+            p, at = int(table[b, (a + j) // page]), (a + j) % page
+            for w, x in zip(want, (Q.packed(kc, fmt), Q.packed(vc, fmt), ks, vs)):
+                w[p, 1, :, at] = x[i]
+            i += 1
+    for name, got, w in zip(("K", "V", "K_scale", "V_scale"), dev, want):
+        assert torch.equal(got.cpu(), w), name                 # and nothing else is touched
+    assert torch.equal(q_out[:i].cpu(), qr[:i].to(DT[dtype])) and (q_out[i:] == 7).all()
+    # and back, the rows of a sequence and what lies before them
+    back = [S.laid(torch.full((n, G, d), 7.0, dtype=DT[dtype], device="cuda"), layout) for _ in range(2)]
+    gk.quant_read(cfg, pages, table.cuda(), _i32(*start), _cu(new).cuda(), *back)
+    for got, c, s in zip(back, (kc, vc), (ks, vs)):
+        assert torch.equal(got[:i].cpu().double(), Q.values(Q.packed(c, fmt), s, fmt)[:i]) and (got[i:] == 7).all()
+
+
+def _edges(fmt, dtype):
+    """Rows of 64 whose blocks stand where a rule changes."""
+    T, top = Q.LIMIT[fmt], Q.LARGEST[fmt]
+    v = Q.numbers(fmt)
+    mid = (v[1:] + v[:-1]) / 2
+    t = DT[dtype]
+    rows = []
+
+    def row(first, rest=0.0):
+        r = torch.zeros(64, dtype=torch.float64)
+        r[:32] = rest
+        f = torch.as_tensor(first, dtype=torch.float64).reshape(-1)
+        r[:len(f)] = f
+        r[32:] = -r[:32]
+        rows.append(r)
+    for e in (-130, -126, -110, -3, 0, 5, 100, 118):
+        for x in (T, top, top * 1.03125, T / 2, 2 * top):
+            y = torch.tensor(x * 2.0 ** e).to(t)               # at the limit and on both sides of it
+            for z in (y, torch.nextafter(y.float(), torch.tensor(math.inf)).to(t) if dtype == "f32" else y * (1 + 2.0 ** -7)):
+                if abs(z.item()) < 2.0 ** 127:
+                    row(z.item(), 2.0 ** min(e, 120))
+    for i in range(0, len(mid), 31):                           # every middle of two codes, at a scale of one
+        row(torch.cat([torch.tensor([top], dtype=torch.float64), mid[i:i + 31]]))
+    for x in (math.inf, -math.inf, math.nan, 2.0 ** 127, -3e38):
+        row(x, 1.0)
+    row(0.0)
+    row(-0.0, -0.0)
+    row(2.0 ** 126 * 1.9, 2.0 ** 120)
+    return torch.stack(rows).to(t)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_append_where_rules_change(dtype, fmt):
+    x = _edges(fmt, dtype)
+    n = x.shape[0]
+    table = torch.arange(-(-n // 16), dtype=torch.int32)[None].cuda()
+    pools = [p.cuda() for p in _pools(torch.Generator().manual_seed(1), table.numel(), 1, 16, 64, fmt)]
+    pages = gk.QuantPages(fmt, *pools)
+    cfg = gk.quant_config(pages, DT[dtype], 1, table)
+    gk.quant_append(cfg, pages, x[:, None].cuda(), -x[:, None].cuda(), table, _i32(0), _cu([n]).cuda())
+    for got, gs, y in ((pools[0], pools[2], x), (pools[1], pools[3], -x)):
+        c, s = Q.quantise(y.double(), fmt)
+        gs, got = gs.cpu().reshape(-1, 2)[:n], got.cpu().reshape(-1, 64 * Q.BITS[fmt] // 8)[:n]
+        assert torch.equal(gs, s)
+        val, want = Q.values(got, gs, fmt), Q.values(Q.packed(c, fmt), s, fmt)
+        assert torch.equal(torch.isnan(val), torch.isnan(want))
+        assert torch.equal(val.nan_to_num(1.0), want.nan_to_num(1.0))
+        # the stated bound: half a step of the block's largest
+        b, g = y.double().view(n, -1, 32), want.view(n, -1, 32)
+        top = b.abs().amax(-1, keepdim=True)
+        least = {gk.E4M3: 2.0 ** -127, gk.E2M1: 2.0 ** -119}[fmt]
+        ok = (b - g).abs() <= torch.maximum(top * {gk.E4M3: 2.0 ** -4, gk.E2M1: 0.25}[fmt], torch.tensor(least))
+        assert (ok | ~(top < 2.0 ** 127)).all()
+    k = torch.empty(n, 1, 64, dtype=DT[dtype], device="cuda")
+    gk.quant_read(cfg, pages, table, _i32(0), _cu([n]).cuda(), k=k)
+    want = Q.values(pools[0].cpu().reshape(-1, 64 * Q.BITS[fmt] // 8)[:n], pools[2].cpu().reshape(-1, 2)[:n], fmt)
+    assert torch.equal(k.cpu().double()[:, 0].nan_to_num(1.0), want.nan_to_num(1.0))
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_read_every_code(dtype, d, fmt):
+    # all codes under scales from end to end, NaN among both; missing pages; one side only
+    scales = [10, 11, 60, 126, 127, 128, 200, 247, 255]
+    n = 256 // (d * Q.BITS[fmt] // 8) or 1
+    per = d * Q.BITS[fmt] // 8
+    codes = torch.arange(max(256, per), dtype=torch.int64).remainder(256).to(torch.uint8).view(-1, per)
+    n = codes.shape[0]
+    rows = codes.repeat(len(scales), 1)
+    s = torch.tensor(scales, dtype=torch.uint8).repeat_interleave(n)[:, None].expand(-1, d // 32).contiguous()
+    m = rows.shape[0]
+    n_pages = -(-m // 16)
+    pad = n_pages * 16 - m
+    K = torch.cat([rows, rows[:1].expand(pad, -1)]).view(n_pages, 1, 16, per).contiguous()
+    Ks = torch.cat([s, s[:1].expand(pad, -1)]).view(n_pages, 1, 16, d // 32).contiguous()
+    pages = gk.QuantPages(fmt, K.cuda(), K.flip(0).contiguous().cuda(), Ks.cuda(), Ks.flip(0).contiguous().cuda())
+    table = torch.cat([torch.arange(n_pages), torch.tensor([-1, n_pages])]).to(torch.int32)[None].cuda()
+    cfg = gk.quant_config(pages, DT[dtype], 1, table)
+    total = (n_pages + 2) * 16 + 5                             # past the table too
+    k, v = (torch.full((total + 3, 1, d), 7.0, dtype=DT[dtype], device="cuda") for _ in range(2))
+    gk.quant_read(cfg, pages, table, _i32(0), _cu([total]).cuda(), k, v)
+    want = torch.zeros(total, d, dtype=torch.float64)
+    for got, C, Sc in ((k, K, Ks), (v, K.flip(0), Ks.flip(0))):
+        # (448 * 2^120 is past the range of either type and reads as infinite: the append writes no such pair)
+        want[:n_pages * 16] = Q.values(C.reshape(-1, per), Sc.reshape(-1, d // 32), fmt).to(DT[dtype]).double()
+        g = got.cpu().double()[:, 0]
+        assert torch.equal(torch.isnan(g[:total]), torch.isnan(want)) and torch.equal(g[:total].nan_to_num(1.0), want.nan_to_num(1.0))
+        assert (g[total:] == 7).all()
+    only = torch.full_like(v, 7.0)
+    gk.quant_read(cfg, pages, table, _i32(-16), _cu([40]).cuda(), v=only)      # places before the first have no page
+    assert (only[:16] == 0).all() and torch.equal(only[16:40].nan_to_num(1.0), v[:24].nan_to_num(1.0)) and (only[40:] == 7).all()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_append_in_place_and_left_out_tokens(fmt):
+    # queries turned where they stand; tokens without a page or a position; places that are negative or past the table
+    gen = torch.Generator().manual_seed(3)
+    page, d, G, Hq = 16, 128, 2, 4
+    start, new = [-2, 30, 14, 0], [4, 4, 4, 2]
+    n = sum(new)
+    table = torch.tensor([[0, 1], [2, 3], [4, -1], [9, 5]], dtype=torch.int32)   # 9 is no page
+    pools = _pools(gen, 7, G, page, d, fmt)
+    dev = [x.cuda() for x in pools]
+    pages = gk.QuantPages(fmt, *dev)
+    k, v, q = (_rand(gen, n, x, d) for x in (G, G, Hq))
+    pos = torch.arange(n, dtype=torch.int32)
+    pos[5], pos[8] = -1, 64
+    cos, sin = _rope(64, d)
+    qd = q.cuda()
+    cfg = gk.quant_config(pages, torch.bfloat16, Hq, table)
+    gk.quant_append(cfg, pages, k.cuda(), v.cuda(), table.cuda(), _i32(*start), _cu(new).cuda(), pos.cuda(), cos.cuda(), sin.cuda(), qd, qd)
+    want, qw = [x.clone() for x in pools], q.clone()
+    i = 0
+    for b, (a, m) in enumerate(zip(start, new)):
+        for j in range(m):
+            place, p = a + j, int(pos[i])
+            if 0 <= place < 32 and 0 <= p < 64 and 0 <= int(table[b, place // page]) < 7:
+                at = int(table[b, place // page]), slice(None), place % page
+                kr = Q.rotated32(k[i:i + 1], cos[p:p + 1], sin[p:p + 1])
+                for (c, s), x, y in ((Q.quantise(kr[0].double(), fmt), 0, 2), (Q.quantise(v[i].double(), fmt), 1, 3)):
+                    want[x][at], want[y][at] = Q.packed(c, fmt), s
+                qw[i] = Q.rotated32(q[i:i + 1], cos[p:p + 1], sin[p:p + 1])[0].bfloat16()
+            i += 1
+    for got, w in zip(dev, want):
+        assert torch.equal(got.cpu(), w)
+    assert torch.equal(qd.cpu(), qw)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_append_and_read_many_sequences(fmt):
+    gen = torch.Generator().manual_seed(4)
+    B, d = 700, 64
+    new = torch.randint(0, 4, (B,), generator=gen).tolist()
+    start = torch.randint(0, 40, (B,), generator=gen).tolist()
+    table, n_pages = _tables(gen, [a + b for a, b in zip(start, new)], 16)
+    dev = [x.cuda() for x in _pools(gen, n_pages, 1, 16, d, fmt)]
+    pages = gk.QuantPages(fmt, *dev)
+    cfg = gk.quant_config(pages, torch.float32, 1, table)
+    k, v = (_rand(gen, sum(new), 1, d, dtype="f32") for _ in range(2))
+    args = table.cuda(), _i32(*start), _cu(new).cuda()
+    gk.quant_append(cfg, pages, k.cuda(), v.cuda(), *args)
+    back = [torch.zeros(sum(new), 1, d, device="cuda") for _ in range(2)]
+    gk.quant_read(cfg, pages, *args, *back)
+    for got, x in zip(back, (k, v)):
+        c, s = Q.quantise(x.double(), fmt)
+        assert torch.equal(got.cpu().double(), Q.values(Q.packed(c, fmt), s, fmt))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_append_and_read_nothing_or_descending(fmt):
+    gen = torch.Generator().manual_seed(5)
+    table, n_pages = _tables(gen, [40, 40, 40], 16)
+    pools = _pools(gen, n_pages, 2, 16, 64, fmt)
+    dev = [x.cuda() for x in pools]
+    pages = gk.QuantPages(fmt, *dev)
+    cfg = gk.quant_config(pages, torch.bfloat16, 4, table)
+    none = torch.zeros(0, 2, 64, dtype=torch.bfloat16, device="cuda")
+    zero = torch.zeros(4, dtype=torch.int32, device="cuda")
+    gk.quant_append(cfg, pages, none, none, table.cuda(), zero[:3], zero)
+    gk.quant_read(cfg, pages, table.cuda(), zero[:3], zero, none, none)
+    gk.quant_read(cfg, pages, table.cuda(), zero[:3], zero)
+    for got, x in zip(dev, pools):
+        assert torch.equal(got.cpu(), x)
+    rows = _rand(gen, 12, 2, 64).cuda()
+    for cu in ([9, 3, 12, 0], [-5, 2 ** 31 - 1, -2 ** 31, 7], [12, 12, 12, 12], [5, 5, 5, 100]):
+        gk.quant_append(cfg, pages, rows, rows, table.cuda(), zero[:3], _i32(*cu))
+        gk.quant_read(cfg, pages, table.cuda(), zero[:3], _i32(*cu), rows.clone(), rows.clone())
+    torch.cuda.synchronize()
+
+
+# ---------------------------------------------------------------------------
+# attention over quantised pages
+
+
+class Cache:
+    """A quantised paged cache with ragged lengths, on the CPU."""
+
+    def __init__(self, dtype, d, fmt, G, Hq, lens, page, seed=0):
+        gen = torch.Generator().manual_seed(seed)
+        self.dtype, self.d, self.fmt, self.G, self.H, self.lens, self.page = dtype, d, fmt, G, Hq, list(lens), page
+        self.table, n_pages = _tables(gen, lens, page)
+        self.K, self.V, self.Ks, self.Vs = _pools(gen, n_pages, G, page, d, fmt)
+        self.q = _rand(gen, len(lens), Hq, d, dtype=dtype)
+        self.len = torch.tensor(lens, dtype=torch.int32)
+
+    def on_gpu(self):
+        table = self.table.cuda()
+        pages = gk.QuantPages(self.fmt, *[x.cuda() for x in (self.K, self.V, self.Ks, self.Vs)])
+        return pages, table, gk.quant_config(pages, DT[self.dtype], self.H, table)
+
+    def call(self, ws=None, part=None):
+        pages, table, cfg = self.on_gpu()
+        out = torch.full(self.q.shape, 7.0, dtype=DT[self.dtype], device="cuda")
+        lse = torch.full(self.q.shape[:2], 7.0, device="cuda")
+        ws = torch.full((gk.paged_ws_bytes(cfg),), 255, dtype=torch.uint8, device="cuda") if ws is None else ws
+        wide = torch.full((self.q.shape[0], self.H + 3, self.d), float("nan"), dtype=self.q.dtype, device="cuda")
+        wide[:, :self.H] = self.q.cuda()
+        gk.quant_attention(cfg, pages, wide[:, :self.H], table, self.len.cuda(), out, ws, lse=lse, part=part)
+        torch.cuda.synchronize()
+        return out.cpu(), lse.cpu()
+
+    def entries(self, b, g):
+        """Keys, values and log m (-inf: no page) of (b, g), in order (float64)."""
+        n = max(0, min(int(self.len[b]), self.table.shape[1] * self.page))
+        ids = self.table[b].long()
+        ok = (ids >= 0) & (ids < self.K.shape[0])
+        at = torch.where(ok, ids, 0)
+        k, v = (Q.values(x[at, g], s[at, g], self.fmt).reshape(-1, self.d)[:n] for x, s in ((self.K, self.Ks), (self.V, self.Vs)))
+        lm = torch.where(ok, 0.0, -math.inf).double().repeat_interleave(self.page)[:n]
+        return k, v, lm
+
+    def check(self, got=None):
+        out, lse = got or self.call()
+        per, parts = self.H // self.G, 2 if self.dtype == "bf16" else 3
+        for b, g in itertools.product(range(len(self.lens)), range(self.G)):
+            k, v, lm = self.entries(b, g)
+            h = slice(g * per, (g + 1) * per)
+            # sums over two (three) parts of the weights, logits over one (three) of the queries
+            S.check_rows(out[b, h], lse[b, h], S.attend64(self.q[b, h].double(), k, v, bias=lm), parts * max(len(k), 1),
+                         self.d * (1 if self.dtype == "bf16" else 3), self.dtype == "bf16", (self.dtype, self.d, self.fmt, self.G, self.H, b, g))
+
+
+LENS = [0, 1, 15, 16, 17, 31, 32, 33, 100, 257]
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("G,Hq", HEADS)
+@pytest.mark.parametrize("page", [16, 64])
+def test_attention(dtype, d, fmt, G, Hq, page):
+    Cache(dtype, d, fmt, G, Hq, LENS, page, seed=Hq).check()
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_attention_long_and_split(dtype, d, fmt):
+    for i, (G, Hq, lens, page) in enumerate([(1, 4, [6001], 16), (2, 8, [4000, 1, 0, 777], 128), (1, 20, [3000, 50], 256),
+                                             (2, 4, [0 if j % 5 == 0 else 20 + j for j in range(129)] + [5003], 16)]):
+        Cache(dtype, d, fmt, G, Hq, lens, page, seed=30 + i).check()
+    c = Cache(dtype, d, fmt, 1, 4, [131072], 64, seed=40)       # more chunks than the join takes at once
+    c.Vs[c.table[0].long()] = (torch.linspace(120, 126, 2048).to(torch.uint8) - (4 if fmt == gk.E4M3 else 0)).view(-1, 1, 1, 1)
+    c.check()
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_attention_masked_places_reach_nothing(dtype, d, fmt):
+    # what lies past the end, or in pages that are nobody's, stands for NaN; a page of the first sequence is missing
+    c = Cache(dtype, d, fmt, 2, 6, [40, 0, 5, 32], 16, seed=6)
+    c.table[0, 1] = -1
+    c.table[3, 0] = c.K.shape[0]
+    used = torch.zeros(c.K.shape[0], dtype=torch.bool)
+    used[c.table[(c.table >= 0) & (c.table < c.K.shape[0])].long()] = True
+    for x, s in ((c.K, c.Ks), (c.V, c.Vs)):
+        x[~used], s[~used] = 127, 255
+        s[c.table[0, 2].long(), :, 8:] = 255                   # past place 40
+        x[c.table[2, 0].long(), :, 5:], s[c.table[2, 0].long(), :, 5:] = 255, 254
+    c.check()
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_attention_values_of_no_number_stay_in_their_block(dtype, d, fmt):
+    c = Cache(dtype, d, fmt, 1, 3, [70], 16, seed=7)
+    p = c.table[0].long()
+    c.Vs[p[1], 0, 3, 1] = 255                                  # dims 32 .. 63 of token 19
+    out, lse = c.call()
+    k, v, lm = c.entries(0, 0)
+    ref = S.attend64(c.q[0].double(), k, v.nan_to_num(0.0), bias=lm)
+    assert torch.isnan(out[0, :, 32:64]).all() and torch.isfinite(lse).all()
+    fine = torch.ones(d, dtype=torch.bool)
+    fine[32:64] = False
+    tol, _ = S.bounds(*ref, 3 * 70, 3 * d, dtype == "bf16")
+    assert ((out[0].double() - ref[0]).abs()[:, fine] <= tol[:, fine]).all()
+    c.Vs[p[1], 0, 3, 1], c.Ks[p[0], 0, 2, 0] = 120, 255        # a key's block: every head's weights
+    out, lse = c.call()
+    assert torch.isnan(out).all() and torch.isnan(lse).all()
+
+
+def test_attention_malformed_inputs_stay_inside():
+    for fmt in FORMATS:
+        c = Cache("bf16", 64, fmt, 2, 4, [40, 20, 33], 16, seed=9)
+        c.table[1, 0], c.table[2, 1] = c.K.shape[0], 2 ** 31 - 1
+        c.len[:] = torch.tensor([2 ** 31 - 1, -5, 33], dtype=torch.int32)
+        c.check()
+
+
+def test_attention_every_batch_size_and_workspace():
+    ws = torch.full((16 << 20,), 127, dtype=torch.uint8, device="cuda")
+    for B in (1, 2, 63, 64, 65, 257, 700):
+        gen = torch.Generator().manual_seed(B)
+        c = Cache("bf16", 64, FORMATS[B % 2], 1, 2, torch.randint(0, 60, (B,), generator=gen).tolist(), 16, seed=B)
+        c.check(c.call(ws=ws))
+
+
+def test_attention_scales_from_end_to_end():
+    # large and small powers of two in the keys and values of one row
+    for fmt, (dtype, d) in itertools.product(FORMATS, TYPES):
+        c = Cache(dtype, d, fmt, 1, 2, [50], 16, seed=11)
+        c.Ks[:] = torch.randint(100, 126, c.Ks.shape, generator=torch.Generator().manual_seed(1)).to(torch.uint8) - (4 if fmt == gk.E4M3 else 0)
+        c.Vs[:] = torch.randint(60, 180, c.Vs.shape, generator=torch.Generator().manual_seed(2)).to(torch.uint8)
+        c.check()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_far_pages(fmt):
+    # codes and scales past 32 bits of bytes: written, read back and attended to on a pool's last page
+    page, d, G, n = 256, 128, 1, 34
+    row, far = d * Q.BITS[fmt] // 8, 1 << 27                   # bytes from page to page: the last begins past 2^32
+    pool = lambda width, far: torch.zeros(n, far, dtype=torch.uint8, device="cuda")[:, :page * width].unflatten(1, (G, page, width))      # noqa: E731
+    pools = [pool(row, far), pool(row, far), pool(4, far), pool(4, far)]
+    pages = gk.QuantPages(fmt, *pools)
+    table = _i32(n - 1, 0)[None]
+    cfg = gk.quant_config(pages, torch.bfloat16, 2, table)
+    gen = torch.Generator().manual_seed(8)
+    k, v, q = _rand(gen, 300, 1, d), _rand(gen, 300, 1, d), _rand(gen, 1, 2, d)
+    gk.quant_append(cfg, pages, k.cuda(), v.cuda(), table, _i32(0), _cu([300]).cuda())
+    back = [torch.zeros(300, 1, d, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    gk.quant_read(cfg, pages, table, _i32(0), _cu([300]).cuda(), *back)
+    want = []
+    for got, x in zip(back, (k, v)):
+        c, s = Q.quantise(x.double(), fmt)
+        want.append(Q.values(Q.packed(c, fmt), s, fmt)[:, 0])
+        assert torch.equal(got[:, 0].cpu().double(), want[-1])
+    out, lse = torch.zeros(1, 2, d, dtype=torch.bfloat16, device="cuda"), torch.zeros(1, 2, device="cuda")
+    ws = torch.empty(gk.paged_ws_bytes(cfg), dtype=torch.uint8, device="cuda")
+    gk.quant_attention(cfg, pages, q.cuda(), table, _i32(300), out, ws, lse=lse)
+    S.check_rows(out[0].cpu(), lse[0].cpu(), S.attend64(q[0].double(), *want), 600, d, True, "far")
+
+
+# ---------------------------------------------------------------------------
+# shared entries
+
+
+class Shared:
+    """Groups of sequences and the entries of each (group, KV head), on the CPU."""
+
+    def __init__(self, dtype, d, G, Hq, groups, counts, behind=0, seed=0):
+        gen = torch.Generator().manual_seed(seed)
+        self.dtype, self.d, self.G, self.H, self.groups = dtype, d, G, Hq, list(groups)
+        self.n = sum(groups) + behind
+        self.q = _rand(gen, self.n, Hq, d, dtype=dtype, scale=1.5)
+        self.cu = _cu(groups)
+        c = torch.tensor(counts, dtype=torch.int64)
+        rows = int(c.sum()) + 3
+        self.pre = dict(start=c.cumsum(0) - c, count=c, K=_rand(gen, rows, d, dtype=dtype), V=_rand(gen, rows, d, dtype=dtype),
+                        logm=torch.rand(rows, generator=gen) * 4)
+
+    def call(self, ws=None):
+        wide = torch.full((self.n, self.H + 3, self.d), float("nan"), dtype=self.q.dtype, device="cuda")
+        wide[:, :self.H] = self.q.cuda()
+        q = wide[:, :self.H]
+        cfg = gk.shared_config(q, self.G, len(self.groups))
+        ws = torch.full((gk.shared_ws_bytes(cfg),), 255, dtype=torch.uint8, device="cuda") if ws is None else ws
+        part = gk.Part(torch.full((self.n, self.H, self.d), 7.0, device="cuda"), torch.full((self.n, self.H), 7.0, device="cuda"))
+        gk.shared_attention(cfg, q, self.cu.cuda(), gk.Prefix(**{k: x.cuda() for k, x in self.pre.items()}), part, ws)
+        torch.cuda.synchronize()
+        return part
+
+    def entries(self, s, g):
+        a = int(self.pre["start"][s * self.G + g])
+        e = a + int(self.pre["count"][s * self.G + g])
+        return self.pre["K"][a:e].double(), self.pre["V"][a:e].double(), self.pre["logm"][a:e].double()
+
+    def check(self, part=None):
+        part = part or self.call()
+        o, lse = part.o.cpu(), part.lse.cpu()
+        per, a = self.H // self.G, 0
+        for s, m in enumerate(self.groups):
+            for g in range(self.G):
+                k, v, lm = self.entries(s, g)
+                h = slice(g * per, (g + 1) * per)
+                if m:
+                    got, want = o[a:a + m, h].reshape(m * per, -1), self.q[a:a + m, h].reshape(m * per, -1).double()
+                    S.check_rows(got, lse[a:a + m, h].reshape(-1), S.attend64(want, k, v, bias=lm), max(len(k), 1), self.d,
+                                 self.dtype == "bf16", (self.dtype, self.d, self.G, self.H, s, g))
+            a += m
+        assert (o[a:] == 7).all() and (lse[a:] == 7).all()      # behind the last group
+
+
+def _counts(seed, n, lo, hi):
+    return torch.randint(lo, hi, (n,), generator=torch.Generator().manual_seed(seed)).tolist()
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("G,Hq", HEADS)
+def test_shared(dtype, d, G, Hq):
+    # few and many rows a group (every split of the waves), no entries, one, odd numbers of them
+    for i, (groups, most) in enumerate([([1], 40), ([3, 0, 1], 300), ([16], 131), ([2, 40, 0, 7], 200), ([64], 129), ([5] * 9, 70)]):
+        counts = _counts(i, len(groups) * G, 0, most)
+        counts[0] = [0, 1, 128, 33, 127, 65][i]
+        Shared(dtype, d, G, Hq, groups, counts, behind=i % 2, seed=50 + i).check()
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_shared_every_number_of_entries(dtype, d):
+    for n in (1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257):
+        for rows in (1, 9, 40):
+            Shared(dtype, d, 1, 2, [rows], [n], seed=n).check()
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_shared_long_and_cut(dtype, d):
+    # rows of many chunks, values that rise along the entries: a chunk that is lost or taken twice shows
+    for i, (G, Hq, groups, counts) in enumerate([(1, 4, [1], [30001]), (2, 8, [17], [9000, 4001]), (1, 8, [30], [20011]),
+                                                 (2, 4, [1, 50, 3], [3000, 0, 5000, 20, 1, 8000])]):
+        c = Shared(dtype, d, G, Hq, groups, counts, seed=60 + i)
+        c.pre["V"] += torch.linspace(0, 4, c.pre["V"].shape[0])[:, None].to(c.pre["V"].dtype)
+        c.check()
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("rows", [2, 12, 40])
+def test_shared_masked_entries(dtype, d, rows):
+    # log m = -inf, alone and for whole rows; what is masked or behind the entries holds NaN and infinities
+    for what in ("some", "head", "all"):
+        c = Shared(dtype, d, 2, 6, [rows, 1], [300, 3, 0, 64], seed=6)
+        lm = c.pre["logm"]
+        mask = torch.zeros_like(lm, dtype=torch.bool)
+        mask[{"some": slice(0, None, 3), "head": slice(0, 303), "all": slice(0, None)}[what]] = True
+        mask[-3:] = True
+        lm[mask] = -math.inf
+        c.pre["V"][mask] = math.nan
+        c.pre["K"][mask, ::2] = math.inf
+        c.check()
+        lm[~mask] = torch.finfo(torch.float32).min             # the lowest value: equal weights among themselves
+        if what == "some":
+            o = c.call()
+            assert torch.isfinite(o.o).all()
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_shared_infinite_values_stay_in_their_dimension(dtype, d):
+    for rows in (1, 12, 40):
+        c = Shared(dtype, d, 1, 2, [rows], [150], seed=7)
+        c.pre["V"][77, 5], c.pre["V"][140, d - 1] = math.inf, -math.inf
+        c.check()
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_shared_large_logits(dtype, d):
+    for rows in (1, 12, 40):
+        c = Shared(dtype, d, 1, 2, [rows], [500], seed=8)
+        c.q *= 16
+        c.check()
+
+
+def test_shared_many_units_and_groups():
+    # more (group, KV head) than a wave looks at in one round
+    for B, G in ((65, 1), (40, 2), (300, 3), (1000, 1)):
+        groups = _counts(B, B, 0, 4)
+        Shared("bf16", 64, G, 2 * G, groups, _counts(B + 1, B * G, 0, 90), behind=2, seed=B).check()
+    Shared("f32", 64, 2, 4, _counts(3, 80, 0, 3), _counts(4, 160, 0, 400), seed=9).check()
+
+
+def test_shared_malformed_inputs_stay_inside():
+    for dtype, d in TYPES:
+        c = Shared(dtype, d, 2, 4, [4, 3, 2], [10, 20, 5, 6, 7, 8], seed=9)
+        c.pre["start"][0], c.pre["count"][1], c.pre["count"][2], c.pre["start"][3] = -4, 1 << 40, -3, 1 << 40
+        part = c.call()
+        n = c.pre["K"].shape[0]
+        c.pre["start"].clamp_(0, n)
+        c.pre["count"].clamp_(min=0)
+        c.pre["count"] = torch.minimum(c.pre["count"], n - c.pre["start"])
+        c.check(part)
+        for cu in ([9, 3, 7, 0], [0, 9, 0, 9], [-5, 2 ** 31 - 1, -2 ** 31, 7], [9, 9, 9, 9], [0, 0, 0, 0]):
+            c.cu = torch.tensor(cu, dtype=torch.int32)
+            c.call()
+
+
+def test_shared_entries_of_no_rows():
+    for dtype, d in TYPES:
+        c = Shared(dtype, d, 2, 6, [3, 2], [0] * 4, seed=22)
+        for name in ("K", "V", "logm"):
+            c.pre[name] = c.pre[name][:0]
+        c.check()
+
+
+@pytest.mark.parametrize("fill", [0, 1, 127, 255])
+def test_shared_workspace_needs_no_clearing(fill):
+    a = Shared("bf16", 128, 2, 8, [20, 1], [4001, 3, 0, 900], seed=20)
+    b = Shared("f32", 64, 1, 20, [3] * 40, [60] * 39 + [3000], seed=21)
+    ws = torch.full((256 << 20,), fill, dtype=torch.uint8, device="cuda")
+    first = {}
+    for c in (a, b, a, a, b):
+        part = c.call(ws=ws)
+        c.check(part)
+        was = first.setdefault(id(c), part)
+        assert torch.equal(was.o, part.o) and torch.equal(was.lse, part.lse)       # the same bits again
+
+
+# ---------------------------------------------------------------------------
+# a part joined to pages
+
+
+def _joined(c, sh, out, lse, entries, n_parts, dtype, d):
+    per = c.H // c.G
+    s_of = [s for s, m in enumerate(sh.groups) for _ in range(m)]
+    for b, g in itertools.product(range(len(s_of)), range(c.G)):
+        k, v, lm = entries(b, g)
+        pk, pv, plm = sh.entries(s_of[b], g)
+        k, v, lm = torch.cat([pk, k]), torch.cat([pv, v]), torch.cat([plm, lm])
+        h = slice(g * per, (g + 1) * per)
+        Q.check_joined(out[b, h], lse[b, h], S.attend64(c.q[b, h].double(), k, v, bias=lm), n_parts * max(len(k), 1),
+                       d * (1 if dtype == "bf16" else 3), dtype == "bf16", (dtype, d, b, g))
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("G,Hq", [(2, 8), (1, 17)])
+def test_quantised_pages_joined_to_shared_entries(dtype, d, fmt, G, Hq):
+    groups, lens = [3, 1, 0, 4], [0, 40, 3000, 17, 1, 0, 100, 33]       # a row of several chunks, rows of neither
+    c = Cache(dtype, d, fmt, G, Hq, lens, 16, seed=70)
+    sh = Shared(dtype, d, G, Hq, groups, [700] * G + [0] * G + [5] * G + [33] * G, seed=71)
+    sh.q = c.q
+    out, lse = c.call(part=sh.call())
+    _joined(c, sh, out, lse, c.entries, 3, dtype, d)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_plain_pages_joined_to_shared_entries(dtype, d):
+    G, Hq, groups, lens, page = 2, 8, [2, 3, 1], [0, 2500, 17, 40, 1, 0], 32
+    gen = torch.Generator().manual_seed(72)
+    sh = Shared(dtype, d, G, Hq, groups, [400, 31, 0, 900, 0, 0], seed=73)
+    table, n_pages = _tables(gen, lens, page)
+    K, V = (_rand(gen, n_pages, G, page, d, dtype=dtype) for _ in range(2))
+    cfg = gk.page_config(K, Hq, table)
+    out, lse = torch.empty(6, Hq, d, dtype=DT[dtype], device="cuda"), torch.empty(6, Hq, device="cuda")
+    ws = torch.empty(gk.paged_ws_bytes(cfg), dtype=torch.uint8, device="cuda")
+    own = torch.tensor([20, 0, 5, 64, 1, 0, 33, 100, 0, 7, 0, 0])             # and packed entries of each sequence's own
+    rows = int(own.sum())
+    pre = dict(start=own.cumsum(0) - own, count=own, K=_rand(gen, rows, d, dtype=dtype), V=_rand(gen, rows, d, dtype=dtype),
+               logm=torch.rand(rows, generator=gen))
+
+    def entries(b, g):
+        ids = table[b, :-(-lens[b] // page)].long()
+        k, v = (x[ids, g].reshape(-1, d)[:lens[b]].double() for x in (K, V))
+        lm = torch.zeros(lens[b], dtype=torch.float64)
+        if not packed:
+            return k, v, lm
+        a = int(pre["start"][b * G + g])
+        e = a + int(own[b * G + g])
+        return torch.cat([pre["K"][a:e].double(), k]), torch.cat([pre["V"][a:e].double(), v]), torch.cat([pre["logm"][a:e].double(), lm])
+    for packed in (False, True):
+        gk.paged_attention(cfg, sh.q.cuda(), K.cuda(), V.cuda(), table.cuda(), _i32(*lens), out, ws, lse=lse, part=sh.call(),
+                           prefix=gk.Prefix(**{n: x.cuda() for n, x in pre.items()}) if packed else None)
+        c = type("Rows", (), dict(q=sh.q, H=Hq, G=G))
+        _joined(c, sh, out.cpu(), lse.cpu(), entries, 3, dtype, d)
+
+
+def test_part_without_entries_changes_nothing():
+    # lse = -inf, whatever the mean holds: bit for bit the attention without it
+    for fmt, (dtype, d) in itertools.product(FORMATS, TYPES):
+        c = Cache(dtype, d, fmt, 2, 8, [0, 2000, 33, 1], 16, seed=74)
+        part = gk.Part(torch.full((4, 8, d), math.nan, device="cuda"), torch.full((4, 8), -math.inf, device="cuda"))
+        a, b = c.call(), c.call(part=part)
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+# ---------------------------------------------------------------------------
+# together, as a serving program runs them
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_questions_on_one_compressed_context(fmt):
+    """A cache compressed; several questions on it, each a chunk whose keys go into quantised pages and whose rows
+    come back for its prompt attention; then tokens of every question, attending to the shared entries and their pages."""
+    sh = small_shape("serve", L=1, G=2, H=8, d=128, N_ctx=600, W=24, x=6.0, n_segments=6, dtype="bf16")
+    case = H.to_dev(make_case(sh, 5, with_hidden=True))
+    ccfg = H.make_cfg(sh)
+    buf = gk.allocate(ccfg)
+    gk.compress(buf, case["K"], case["V"], case["Q"], case["rope_cos"], case["rope_sin"], case["hidden"], case["surprisal"], case["omega_raw"])
+    gk.check(ccfg, buf.trees)
+    entries = gk.Prefix(buf.offsets[:sh.G].contiguous(), buf.counts[:sh.G].contiguous(), buf.K_out, buf.V_out, buf.logm_out)
+    gen = torch.Generator().manual_seed(2)
+    lens, steps, d = [33, 7, 50], 3, sh.d
+    B = len(lens)
+    table, n_pages = _tables(gen, [n + steps for n in lens], 16)
+    pages = gk.QuantPages(fmt, *[x.cuda() for x in _pools(gen, n_pages, sh.G, 16, d, fmt)])
+    table = table.cuda()
+    cfg = gk.quant_config(pages, torch.bfloat16, sh.H, table)
+    cos, sin = (x.cuda() for x in _rope(sh.T + 64, d))
+    n = sum(lens)
+    k, v, q = (_rand(gen, n, x, d).cuda() for x in (sh.G, sh.G, sh.H))
+    pos = torch.cat([torch.arange(m) + sh.N_ctx for m in lens]).to(torch.int32).cuda()
+    zero, cu = torch.zeros(B, dtype=torch.int32, device="cuda"), _cu(lens).cuda()
+    qr = torch.empty_like(q)
+    gk.quant_append(cfg, pages, k, v, table, zero, cu, pos, cos, sin, q, qr)
+    kb, vb = torch.empty_like(k), torch.empty_like(v)
+    gk.quant_read(cfg, pages, table, zero, cu, kb, vb)
+    held = {b: [x[int(cu[b]):int(cu[b + 1])].cpu().double() for x in (kb, vb)] for b in range(B)}
+    c, s = Q.quantise(Q.rotated32(k.cpu(), cos.cpu()[pos.cpu().long()], sin.cpu()[pos.cpu().long()]).double(), fmt)
+    assert torch.equal(kb.cpu().double(), Q.values(Q.packed(c, fmt), s, fmt))
+    out, lse = torch.empty_like(q), torch.empty(n, sh.H, device="cuda")
+    pcfg = gk.prompt_config(qr, kb, vb, out, B)
+    pws = torch.empty(max(gk.prompt_ws_bytes(pcfg), 1), dtype=torch.uint8, device="cuda")
+    gk.prompt_attention(pcfg, qr, kb, vb, cu, cu, out, pws, lse=lse)
+    S.prompt64(qr.cpu().double(), kb.cpu().double(), vb.cpu().double(), lens, lens,
+               lambda rows, h, ref, m: S.check_rows(out[rows, h].cpu(), lse[rows, h].cpu(), ref, m, d, True, h))
+    scfg = gk.shared_config(torch.empty(B, sh.H, d, dtype=torch.bfloat16, device="cuda"), sh.G, 1)
+    sws = torch.empty(gk.shared_ws_bytes(scfg), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(gk.paged_ws_bytes(cfg), dtype=torch.uint8, device="cuda")
+    part = gk.Part(torch.empty(B, sh.H, d, device="cuda"), torch.empty(B, sh.H, device="cuda"))
+    off, per = buf.offsets.cpu(), sh.H // sh.G
+    for step in range(steps):
+        k, v, q = (_rand(gen, B, x, d).cuda() for x in (sh.G, sh.G, sh.H))
+        at = torch.tensor(lens, dtype=torch.int32).cuda() + step
+        qr, one = torch.empty_like(q), _cu([1] * B).cuda()
+        gk.quant_append(cfg, pages, k, v, table, at, one, at + sh.N_ctx, cos, sin, q, qr)
+        gk.shared_attention(scfg, qr, _i32(0, B), entries, part, sws)
+        out, lse = torch.empty_like(q), torch.empty(B, sh.H, device="cuda")
+        gk.quant_attention(cfg, pages, qr, table, at + 1, out, ws, lse=lse, part=part)
+        kb, vb = torch.empty_like(k), torch.empty_like(v)
+        gk.quant_read(cfg, pages, table, at, one, kb, vb)
+        for b, g in itertools.product(range(B), range(sh.G)):
+            if g == 0:
+                held[b] = [torch.cat([x, y[b:b + 1].cpu().double()]) for x, y in zip(held[b], (kb, vb))]
+            a, e = int(off[g]), int(off[g + 1])
+            kk, vv = (torch.cat([x[a:e].cpu().double(), y[:, g]]) for x, y in zip((buf.K_out, buf.V_out), held[b]))
+            lm = torch.cat([buf.logm_out[a:e].cpu().double(), torch.zeros(len(held[b][0]), dtype=torch.float64)])
+            h = slice(g * per, g * per + per)
+            Q.check_joined(out[b, h].cpu(), lse[b, h].cpu(), S.attend64(qr[b, h].cpu().double(), kk, vv, bias=lm), 2 * len(kk), d, True, (step, b, g))
+
+
+class Step:
+    """Append, shared entries and attention of a batch's next tokens, on the GPU."""
+
+    def __init__(self, dtype, d, fmt, groups, seed):
+        gen = torch.Generator().manual_seed(seed)
+        lens = torch.randint(1, 300, (sum(groups),), generator=gen).tolist()
+        lens[0] = 2000
+        self.c = Cache(dtype, d, fmt, 2, 8, lens, 16, seed=seed)
+        self.s = Shared(dtype, d, 2, 8, groups, _counts(seed, 2 * len(groups), 0, 900), seed=seed + 1)
+        self.s.q = self.c.q
+        self.pages, self.table, self.cfg = self.c.on_gpu()
+        B = len(lens)
+        self.q, self.len, self.cu = self.c.q.cuda(), self.c.len.cuda(), self.s.cu.cuda()
+        self.k, self.v = (_rand(gen, B, 2, d, dtype=dtype).cuda() for _ in range(2))
+        self.pos, self.one, (self.cos, self.sin) = torch.arange(B, dtype=torch.int32).cuda(), _cu([1] * B).cuda(), (x.cuda() for x in _rope(600, d))
+        self.start = (self.len - 1).contiguous()
+        self.pre = gk.Prefix(**{n: x.cuda() for n, x in self.s.pre.items()})
+        self.scfg = gk.shared_config(self.q, 2, len(groups))
+        self.fresh()
+
+    def fresh(self):
+        self.qr, self.out, self.lse = torch.zeros_like(self.q), torch.zeros_like(self.q), torch.zeros(self.q.shape[:2], device="cuda")
+        self.part = gk.Part(torch.zeros(self.q.shape, device="cuda"), torch.zeros(self.q.shape[:2], device="cuda"))
+        self.ws = torch.empty(gk.paged_ws_bytes(self.cfg), dtype=torch.uint8, device="cuda")
+        self.sws = torch.empty(gk.shared_ws_bytes(self.scfg), dtype=torch.uint8, device="cuda")
+        self.back = [torch.zeros_like(self.k) for _ in range(2)]
+
+    def run(self, stream=None):
+        gk.quant_append(self.cfg, self.pages, self.k, self.v, self.table, self.start, self.one, self.pos, self.cos, self.sin, self.q, self.qr, stream=stream)
+        gk.shared_attention(self.scfg, self.qr, self.cu, self.pre, self.part, self.sws, stream=stream)
+        gk.quant_attention(self.cfg, self.pages, self.qr, self.table, self.len, self.out, self.ws, lse=self.lse, part=self.part, stream=stream)
+        gk.quant_read(self.cfg, self.pages, self.table, self.start, self.one, *self.back, stream=stream)
+
+    def results(self):
+        return [self.out, self.lse, self.qr, self.part.o, self.part.lse, *self.back, self.pages.K, self.pages.V, self.pages.K_scale, self.pages.V_scale]
+
+
+@pytest.mark.parametrize("dtype,d,fmt", [("bf16", 128, gk.E4M3), ("f32", 64, gk.E2M1)])
+def test_step_captured_and_replayed(dtype, d, fmt):
+    a = Step(dtype, d, fmt, [3, 9, 0, 1], 80)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        a.run()
+    gen = torch.Generator().manual_seed(6)
+    for i in range(5):
+        a.k.copy_(_rand(gen, *a.k.shape, dtype=dtype))
+        a.q.copy_(_rand(gen, *a.q.shape, dtype=dtype))
+        a.len.copy_(torch.randint(1, a.table.shape[1] * 16, a.len.shape, generator=gen).to(torch.int32).cuda().minimum(a.c.len.cuda()))
+        a.start.copy_(a.len - 1)
+        a.cu.copy_(_cu([[3, 9, 0, 1], [13, 0, 0, 0], [1, 1, 1, 10], [0, 0, 13, 0], [4, 4, 4, 1]][i]))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [x.clone() for x in a.results()]
+        for x in (a.out, a.lse, a.qr, a.part.o, a.part.lse):
+            x.zero_()
+        with torch.cuda.stream(side):                            # eager, on the side stream
+            a.run()
+        side.synchronize()
+        for x, y in zip(got, a.results()):
+            assert torch.equal(x, y)
+
+
+def test_two_graphs_in_turn_on_one_workspace():
+    a, b = Step("bf16", 128, gk.E4M3, [20, 2], 81), Step("f32", 64, gk.E2M1, [1, 1, 3], 82)
+    for name in ("ws", "sws"):
+        size = max(getattr(x, name).numel() for x in (a, b))
+        a.__dict__[name] = b.__dict__[name] = torch.full((size,), 255, dtype=torch.uint8, device="cuda")
+    want, graphs, side = [], [], torch.cuda.Stream()
+    for x in (a, b):
+        x.run()
+        torch.cuda.synchronize()
+        want.append([y.clone() for y in x.results()])
+        side.wait_stream(torch.cuda.current_stream())
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=side):
+            x.run()
+    for _ in range(4):
+        for x, graph in zip((a, b), graphs):
+            x.out.fill_(7.0)
+            graph.replay()
+        torch.cuda.synchronize()
+        for x, w in zip((a, b), want):
+            for y, z in zip(x.results(), w):
+                assert torch.equal(y, z)
+
+
+def test_calls_at_once_on_two_streams():
+    a, b = Step("bf16", 128, gk.E4M3, [20, 2], 83), Step("bf16", 128, gk.E4M3, [20, 2], 83)
+    c = Step("bf16", 128, gk.E4M3, [20, 2], 83)
+    c.run()
+    sides = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for x, stream in zip((a, b), sides):
+            x.run(stream)
+    torch.cuda.synchronize()
+    for x in (a, b):
+        for y, z in zip(x.results(), c.results()):
+            assert torch.equal(y, z)
