@@ -521,48 +521,58 @@ def paged_attention(cfg: PageConfig, q, K_pages, V_pages, block_table, seq_len, 
         "paged_attention")
 
 
-@dataclasses.dataclass
+@dataclasses.dataclass(frozen=True)
 class QuantPages:
     """Quantised pages of one layer (gracekv_quant_pages): codes K, V uint8 [n_pages][G][page_size][d]
     (E4M3) or [..][d / 2] (E2M1), scales K_scale, V_scale uint8 [n_pages][G][page_size][d / 32]; pages
-    any distance apart, the same for K and V, each contiguous."""
+    any distance apart, the same for K and V, each contiguous.  Looked over once, when it is
+    made; it holds the four tensors, which stay where they are."""
     format: int
     K: torch.Tensor
     V: torch.Tensor
     K_scale: torch.Tensor
     V_scale: torch.Tensor
 
+    def __post_init__(self):
+        if self.format not in (E4M3, E2M1):
+            raise ValueError(f"format: got {self.format}, need E4M3 or E2M1")
+        if self.K.dim() != 4 or self.K_scale.dim() != 4:
+            raise ValueError(f"need [n_pages][G][page_size][bytes], got {tuple(self.K.shape)}, {tuple(self.K_scale.shape)}")
+        each, dev, u8 = (1 if self.format == E4M3 else 2), self.K.get_device(), torch.uint8
+        n, G, page, row = self.K.shape
+        d = row * each
+        far, scale_far = (self.K.stride(0), self.K_scale.stride(0)) if n > 1 else (G * page * row, G * page * (d // 32))
+        for names, width, apart in ((("K", "V"), row, far), (("K_scale", "V_scale"), d // 32, scale_far)):
+            shape, strides = (n, G, page, width), (apart, page * width, width, 1)
+            for name in names:
+                x = getattr(self, name)
+                if x.dtype is not u8 or x.shape != shape or x.get_device() != dev:
+                    _refuse(name, x, u8, shape, dev, strides)
+                if any(k > 1 and a != b for k, a, b in zip(shape, x.stride(), strides)):
+                    raise ValueError(f"{name}: strides {x.stride()}, need {strides}")
+        held = object.__setattr__
+        held(self, "device", dev)
+        held(self, "shape", (n, G, page, d, far * each))
+        held(self, "arrays", QuantArrays(self.format, 0, scale_far, *(x.data_ptr() for x in (self.K, self.V, self.K_scale, self.V_scale))))
+
 
 def quant_config(pages: QuantPages, dtype: torch.dtype, H: int, block_table) -> PageConfig:
     """The shapes of a quantised paged cache with rows of ``dtype`` around it (torch.bfloat16 or
     torch.float32), block_table [n_seq][table_width] int32, H query heads."""
-    K = pages.K
-    if pages.format not in (E4M3, E2M1):
-        raise ValueError(f"format: got {pages.format}, need E4M3 or E2M1")
-    if K.dim() != 4 or block_table.dim() != 2:
-        raise ValueError(f"need [n_pages][G][page_size][bytes] and [n_seq][table_width], got {tuple(K.shape)}, {tuple(block_table.shape)}")
+    if block_table.dim() != 2:
+        raise ValueError(f"block_table: need [n_seq][table_width], got {tuple(block_table.shape)}")
     if dtype not in _DTYPE:
         raise ValueError(f"dtype: got {dtype}, need one of {list(_DTYPE)}")
-    n, G, page, row = K.shape
-    each = 1 if pages.format == E4M3 else 2             # codes of a byte
-    far = (K.stride(0) if n > 1 else G * page * row) * each
-    return PageConfig(_DTYPE[dtype], G, H, row * each, block_table.shape[0], page, block_table.shape[1], 0, n, far)
+    n, G, page, d, far = pages.shape
+    return PageConfig(_DTYPE[dtype], G, H, d, block_table.shape[0], page, block_table.shape[1], 0, n, far)
 
 
 def _quantised(cfg: PageConfig, p: QuantPages, dev: int):
-    """The pools of a quantised cache, all four alike."""
-    each = 1 if p.format == E4M3 else 2
-    n, G, page, d, u8 = cfg.n_pages, cfg.G, cfg.page_size, cfg.d, torch.uint8
-    scale_far = p.K_scale.stride(0) if n > 1 else G * page * (d // 32)
-    for names, row, far in ((("K", "V"), d // each, cfg.page_stride // each), (("K_scale", "V_scale"), d // 32, scale_far)):
-        shape, strides = (n, G, page, row), (far, page * row, row, 1)
-        for name in names:
-            x = getattr(p, name)
-            if x.dtype is not u8 or x.shape != shape or x.get_device() != dev:
-                _refuse(name, x, u8, shape, dev, strides)
-            if x.stride() != strides and any(k > 1 and a != b for k, a, b in zip(shape, x.stride(), strides)):
-                raise ValueError(f"{name}: strides {x.stride()}, need {strides}")
-    return ctypes.byref(QuantArrays(p.format, 0, scale_far, p.K.data_ptr(), p.V.data_ptr(), p.K_scale.data_ptr(), p.V_scale.data_ptr()))
+    """The pools of a quantised cache of these shapes on device ``dev``."""
+    if p.device != dev or p.shape != (cfg.n_pages, cfg.G, cfg.page_size, cfg.d, cfg.page_stride):
+        raise ValueError(f"pages: got (n_pages, G, page_size, d, page_stride) {p.shape} on device {p.device}, need "
+                         f"{(cfg.n_pages, cfg.G, cfg.page_size, cfg.d, cfg.page_stride)} on the current device cuda:{dev}")
+    return ctypes.byref(p.arrays)
 
 
 def quant_append(cfg: PageConfig, pages: QuantPages, k, v, block_table, start, cu_new, pos=None, rope_cos=None, rope_sin=None,

@@ -247,11 +247,20 @@ def test_binding_refuses_other_tensors(monkeypatch):
     cfg = gk.quant_config(pages, torch.float32, 4, table)
     assert (cfg.d, cfg.G, cfg.H, cfg.page_size, cfg.page_stride) == (64, 2, 4, 16, 2048)
     with pytest.raises(ValueError, match="format"):
-        gk.quant_config(gk.QuantPages(7, *[pages.K] * 4), torch.float32, 4, table)
+        gk.QuantPages(7, *[pages.K] * 4)
+    with pytest.raises(ValueError, match="page_size"):
+        gk.QuantPages(gk.E4M3, *[u8(3, 2, 64)] * 4)
+    for name, x in (("K", u8(3, 2, 16, 64)), ("V", u8(2, 2, 16, 32)), ("K_scale", u8(3, 2, 16, 4)),
+                    ("V_scale", torch.zeros(3, 2, 16, 2, dtype=torch.int8)), ("V", u8(6, 2, 16, 32)[::2]),
+                    ("V_scale", u8(6, 2, 16, 2)[::2]), ("K_scale", u8(3, 2, 2, 16).transpose(2, 3))):
+        with pytest.raises(ValueError, match="K_scale|V" if name == "K" else name):
+            gk.QuantPages(**{f: x if f == name else getattr(pages, f) for f in ("format", "K", "V", "K_scale", "V_scale")})
+    with pytest.raises(AttributeError):                          # the tensors are looked over once
+        pages.K = u8(3, 2, 16, 32)
     with pytest.raises(ValueError, match="float16"):
         gk.quant_config(pages, torch.float16, 4, table)
-    with pytest.raises(ValueError, match="page_size"):
-        gk.quant_config(gk.QuantPages(gk.E4M3, *[u8(3, 2, 64)] * 4), torch.float32, 4, table)
+    with pytest.raises(ValueError, match="table_width"):
+        gk.quant_config(pages, torch.float32, 4, table[0])
     q, kv, i = torch.zeros(1, 4, 64), torch.zeros(1, 2, 64), torch.zeros(1, dtype=torch.int32)
     cu = torch.zeros(2, dtype=torch.int32)
     with pytest.raises(ValueError, match="on cpu"):              # no copies behind the caller's back
@@ -261,12 +270,12 @@ def test_binding_refuses_other_tensors(monkeypatch):
     with pytest.raises(ValueError, match="on cpu"):
         gk.quant_attention(cfg, pages, q, table, i, q, None)
     monkeypatch.setattr(torch.Tensor, "get_device", lambda self: 0)
-    for name, x in (("K", u8(3, 2, 16, 64)), ("V", u8(2, 2, 16, 32)), ("K_scale", u8(3, 2, 16, 4)),
-                    ("V_scale", torch.zeros(3, 2, 16, 2, dtype=torch.int8)), ("V", u8(6, 2, 16, 32)[::2]),
-                    ("V_scale", u8(6, 2, 16, 2)[::2]), ("K_scale", u8(3, 2, 2, 16).transpose(2, 3))):
-        other = gk.QuantPages(**dict(pages.__dict__, **{name: x}))
-        with pytest.raises(ValueError, match=name):
-            gk.quant_attention(cfg, other, q, table, i, q, None)
+    with pytest.raises(ValueError, match="on device -1"):
+        gk.quant_attention(cfg, pages, q, table, i, q, None)
+    four = gk.QuantPages(gk.E2M1, *[torch.cat([x, x[:1]]) for x in (pages.K, pages.V, pages.K_scale, pages.V_scale)])
+    with pytest.raises(ValueError, match="n_pages"):             # another cache's shapes
+        gk.quant_attention(cfg, four, q, table, i, q, None)
+    pages = gk.QuantPages(gk.E2M1, pages.K, pages.V, pages.K_scale, pages.V_scale)
     part = gk.Part(torch.zeros(1, 4, 64), torch.zeros(1, 3))
     with pytest.raises(ValueError, match="part.lse"):
         gk.quant_attention(cfg, pages, q, table, i, q, None, part=part)
