@@ -345,7 +345,7 @@ __global__ __launch_bounds__(PA_T, PA_OCC) void k_paged(PageDims pg, int64_t q_t
           *(float4*)&sO[w][i16][64 * p + VD * (4 * g4 + r) + j] = make_float4(o[p][j][r], o[p][j + 1][r], o[p][j + 2][r], o[p][j + 3][r]);
   }
   sync_after_lds_stores();
-  finish_row<T, D>(pg, ck, ws, part, bid, group, groups, sM, sL, sO, out, lse);
+  finish_row<T, D, false, PA_JOIN>(pg, ck, ws, part, bid, group, groups, sM, sL, sO, out, lse);
 }
 
 hipError_t launch_paged(const PageDims& pg, int64_t q_tok, const void* q, const void* Kp, const void* Vp,

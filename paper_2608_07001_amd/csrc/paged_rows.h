@@ -52,14 +52,19 @@ static inline PagedWs paged_view(void* base, const PageDims& pg) {
 // chunks of a row 20 us, one after the other.)
 constexpr unsigned long long PA_BASE = 0x7fffffffffff0000ull;
 static_assert(PA_TARGET <= 0xfff, "the words that the header excludes");
-__device__ __forceinline__ bool last_of(unsigned long long* word, int parts) {
+// RAISED: raise() came before, by the same thread
+__device__ __forceinline__ void raise(unsigned long long* word) {
+  __hip_atomic_fetch_max(word, PA_BASE, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <bool RAISED> __device__ __forceinline__ bool last_of(unsigned long long* word, int parts) {
   const unsigned long long end = PA_BASE + parts - 1;
   unsigned long long was;
-  do {
-    __hip_atomic_fetch_max(word, PA_BASE, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (!RAISED) raise(word);
+  for (;;) {
     was = __builtin_amdgcn_atomic_inc64((unsigned long*)word, end, __ATOMIC_RELAXED, "agent");
-  } while (was > end || was < PA_BASE);       // below: put to 0 by another between the two steps
-  return was == end;
+    if (was <= end && was >= PA_BASE) return was == end;
+    raise(word);                              // below: put to 0 by another between the two steps
+  }
 }
 // the thread's stores are where every other workgroup sees them
 __device__ __forceinline__ void stores_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
@@ -188,7 +193,7 @@ __device__ __forceinline__ bool find_chunk(const PageDims& pg, const PrefixView&
 // result where the chunk is all of it, else left in the workspace, for the last of the row's
 // chunks to join.  `part` (o not null): an attention of the same queries over other entries,
 // joined to the row's as a state of its own, maximum lse, sum 1 and its mean.
-template <typename T, int D>
+template <typename T, int D, bool RAISED, int JOIN>
 __device__ __forceinline__ void finish_row(const PageDims& pg, const Chunk& ck, const PagedWs& ws, const PartView& part, int bid,
                                            int group, int groups, const float (*sM)[PA_HEADS], const float (*sL)[PA_HEADS],
                                            const float (*sO)[PA_HEADS][D + 4], T* __restrict__ out, float* __restrict__ lse) {
@@ -234,7 +239,7 @@ __device__ __forceinline__ void finish_row(const PageDims& pg, const Chunk& ck, 
   if (ck.chunks == 1) return;
   stores_done();
   __syncthreads();
-  if (tid == 0) joins = last_of(ws.ticket + row * groups + group, ck.chunks);
+  if (tid == 0) joins = last_of<RAISED>(ws.ticket + row * groups + group, ck.chunks);
   sync_after_lds_stores();
   if (!joins) return;
   // A head's pairs of dims lie on LH neighbouring lanes, which hold the (max, sum) of LH
@@ -248,10 +253,10 @@ __device__ __forceinline__ void finish_row(const PageDims& pg, const Chunk& ck, 
       const int nb = min(ck.chunks - b0, LH);
       const unsigned long long* src = (const unsigned long long*)(ws.o + (base + (int64_t)b0 * pg.hpg + h) * D + dd);
       const int64_t step = (int64_t)pg.hpg * LH;
-      unsigned long long ov[PA_JOIN];
+      unsigned long long ov[JOIN];
       auto load = [&](int c0) {                 // past the last: that one again
 #pragma unroll
-        for (int c = 0; c < PA_JOIN; ++c) ov[c] = ld_agent(src + min(c0 + c, nb - 1) * step);
+        for (int c = 0; c < JOIN; ++c) ov[c] = ld_agent(src + min(c0 + c, nb - 1) * step);
       };
       float2 ml = make_float2(-INFINITY, 0.f);
       if (sub < nb) ml = pair_of(ld_agent(ws.ml + base + (int64_t)(b0 + sub) * pg.hpg + h));
@@ -264,10 +269,10 @@ __device__ __forceinline__ void finish_row(const PageDims& pg, const Chunk& ck, 
 #pragma unroll
       for (int o = LH / 2; o > 0; o >>= 1) sb += __shfl_xor(sb, o, 64);
       float a0 = 0.f, a1 = 0.f;
-      for (int c0 = 0; c0 < nb; c0 += PA_JOIN) {
+      for (int c0 = 0; c0 < nb; c0 += JOIN) {
         if (c0) load(c0);
 #pragma unroll
-        for (int c = 0; c < PA_JOIN; ++c) {
+        for (int c = 0; c < JOIN; ++c) {
           const float g = c0 + c < nb ? __shfl(f, (tid & 63 & ~(LH - 1)) + c0 + c, 64) : 0.f;
           const float2 v = pair_of(ov[c]);
           a0 += g == 0.f ? 0.f : v.x * g;

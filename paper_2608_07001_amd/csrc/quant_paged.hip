@@ -21,11 +21,27 @@
 
 namespace gkv {
 
+#ifndef QP_JOIN
+#define QP_JOIN 8
+#endif
+#ifndef QP_FEW
+#define QP_FEW 768
+#define QP_MANY 1536
+#endif
+#ifndef QP_OCC
+#define QP_OCC 3
+#endif
+
 // a float's upper 16 bits and what is left
 __device__ __forceinline__ float upper(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
 // the upper 16 bits of two floats, low half first
 __device__ __forceinline__ uint32_t uppers(float a, float b) {
   return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+}
+
+// the value of one lane of the quad
+template <int CTRL> __device__ __forceinline__ float quad_of(float x) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xf, 0xf, true));
 }
 
 template <typename T, int D, int FMT, int OCC>
@@ -54,10 +70,10 @@ __global__ __launch_bounds__(PA_T, OCC) void k_quant_paged(PageDims pg, QuantDim
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i16 = lane & 15, g4 = lane >> 4;
   const int h0 = group * PA_HEADS, heads = min(PA_HEADS, pg.hpg - h0);
   constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
-  const float scale = 1.0f / sqrtf((float)D);
+  const float scale = 1.0f / sqrtf((float)D), sc2 = scale * LOG2E;
+  constexpr float LAG = 8.f;
   const int seq = ck.b, kv = ck.g;
   const int64_t n_page = held_len(pg, len[seq]);
-
   // the lane's dims of product s: the eight from 4 PD (s / (PD / 8)) + PD g4 + 8 (s % (PD / 8)) on
   uint4 qv[QP][KS];
 #pragma unroll
@@ -80,35 +96,49 @@ __global__ __launch_bounds__(PA_T, OCC) void k_quant_paged(PageDims pg, QuantDim
     }
   }
 
-  // One tile's codes and scales (a key's SB bytes; those of the lane's four value rows of a half)
+  // One tile's codes and scales.  Row j of a product's 16 is entry j / 4 + 4 (j % 4) of a half, so that the
+  // lanes of the four value rows r of a lane, entries g4 + 4 r, lie side by side: a load of values is one
+  // piece of memory, not four.  A quad of lanes has the scales of its lane group's four rows, one each.
   uint32_t tk[NS][KP][PB / 4], tv[NS][4][VW];
-  uint32_t sk[NS], sv[NS][SB];
+  uint32_t sk[NS], sv[NS];
   struct Where {                  // of a tile, the same for the wave: bytes, entries there are
     int64_t at[NS], sc[NS];
     int n[NS];
   };
+  // The page ids of a tile are asked for a tile earlier still: they would stand in front of its loads
   const int32_t* tab = table + (int64_t)seq * pg.width;
-  auto where = [&](int ti) __attribute__((always_inline)) {
+  struct Ids {
+    int id[NS];
+  };
+  auto pages_of = [&](int ti) __attribute__((always_inline)) {
+    Ids r;
+#pragma unroll
+    for (int h = 0; h < NS; ++h) {
+      const int64_t e = (int64_t)ti * TILE + 16 * h;
+      r.id[h] = e < n_page ? tab[e >> pg.shift] : -1;
+    }
+    return r;
+  };
+  auto where = [&](int ti, const Ids& ids) __attribute__((always_inline)) {
     Where r;
 #pragma unroll
     for (int h = 0; h < NS; ++h) {
       const int64_t e = (int64_t)ti * TILE + 16 * h;
       int64_t left = n_page - e;
       r.at[h] = r.sc[h] = 0;
-      if (left > 0) {
-        const int64_t id = tab[e >> pg.shift];
-        if (id < 0 || id >= pg.n_pages) {
-          left = 0;
-        } else {
-          const int at = (int)(e & (((int64_t)1 << pg.shift) - 1));
-          r.at[h] = code_row<FMT>(pg, qd, id, kv, at);
-          r.sc[h] = scale_row(pg, qd, id, kv, at);
-        }
+      const int64_t id = ids.id[h];
+      if (id < 0 || id >= pg.n_pages) {
+        left = 0;
+      } else {
+        const int at = (int)(e & (((int64_t)1 << pg.shift) - 1));
+        r.at[h] = code_row<FMT>(pg, qd, id, kv, at);
+        r.sc[h] = scale_row(pg, qd, id, kv, at);
       }
       r.n[h] = left > 16 ? 16 : (left < 0 ? 0 : (int)left);
     }
     return r;
   };
+  const int row_j = (i16 >> 2) + 4 * (i16 & 3), row_s = g4 + 4 * (i16 & 3);
   // a page holds all 16 rows, written or not
   auto load_keys = [&](const Where& t) __attribute__((always_inline)) {
 #pragma unroll
@@ -121,8 +151,8 @@ __global__ __launch_bounds__(PA_T, OCC) void k_quant_paged(PageDims pg, QuantDim
       if (t.n[h] == 0) continue;
       const uint8_t* base = qd.K + t.at[h];
 #pragma unroll
-      for (int p = 0; p < KP; ++p) __builtin_memcpy(tk[h][p], __builtin_assume_aligned(base + (i16 * RB + PB * g4) + 4 * PB * p, PB), PB);
-      const uint8_t* s = qd.Ks + t.sc[h] + SB * i16;
+      for (int p = 0; p < KP; ++p) __builtin_memcpy(tk[h][p], __builtin_assume_aligned(base + (row_j * RB + PB * g4) + 4 * PB * p, PB), PB);
+      const uint8_t* s = qd.Ks + t.sc[h] + SB * row_j;
       sk[h] = SB == 4 ? *(const uint32_t*)s : *(const uint16_t*)s;
     }
   };
@@ -133,18 +163,18 @@ __global__ __launch_bounds__(PA_T, OCC) void k_quant_paged(PageDims pg, QuantDim
       for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int x = 0; x < VW; ++x) tv[h][r][x] = 0;
-#pragma unroll
-      for (int x = 0; x < SB; ++x) sv[h][x] = 0;
+      sv[h] = 0;
       if (t.n[h] == 0) continue;
       const uint8_t* base = qd.V + t.at[h];
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const uint8_t* x = base + ((4 * g4 + r) * RB + VB * i16);
+        const uint8_t* x = base + ((g4 + 4 * r) * RB + VB * i16);
         if constexpr (VB == 8) __builtin_memcpy(tv[h][r], __builtin_assume_aligned(x, 8), 8);
         else if constexpr (VB == 4) tv[h][r][0] = *(const uint32_t*)x;
         else tv[h][r][0] = *(const uint16_t*)x;
       }
-      __builtin_memcpy(sv[h], __builtin_assume_aligned(qd.Vs + t.sc[h] + 4 * SB * g4, 4 * SB), 4 * SB);
+      const uint8_t* s = qd.Vs + t.sc[h] + SB * row_s;
+      sv[h] = SB == 4 ? *(const uint32_t*)s : *(const uint16_t*)s;
     }
   };
 
@@ -155,14 +185,19 @@ __global__ __launch_bounds__(PA_T, OCC) void k_quant_paged(PageDims pg, QuantDim
 
   int ti = ck.t0 + w;
   Where now{}, next{};
+  Ids ids{};
   if (ti < ck.t1) {
-    now = where(ti);
+    now = where(ti, pages_of(ti));
+    ids = pages_of(min(ti + PA_W, ck.t1 - 1));
     load_keys(now);
     load_values(now);
   }
   for (; ti < ck.t1; ti += PA_W) {
     const bool more = ti + PA_W < ck.t1;
-    if (more) next = where(ti + PA_W);
+    if (more) {
+      next = where(ti + PA_W, ids);
+      ids = pages_of(min(ti + 2 * PA_W, ck.t1 - 1));
+    }
     float x[NS][4];
 #pragma unroll
     for (int h = 0; h < NS; ++h) {
@@ -178,7 +213,7 @@ __global__ __launch_bounds__(PA_T, OCC) void k_quant_paged(PageDims pg, QuantDim
         for (int y = QP - 1; y >= 0; --y) acc = mfma_bf16_16x16x32(k8, pk8(qv[y][s]), acc);
       }
 #pragma unroll
-      for (int r = 0; r < 4; ++r) x[h][r] = acc[r] * scale;
+      for (int r = 0; r < 4; ++r) x[h][r] = BF ? acc[r] : acc[r] * scale;
     }
     if (more) load_keys(next);
     bool all = true;
@@ -186,16 +221,16 @@ __global__ __launch_bounds__(PA_T, OCC) void k_quant_paged(PageDims pg, QuantDim
     for (int h = 0; h < NS; ++h) all &= now.n[h] == 16;
     if (!all) {                   // absent entries: no weight, and values that are 0 whatever they hold
 #pragma unroll
-      for (int h = 0; h < NS; ++h)
+      for (int h = 0; h < NS; ++h) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const bool none = 4 * g4 + r >= now.n[h];
+          const bool none = g4 + 4 * r >= now.n[h];
           x[h][r] = none ? -INFINITY : x[h][r];
 #pragma unroll
           for (int i = 0; i < VW; ++i) tv[h][r][i] = none ? 0 : tv[h][r][i];
-          if constexpr (SB == 4) sv[h][r] = none ? 0 : sv[h][r];
-          else if (none) sv[h][r / 2] &= r & 1 ? 0xffffu : 0xffff0000u;
         }
+        sv[h] = row_s >= now.n[h] ? 0 : sv[h];
+      }
     }
     float mx = x[0][0];
 #pragma unroll
@@ -208,9 +243,13 @@ __global__ __launch_bounds__(PA_T, OCC) void k_quant_paged(PageDims pg, QuantDim
       const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
       mx = fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
     }
+    // bf16 rows: base-2 units from here, formed with the exponent's argument in one step, and what is
+    // subtracted stands LAG above a maximum that may lag behind by as much, so that sums are
+    // rescaled seldom (no weight is above 1, the row's largest at least 2^-LAG)
+    if constexpr (BF) mx *= sc2;
     if (__any(mx > m)) {
-      const float mn = fmaxf(m, mx);
-      const float c = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - mn) * LOG2E);
+      const float mn = BF ? fmaxf(m, mx + LAG) : fmaxf(m, mx);
+      const float c = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(BF ? m - mn : (m - mn) * LOG2E);
       m = mn;
       l *= c;
 #pragma unroll
@@ -224,10 +263,14 @@ __global__ __launch_bounds__(PA_T, OCC) void k_quant_paged(PageDims pg, QuantDim
       for (int h = 0; h < NS; ++h)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const float y = (x[h][r] - ms) * LOG2E;
-          pr[h][r] = __builtin_amdgcn_exp2f(y);
-          // fp32: what the product lost, to first order
-          if (!BF && pr[h][r] > 0.f) pr[h][r] = __builtin_fmaf(pr[h][r], __builtin_fmaf(x[h][r] - ms, LOG2E, -y) * LN2, pr[h][r]);
+          if constexpr (BF) {
+            pr[h][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[h][r], sc2, -ms));
+          } else {
+            const float y = (x[h][r] - ms) * LOG2E;
+            pr[h][r] = __builtin_amdgcn_exp2f(y);
+            // what the product lost, to first order
+            if (pr[h][r] > 0.f) pr[h][r] = __builtin_fmaf(pr[h][r], __builtin_fmaf(x[h][r] - ms, LOG2E, -y) * LN2, pr[h][r]);
+          }
           l += pr[h][r];
         }
 #pragma unroll
@@ -246,20 +289,25 @@ __global__ __launch_bounds__(PA_T, OCC) void k_quant_paged(PageDims pg, QuantDim
     // values of the lane's eight rows as bf16 pairs of neighbouring dims
     uint32_t vv[NS][4][VD / 2];
 #pragma unroll
-    for (int h = 0; h < NS; ++h)
+    for (int h = 0; h < NS; ++h) {
+      // a quad's lanes have dims of one block
+      const float own = scale_of((sv[h] >> (8 * (uint32_t)(VD * i16 / Q_BLOCK))) & 255u);
+      float f[4];
+      f[0] = quad_of<0x00>(own);
+      f[1] = quad_of<0x55>(own);
+      f[2] = quad_of<0xAA>(own);
+      f[3] = quad_of<0xFF>(own);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const uint32_t blk = (uint32_t)(VD * i16) / Q_BLOCK;
-        const uint32_t sw = SB == 4 ? sv[h][r] : sv[h][r / 2] >> (16 * (r & 1));
-        const float f = scale_of((sw >> (8 * blk)) & 255u);
         if constexpr (VD == 8) {
-          const uint4 u = eight_bf16<FMT>(tv[h][r], f);
+          const uint4 u = eight_bf16<FMT>(tv[h][r], f[r]);
           vv[h][r][0] = u.x; vv[h][r][1] = u.y; vv[h][r][2] = u.z; vv[h][r][3] = u.w;
         } else {
-          vv[h][r][0] = pair_bf16<FMT, 0>(tv[h][r][0], f);
-          vv[h][r][1] = pair_bf16<FMT, 1>(tv[h][r][0], f);
+          vv[h][r][0] = pair_bf16<FMT, 0>(tv[h][r][0], f[r]);
+          vv[h][r][1] = pair_bf16<FMT, 1>(tv[h][r][0], f[r]);
         }
       }
+    }
     if (more) load_values(next);
 #pragma unroll
     for (int j = 0; j < VD; ++j) {
@@ -275,11 +323,13 @@ __global__ __launch_bounds__(PA_T, OCC) void k_quant_paged(PageDims pg, QuantDim
     }
     if (more) now = next;
   }
+  // the row's ticket word is made ready now, for its chunks to count themselves in one step
+  if (ck.chunks > 1 && tid == 0) raise(ws.ticket + ((int64_t)seq * pg.G + kv) * groups + group);
 #pragma unroll
   for (int j = 0; j < VD; ++j) mfma_done(o[j]);
   l = col_sum4(l);
   // row 4 g4 + r of product j is dimension VD (4 g4 + r) + j, column i16 the head
-  if (g4 == 0) { sM[w][i16] = m; sL[w][i16] = l; }
+  if (g4 == 0) { sM[w][i16] = BF ? m * LN2 : m; sL[w][i16] = l; }
   if (i16 < heads) {
 #pragma unroll
     for (int r = 0; r < 4; ++r)
@@ -288,18 +338,18 @@ __global__ __launch_bounds__(PA_T, OCC) void k_quant_paged(PageDims pg, QuantDim
         *(float4*)&sO[w][i16][VD * (4 * g4 + r) + j] = make_float4(o[j][r], o[j + 1][r], o[j + 2][r], o[j + 3][r]);
   }
   sync_after_lds_stores();
-  finish_row<T, D>(pg, ck, ws, part, bid, group, groups, sM, sL, sO, out, lse);
+  finish_row<T, D, true, QP_JOIN>(pg, ck, ws, part, bid, group, groups, sM, sL, sO, out, lse);
 }
 
 hipError_t launch_quant_paged(const PageDims& pg, int format, const QuantDims& qd, int64_t q_tok, const void* q, const int32_t* table,
                               const int32_t* len, const PartView& part, void* out, float* lse, void* ws, hipStream_t st) {
   const PagedWs v = paged_view(ws, pg);
-  const int64_t room = chunk_room(pg, 0, 32);
+  const int64_t room = chunk_room(pg, 0, 32, QP_FEW, QP_MANY);
   const dim3 grid((unsigned)(((int64_t)pg.n_seq * pg.G + room) * ((pg.hpg + PA_HEADS - 1) / PA_HEADS)));
   by_type(pg, format, [&](auto type, auto dim, auto fmt) {
     using T = decltype(type);
     constexpr int D = decltype(dim)::value, FMT = decltype(fmt)::value;
-    hipLaunchKernelGGL((k_quant_paged<T, D, FMT, 3>), grid, dim3(PA_T), 0, st, pg, qd, q_tok, (const T*)q, table, len, part, (T*)out, lse, v);
+    hipLaunchKernelGGL((k_quant_paged<T, D, FMT, QP_OCC>), grid, dim3(PA_T), 0, st, pg, qd, q_tok, (const T*)q, table, len, part, (T*)out, lse, v);
   });
   return hipGetLastError();
 }
