@@ -23,13 +23,14 @@ struct PagedWs {
   float* o;
   size_t bytes;
 };
+GKV_HD int ticket_step(const PageDims& pg) { return (int64_t)pg.n_seq * pg.G * ((pg.hpg + PA_HEADS - 1) / PA_HEADS) <= 4096 ? 16 : 1; }
 static inline PagedWs paged_view(void* base, const PageDims& pg) {
   const size_t R = (size_t)pg.n_seq * pg.G, chunks = R + PA_TARGET;
   char* p = (char*)base;
   PagedWs w;
   size_t o = 0;
   w.ticket = (unsigned long long*)(p + o);
-  o += al256(R * ((pg.hpg + PA_HEADS - 1) / PA_HEADS) * 8);
+  o += al256(R * ((pg.hpg + PA_HEADS - 1) / PA_HEADS) * ticket_step(pg) * 8);
   w.ml = (unsigned long long*)(p + o);
   o += al256(chunks * pg.hpg * 8);
   w.o = (float*)(p + o);
@@ -239,7 +240,7 @@ __device__ __forceinline__ void finish_row(const PageDims& pg, const Chunk& ck, 
   if (ck.chunks == 1) return;
   stores_done();
   __syncthreads();
-  if (tid == 0) joins = last_of<RAISED>(ws.ticket + row * groups + group, ck.chunks);
+  if (tid == 0) joins = last_of<RAISED>(ws.ticket + (row * groups + group) * ticket_step(pg), ck.chunks);
   sync_after_lds_stores();
   if (!joins) return;
   // A head's pairs of dims lie on LH neighbouring lanes, which hold the (max, sum) of LH

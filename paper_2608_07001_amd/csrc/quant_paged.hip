@@ -28,6 +28,9 @@ namespace gkv {
 #define QP_FEW 768
 #define QP_MANY 1536
 #endif
+#ifndef QP_COST
+#define QP_COST 1.0f
+#endif
 #ifndef QP_OCC
 #define QP_OCC 3
 #endif
@@ -66,7 +69,7 @@ __global__ __launch_bounds__(PA_T, OCC) void k_quant_paged(PageDims pg, QuantDim
   const int bid = groups > 1 ? blockIdx.x / groups : blockIdx.x, group = groups > 1 ? blockIdx.x % groups : 0;
   Chunk ck;
   const int places = groups > 1 ? gridDim.x / groups : gridDim.x;
-  if (!find_chunk<TILE, false>(pg, PrefixView{}, len, bid, places, join_cost(pg.hpg, D), ck)) return;
+  if (!find_chunk<TILE, false>(pg, PrefixView{}, len, bid, places, join_cost(pg.hpg, D) * QP_COST, ck)) return;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i16 = lane & 15, g4 = lane >> 4;
   const int h0 = group * PA_HEADS, heads = min(PA_HEADS, pg.hpg - h0);
   constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
@@ -324,7 +327,7 @@ __global__ __launch_bounds__(PA_T, OCC) void k_quant_paged(PageDims pg, QuantDim
     if (more) now = next;
   }
   // the row's ticket word is made ready now, for its chunks to count themselves in one step
-  if (ck.chunks > 1 && tid == 0) raise(ws.ticket + ((int64_t)seq * pg.G + kv) * groups + group);
+  if (ck.chunks > 1 && tid == 0) raise(ws.ticket + (((int64_t)seq * pg.G + kv) * groups + group) * ticket_step(pg));
 #pragma unroll
   for (int j = 0; j < VD; ++j) mfma_done(o[j]);
   l = col_sum4(l);
