@@ -31,24 +31,38 @@ GKV_HD int shared_chunk(uint64_t total, int room, int least) {
   return size < (uint64_t)least ? least : (size > 0x7fffffff ? 0x7fffffff : (int)size);
 }
 
-// Rows and keys of a workgroup's tile: SPLIT of its waves have the same rows, and parts of a key tile
 constexpr int SH_T = 256;
 constexpr int SH_W = SH_T / 64;
+// Rows and keys of a workgroup's tile: SPLIT of its waves have the same rows, and parts of a key tile
 template <bool BF, int SPLIT> constexpr int shared_rows() { return (BF ? 32 : 16) * SH_W / SPLIT; }
-template <bool BF, int SPLIT> constexpr int shared_keys() { return BF ? 32 * SPLIT : (SPLIT == 4 ? 64 : 32); }
+template <bool BF, int SPLIT> constexpr int shared_keys() { return BF ? 32 * SPLIT : 32; }
 
 struct SharedPlan {
-  int split, rows, places;     // waves to the same rows; rows of a tile; workgroups, a multiple of 8
+  bool few;                    // 16 rows a workgroup, its waves a tile of keys each
+  int split, rows, places;     // else: waves to the same rows; rows of a tile; workgroups, a multiple of 8
   int64_t tiles;               // row tiles of all KV heads, at most
 };
 inline SharedPlan shared_plan(const SharedDims& sd) {
   const bool bf = sd.dtype == 1;               // GRACEKV_BF16
   const int64_t mean = ((int64_t)sd.n_seq * sd.hpg + sd.n_group - 1) / sd.n_group;
+#ifndef SH_FEWROWS
+#define SH_FEWROWS 16
+#endif
+#ifndef SH_TARGET
+#define SH_TARGET 512
+#endif
+#ifndef SH_SPLIT
+#define SH_SPLIT 2
+#endif
+#ifndef SF_TARGET
+#define SF_TARGET 768
+#endif
   SharedPlan p;
-  p.split = bf ? (mean > 64 ? 1 : mean > 32 ? 2 : 4) : (mean > 16 ? 1 : 4);
-  p.rows = (bf ? 32 : 16) * SH_W / p.split;
+  p.few = mean <= SH_FEWROWS;
+  p.split = bf ? SH_SPLIT : 1;
+  p.rows = p.few ? 16 : (bf ? 32 : 16) * SH_W / p.split;
   p.tiles = most_tiles(sd, p.rows) * sd.G;
-  const int64_t target = 512;
+  const int64_t target = p.few ? SF_TARGET : SH_TARGET;
   const int64_t room = target - p.tiles / 2 > target / 4 ? target - p.tiles / 2 : target / 4;
   p.places = (int)((p.tiles + room + 7) & ~(int64_t)7);
   return p;

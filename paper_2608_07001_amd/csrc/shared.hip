@@ -18,21 +18,31 @@
 // bf16 weights are rounded to bf16 (nearest even) for the second product, their sum takes them
 // unrounded, as in prompts: each is off by at most 2^-8 of itself, at random.  fp32 uses the
 // fp32 matrix instructions.
+#include "tickets.h"
 #include "tiles.h"
 
 namespace gkv {
 
+#ifndef SF_OCC
+#define SF_OCC 3
+#endif
+#ifndef SF_COST
+#define SF_COST 0.6f
+#endif
+#ifndef SF_JOIN
+#define SF_JOIN 8
+#endif
 constexpr float SH_LAG = 8.f, SH_TOP = 256.f;  // as in prompt.hip: base-2 units, and as a factor
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 
-static inline size_t al256(size_t x) { return (x + 255) & ~(size_t)255; }
-
 int64_t shared_items(const SharedDims& sd) { return most_tiles(sd, 16) * sd.G + 1024; }   // no plan has more workgroups
 
-// Workspace: (first chunk's place, chunks) of every row tile, then per place and row (max, sum) and
+// Workspace: (first chunk's place, chunks) or a ticket word of every row tile, then per place and row (max, sum) and
 // the weighted values.
 struct SharedWs {
   int2* info;
+  unsigned long long* ticket;
+  int step;                    // words from ticket to ticket
   float2* ml;
   float* o;
   size_t bytes;
@@ -41,7 +51,9 @@ static SharedWs shared_view(void* base, const SharedDims& sd, const SharedPlan& 
   SharedWs w;
   size_t o = 0;
   w.info = (int2*)base;
-  o += al256((size_t)p.tiles * 8);
+  w.ticket = (unsigned long long*)base;               // few rows: in place of the other
+  w.step = p.tiles <= 4096 ? 16 : 1;
+  o += al256((size_t)p.tiles * 8 * (p.few ? w.step : 1));
   w.ml = (float2*)((char*)base + o);
   o += al256((size_t)p.places * p.rows * 8);
   w.o = (float*)((char*)base + o);
@@ -62,21 +74,26 @@ __device__ __forceinline__ int64_t held_entries(const PrefixView& px, int64_t ro
 // What a workgroup works on: key tiles [t0, t1), chunk c of `chunks`, of row tile `tile` of (group b, KV head g)
 struct Item {
   int b, g, tile, tiles, c, chunks, t0, t1, id;
+  int a, n;                    // the group's sequences
+  int n_keys;
+  int64_t p_start;             // ... and entries
 };
 
 // The item of workgroup blockIdx.x; false where there is none.  Units are (group, KV head);
 // every wave looks at 64 of them at a time.
-template <int ROWS, int KEYS, int LEAST>
-__device__ __forceinline__ bool find_item(const SharedDims& sd, const int32_t* cu, const PrefixView& px, int room, Item& it) {
+template <int ROWS, int KEYS, int LEAST, typename F>
+__device__ __forceinline__ bool find_item(const SharedDims& sd, const int32_t* cu, const PrefixView& px, int room, F chunks_for, Item& it) {
   const int lane = threadIdx.x & 63, units = sd.n_group * sd.G;
   // row tiles of unit u, and key tiles of each
+  Span sp{0, 0};
+  int64_t start = 0, count = 0;
   auto shape = [&](int u, int& mt, int& n) {
     mt = n = 0;
     if (u >= units) return;
-    const Span sp = span_of(cu, u / sd.G, sd.n_seq);
+    sp = span_of(cu, u / sd.G, sd.n_seq);
     mt = tiles_of_group(sd, sp.n, ROWS);
-    int64_t s = 0;
-    n = (int)((held_entries(px, u, s) + KEYS - 1) / KEYS);
+    count = held_entries(px, u, start);
+    n = (int)((count + KEYS - 1) / KEYS);
     if (n == 0) n = 1;                 // its zeros are written too
   };
   auto sum64 = [&](uint64_t v) {
@@ -108,7 +125,7 @@ __device__ __forceinline__ bool find_item(const SharedDims& sd, const int32_t* c
 #pragma unroll 1
   for (int u0 = 0; u0 < units; u0 += 64) {
     if (u0) shape(u0 + lane, mt, n);
-    const int ch = n / size + (n % size != 0);
+    const int ch = n ? chunks_for(n, size) : 0;
     const int64_t all64 = (int64_t)mt * ch;
     const int x = all64 > (1 << 24) ? 1 << 24 : (int)all64;
     int to = x;                          // inclusive sum over the lanes: at most 2^30
@@ -138,6 +155,11 @@ __device__ __forceinline__ bool find_item(const SharedDims& sd, const int32_t* c
       it.t0 = it.c * each + min(it.c, more);
       it.t1 = it.t0 + each + (it.c < more);
       it.id = id;
+      it.a = __builtin_amdgcn_readlane((int)sp.a, at);
+      it.n = __builtin_amdgcn_readlane((int)sp.n, at);
+      it.n_keys = __builtin_amdgcn_readlane((int)count, at);
+      it.p_start = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)start, at) |
+                             (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(start >> 32), at) << 32);
       return true;
     }
     base = all;
@@ -145,20 +167,28 @@ __device__ __forceinline__ bool find_item(const SharedDims& sd, const int32_t* c
   return false;
 }
 
+// chunks of a row tile with n key tiles, `size` or fewer of them each
+struct {
+  __device__ int operator()(int n, int size) const { return n / size + (n % size != 0); }
+} constexpr whole_chunks{};
+
 // the rows of an item's tile: the lane's row, and where its query and its result lie
 struct Row {
   int row, rows;               // of the group
   int64_t hd;                  // sequence * H + head
 };
-__device__ __forceinline__ Row row_of(const SharedDims& sd, const int32_t* cu, const Item& it, int R, int r, int64_t& seq) {
-  const Span sp = span_of(cu, it.b, sd.n_seq);
+__device__ __forceinline__ Row row_of(const SharedDims& sd, const Item& it, int R, int r, int64_t& seq) {
   Row x;
-  x.rows = (int)(sp.n * sd.hpg);
+  x.rows = it.n * sd.hpg;
   x.row = it.tile * R + r;
   const int c = min(x.row, x.rows - 1), tok = (int)((uint32_t)c / (uint32_t)sd.hpg);
-  seq = sp.a + tok;
+  seq = it.a + tok;
   x.hd = seq * sd.H + (int64_t)it.g * sd.hpg + (c - tok * sd.hpg);
   return x;
+}
+// the row tile's place among all of them
+__device__ __forceinline__ int64_t slot_of(const SharedDims& sd, const Item& it, int R) {
+  return (int64_t)((int)((uint32_t)(it.a * sd.hpg) / (uint32_t)R) + it.b + it.tile) * sd.G + it.g;
 }
 
 template <int D, int SPLIT>
@@ -175,13 +205,13 @@ __global__ __launch_bounds__(SH_T, SPLIT == 4 ? 1 : SPLIT == 2 ? 2 : 3) void k_s
   __shared__ __align__(16) uint4 sK0[KEYS * CH], sK1[KEYS * CH], sV0[KEYS * CH], sV1[KEYS * CH];
   __shared__ __align__(16) float sL0[LN], sL1[LN];
   Item it;
-  if (!find_item<ROWS, KEYS, SPLIT == 1 ? 2 : 1>(sd, cu, px, room, it)) return;
+  if (!find_item<ROWS, KEYS, SPLIT == 1 ? 2 : 1>(sd, cu, px, room, whole_chunks, it)) return;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i32 = lane & 31, half = lane >> 5;
   const int rw = w / SPLIT, kw = w % SPLIT;     // the wave's 32 rows, its 32 keys of a tile
-  int64_t seq, p_start;
-  const Row me = row_of(sd, cu, it, ROWS, 32 * rw + i32, seq);
-  const int n_keys = (int)held_entries(px, (int64_t)it.b * sd.G + it.g, p_start);
-  if (it.c == 0 && tid == 0) ws.info[(int64_t)(first_tile(sd, cu, it.b, ROWS) + it.tile) * sd.G + it.g] = make_int2(it.id, it.chunks);
+  int64_t seq;
+  const Row me = row_of(sd, it, ROWS, 32 * rw + i32, seq);
+  const int n_keys = it.n_keys;
+  if (it.c == 0 && tid == 0) ws.info[slot_of(sd, it, ROWS)] = make_int2(it.id, it.chunks);
 
   uint4 qv[KS];
   {
@@ -197,9 +227,9 @@ __global__ __launch_bounds__(SH_T, SPLIT == 4 ? 1 : SPLIT == 2 ? 2 : 3) void k_s
   float m = -INFINITY, l = 0.f;                 // what is subtracted, base-2 units; l: this lane's keys only
   const float sc2 = LOG2E / sqrtf((float)D);
 
-  const uint16_t* kp = (const uint16_t*)px.K + p_start * D;
-  const uint16_t* vp = (const uint16_t*)px.V + p_start * D;
-  const float* lp = px.logm + p_start;
+  const uint16_t* kp = (const uint16_t*)px.K + it.p_start * D;
+  const uint16_t* vp = (const uint16_t*)px.V + it.p_start * D;
+  const float* lp = px.logm + it.p_start;
   // Load i of a wave brings rows RI (w + SH_W i) .. + RI - 1 straight into LDS (prompt.hip)
   const int lr = RI * w + lane / CH, lc = swz<D>(lr, lane % CH) - lr * CH;
   const int off = lr * D * 2 + lc * 16;
@@ -379,23 +409,329 @@ __global__ __launch_bounds__(SH_T, SPLIT == 4 ? 1 : SPLIT == 2 ? 2 : 3) void k_s
   }
 }
 
-// fp32: 16 rows a wave, fp32 matrix instructions; SPLIT = 4: the four waves have the same rows and
-// a quarter of a tile's keys each
-template <int D, int SPLIT>
+// 16 bytes of a state, written and read past the caches that only one XCD sees (the cache policy of a
+// relaxed access of device scope)
+constexpr int AGENT = 16;
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ Buffer state_buffer(float* base, int n) {
+  return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, 4 * n, 0x00020000);
+}
+__device__ __forceinline__ void put_agent16(Buffer b, int byte, const float* x) {
+  const u32x4 v = {__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
+  __builtin_amdgcn_raw_buffer_store_b128(v, b, byte, 0, AGENT);
+}
+__device__ __forceinline__ float4 ld_agent16(Buffer b, int byte) {
+  return __builtin_bit_cast(float4, __builtin_amdgcn_raw_buffer_load_b128(b, byte, 0, AGENT));
+}
+
+// Few rows a group: 16 of them a workgroup, whose waves have a tile of 16 NS entries each at a time, keys
+// straight from memory as the product's operand and values paired up in registers, as over pages
+// (paged.hip), and no LDS before the waves are merged.  The last of a row tile's chunks joins them.
+// bf16 weights are in two bf16 parts here, which costs a memory-bound kernel nothing.
+template <typename T, int D, int NS>
+__global__ __launch_bounds__(SH_T, SF_OCC) void k_shared_few(SharedDims sd, int room, const T* __restrict__ q, const int32_t* __restrict__ cu,
+                                                             PrefixView px, float* __restrict__ out, float* __restrict__ lse, SharedWs ws) {
+  constexpr bool BF = sizeof(T) == 2;
+  constexpr int ROWS = 16, TILE = 16 * NS;
+  constexpr int E = 16 / (int)sizeof(T);      // elements of 16 bytes
+  constexpr int KC = D / 4 / E;               // 16-byte pieces of a lane's quarter of a key
+  constexpr int VD = BF ? D / 16 : 4;         // neighbouring dims of a lane
+  constexpr int VB = BF ? 1 : D / 64;         // ... in so many places of the row
+  constexpr int VW = VD * (int)sizeof(T) / 4; // words of one place
+  __shared__ float sM[SH_W][ROWS], sL[SH_W][ROWS];
+  __shared__ __align__(16) float sO[SH_W][ROWS][D + 4];      // rows start in other banks
+  __shared__ int joins;
+  Item it;
+  const float join = SF_COST * (D / 64);
+  if (!find_item<ROWS, TILE, PA_MIN>(sd, cu, px, room, [&](int n, int size) { return chunks_of(n, size, join); }, it)) return;
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i16 = lane & 15, g4 = lane >> 4;
+  const float scale = 1.0f / sqrtf((float)D);
+  int64_t seq;
+  const Row me = row_of(sd, it, ROWS, i16, seq);
+  const int n_keys = it.n_keys;
+  const T* kp = (const T*)px.K + it.p_start * D;
+  const T* vp = (const T*)px.V + it.p_start * D;
+  const float* lp = px.logm + it.p_start;
+  uint4 qv[KC];                               // pieces g4, g4 + 4, ... of the row
+#pragma unroll
+  for (int s = 0; s < KC; ++s) qv[s] = *(const uint4*)(q + seq * sd.q_tok + (me.hd - seq * sd.H) * D + (4 * s + g4) * E);
+
+  uint4 tk[NS][KC];
+  uint32_t tv[NS][4][VB][VW];
+  float lm[NS][4];
+  constexpr uint32_t RB = D * sizeof(T);
+  // entries behind the last one read that in place of their own
+  auto load_keys = [&](int ti) __attribute__((always_inline)) {
+    const char* base = (const char*)(kp + (int64_t)ti * TILE * D);
+    const int last = n_keys - ti * TILE - 1;
+#pragma unroll
+    for (int h = 0; h < NS; ++h) {
+      const uint32_t r = min(16 * h + i16, last);
+#pragma unroll
+      for (int s = 0; s < KC; ++s) tk[h][s] = *(const uint4*)(base + (r * RB + 16 * g4) + 64 * s);
+    }
+  };
+  auto load_values = [&](int ti) __attribute__((always_inline)) {
+    const char* base = (const char*)(vp + (int64_t)ti * TILE * D);
+    const float* lb = lp + (int64_t)ti * TILE;
+    const int last = n_keys - ti * TILE - 1;
+#pragma unroll
+    for (int h = 0; h < NS; ++h)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int e = 16 * h + 4 * g4 + r;
+        const uint32_t at = min(e, last);
+        lm[h][r] = lb[at];
+        if (e > last) lm[h][r] = -INFINITY;
+#pragma unroll
+        for (int p = 0; p < VB; ++p) {
+          const char* x = base + (at * RB + VD * sizeof(T) * i16) + 64 * sizeof(T) * p;
+          if constexpr (VW == 4) {
+            const uint4 u = *(const uint4*)x;
+            tv[h][r][p][0] = u.x; tv[h][r][p][1] = u.y; tv[h][r][p][2] = u.z; tv[h][r][p][3] = u.w;
+          } else {
+            const uint2 u = *(const uint2*)x;
+            tv[h][r][p][0] = u.x; tv[h][r][p][1] = u.y;
+          }
+        }
+      }
+  };
+  f32x4 o[VB][VD];
+#pragma unroll
+  for (int p = 0; p < VB; ++p)
+#pragma unroll
+    for (int j = 0; j < VD; ++j) o[p][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;               // of row i16, natural units; l: this lane's entries only
+  const int t1 = n_keys > 0 ? it.t1 : it.t0;
+  int ti = it.t0 + w;
+  if (ti < t1) {
+    load_keys(ti);
+    load_values(ti);
+  }
+  for (; ti < t1; ti += SH_W) {
+    const bool more = ti + SH_W < t1;
+    float x[NS][4];
+#pragma unroll
+    for (int h = 0; h < NS; ++h) {
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f}, odd = acc;       // fp32: two chains, which round half as often
+#pragma unroll
+      for (int s = 0; s < KC; ++s) {
+        if constexpr (BF) {
+          acc = mfma_bf16_16x16x32(pk8(tk[h][s]), pk8(qv[s]), acc);
+        } else {
+          const uint32_t a[4] = {tk[h][s].x, tk[h][s].y, tk[h][s].z, tk[h][s].w};
+          const uint32_t b[4] = {qv[s].x, qv[s].y, qv[s].z, qv[s].w};
+#pragma unroll
+          for (int i = 0; i < 4; i += 2) {
+            acc = mfma_f32_16x16x4(__uint_as_float(a[i]), __uint_as_float(b[i]), acc);
+            odd = mfma_f32_16x16x4(__uint_as_float(a[i + 1]), __uint_as_float(b[i + 1]), odd);
+          }
+        }
+      }
+      if constexpr (!BF) acc += odd;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[h][r] = acc[r] * scale;
+    }
+    if (more) load_keys(ti + SH_W);
+    bool any = false;
+#pragma unroll
+    for (int h = 0; h < NS; ++h)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        any |= lm[h][r] == -INFINITY;
+        x[h][r] += lm[h][r];
+      }
+    if (__any(any)) {             // absent entries and those without weight
+#pragma unroll
+      for (int h = 0; h < NS; ++h)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const bool none = lm[h][r] == -INFINITY;
+          x[h][r] = none ? -INFINITY : x[h][r];
+#pragma unroll
+          for (int p = 0; p < VB; ++p)
+#pragma unroll
+            for (int i = 0; i < VW; ++i) tv[h][r][p][i] = none ? 0 : tv[h][r][p][i];     // 0 times an infinity is not 0
+        }
+    }
+    float mx = x[0][0];
+#pragma unroll
+    for (int h = 0; h < NS; ++h)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) mx = fmaxf(mx, x[h][r]);
+    {
+      const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+      mx = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+      const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+      mx = fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+    }
+    if (__any(mx > m)) {
+      const float mn = fmaxf(m, mx);
+      const float c = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - mn) * LOG2E);
+      m = mn;
+      l *= c;
+#pragma unroll
+      for (int p = 0; p < VB; ++p)
+#pragma unroll
+        for (int j = 0; j < VD; ++j) o[p][j] *= c;
+    }
+    const float ms = m == -INFINITY ? 0.f : m;
+    float pr[NS][4];
+#pragma unroll
+    for (int h = 0; h < NS; ++h)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float y = (x[h][r] - ms) * LOG2E;
+        pr[h][r] = __builtin_amdgcn_exp2f(y);
+        // fp32: what the product lost, to first order
+        if (!BF && pr[h][r] > 0.f) pr[h][r] = __builtin_fmaf(pr[h][r], __builtin_fmaf(x[h][r] - ms, LOG2E, -y) * LN2, pr[h][r]);
+        l += pr[h][r];
+      }
+    if constexpr (BF) {
+      // the second part is never 0 where the weight is not, so that an infinite value stays one (paged.hip)
+      static_assert(NS == 2, "32 entries a product");
+      uint32_t pb[NS][2], pl[NS][2];
+#pragma unroll
+      for (int h = 0; h < NS; ++h)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float a = pr[h][2 * i], b = pr[h][2 * i + 1];
+          const uint32_t ua = __float_as_uint(a), ub = __float_as_uint(b);
+          pb[h][i] = __builtin_amdgcn_perm(ub, ua, 0x07060302u);
+          pl[h][i] = pack_bf16(fmaxf(a - __uint_as_float(ua & 0xffff0000u), a * 0x1p-16f),
+                               fmaxf(b - __uint_as_float(ub & 0xffff0000u), b * 0x1p-16f));
+        }
+#pragma unroll
+      for (int j = 0; j < VD; ++j) {
+        const uint32_t sel = (j & 1) ? 0x07060302u : 0x05040100u;
+        uint32_t a[NS][2];
+#pragma unroll
+        for (int h = 0; h < NS; ++h)
+#pragma unroll
+          for (int r = 0; r < 2; ++r) a[h][r] = __builtin_amdgcn_perm(tv[h][2 * r + 1][0][j / 2], tv[h][2 * r][0][j / 2], sel);
+        const auto v8 = pk8(make_uint4(a[0][0], a[0][1], a[1][0], a[1][1]));
+        o[0][j] = mfma_bf16_16x16x32(v8, pk8(make_uint4(pl[0][0], pl[0][1], pl[1][0], pl[1][1])), o[0][j]);
+        o[0][j] = mfma_bf16_16x16x32(v8, pk8(make_uint4(pb[0][0], pb[0][1], pb[1][0], pb[1][1])), o[0][j]);
+      }
+    } else {
+#pragma unroll
+      for (int h = 0; h < NS; ++h)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int p = 0; p < VB; ++p)
+#pragma unroll
+            for (int j = 0; j < VD; ++j) o[p][j] = mfma_f32_16x16x4(__uint_as_float(tv[h][r][p][j]), pr[h][r], o[p][j]);
+    }
+    if (more) load_values(ti + SH_W);
+  }
+  // the tile's ticket word is made ready now, for its chunks to count themselves in one step
+  unsigned long long* ticket = ws.ticket + slot_of(sd, it, ROWS) * ws.step;
+  if (it.chunks > 1 && tid == 0) raise(ticket);
+#pragma unroll
+  for (int p = 0; p < VB; ++p)
+#pragma unroll
+    for (int j = 0; j < VD; ++j) mfma_done(o[p][j]);
+  l = col_sum4(l);
+  // row 4 g4 + r of product (p, j) is dimension 64 p + VD (4 g4 + r) + j, column i16 the row
+  if (g4 == 0) { sM[w][i16] = m; sL[w][i16] = l; }
+#pragma unroll
+  for (int p = 0; p < VB; ++p)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int j = 0; j < VD; j += 4)
+        *(float4*)&sO[w][i16][64 * p + VD * (4 * g4 + r) + j] = make_float4(o[p][j][r], o[p][j + 1][r], o[p][j + 2][r], o[p][j + 3][r]);
+  sync_after_lds_stores();
+  // from here a thread has eight dims of one row
+  constexpr int LH = D / 8;
+  const int r = tid / LH, c = 8 * (tid % LH);
+  const Row at = row_of(sd, it, ROWS, r < ROWS ? r : 0, seq);
+  const bool mine = r < ROWS && at.row < at.rows;
+  float M = -INFINITY, S = 0.f, O[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) O[i] = 0.f;
+  // state (m2, s2, a) onto (M, S, O): one of no entry has the maximum -inf and adds nothing, unless its
+  // sum is no number
+  auto add = [&](float m2, float s2, const float* a) {
+    const float mn = fmaxf(M, m2);
+    const float f = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((M - mn) * LOG2E);
+    const float g = m2 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m2 - mn) * LOG2E);
+    S = (f == 0.f && S == S ? 0.f : S * f) + (g == 0.f && s2 == s2 ? 0.f : s2 * g);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) O[i] = (f == 0.f ? 0.f : O[i] * f) + (g == 0.f ? 0.f : a[i] * g);
+    M = mn;
+  };
+  auto finish = [&] {
+    const float inv = S > 0.f ? 1.f / S : S;                    // no entry: the sums are 0; NaN stays
+    *(float4*)(out + at.hd * D + c) = make_float4(O[0] * inv, O[1] * inv, O[2] * inv, O[3] * inv);
+    *(float4*)(out + at.hd * D + c + 4) = make_float4(O[4] * inv, O[5] * inv, O[6] * inv, O[7] * inv);
+    if (c == 0) lse[at.hd] = M + logf(S);
+  };
+  if (mine) {
+#pragma unroll
+    for (int x = 0; x < SH_W; ++x) {
+      float a[8];
+#pragma unroll
+      for (int i = 0; i < 8; i += 4) *(float4*)(a + i) = *(const float4*)&sO[x][r][c + i];
+      add(sM[x][r], sL[x][r], a);
+    }
+    if (it.chunks == 1) {
+      finish();
+    } else {
+      const Buffer to = state_buffer(ws.o + (int64_t)it.id * ROWS * D, ROWS * D);
+#pragma unroll
+      for (int i = 0; i < 8; i += 4) put_agent16(to, 4 * (r * D + c + i), O + i);
+      if (c == 0) put_agent((unsigned long long*)(ws.ml + (int64_t)it.id * ROWS + r), pair_bits(M, S));
+    }
+  }
+  if (it.chunks == 1) return;
+  stores_done();
+  __syncthreads();
+  if (tid == 0) joins = last_of<true>(ticket, it.chunks);
+  sync_after_lds_stores();
+  if (!joins || !mine) return;
+  const int64_t first = it.id - it.c * it.tiles;          // the tile's chunks: places first + x * it.tiles
+  M = -INFINITY; S = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) O[i] = 0.f;
+  for (int c0 = 0; c0 < it.chunks; c0 += SF_JOIN) {
+    unsigned long long ml[SF_JOIN];
+    float4 ov[SF_JOIN][2];
+#pragma unroll
+    for (int x = 0; x < SF_JOIN; ++x) {            // past the last: that one again
+      const int64_t p = (first + (int64_t)min(c0 + x, it.chunks - 1) * it.tiles) * ROWS;
+      ml[x] = ld_agent((const unsigned long long*)(ws.ml + p + r));
+      const Buffer from = state_buffer(ws.o + p * D, ROWS * D);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) ov[x][i] = ld_agent16(from, 4 * (r * D + c + 4 * i));
+    }
+#pragma unroll
+    for (int x = 0; x < SF_JOIN; ++x)
+      if (c0 + x < it.chunks) {
+        const float a[8] = {ov[x][0].x, ov[x][0].y, ov[x][0].z, ov[x][0].w, ov[x][1].x, ov[x][1].y, ov[x][1].z, ov[x][1].w};
+        const float2 y = pair_of(ml[x]);
+        add(y.x, y.y, a);
+      }
+  }
+  finish();
+}
+
+// fp32: 16 rows a wave, fp32 matrix instructions
+template <int D>
 __global__ __launch_bounds__(SH_T, 2) void k_shared_f32(SharedDims sd, int room, const float* __restrict__ q, const int32_t* __restrict__ cu,
                                                         PrefixView px, float* __restrict__ out, float* __restrict__ lse, SharedWs ws) {
-  constexpr int ROWS = shared_rows<false, SPLIT>(), KEYS = shared_keys<false, SPLIT>(), WK = KEYS / SPLIT;    // a wave's keys
+  constexpr int ROWS = shared_rows<false, 1>(), KEYS = shared_keys<false, 1>();
   constexpr int CH = D / 4, NL = KEYS * CH / SH_T, LD = D + 4;
   constexpr int KC = D / 16, VB = D / 64;
   __shared__ __align__(16) float sK[KEYS * LD], sV[KEYS * LD], sL[KEYS];
   Item it;
-  if (!find_item<ROWS, KEYS, 1>(sd, cu, px, room, it)) return;
+  if (!find_item<ROWS, KEYS, 1>(sd, cu, px, room, whole_chunks, it)) return;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i16 = lane & 15, g4 = lane >> 4;
-  const int rw = SPLIT == 1 ? w : 0, kw = SPLIT == 1 ? 0 : w;
-  int64_t seq, p_start;
-  const Row me = row_of(sd, cu, it, ROWS, 16 * rw + i16, seq);
-  const int n_keys = (int)held_entries(px, (int64_t)it.b * sd.G + it.g, p_start);
-  if (it.c == 0 && tid == 0) ws.info[(int64_t)(first_tile(sd, cu, it.b, ROWS) + it.tile) * sd.G + it.g] = make_int2(it.id, it.chunks);
+  int64_t seq;
+  const Row me = row_of(sd, it, ROWS, 16 * w + i16, seq);
+  const int n_keys = it.n_keys;
+  if (it.c == 0 && tid == 0) ws.info[slot_of(sd, it, ROWS)] = make_int2(it.id, it.chunks);
 
   float4 qv[KC];                                // pieces g4, g4 + 4, ... of the row
   {
@@ -410,9 +746,9 @@ __global__ __launch_bounds__(SH_T, 2) void k_shared_f32(SharedDims sd, int room,
     for (int j = 0; j < 4; ++j) o[p][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;                 // natural units; l: this lane's keys only
   const float scale = 1.f / sqrtf((float)D);
-  const float* kp = (const float*)px.K + p_start * D;
-  const float* vp = (const float*)px.V + p_start * D;
-  const float* lp = px.logm + p_start;
+  const float* kp = (const float*)px.K + it.p_start * D;
+  const float* vp = (const float*)px.V + it.p_start * D;
+  const float* lp = px.logm + it.p_start;
   uint4 rk[NL], rv[NL];
   float rl = 0.f;
   // entries that are absent or have no weight: log m = -inf, and a value of 0
@@ -447,13 +783,13 @@ __global__ __launch_bounds__(SH_T, 2) void k_shared_f32(SharedDims sd, int room,
         if (sL[i / CH] == -INFINITY) *(uint4*)(sV + i / CH * LD + 4 * (i % CH)) = make_uint4(0, 0, 0, 0);
       sync_after_lds_stores();
     }
-    float x[WK / 16][4];
+    float x[KEYS / 16][4];
 #pragma unroll
-    for (int b = 0; b < WK / 16; ++b) {
+    for (int b = 0; b < KEYS / 16; ++b) {
       f32x4 acc = {0.f, 0.f, 0.f, 0.f}, odd = acc;       // two chains, which round half as often
 #pragma unroll
       for (int s = 0; s < KC; ++s) {
-        const float4 a = *(const float4*)(sK + (WK * kw + 16 * b + i16) * LD + 16 * s + 4 * g4);
+        const float4 a = *(const float4*)(sK + (16 * b + i16) * LD + 16 * s + 4 * g4);
         acc = mfma_f32_16x16x4(a.x, qv[s].x, acc);
         odd = mfma_f32_16x16x4(a.y, qv[s].y, odd);
         acc = mfma_f32_16x16x4(a.z, qv[s].z, acc);
@@ -462,14 +798,14 @@ __global__ __launch_bounds__(SH_T, 2) void k_shared_f32(SharedDims sd, int room,
       mfma_done(acc);
       mfma_done(odd);
       acc += odd;
-      const float4 g = *(const float4*)(sL + WK * kw + 16 * b + 4 * g4);
+      const float4 g = *(const float4*)(sL + 16 * b + 4 * g4);
       const float lg[4] = {g.x, g.y, g.z, g.w};
 #pragma unroll
       for (int r = 0; r < 4; ++r) x[b][r] = lg[r] == -INFINITY ? -INFINITY : acc[r] * scale + lg[r];
     }
     float mx = x[0][0];
 #pragma unroll
-    for (int b = 0; b < WK / 16; ++b)
+    for (int b = 0; b < KEYS / 16; ++b)
 #pragma unroll
       for (int r = 0; r < 4; ++r) mx = fmaxf(mx, x[b][r]);
     {
@@ -490,7 +826,7 @@ __global__ __launch_bounds__(SH_T, 2) void k_shared_f32(SharedDims sd, int room,
     }
     const float ms = m == -INFINITY ? 0.f : m;
 #pragma unroll
-    for (int b = 0; b < WK / 16; ++b)
+    for (int b = 0; b < KEYS / 16; ++b)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const float y = (x[b][r] - ms) * LOG2E;
@@ -500,7 +836,7 @@ __global__ __launch_bounds__(SH_T, 2) void k_shared_f32(SharedDims sd, int room,
         l += e;
 #pragma unroll
         for (int p = 0; p < VB; ++p) {
-          const float4 a = *(const float4*)(sV + (WK * kw + 16 * b + 4 * g4 + r) * LD + 64 * p + 4 * i16);
+          const float4 a = *(const float4*)(sV + (16 * b + 4 * g4 + r) * LD + 64 * p + 4 * i16);
           o[p][0] = mfma_f32_16x16x4(a.x, e, o[p][0]);
           o[p][1] = mfma_f32_16x16x4(a.y, e, o[p][1]);
           o[p][2] = mfma_f32_16x16x4(a.z, e, o[p][2]);
@@ -512,7 +848,7 @@ __global__ __launch_bounds__(SH_T, 2) void k_shared_f32(SharedDims sd, int room,
   }
   l = col_sum4(l);
   const bool mine = me.row < me.rows;
-  const int64_t place = (int64_t)it.id * ROWS + 16 * rw + i16;
+  const int64_t place = (int64_t)it.id * ROWS + 16 * w + i16;
   float* to = it.chunks > 1 ? ws.o + place * D : out + me.hd * D;
   // states of chunks are left in natural units, the bf16 kernel's in base-2 units
   auto sums = [&](float mm, float ll) {
@@ -520,51 +856,14 @@ __global__ __launch_bounds__(SH_T, 2) void k_shared_f32(SharedDims sd, int room,
     else lse[me.hd] = mm == -INFINITY ? logf(ll) : mm + logf(ll);
   };
   // row 4 g4 + r of product (p, j) is dimension 64 p + 4 (4 g4 + r) + j
-  if constexpr (SPLIT == 1) {
-    if (!mine) return;
-    const float inv = it.chunks > 1 ? 1.f : (l > 0.f ? 1.f / l : l);
+  if (!mine) return;
+  const float inv = it.chunks > 1 ? 1.f : (l > 0.f ? 1.f / l : l);
 #pragma unroll
-    for (int p = 0; p < VB; ++p)
+  for (int p = 0; p < VB; ++p)
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
-        *(float4*)(to + 64 * p + 4 * (4 * g4 + r)) = make_float4(o[p][0][r] * inv, o[p][1][r] * inv, o[p][2][r] * inv, o[p][3][r] * inv);
-    if (g4 == 0) sums(m, l);
-  } else {
-    static_assert(KEYS * LD >= SH_W * 16 * LD, "a wave's sums in its share of a tile");
-    __shared__ float2 sml[SH_W][16];
-    sync_after_lds_stores();
-    if (g4 == 0) sml[w][i16] = make_float2(m, l);
-#pragma unroll
-    for (int p = 0; p < VB; ++p)
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        *(float4*)(sK + (16 * w + i16) * LD + 64 * p + 4 * (4 * g4 + r)) = make_float4(o[p][0][r], o[p][1][r], o[p][2][r], o[p][3][r]);
-    sync_after_lds_stores();
-    float mm = -INFINITY, ll = 0.f, f[SH_W];
-#pragma unroll
-    for (int x = 0; x < SH_W; ++x) mm = fmaxf(mm, sml[x][i16].x);
-#pragma unroll
-    for (int x = 0; x < SH_W; ++x) {
-      const float2 y = sml[x][i16];
-      f[x] = y.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((y.x - mm) * LOG2E);
-      ll += f[x] == 0.f && y.y == y.y ? 0.f : y.y * f[x];
-    }
-    if (!mine) return;
-    const float inv = it.chunks > 1 ? 1.f : (ll > 0.f ? 1.f / ll : ll);
-    // 16 lanes have a row's pieces in turn
-    for (int c = 4 * (4 * w + g4); c < D; c += 64) {
-      float a[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int x = 0; x < SH_W; ++x) {
-        const float4 y = *(const float4*)(sK + (16 * x + i16) * LD + c);
-        const float v[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) a[i] += f[x] == 0.f ? 0.f : v[i] * f[x];
-      }
-      *(float4*)(to + c) = make_float4(a[0] * inv, a[1] * inv, a[2] * inv, a[3] * inv);
-    }
-    if (w == 0 && g4 == 0) sums(mm, ll);
-  }
+    for (int r = 0; r < 4; ++r)
+      *(float4*)(to + 64 * p + 4 * (4 * g4 + r)) = make_float4(o[p][0][r] * inv, o[p][1][r] * inv, o[p][2][r] * inv, o[p][3][r] * inv);
+  if (g4 == 0) sums(m, l);
 }
 
 // The chunks' states of (sequence, head) rows: a lane for four dims, `over` (a power of two) groups
@@ -641,23 +940,24 @@ hipError_t launch_shared(const SharedDims& sd, const void* q, const int32_t* cu,
   const dim3 grid((unsigned)p.places);
   const bool bf = sd.dtype == GRACEKV_BF16;
 #define GKV_SHARED(TT, ...) hipLaunchKernelGGL((__VA_ARGS__), grid, dim3(SH_T), 0, st, sd, room, (const TT*)q, cu, px, out, lse, ws)
-  if (bf) {
-    if (sd.d == 128) {
-      if (p.split == 1) GKV_SHARED(uint16_t, k_shared_bf<128, 1>);
-      else if (p.split == 2) GKV_SHARED(uint16_t, k_shared_bf<128, 2>);
-      else GKV_SHARED(uint16_t, k_shared_bf<128, 4>);
+  if (p.few) {
+    if (bf) {
+      if (sd.d == 128) GKV_SHARED(uint16_t, k_shared_few<uint16_t, 128, 2>); else GKV_SHARED(uint16_t, k_shared_few<uint16_t, 64, 2>);
     } else {
-      if (p.split == 1) GKV_SHARED(uint16_t, k_shared_bf<64, 1>);
-      else if (p.split == 2) GKV_SHARED(uint16_t, k_shared_bf<64, 2>);
-      else GKV_SHARED(uint16_t, k_shared_bf<64, 4>);
+      if (sd.d == 128) GKV_SHARED(float, k_shared_few<float, 128, 1>); else GKV_SHARED(float, k_shared_few<float, 64, 2>);
+    }
+  } else if (bf) {
+    if (sd.d == 128) {
+      if (p.split == 1) GKV_SHARED(uint16_t, k_shared_bf<128, 1>); else GKV_SHARED(uint16_t, k_shared_bf<128, 2>);
+    } else {
+      if (p.split == 1) GKV_SHARED(uint16_t, k_shared_bf<64, 1>); else GKV_SHARED(uint16_t, k_shared_bf<64, 2>);
     }
   } else {
-    if (sd.d == 128) { if (p.split == 1) GKV_SHARED(float, k_shared_f32<128, 1>); else GKV_SHARED(float, k_shared_f32<128, 4>); }
-    else { if (p.split == 1) GKV_SHARED(float, k_shared_f32<64, 1>); else GKV_SHARED(float, k_shared_f32<64, 4>); }
+    if (sd.d == 128) GKV_SHARED(float, k_shared_f32<128>); else GKV_SHARED(float, k_shared_f32<64>);
   }
 #undef GKV_SHARED
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || p.few) return e;
   auto join = [&](auto dim, auto bf16) {
     constexpr int D = decltype(dim)::value, GR = SH_T / (D / 4);
     const int chunks = room / (int)p.tiles;
