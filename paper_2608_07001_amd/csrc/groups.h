@@ -33,34 +33,27 @@ GKV_HD int shared_chunk(uint64_t total, int room, int least) {
 
 constexpr int SH_T = 256;
 constexpr int SH_W = SH_T / 64;
-// Rows and keys of a workgroup's tile: SPLIT of its waves have the same rows, and parts of a key tile
-template <bool BF, int SPLIT> constexpr int shared_rows() { return (BF ? 32 : 16) * SH_W / SPLIT; }
-template <bool BF, int SPLIT> constexpr int shared_keys() { return BF ? 32 * SPLIT : 32; }
-
 struct SharedPlan {
   bool few;                    // 16 rows a workgroup, its waves a tile of keys each
-  int split, rows, places;     // else: waves to the same rows; rows of a tile; workgroups, a multiple of 8
+  int waves, rows, places;     // of a workgroup; rows of a tile; workgroups, a multiple of 8
   int64_t tiles;               // row tiles of all KV heads, at most
 };
-inline SharedPlan shared_plan(const SharedDims& sd) {
-  const bool bf = sd.dtype == 1;               // GRACEKV_BF16
-  const int64_t mean = ((int64_t)sd.n_seq * sd.hpg + sd.n_group - 1) / sd.n_group;
 #ifndef SH_FEWROWS
 #define SH_FEWROWS 16
 #endif
 #ifndef SH_TARGET
-#define SH_TARGET 512
-#endif
-#ifndef SH_SPLIT
-#define SH_SPLIT 2
+#define SH_TARGET 256
 #endif
 #ifndef SF_TARGET
 #define SF_TARGET 768
 #endif
+inline SharedPlan shared_plan(const SharedDims& sd) {
+  const bool bf = sd.dtype == 1;               // GRACEKV_BF16
+  const int64_t mean = ((int64_t)sd.n_seq * sd.hpg + sd.n_group - 1) / sd.n_group;
   SharedPlan p;
   p.few = mean <= SH_FEWROWS;
-  p.split = bf ? SH_SPLIT : 1;
-  p.rows = p.few ? 16 : (bf ? 32 : 16) * SH_W / p.split;
+  p.waves = !p.few && bf && mean > 64 ? 8 : 4;
+  p.rows = p.few ? 16 : 16 * p.waves;
   p.tiles = most_tiles(sd, p.rows) * sd.G;
   const int64_t target = p.few ? SF_TARGET : SH_TARGET;
   const int64_t room = target - p.tiles / 2 > target / 4 ? target - p.tiles / 2 : target / 4;

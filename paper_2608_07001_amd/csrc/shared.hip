@@ -23,6 +23,9 @@
 
 namespace gkv {
 
+#ifndef SH_NU
+#define SH_NU 2
+#endif
 #ifndef SF_OCC
 #define SF_OCC 3
 #endif
@@ -37,10 +40,10 @@ constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 
 int64_t shared_items(const SharedDims& sd) { return most_tiles(sd, 16) * sd.G + 1024; }   // no plan has more workgroups
 
-// Workspace: (first chunk's place, chunks) or a ticket word of every row tile, then per place and row (max, sum) and
+// Workspace: where every row's states are, or a ticket word of every row tile, then per place and row (max, sum) and
 // the weighted values.
 struct SharedWs {
-  int2* info;
+  int4* info;
   unsigned long long* ticket;
   int step;                    // words from ticket to ticket
   float2* ml;
@@ -50,10 +53,10 @@ struct SharedWs {
 static SharedWs shared_view(void* base, const SharedDims& sd, const SharedPlan& p) {
   SharedWs w;
   size_t o = 0;
-  w.info = (int2*)base;
+  w.info = (int4*)base;
   w.ticket = (unsigned long long*)base;               // few rows: in place of the other
   w.step = p.tiles <= 4096 ? 16 : 1;
-  o += al256((size_t)p.tiles * 8 * (p.few ? w.step : 1));
+  o += al256(p.few ? (size_t)p.tiles * 8 * w.step : (size_t)sd.n_seq * sd.H * 16);
   w.ml = (float2*)((char*)base + o);
   o += al256((size_t)p.places * p.rows * 8);
   w.o = (float*)((char*)base + o);
@@ -81,7 +84,7 @@ struct Item {
 
 // The item of workgroup blockIdx.x; false where there is none.  Units are (group, KV head);
 // every wave looks at 64 of them at a time.
-template <int ROWS, int KEYS, int LEAST, typename F>
+template <int ROWS, int KEYS, int LEAST, int W, typename F>
 __device__ __forceinline__ bool find_item(const SharedDims& sd, const int32_t* cu, const PrefixView& px, int room, F chunks_for, Item& it) {
   const int lane = threadIdx.x & 63, units = sd.n_group * sd.G;
   // row tiles of unit u, and key tiles of each
@@ -107,8 +110,8 @@ __device__ __forceinline__ bool find_item(const SharedDims& sd, const int32_t* c
     shape(lane, mt, n);
     total = sum64((uint64_t)mt * n);
   } else {
-    __shared__ uint64_t part[SH_W];
-    for (int u = threadIdx.x; u < units; u += SH_T) {
+    __shared__ uint64_t part[W];
+    for (int u = threadIdx.x; u < units; u += 64 * W) {
       shape(u, mt, n);
       total += (uint64_t)mt * n;
     }
@@ -117,7 +120,7 @@ __device__ __forceinline__ bool find_item(const SharedDims& sd, const int32_t* c
     sync_after_lds_stores();
     total = 0;
 #pragma unroll
-    for (int i = 0; i < SH_W; ++i) total += part[i];
+    for (int i = 0; i < W; ++i) total += part[i];
     shape(lane, mt, n);
   }
   const int size = __builtin_amdgcn_readfirstlane(shared_chunk(total, room, LEAST));
@@ -191,27 +194,28 @@ __device__ __forceinline__ int64_t slot_of(const SharedDims& sd, const Item& it,
   return (int64_t)((int)((uint32_t)(it.a * sd.hpg) / (uint32_t)R) + it.b + it.tile) * sd.G + it.g;
 }
 
-template <int D, int SPLIT>
-__global__ __launch_bounds__(SH_T, SPLIT == 4 ? 1 : SPLIT == 2 ? 2 : 3) void k_shared_bf(SharedDims sd, int room, const uint16_t* __restrict__ q,
-                                                                           const int32_t* __restrict__ cu, PrefixView px,
-                                                                           float* __restrict__ out, float* __restrict__ lse, SharedWs ws) {
-  constexpr int ROWS = shared_rows<true, SPLIT>(), KEYS = shared_keys<true, SPLIT>();
+// Many rows a group: W waves, pairs of them to the same 32 rows with 32 NU keys each of a tile.  One tile is in
+// LDS and the next on its way.
+template <int D, int W>
+__global__ __launch_bounds__(64 * W, W / 4) void k_shared_bf(SharedDims sd, int room, const uint16_t* __restrict__ q,
+                                                             const int32_t* __restrict__ cu, PrefixView px, float* __restrict__ out,
+                                                             float* __restrict__ lse, SharedWs ws) {
+  constexpr int SPLIT = 2, NU = SH_NU, ROWS = 32 * W / SPLIT, KEYS = 32 * NU * SPLIT;
   constexpr int CH = D / 8;                     // 16-byte pieces of a row
   constexpr int RI = 64 / CH;                   // rows that one load of a wave brings
-  constexpr int NI = KEYS / RI / SH_W;          // such loads of a wave and array
+  constexpr int NI = KEYS / RI / W;             // such loads of a wave and array
   constexpr int KS = D / 16;                    // product steps over the dims
   constexpr int DT = D / 32;                    // 32-dim tiles of the output
-  constexpr int LN = KEYS < 64 ? 64 : KEYS;
-  __shared__ __align__(16) uint4 sK0[KEYS * CH], sK1[KEYS * CH], sV0[KEYS * CH], sV1[KEYS * CH];
-  __shared__ __align__(16) float sL0[LN], sL1[LN];
+  constexpr int V0 = KEYS * CH, L0 = 2 * V0;    // of a stage: keys, values, each wave's own copy of log m
+  constexpr int STAGE = L0 + W * KEYS / 4;
+  __shared__ __align__(16) uint4 st0[STAGE], st1[STAGE];      // of their own, so that loads into one and reads of the other are told apart
   Item it;
-  if (!find_item<ROWS, KEYS, SPLIT == 1 ? 2 : 1>(sd, cu, px, room, whole_chunks, it)) return;
+  if (!find_item<ROWS, KEYS, 1, W>(sd, cu, px, room, whole_chunks, it)) return;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i32 = lane & 31, half = lane >> 5;
   const int rw = w / SPLIT, kw = w % SPLIT;     // the wave's 32 rows, its 32 keys of a tile
   int64_t seq;
   const Row me = row_of(sd, it, ROWS, 32 * rw + i32, seq);
   const int n_keys = it.n_keys;
-  if (it.c == 0 && tid == 0) ws.info[slot_of(sd, it, ROWS)] = make_int2(it.id, it.chunks);
 
   uint4 qv[KS];
   {
@@ -219,126 +223,164 @@ __global__ __launch_bounds__(SH_T, SPLIT == 4 ? 1 : SPLIT == 2 ? 2 : 3) void k_s
 #pragma unroll
     for (int s = 0; s < KS; ++s) qv[s] = *(const uint4*)(qp + 16 * s + 8 * half);
   }
+  // where the row's states will be, for the kernel that joins them
+  if (it.c == 0 && kw == 0 && half == 0 && me.row < me.rows)
+    ws.info[me.hd] = make_int4(it.id, it.chunks, it.tiles, 32 * rw + i32);
   f32x16 o[DT];
 #pragma unroll
   for (int t = 0; t < DT; ++t)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[t][r] = 0.f;
-  float m = -INFINITY, l = 0.f;                 // what is subtracted, base-2 units; l: this lane's keys only
-  const float sc2 = LOG2E / sqrtf((float)D);
+  float m = -INFINITY, l = 0.f;                 // what is subtracted, natural units; l: this lane's keys only
+  const float root = sqrtf((float)D), scale = 1.f / root, sc2 = LOG2E / root;
 
   const uint16_t* kp = (const uint16_t*)px.K + it.p_start * D;
   const uint16_t* vp = (const uint16_t*)px.V + it.p_start * D;
   const float* lp = px.logm + it.p_start;
-  // Load i of a wave brings rows RI (w + SH_W i) .. + RI - 1 straight into LDS (prompt.hip)
+  const int t1 = n_keys > 0 ? it.t1 : it.t0;     // an empty row: its zeros only
+  // Load i of a wave brings rows RI (w + W i) .. + RI - 1 straight into LDS (prompt.hip)
   const int lr = RI * w + lane / CH, lc = swz<D>(lr, lane % CH) - lr * CH;
   const int off = lr * D * 2 + lc * 16;
-  constexpr int STEP = RI * SH_W * D * 2;
-  auto load = [&](const uint16_t* rows, int t, uint4* to) {
-    const Buffer b = tile_buffer<uint16_t, D>(rows + (int64_t)t * KEYS * D, D, min(n_keys - t * KEYS, KEYS));
+  constexpr int STEP = RI * W * D * 2;
+  auto load_tile = [&](int t, uint4* to) __attribute__((always_inline)) {
+    const int n = min(n_keys - t * KEYS, KEYS);
+    const int64_t at = (int64_t)t * KEYS;
+    const Buffer k = __builtin_amdgcn_make_buffer_rsrc((void*)(kp + at * D), 0, n * D * 2, 0x00020000);
+    const Buffer v = __builtin_amdgcn_make_buffer_rsrc((void*)(vp + at * D), 0, n * D * 2, 0x00020000);
+    const Buffer g = __builtin_amdgcn_make_buffer_rsrc((void*)(lp + at), 0, n * 4, 0x00020000);
 #pragma unroll
-    for (int i = 0; i < NI; ++i) buffer_load_lds(b, to + 64 * (w + SH_W * i), off + i * STEP);
-  };
-  auto load_logm = [&](int t, float* to) {      // the first LN / 64 waves, 64 a wave; past the last: 0
-    if (w < LN / 64) {
-      const int n = min(n_keys - t * KEYS, KEYS);
-      const Buffer b = __builtin_amdgcn_make_buffer_rsrc((void*)(lp + (int64_t)t * KEYS), 0, n * 4, 0x00020000);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (__attribute__((address_space(3))) void*)(to + 64 * w), 4, 256 * w + 4 * lane, 0, 0, 0);
-    }
-  };
-  auto load_tile = [&](int t, uint4* K, uint4* V, float* L) {
-    load(kp, t, K);
-    load(vp, t, V);
-    load_logm(t, L);
+    for (int i = 0; i < NI; ++i) buffer_load_lds(k, to + 64 * (w + W * i), off + i * STEP);
+#pragma unroll
+    for (int i = 0; i < NI; ++i) buffer_load_lds(v, to + V0 + 64 * (w + W * i), off + i * STEP);
+#pragma unroll
+    for (int i = 0; i < KEYS / 64; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(g, (__attribute__((address_space(3))) void*)(to + L0 + w * KEYS / 4 + 16 * i), 4, 4 * lane + 256 * i, 0, 0, 0);
   };
   constexpr int RB = 2 * D;
   int k_at = 16 * swz<D>(i32, half);
   const int v_at = 16 * swz<D>(4 * half + ((lane & 15) >> 2), 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + 8 * (lane & 1);
-  auto step = [&](int t, uint4* cK, uint4* cV, float* cL, uint4* nK, uint4* nV, float* nL) __attribute__((always_inline)) {
-    // the wave's own loads of tile t are there, then everyone's; and everyone is done with tile t - 1
-    wait_vm();
-    sync_after_lds_stores();
-    const int left = n_keys - t * KEYS;          // entries from this tile on
-    // entries without weight: their values have to be 0
-    bool none = false;
+  // Below LOW, which only a mask is (-inf, the type's lowest value), log m is all of a logit: nothing beside
+  // others, and where a row has seen no others, its weight is 1 at the largest and 0 else.  Units of the sums would
+  // take it out of range.
+  constexpr float LOW = -1e36f;
+  auto log_m = [&](const uint4* tile, int u, float* lm) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < KEYS; i += 64)
-      if (i + lane < KEYS && i + lane < left) none |= cL[i + lane] == -INFINITY;
-    const bool masked = __any(none);             // the same for every wave
-    if (masked) {
-      for (int i = tid; i < KEYS * CH; i += SH_T)
+    for (int b = 0; b < 4; ++b) {                // register r: key 8 (r / 4) + 4 half + r % 4 of the wave's u-th 32
+      const uint4 g = lds_at(tile, 16 * (L0 + w * KEYS / 4) + 4 * (32 * (NU * kw + u) + 4 * half + 8 * b));
+      lm[4 * b] = __uint_as_float(g.x); lm[4 * b + 1] = __uint_as_float(g.y);
+      lm[4 * b + 2] = __uint_as_float(g.z); lm[4 * b + 3] = __uint_as_float(g.w);
+    }
+  };
+  auto step = [&](int t, uint4* cur, uint4* next) __attribute__((always_inline)) {
+    // the wave's own loads of tile t are there, then everyone's; and everyone is done with tile t - 1
+    loaded_barrier<0>();
+    if (t + 1 < t1) load_tile(t + 1, next);
+    uint4* cV = cur + V0;
+    const int left = n_keys - t * KEYS;          // entries from this tile on
+    const float* cL = (const float*)(cur + L0 + w * KEYS / 4);
+    bool low = false;                            // some log m is below LOW
+#pragma unroll
+    for (int i = 0; i < KEYS; i += 64) low |= i + lane < left && cL[i + lane] < LOW;
+    low = __any(low);                            // the same for every wave
+    f32x16 s[NU];
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {               // log m stands in the sums from the start, in their units
+      float lm[16];
+      log_m(cur, u, lm);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[u][r] = lm[r] * root;
+      asm volatile("" : "+v"(k_at));             // eight places: formed anew, not held in registers
+#pragma unroll
+      for (int x = 0; x < KS; ++x) s[u] = mfma_bf16_32x32x16(lds_at(cur, (k_at ^ (32 * x)) + 32 * (NU * kw + u) * RB), qv[x], s[u]);
+    }
+    reads_ahead<NU * KS, 1, 4>();
+#pragma unroll
+    for (int u = 0; u < NU; ++u) mfma_done16(s[u]);
+    if (left < KEYS) {
+#pragma unroll
+      for (int u = 0; u < NU; ++u) {
+        const int rel = left - 32 * (NU * kw + u) - 4 * half;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[u][r] = 8 * (r / 4) + r % 4 >= rel ? -INFINITY : s[u][r];
+      }
+    }
+    float most = -INFINITY;
+    if (low) {
+      for (int i = tid; i < KEYS * CH; i += 64 * W)        // no weight: a value of 0, whatever it was
         if (cL[i / CH] == -INFINITY) cV[i] = make_uint4(0, 0, 0, 0);       // a row's pieces stay in its places
+#pragma unroll
+      for (int u = 0; u < NU; ++u) {
+        float lm[16];
+        log_m(cur, u, lm);
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (8 * (r / 4) + r % 4 < left - 32 * (NU * kw + u) - 4 * half && lm[r] < LOW) {
+            most = fmaxf(most, lm[r]);
+            s[u][r] = -INFINITY;
+          }
+      }
       sync_after_lds_stores();
     }
-    if (t + 1 < it.t1) load_tile(t + 1, nK, nV, nL);
-    f32x16 s;
-    asm volatile("" : "+v"(k_at));               // eight places: formed anew, not held in registers
+    float mx = s[0][0];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] = 0.f;
+    for (int u = 0; u < NU; ++u)
 #pragma unroll
-    for (int x = 0; x < KS; ++x) s = mfma_bf16_32x32x16(lds_at(cK, (k_at ^ (32 * x)) + 32 * kw * RB), qv[x], s);
-    reads_ahead<KS, 1, 4>();
-    mfma_done16(s);
-    // register r: key 8 (r / 4) + 4 half + r % 4 of the wave's
-    const float* lw = cL + 32 * kw + 4 * half;
-#pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      const float4 g = *(const float4*)(lw + 8 * b);
-      s[4 * b] = __builtin_fmaf(s[4 * b], sc2, g.x * LOG2E);
-      s[4 * b + 1] = __builtin_fmaf(s[4 * b + 1], sc2, g.y * LOG2E);
-      s[4 * b + 2] = __builtin_fmaf(s[4 * b + 2], sc2, g.z * LOG2E);
-      s[4 * b + 3] = __builtin_fmaf(s[4 * b + 3], sc2, g.w * LOG2E);
-    }
-    if (masked) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = lw[8 * (r / 4) + r % 4] == -INFINITY ? -INFINITY : s[r];
-    }
-    if (left < KEYS) {
-      const int rel = left - 32 * kw - 4 * half;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = 8 * (r / 4) + r % 4 >= rel ? -INFINITY : s[r];
-    }
-    float mx = s[0];
-#pragma unroll
-    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[u][r]);
+    mx = fmaxf(mx * scale, most);
     {
       const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
       mx = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
     }
     if (__any(mx > m)) {                         // (prompt.hip on what is subtracted)
-      const float mn = fmaxf(m, mx + SH_LAG);
-      const float c = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+      const float mn = fmaxf(m, mx + SH_LAG * LN2);
+      const float c = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - mn) * LOG2E);
       m = mn;
       l *= c;
 #pragma unroll
       for (int d = 0; d < DT; ++d) o[d] *= c;
     }
-    const float ms = m == -INFINITY ? 0.f : m;
-    uint4 pr[2];
+    float ms2 = m == -INFINITY ? 0.f : m * LOG2E;
+    if (__any(m < LOW && m > -INFINITY)) {       // rows that have seen such entries only
+      if (m < LOW && m > -INFINITY) ms2 = 0.f;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      float e[8];
+      for (int u = 0; u < NU; ++u) {
+        float lm[16];
+        log_m(cur, u, lm);
 #pragma unroll
-      for (int r = 0; r < 8; ++r) e[r] = __builtin_amdgcn_exp2f(s[8 * h + r] - ms);
-      l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
-      pr[h] = make_uint4(pack_bf16(e[0], e[1]), pack_bf16(e[2], e[3]), pack_bf16(e[4], e[5]), pack_bf16(e[6], e[7]));
+        for (int r = 0; r < 16; ++r)
+          if (m < LOW && m > -INFINITY)
+            s[u][r] = 8 * (r / 4) + r % 4 < left - 32 * (NU * kw + u) - 4 * half && lm[r] == m ? 0.f : -INFINITY;
+      }
     }
+    uint4 pr[NU][2];
+#pragma unroll
+    for (int u = 0; u < NU; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float e[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) e[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][8 * h + r], sc2, -ms2));
+        l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+        pr[u][h] = make_uint4(pack_bf16(e[0], e[1]), pack_bf16(e[2], e[3]), pack_bf16(e[4], e[5]), pack_bf16(e[6], e[7]));
+      }
     // product step x: keys 16 x + 8 (j / 4) + 4 half + j % 4 in place 8 half + j
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
+    for (int u = 0; u < NU; ++u)
 #pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        const uint2 a = lds_read_tr(cV, (v_at ^ (64 * d)) + (32 * kw + 16 * x) * RB);
-        const uint2 b = lds_read_tr(cV, (v_at ^ (64 * d + 32)) + (32 * kw + 16 * x + 8) * RB);
-        o[d] = mfma_bf16_32x32x16(make_uint4(a.x, a.y, b.x, b.y), pr[x], o[d]);
-      }
-    reads_ahead<2 * DT, 2, 3>();
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          const int row = 32 * (NU * kw + u) + 16 * x;
+          const uint2 a = lds_read_tr(cV, (v_at ^ (64 * d)) + row * RB);
+          const uint2 b = lds_read_tr(cV, (v_at ^ (64 * d + 32)) + (row + 8) * RB);
+          o[d] = mfma_bf16_32x32x16(make_uint4(a.x, a.y, b.x, b.y), pr[u][x], o[d]);
+        }
+    reads_ahead<2 * DT * NU, 2, 3>();
   };
-  const int t1 = n_keys > 0 ? it.t1 : it.t0;     // an empty row: its zeros only
-  if (it.t0 < t1) load_tile(it.t0, sK0, sV0, sL0);
+  if (it.t0 < t1) load_tile(it.t0, st0);
   for (int t = it.t0; t < t1; t += 2) {
-    step(t, sK0, sV0, sL0, sK1, sV1, sL1);
-    if (t + 1 < t1) step(t + 1, sK1, sV1, sL1, sK0, sV0, sL0);
+    step(t, st0, st1);
+    if (t + 1 < t1) step(t + 1, st1, st0);
   }
 #pragma unroll
   for (int d = 0; d < DT; ++d) mfma_done16(o[d]);
@@ -347,65 +389,44 @@ __global__ __launch_bounds__(SH_T, SPLIT == 4 ? 1 : SPLIT == 2 ? 2 : 3) void k_s
     l = __uint_as_float(p[0]) + __uint_as_float(p[1]);
   }
   const bool mine = me.row < me.rows;
-  // where dim tile d goes: the result, or the place's state
+  // the two waves of the same rows join their states, each half of the dims, through the tiles' LDS
+  static_assert(2 * STAGE * 16 >= W * 64 * 4 * 16 * DT, "a stage for half of the waves");
+  __shared__ float2 sml[W][32];
+  sync_after_lds_stores();
+  auto sums = [&](int x) { return (float*)(x < W / 2 ? st0 : st1) + (x % (W / 2)) * 64 * 16 * DT; };
+  float* so = sums(w);
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) so[64 * (16 * d + r) + lane] = o[d][r];
+  if (half == 0) sml[w][i32] = make_float2(m, l);
+  sync_after_lds_stores();
+  if (!mine) return;
+  const float2 x0 = sml[SPLIT * rw][i32], x1 = sml[SPLIT * rw + 1][i32];
+  const float mm = fmaxf(x0.x, x1.x);
+  const float f0 = x0.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((x0.x - mm) * LOG2E), f1 = x1.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((x1.x - mm) * LOG2E);
+  const float ll = (f0 == 0.f && x0.y == x0.y ? 0.f : x0.y * f0) + (f1 == 0.f && x1.y == x1.y ? 0.f : x1.y * f1);       // NaN stays
+  // the result, or the place's state
   const int64_t place = (int64_t)it.id * ROWS + 32 * rw + i32;
   float* to = it.chunks > 1 ? ws.o + place * D : out + me.hd * D;
-  const float M = m, S = l;
-  auto put = [&](int d, const f32x16& x, float mm, float ll) __attribute__((always_inline)) {
-    const float inv = it.chunks > 1 ? 1.f : (ll > 0.f ? 1.f / ll : ll);    // no entry: the sums are 0; NaN stays
+  const float inv = it.chunks > 1 ? 1.f : (ll > 0.f ? 1.f / ll : ll);    // no entry: the sums are 0; NaN stays
+  const float *s0 = sums(SPLIT * rw), *s1 = sums(SPLIT * rw + 1);
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-      *(float4*)(to + 32 * d + 8 * r + 4 * half) = make_float4(x[4 * r] * inv, x[4 * r + 1] * inv, x[4 * r + 2] * inv, x[4 * r + 3] * inv);
-    if (d == 0 && half == 0) {
-      if (it.chunks > 1) ws.ml[place] = make_float2(mm, ll);
-      // (with the sum in units of its largest weight, whose logarithm is small)
-      else lse[me.hd] = mm == -INFINITY ? logf(ll) : ((mm - SH_LAG) + log2f(ll * SH_TOP)) * LN2;
+  for (int d0 = 0; d0 < DT / 2; ++d0) {
+    const int d = d0 + kw * (DT / 2);
+    float a[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float y0 = s0[64 * (16 * d + r) + lane], y1 = s1[64 * (16 * d + r) + lane];
+      a[r] = ((f0 == 0.f ? 0.f : y0 * f0) + (f1 == 0.f ? 0.f : y1 * f1)) * inv;
     }
-  };
-  if constexpr (SPLIT == 1) {
-    if (!mine) return;
 #pragma unroll
-    for (int d = 0; d < DT; ++d) put(d, o[d], M, S);
-  } else {
-    // the waves of the same rows join their states, each a share of the dims, through the tiles' LDS
-    static_assert(KEYS * CH * 16 >= 64 * 4 * 16 * DT, "an array for each wave");
-    __shared__ float2 sml[SH_W][32];
-    sync_after_lds_stores();
-    auto sums = [&](int x) { return (float*)(x == 0 ? sK0 : x == 1 ? sK1 : x == 2 ? sV0 : sV1); };
-    float* so = sums(w);
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) so[64 * (16 * d + r) + lane] = o[d][r];
-    if (half == 0) sml[w][i32] = make_float2(M, S);
-    sync_after_lds_stores();
-    float mm = -INFINITY, ll = 0.f, f[SPLIT];
-#pragma unroll
-    for (int x = 0; x < SPLIT; ++x) mm = fmaxf(mm, sml[SPLIT * rw + x][i32].x);
-#pragma unroll
-    for (int x = 0; x < SPLIT; ++x) {
-      const float2 y = sml[SPLIT * rw + x][i32];
-      f[x] = y.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(y.x - mm);
-      ll += f[x] == 0.f && y.y == y.y ? 0.f : y.y * f[x];        // NaN stays
-    }
-    if (!mine) return;
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-      if (d % SPLIT == kw) {
-        f32x16 a;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) a[r] = 0.f;
-#pragma unroll
-        for (int x = 0; x < SPLIT; ++x) {
-          const float* src = sums(SPLIT * rw + x);
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const float y = src[64 * (16 * d + r) + lane];
-            a[r] += f[x] == 0.f ? 0.f : y * f[x];
-          }
-        }
-        put(d, a, mm, ll);
-      }
+    for (int r = 0; r < 4; ++r) *(float4*)(to + 32 * d + 8 * r + 4 * half) = make_float4(a[4 * r], a[4 * r + 1], a[4 * r + 2], a[4 * r + 3]);
+  }
+  if (kw == 0 && half == 0) {
+    if (it.chunks > 1) ws.ml[place] = make_float2(mm, ll);
+    // (with the sum in units of its largest weight, whose logarithm is small)
+    else lse[me.hd] = mm == -INFINITY ? logf(ll) : (mm - SH_LAG * LN2) + logf(ll * SH_TOP);
   }
 }
 
@@ -443,7 +464,7 @@ __global__ __launch_bounds__(SH_T, SF_OCC) void k_shared_few(SharedDims sd, int 
   __shared__ int joins;
   Item it;
   const float join = SF_COST * (D / 64);
-  if (!find_item<ROWS, TILE, PA_MIN>(sd, cu, px, room, [&](int n, int size) { return chunks_of(n, size, join); }, it)) return;
+  if (!find_item<ROWS, TILE, PA_MIN, SH_W>(sd, cu, px, room, [&](int n, int size) { return chunks_of(n, size, join); }, it)) return;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i16 = lane & 15, g4 = lane >> 4;
   const float scale = 1.0f / sqrtf((float)D);
   int64_t seq;
@@ -721,17 +742,17 @@ __global__ __launch_bounds__(SH_T, SF_OCC) void k_shared_few(SharedDims sd, int 
 template <int D>
 __global__ __launch_bounds__(SH_T, 2) void k_shared_f32(SharedDims sd, int room, const float* __restrict__ q, const int32_t* __restrict__ cu,
                                                         PrefixView px, float* __restrict__ out, float* __restrict__ lse, SharedWs ws) {
-  constexpr int ROWS = shared_rows<false, 1>(), KEYS = shared_keys<false, 1>();
+  constexpr int ROWS = 16 * SH_W, KEYS = 32;
   constexpr int CH = D / 4, NL = KEYS * CH / SH_T, LD = D + 4;
   constexpr int KC = D / 16, VB = D / 64;
   __shared__ __align__(16) float sK[KEYS * LD], sV[KEYS * LD], sL[KEYS];
   Item it;
-  if (!find_item<ROWS, KEYS, 1>(sd, cu, px, room, whole_chunks, it)) return;
+  if (!find_item<ROWS, KEYS, 1, SH_W>(sd, cu, px, room, whole_chunks, it)) return;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i16 = lane & 15, g4 = lane >> 4;
   int64_t seq;
   const Row me = row_of(sd, it, ROWS, 16 * w + i16, seq);
   const int n_keys = it.n_keys;
-  if (it.c == 0 && tid == 0) ws.info[slot_of(sd, it, ROWS)] = make_int2(it.id, it.chunks);
+  if (it.c == 0 && g4 == 0 && me.row < me.rows) ws.info[me.hd] = make_int4(it.id, it.chunks, it.tiles, 16 * w + i16);
 
   float4 qv[KC];                                // pieces g4, g4 + 4, ... of the row
   {
@@ -850,7 +871,6 @@ __global__ __launch_bounds__(SH_T, 2) void k_shared_f32(SharedDims sd, int room,
   const bool mine = me.row < me.rows;
   const int64_t place = (int64_t)it.id * ROWS + 16 * w + i16;
   float* to = it.chunks > 1 ? ws.o + place * D : out + me.hd * D;
-  // states of chunks are left in natural units, the bf16 kernel's in base-2 units
   auto sums = [&](float mm, float ll) {
     if (it.chunks > 1) ws.ml[place] = make_float2(mm, ll);
     else lse[me.hd] = mm == -INFINITY ? logf(ll) : mm + logf(ll);
@@ -877,27 +897,21 @@ __global__ __launch_bounds__(SH_T) void k_shared_join(SharedDims sd, int R, int 
   const int group = threadIdx.x / LH, gr = group & (over - 1), c = 4 * (threadIdx.x % LH);
   const int64_t hd = (int64_t)blockIdx.x * (GR / over) + group / over, rows = (int64_t)sd.n_seq * sd.H;
   const int64_t at = hd < rows ? hd : rows - 1;
-  const int seq = (int)((uint32_t)at / (uint32_t)sd.H), head = (int)at - seq * sd.H, g = head / sd.hpg;
+  const int seq = (int)((uint32_t)at / (uint32_t)sd.H);
   const int b = sd.n_group > 1 ? span_with(cu, sd.n_group, seq) : 0;
   const Span sp = span_of(cu, b, sd.n_seq);
   bool on = hd < rows && seq >= sp.a && seq < sp.a + sp.n;      // in a group?
-  int first = 0, chunks = 0, tiles = 1, r = 0;
-  if (on) {
-    r = (int)(seq - sp.a) * sd.hpg + (head - g * sd.hpg);
-    tiles = tiles_of_group(sd, sp.n, R);
-    const int2 x = ws.info[(int64_t)(first_tile(sd, cu, b, R) + r / R) * sd.G + g];
-    first = x.x;
-    chunks = x.y < places ? x.y : places;
-    on = chunks > 1;                                             // one: written already
-  }
+  const int4 x = ws.info[at];                                    // first chunk's place, chunks, places from one to the next, row there
+  const int first = x.x, tiles = x.z, r = x.w & (R - 1);
+  int chunks = x.y < places ? x.y : places;
+  on &= chunks > 1;                                              // one: written already
   if (!on) chunks = 0;
-  constexpr float UNIT = BF ? 1.f : LOG2E;                       // of the maxima
   float M = -INFINITY, S = 0.f, O[4] = {0.f, 0.f, 0.f, 0.f};
   // a state of no entry has the maximum -inf and adds nothing, unless its sum is no number
   auto add = [&](float m, float s, const float4& x) {
     const float mn = fmaxf(M, m);
-    const float f = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((M - mn) * UNIT);
-    const float h = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mn) * UNIT);
+    const float f = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((M - mn) * LOG2E);
+    const float h = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mn) * LOG2E);
     S = (f == 0.f && S == S ? 0.f : S * f) + (h == 0.f && s == s ? 0.f : s * h);
     const float v[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
@@ -913,8 +927,8 @@ __global__ __launch_bounds__(SH_T) void k_shared_join(SharedDims sd, int R, int 
       const int p = p0 + i * over < chunks ? p0 + i * over : p0;
       int64_t id = first + (int64_t)p * tiles;
       id = id < 0 ? 0 : (id >= places ? places - 1 : id);
-      ml[i] = ws.ml[id * R + r % R];
-      x[i] = *(const float4*)(ws.o + (id * R + r % R) * D + c);
+      ml[i] = ws.ml[id * R + r];
+      x[i] = *(const float4*)(ws.o + (id * R + r) * D + c);
     }
 #pragma unroll
     for (int i = 0; i < UN; ++i)
@@ -929,7 +943,7 @@ __global__ __launch_bounds__(SH_T) void k_shared_join(SharedDims sd, int R, int 
   for (int i = 1; i < over; ++i) add(sM[group + i], sS[group + i], *(const float4*)&sO[group + i][c]);
   const float inv = S > 0.f ? 1.f / S : S;
   *(float4*)(out + at * D + c) = make_float4(O[0] * inv, O[1] * inv, O[2] * inv, O[3] * inv);
-  if (c == 0) lse[at] = M == -INFINITY ? logf(S) : BF ? ((M - SH_LAG) + log2f(S * SH_TOP)) * LN2 : M + logf(S);
+  if (c == 0) lse[at] = M == -INFINITY ? logf(S) : BF ? (M - SH_LAG * LN2) + logf(S * SH_TOP) : M + logf(S);
 }
 
 hipError_t launch_shared(const SharedDims& sd, const void* q, const int32_t* cu, const PrefixView& px, float* out, float* lse, void* base,
@@ -939,7 +953,7 @@ hipError_t launch_shared(const SharedDims& sd, const void* q, const int32_t* cu,
   const int room = p.places - (int)p.tiles;
   const dim3 grid((unsigned)p.places);
   const bool bf = sd.dtype == GRACEKV_BF16;
-#define GKV_SHARED(TT, ...) hipLaunchKernelGGL((__VA_ARGS__), grid, dim3(SH_T), 0, st, sd, room, (const TT*)q, cu, px, out, lse, ws)
+#define GKV_SHARED(TT, ...) hipLaunchKernelGGL((__VA_ARGS__), grid, dim3(64 * p.waves), 0, st, sd, room, (const TT*)q, cu, px, out, lse, ws)
   if (p.few) {
     if (bf) {
       if (sd.d == 128) GKV_SHARED(uint16_t, k_shared_few<uint16_t, 128, 2>); else GKV_SHARED(uint16_t, k_shared_few<uint16_t, 64, 2>);
@@ -948,9 +962,9 @@ hipError_t launch_shared(const SharedDims& sd, const void* q, const int32_t* cu,
     }
   } else if (bf) {
     if (sd.d == 128) {
-      if (p.split == 1) GKV_SHARED(uint16_t, k_shared_bf<128, 1>); else GKV_SHARED(uint16_t, k_shared_bf<128, 2>);
+      if (p.waves == 8) GKV_SHARED(uint16_t, k_shared_bf<128, 8>); else GKV_SHARED(uint16_t, k_shared_bf<128, 4>);
     } else {
-      if (p.split == 1) GKV_SHARED(uint16_t, k_shared_bf<64, 1>); else GKV_SHARED(uint16_t, k_shared_bf<64, 2>);
+      if (p.waves == 8) GKV_SHARED(uint16_t, k_shared_bf<64, 8>); else GKV_SHARED(uint16_t, k_shared_bf<64, 4>);
     }
   } else {
     if (sd.d == 128) GKV_SHARED(float, k_shared_f32<128>); else GKV_SHARED(float, k_shared_f32<64>);

@@ -50,6 +50,16 @@ __device__ __forceinline__ void buffer_load_lds(Buffer b, uint4* dst, int off) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (__attribute__((address_space(3))) void*)dst, 16, off, 0, 0, 0);
 }
 
+// Workgroup barrier behind the wave's LDS accesses and its loads into LDS but for the last N vector
+// memory operations.  (A fence, as __syncthreads() has it, would wait for those as well.)
+template <int N> __device__ __forceinline__ void loaded_barrier() {
+  static_assert(N >= 0 && N < 64, "the counter's range");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | (N >> 4) << 14);      // s_waitcnt vmcnt(N) lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 // place of 16-byte piece c of key row t in a staged tile: neighbouring rows start in
 // other banks, for the reads along a row (16 rows, one piece) and the transposing ones
 // (8 rows, four pieces)
