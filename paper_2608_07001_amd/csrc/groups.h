@@ -21,7 +21,9 @@ struct SharedDims {
 GKV_HD int first_tile(const SharedDims& sd, const int32_t* cu, int b, int R) {
   return (int)((uint32_t)(held(cu[b], sd.n_seq) * sd.hpg) / (uint32_t)R) + b;
 }
-GKV_HD int64_t most_tiles(const SharedDims& sd, int R) { return (int64_t)sd.n_seq * sd.hpg / R + sd.n_group; }
+GKV_HD int64_t most_tiles(const SharedDims& sd, int R) {
+  return sd.n_group > 1 ? (int64_t)sd.n_seq * sd.hpg / R + sd.n_group : ((int64_t)sd.n_seq * sd.hpg + R - 1) / R;
+}
 GKV_HD int tiles_of_group(const SharedDims& sd, int64_t n, int R) { return (int)((n * sd.hpg + R - 1) / R); }
 
 // Key tiles of a chunk: all row tiles' key tiles over the places that the grid has beside
@@ -38,24 +40,22 @@ struct SharedPlan {
   int waves, rows, places;     // of a workgroup; rows of a tile; workgroups, a multiple of 8
   int64_t tiles;               // row tiles of all KV heads, at most
 };
-#ifndef SH_FEWROWS
-#define SH_FEWROWS 16
-#endif
-#ifndef SH_TARGET
-#define SH_TARGET 256
-#endif
-#ifndef SF_TARGET
-#define SF_TARGET 768
-#endif
-inline SharedPlan shared_plan(const SharedDims& sd) {
+// `entries`: rows of the packed arrays.  The rows and entries of a (group, KV head) are taken as the
+// mean.  Up to 16 rows are few, and up to 64 where they have few entries, which the small tiles spread
+// over the chip with fewer states: the 8B heads, few and many, us: 1 sequence over 512 entries a head 8.8 and
+// 13.9, 8 over 512 10.4 and 13.2, 16 over 2048 15.5 and 15.5, 16 over 16384 40 and 27; fp32 with 64 rows over 2000 12.3 and
+// 15.2.  Beyond, four waves take 64 rows (bf16), eight 128.  The chip holds three of the
+// few's workgroups a CU and one of the others (their tiles fill LDS): with twice the places 64 sequences over 16384
+// entries took 54 us for 41, waiting for a second round.
+inline SharedPlan shared_plan(const SharedDims& sd, int64_t entries) {
   const bool bf = sd.dtype == 1;               // GRACEKV_BF16
   const int64_t mean = ((int64_t)sd.n_seq * sd.hpg + sd.n_group - 1) / sd.n_group;
   SharedPlan p;
-  p.few = mean <= SH_FEWROWS;
+  p.few = mean <= 16 || (mean <= 64 && entries / ((int64_t)sd.n_group * sd.G) <= 2048);
   p.waves = !p.few && bf && mean > 64 ? 8 : 4;
   p.rows = p.few ? 16 : 16 * p.waves;
   p.tiles = most_tiles(sd, p.rows) * sd.G;
-  const int64_t target = p.few ? SF_TARGET : SH_TARGET;
+  const int64_t target = p.few ? 768 : 256;
   const int64_t room = target - p.tiles / 2 > target / 4 ? target - p.tiles / 2 : target / 4;
   p.places = (int)((p.tiles + room + 7) & ~(int64_t)7);
   return p;

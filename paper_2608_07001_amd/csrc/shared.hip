@@ -18,27 +18,20 @@
 // bf16 weights are rounded to bf16 (nearest even) for the second product, their sum takes them
 // unrounded, as in prompts: each is off by at most 2^-8 of itself, at random.  fp32 uses the
 // fp32 matrix instructions.
+#include <algorithm>
+
 #include "tickets.h"
 #include "tiles.h"
 
 namespace gkv {
 
-#ifndef SH_NU
-#define SH_NU 2
-#endif
-#ifndef SF_OCC
-#define SF_OCC 3
-#endif
-#ifndef SF_COST
-#define SF_COST 0.6f
-#endif
-#ifndef SF_JOIN
-#define SF_JOIN 8
-#endif
+constexpr int SF_OCC = 3;                      // few rows: waves a SIMD
+constexpr int SF_JOIN = 8;                     // ... and states that the last of a tile's chunks joins at a time
+constexpr float SF_COST = 0.6f;                // ... and what joining one costs, in steps of a tile, at d = 64 (chunks_of)
 constexpr float SH_LAG = 8.f, SH_TOP = 256.f;  // as in prompt.hip: base-2 units, and as a factor
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 
-int64_t shared_items(const SharedDims& sd) { return most_tiles(sd, 16) * sd.G + 1024; }   // no plan has more workgroups
+int64_t shared_items(const SharedDims& sd) { return most_tiles(sd, 16) * sd.G + 1024; }   // no plan has as many
 
 // Workspace: where every row's states are, or a ticket word of every row tile, then per place and row (max, sum) and
 // the weighted values.
@@ -64,7 +57,10 @@ static SharedWs shared_view(void* base, const SharedDims& sd, const SharedPlan& 
   w.bytes = o;
   return w;
 }
-size_t shared_ws_bytes(const SharedDims& sd) { return shared_view(nullptr, sd, shared_plan(sd)).bytes; }
+// (of either kernel: how many entries there are is told with the call)
+size_t shared_ws_bytes(const SharedDims& sd) {
+  return std::max(shared_view(nullptr, sd, shared_plan(sd, 0)).bytes, shared_view(nullptr, sd, shared_plan(sd, INT64_MAX)).bytes);
+}
 
 __device__ __forceinline__ int64_t held_entries(const PrefixView& px, int64_t row, int64_t& start) {
   int64_t s = px.start[row], c = px.count[row];
@@ -200,7 +196,7 @@ template <int D, int W>
 __global__ __launch_bounds__(64 * W, W / 4) void k_shared_bf(SharedDims sd, int room, const uint16_t* __restrict__ q,
                                                              const int32_t* __restrict__ cu, PrefixView px, float* __restrict__ out,
                                                              float* __restrict__ lse, SharedWs ws) {
-  constexpr int SPLIT = 2, NU = SH_NU, ROWS = 32 * W / SPLIT, KEYS = 32 * NU * SPLIT;
+  constexpr int SPLIT = 2, NU = 2, ROWS = 32 * W / SPLIT, KEYS = 32 * NU * SPLIT;
   constexpr int CH = D / 8;                     // 16-byte pieces of a row
   constexpr int RI = 64 / CH;                   // rows that one load of a wave brings
   constexpr int NI = KEYS / RI / W;             // such loads of a wave and array
@@ -278,25 +274,37 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_shared_bf(SharedDims sd, int 
     uint4* cV = cur + V0;
     const int left = n_keys - t * KEYS;          // entries from this tile on
     const float* cL = (const float*)(cur + L0 + w * KEYS / 4);
-    bool low = false;                            // some log m is below LOW
+    float lk[NU];                                // of the lane's keys
 #pragma unroll
-    for (int i = 0; i < KEYS; i += 64) low |= i + lane < left && cL[i + lane] < LOW;
+    for (int u = 0; u < NU; ++u) lk[u] = cL[32 * (NU * kw + u) + i32];
+    bool low = false;                            // some log m is below LOW, or no number
+#pragma unroll
+    for (int i = 0; i < KEYS; i += 64) low |= i + lane < left && !(cL[i + lane] >= LOW);
     low = __any(low);                            // the same for every wave
+    // log m comes into the sums by a product of its own, in their units and in three bf16 parts, which
+    // hold it, with ones: read from LDS into every lane's sums it would take half as long again as the keys
     f32x16 s[NU];
+    const uint32_t lower = half == 0 ? 0xffffffffu : 0u;
 #pragma unroll
-    for (int u = 0; u < NU; ++u) {               // log m stands in the sums from the start, in their units
-      float lm[16];
-      log_m(cur, u, lm);
+    for (int u = 0; u < NU; ++u) {
+      float g = fmaxf(lk[u], LOW) * root;
+      const uint32_t hi = __float_as_uint(g) & 0xffff0000u;
+      g -= __uint_as_float(hi);
+      const uint32_t mid = __float_as_uint(g) & 0xffff0000u;
+      g -= __uint_as_float(mid);
+      const uint4 part = make_uint4((hi >> 16 | mid) & lower, (__float_as_uint(g) >> 16) & lower, 0, 0);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[u][r] = lm[r] * root;
+      for (int r = 0; r < 16; ++r) s[u][r] = 0.f;
+      s[u] = mfma_bf16_32x32x16(part, make_uint4(0x3f803f80u, 0x3f80u, 0, 0), s[u]);
       asm volatile("" : "+v"(k_at));             // eight places: formed anew, not held in registers
 #pragma unroll
       for (int x = 0; x < KS; ++x) s[u] = mfma_bf16_32x32x16(lds_at(cur, (k_at ^ (32 * x)) + 32 * (NU * kw + u) * RB), qv[x], s[u]);
     }
-    reads_ahead<NU * KS, 1, 4>();
+    reads_ahead<NU * (KS + 1), 1, 8>();
 #pragma unroll
     for (int u = 0; u < NU; ++u) mfma_done16(s[u]);
     if (left < KEYS) {
+      asm volatile("");                          // (a branch: 64 selects in every tile otherwise)
 #pragma unroll
       for (int u = 0; u < NU; ++u) {
         const int rel = left - 32 * (NU * kw + u) - 4 * half;
@@ -314,9 +322,9 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_shared_bf(SharedDims sd, int 
         log_m(cur, u, lm);
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          if (8 * (r / 4) + r % 4 < left - 32 * (NU * kw + u) - 4 * half && lm[r] < LOW) {
+          if (8 * (r / 4) + r % 4 < left - 32 * (NU * kw + u) - 4 * half && !(lm[r] >= LOW)) {
             most = fmaxf(most, lm[r]);
-            s[u][r] = -INFINITY;
+            s[u][r] = lm[r] < LOW ? -INFINITY : lm[r];
           }
       }
       sync_after_lds_stores();
@@ -340,7 +348,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_shared_bf(SharedDims sd, int 
       for (int d = 0; d < DT; ++d) o[d] *= c;
     }
     float ms2 = m == -INFINITY ? 0.f : m * LOG2E;
-    if (__any(m < LOW && m > -INFINITY)) {       // rows that have seen such entries only
+    if (__any(m < LOW && m > -INFINITY)) {       // rows that have seen such entries only (so `low` is true, or the row's keys are none)
       if (m < LOW && m > -INFINITY) ms2 = 0.f;
 #pragma unroll
       for (int u = 0; u < NU; ++u) {
@@ -948,7 +956,7 @@ __global__ __launch_bounds__(SH_T) void k_shared_join(SharedDims sd, int R, int 
 
 hipError_t launch_shared(const SharedDims& sd, const void* q, const int32_t* cu, const PrefixView& px, float* out, float* lse, void* base,
                          hipStream_t st) {
-  const SharedPlan p = shared_plan(sd);
+  const SharedPlan p = shared_plan(sd, px.rows);
   const SharedWs ws = shared_view(base, sd, p);
   const int room = p.places - (int)p.tiles;
   const dim3 grid((unsigned)p.places);

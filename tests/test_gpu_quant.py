@@ -533,10 +533,30 @@ def test_shared_masked_entries(dtype, d, rows):
         c.pre["V"][mask] = math.nan
         c.pre["K"][mask, ::2] = math.inf
         c.check()
-        lm[~mask] = torch.finfo(torch.float32).min             # the lowest value: equal weights among themselves
-        if what == "some":
-            o = c.call()
-            assert torch.isfinite(o.o).all()
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("rows", [2, 40, 140])
+def test_shared_lowest_log_m(dtype, d, rows):
+    # the type's lowest value as a mask: no weight beside other entries, equal weights among themselves; -inf
+    # beside it, rows of whole tiles of them before and behind others
+    low = torch.finfo(torch.float32).min
+    for n, place in ((40, 3), (700, 3), (700, 650)):
+        c = Shared(dtype, d, 1, 3, [rows], [n], seed=7)
+        c.q[:] = 0.0
+        lm = c.pre["logm"]
+        lm[:n] = low
+        lm[5:n:7] = -math.inf
+        c.pre["V"][5:n:7] = math.inf
+        part = c.call()
+        k, v, _ = c.entries(0, 0)
+        seen = lm[:n] == low
+        mean, tol = v[seen].mean(0), (S.B16 * 2 if dtype == "bf16" else 1e-5) * v[seen].abs().mean(0) + 1e-6
+        assert ((part.o.cpu().double() - mean).abs() <= tol).all(), (n, place)
+        assert torch.isfinite(part.lse).all() and (part.lse <= low * 0.999).all()
+        lm[place] = 0.5
+        c.pre["V"][place] = 1.0
+        c.check()
 
 
 @pytest.mark.parametrize("dtype,d", TYPES)

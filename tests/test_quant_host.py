@@ -176,22 +176,25 @@ GROUPS = r"""
 #include <vector>
 #include "groups.h"
 using namespace gkv;
-// rows, key tile's keys as the kernels have them
-static int keys_of(const SharedPlan& p, bool bf) { return bf ? 32 * p.split : (p.split == 4 ? 64 : 32); }
+// a key tile's keys, a chunk's fewest tiles and a row's chunks as the kernels have them
+static int keys_of(const SharedPlan& p, bool bf, int d) { return p.few ? (bf || d == 64 ? 32 : 16) : (bf ? 128 : 32); }
+static int chunks(const SharedPlan& p, int n, int size, int d) { return p.few ? chunks_of(n, size, 0.6f * (d / 64)) : (n + size - 1) / size; }
 int main() {
-  int bf, G, per, B, S;
-  while (scanf("%d %d %d %d %d", &bf, &G, &per, &B, &S) == 5) {
-    SharedDims sd{bf, G, G * per, 64, per, B, S, 0};
+  int bf, G, per, d, B, S;
+  while (scanf("%d %d %d %d %d %d", &bf, &G, &per, &d, &B, &S) == 6) {
+    SharedDims sd{bf, G, G * per, d, per, B, S, 0};
     std::vector<int32_t> cu(S + 1);
     std::vector<long> count(S * G);
     for (auto& x : cu) if (scanf("%d", &x) != 1) return 1;
     for (auto& x : count) if (scanf("%ld", &x) != 1) return 1;
-    const SharedPlan p = shared_plan(sd);
+    long rows = 0;
+    for (long x : count) rows += x;
+    const SharedPlan p = shared_plan(sd, rows);
     int bad = 0;
     // row tiles: each group's own, in order, inside the table
     int64_t last = -1;
     unsigned long long total = 0;
-    const int keys = keys_of(p, bf);
+    const int keys = keys_of(p, bf, d);
     std::vector<std::pair<int, long>> unit;
     for (int b = 0; b < S; ++b) {
       const Span sp = span_of(cu.data(), b, B);
@@ -209,11 +212,11 @@ int main() {
     }
     const int room = (int)(p.places - p.tiles);
     if (room < 1 || p.places % 8) ++bad;
-    const int size = shared_chunk(total, room, 1);
+    const int size = shared_chunk(total, room, p.few ? PA_MIN : 1);
     long long all = 0;
-    for (auto& u : unit) all += (long long)u.first * ((u.second + size - 1) / size);
+    for (auto& u : unit) all += (long long)u.first * chunks(p, (int)u.second, size, d);
     if (all > p.places) ++bad;                  // every chunk has a place
-    printf("%d %d %lld\n", bad, p.places, all);
+    printf("%d %d %d %lld\n", bad, p.few, p.waves, all);
   }
   return 0;
 }
@@ -232,11 +235,12 @@ def test_groups_are_cut_into_what_the_grid_holds(tmp_path):
         cu = [sum(groups[:j]) for j in range(S + 1)]
         top = int(2 ** r.uniform(0, 17))
         counts = [r.randint(0, top) if r.random() < 0.8 else 0 for _ in range(S * G)]
-        text.append(" ".join(map(str, [i % 2, G, per, B, S] + cu + counts)))
+        text.append(" ".join(map(str, [i % 2, G, per, r.choice([64, 128]), B, S] + cu + counts)))
     out = subprocess.run([str(tmp_path / "g")], input="\n".join(text), capture_output=True, text=True, check=True).stdout.splitlines()
     assert len(out) == len(text)
     for line, case in zip(out, text):
         assert line.split()[0] == "0", (line, case[:200])
+    assert {tuple(line.split()[1:3]) for line in out} == {("1", "4"), ("0", "4"), ("0", "8")}       # every kernel among them
 
 
 def test_binding_refuses_other_tensors(monkeypatch):
