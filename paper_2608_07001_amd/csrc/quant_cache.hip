@@ -94,15 +94,21 @@ __device__ __forceinline__ void find_places(const PageDims& pg, const int32_t* t
   if (pg.n_seq <= 64) {
     const int x = min(lane, pg.n_seq - 1);
     const int c0 = cu[x], c1 = cu[x + 1], s = start[x];
-    for (int r = 0; r < rows; ++r) {
-      const int at = max(__popcll(__ballot(lane < pg.n_seq && c0 <= t0 + r)) - 1, 0);      // as find_span has it
+    auto last_at = [&](int64_t row) { return max(__popcll(__ballot(lane < pg.n_seq && c0 <= row)) - 1, 0); };      // as find_span has it
+    auto take = [&](int at) {
       const int32_t span[2] = {__builtin_amdgcn_readlane(c0, at), __builtin_amdgcn_readlane(c1, at)};
-      const int f = __builtin_amdgcn_readlane(s, at);
-      if (lane == r) {
-        b = at;
-        first = f;
-        sp = span_of(span, 0, n);
-      }
+      b = at;
+      first = __builtin_amdgcn_readlane(s, at);
+      sp = span_of(span, 0, n);
+    };
+    const int lo = last_at(t0), hi = last_at(t0 + rows - 1);
+    take(lo);
+    for (int r = 1; r < rows && lo != hi; ++r) {         // a sequence ends among them
+      const int at = last_at(t0 + r);
+      const int was_b = b, was_first = first;
+      const Span was = sp;
+      take(at);
+      if (lane < r) { b = was_b; first = was_first; sp = was; }
     }
   } else {
     b = find_span(cu, pg.n_seq, t0);

@@ -473,19 +473,31 @@ class Prefix:
     logm: torch.Tensor
 
 
-@dataclasses.dataclass
+@dataclasses.dataclass(frozen=True)
 class Part:
     """An attention of the same queries over other entries (gracekv_part), as shared_attention
-    writes it: o [n_seq][H][d] and lse [n_seq][H], fp32."""
+    writes it: o [n_seq][H][d] and lse [n_seq][H], fp32.  Looked over once, when it is made; it
+    holds both tensors, which stay where they are."""
     o: torch.Tensor
     lse: torch.Tensor
+
+    def __post_init__(self):
+        f32, dev = torch.float32, self.o.get_device()
+        if self.o.dim() != 3:
+            raise ValueError(f"part.o: need [n_seq][H][d], got {tuple(self.o.shape)}")
+        arrays = PartArrays(_tensor("part.o", self.o, f32, self.o.shape, dev), _tensor("part.lse", self.lse, f32, self.o.shape[:2], dev))
+        held = object.__setattr__
+        held(self, "device", dev)
+        held(self, "shape", tuple(self.o.shape))
+        held(self, "arrays", arrays)
 
 
 def _part(part: Optional[Part], n: int, H: int, d: int, dev: int):
     if part is None:
         return None
-    return ctypes.byref(PartArrays(_tensor("part.o", part.o, torch.float32, (n, H, d), dev),
-                                   _tensor("part.lse", part.lse, torch.float32, (n, H), dev)))
+    if part.device != dev or part.shape != (n, H, d):
+        raise ValueError(f"part: got {part.shape} on device {part.device}, need {(n, H, d)} on the current device cuda:{dev}")
+    return ctypes.byref(part.arrays)
 
 
 def _packed(prefix: Prefix, n: int, dtype: torch.dtype, d: int, dev: int):

@@ -280,9 +280,15 @@ def test_binding_refuses_other_tensors(monkeypatch):
     with pytest.raises(ValueError, match="n_pages"):             # another cache's shapes
         gk.quant_attention(cfg, four, q, table, i, q, None)
     pages = gk.QuantPages(gk.E2M1, pages.K, pages.V, pages.K_scale, pages.V_scale)
-    part = gk.Part(torch.zeros(1, 4, 64), torch.zeros(1, 3))
     with pytest.raises(ValueError, match="part.lse"):
-        gk.quant_attention(cfg, pages, q, table, i, q, None, part=part)
+        gk.Part(torch.zeros(1, 4, 64), torch.zeros(1, 3))
+    with pytest.raises(ValueError, match="part.o"):
+        gk.Part(torch.zeros(1, 4, 64, dtype=torch.bfloat16), torch.zeros(1, 4))
+    with pytest.raises(ValueError, match="part.o"):
+        gk.Part(torch.zeros(1, 64), torch.zeros(1))
+    with pytest.raises(ValueError, match="part: got"):
+        gk.quant_attention(cfg, pages, q, table, i, q, None, part=gk.Part(torch.zeros(2, 4, 64), torch.zeros(2, 4)))
+    part = gk.Part(torch.zeros(1, 4, 64), torch.zeros(1, 4))
     sc = gk.shared_config(q, 2, 1)
     pre = gk.Prefix(torch.zeros(2, dtype=torch.int64), torch.zeros(2, dtype=torch.int64), torch.zeros(5, 64), torch.zeros(5, 64), torch.zeros(5))
     with pytest.raises(ValueError, match="cu_group"):
