@@ -582,7 +582,7 @@ gracekv_status gracekv_quant_attention(const gracekv_page_config* cfg, const gra
  * share (many questions on one compressed context), each gone through once for its group. */
 typedef struct {
   int32_t dtype, G, H, d;
-  int32_t n_seq, n_group;           /* at least 1; n_group * G <= 65536 */
+  int32_t n_seq, n_group;           /* at least 1; n_group * G <= 65536, n_seq * H <= 2^26 */
   int64_t q_tok;                    /* stride of q's rows */
 } gracekv_shared_config;
 
@@ -600,9 +600,14 @@ gracekv_status gracekv_shared_ws_bytes(const gracekv_shared_config* cfg, size_t*
  *   part       host structure, read by the call: its arrays are written, o 16-byte aligned;
  *              sequences outside every group are left as they are (one without entries belongs to
  *              a group of count 0 and gets 0 and -inf)
- *   ws         gracekv_shared_ws_bytes bytes, which need no initialisation; calls that overlap
- *              on one workspace race
- * bf16: weights are rounded to bf16 for the product with the values, as a prompt's are.
+ *   ws         gracekv_shared_ws_bytes bytes, which need no initialisation unless a word of
+ *              them is one that gracekv_paged_attention excludes; calls that overlap on one
+ *              workspace race, and what they leave in it, or a call whose cu_group descends, has
+ *              to be cleared
+ * bf16: for the product with the values, weights are rounded to bf16, as a prompt's are (groups
+ * of many rows), or in two bf16 parts.  An entry whose logm is finite and below -1e36 (the type's
+ * lowest value, as masks have it) weighs nothing beside others; where a row has only such entries,
+ * the largest of their logm decide, and q.k may be lost beside them.
  * Starts, counts and groups must not change while the call runs. */
 gracekv_status gracekv_shared_attention(const gracekv_shared_config* cfg, const void* q, const int32_t* cu_group,
                                         const gracekv_prefix* prefix, const gracekv_part* part, void* ws,

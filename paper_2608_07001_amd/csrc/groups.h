@@ -16,11 +16,9 @@ struct SharedDims {
   int64_t q_tok;
 };
 
-// Row tiles of every KV head: group b's begin at cu[b] * hpg / R + b, which leaves each
-// at least as many as it needs whatever the groups are.
-GKV_HD int first_tile(const SharedDims& sd, const int32_t* cu, int b, int R) {
-  return (int)((uint32_t)(held(cu[b], sd.n_seq) * sd.hpg) / (uint32_t)R) + b;
-}
+// Row tiles of every KV head: those of group b, whose first sequence is `a`, begin at a * hpg / R + b,
+// which leaves each at least as many as it needs whatever the groups are.
+GKV_HD int first_tile(const SharedDims& sd, int a, int b, int R) { return (int)((uint32_t)(a * sd.hpg) / (uint32_t)R) + b; }
 GKV_HD int64_t most_tiles(const SharedDims& sd, int R) {
   return sd.n_group > 1 ? (int64_t)sd.n_seq * sd.hpg / R + sd.n_group : ((int64_t)sd.n_seq * sd.hpg + R - 1) / R;
 }

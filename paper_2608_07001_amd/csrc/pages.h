@@ -83,11 +83,11 @@ template <int TILE> GKV_HD int tiles_of(int64_t len, int64_t count) {
 // entries come from L2, and joining is not free.  64 sequences with 8 KV heads over 2048
 // shared entries a head 50 us, 61 with the entries counted for every row; 200 with 4 over 1024
 // 33 and 46; 4 with 8 over 2048 16.0 and 16.6; but 16 with 8 over 4096 36 and 31.
-GKV_HD int64_t chunk_room(const PageDims& p, int64_t px_rows, int tile, int few = PA_TARGET / 2, int many = PA_TARGET) {
+GKV_HD int64_t chunk_room(const PageDims& p, int64_t px_rows, int tile) {
   const int64_t R = (int64_t)p.n_seq * p.G;
   const int64_t tiles = R * ((((int64_t)p.width << p.shift) + tile - 1) / tile) + (px_rows ? px_rows / tile + R : 0);
   const int64_t room = (tiles + PA_MIN - 1) / PA_MIN;
-  const int64_t target = R < PA_FEW ? few : many;
+  const int64_t target = R < PA_FEW ? PA_TARGET / 2 : PA_TARGET;
   const int64_t most = target - R / 2 > target / 4 ? target - R / 2 : target / 4;
   return room < 1 ? 1 : (room > most ? most : room);
 }

@@ -6,34 +6,41 @@
 // and lse are joined to that.  No entry: 0 and -inf.
 //
 // The work is a stream over codes, each read once for all query heads of its group: bound by
-// HBM, d + d / 32 bytes a row of e4m3 and half of that for e2m1.  Rows are cut into chunks, found and joined as those of plain
-// pages are (paged_rows.h).
+// HBM, d + d / 32 bytes of a row of e4m3 and d / 2 + d / 32 of e2m1.  Rows are cut into chunks, found and
+// joined as those of plain pages are (paged_rows.h).
 //
 // A wave takes tiles of 32 entries.  Codes become bf16 in registers, two a conversion, the
 // block's power of two in the same instruction, exactly, and everything goes through the bf16 matrix
 // instructions: S^T = K Q^T (entries x heads), whose accumulator holds four entries of one
 // head a lane, the operand layout of O^T = V^T P^T.  Which dims a lane has of a key is
-// free as long as the query agrees, so a key's codes are loaded 16 bytes a lane.
+// free as long as the query agrees, so a key's codes are loaded 16 bytes a lane; which entry is which row
+// of a product is free as well, and is chosen so that a load of values is one piece of memory.
+// (The matrix instructions that take codes and scales themselves were measured first: they keep about 14 bits
+// below the largest of the products that they add at a time, which a logit's error shows, and a query
+// would have to be given to them in 8 bits.)
 // bf16 rows: weights in two bf16 parts, off by at most 2^-15 of themselves; fp32 rows: queries and
 // weights in three, which is all their bits.
+//
+// Measured, bf16: 64 sequences of 1 to 8192 tokens, 8 KV heads of 128, 32 query heads, e4m3: 44 us (4.0 TB/s; the
+// loads alone take 42: pages of 16 tokens lie 2 KB a head apart); 4 sequences of about 128K, 64 query heads,
+// e2m1: 110 to 125 us as the pages lie (4.3 to 4.8 TB/s; the loads alone 104 to 120); one sequence of 8201 tokens
+// 13.1 us, bound by latency: finding the chunk, page ids, two tiles a wave, the states and their join, one
+// after the other.  Two tiles of loads in flight were slower everywhere (15.6, 50.7 and 127 us where one tile
+// in flight took 14.6, 44 and 126): their registers leave a wave less a SIMD.
 #include "paged_rows.h"
 #include "quant.h"
 
 namespace gkv {
 
-#ifndef QP_JOIN
-#define QP_JOIN 8
-#endif
-#ifndef QP_FEW
-#define QP_FEW 768
-#define QP_MANY 1536
-#endif
-#ifndef QP_COST
-#define QP_COST 1.0f
-#endif
-#ifndef QP_OCC
-#define QP_OCC 3
-#endif
+constexpr int QP_JOIN = 8;         // states joined at a time: one sequence 13.9 us with 4, 13.1 with 8, 13.4 with 16
+constexpr float LAG = 8.f;         // (below) a weight is 2^-8 at the row's largest at the least
+
+// Waves a SIMD that the registers have to leave room for.  With four everything spills: 64 sequences
+// 106 us for 44.  e4m3 keys beside an fp32 query's three parts do not fit three either: 64 sequences of 4096 tokens,
+// 8 KV heads of 128, 32 query heads 171 us with three and 114 with two; of e2m1 80 and 87.
+template <typename T, int D, int FMT> constexpr int quant_waves() {
+  return sizeof(T) == 4 && D == 128 && FMT == GRACEKV_E4M3 ? 2 : 3;
+}
 
 // a float's upper 16 bits and what is left
 __device__ __forceinline__ float upper(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
@@ -47,10 +54,10 @@ template <int CTRL> __device__ __forceinline__ float quad_of(float x) {
   return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xf, 0xf, true));
 }
 
-template <typename T, int D, int FMT, int OCC>
-__global__ __launch_bounds__(PA_T, OCC) void k_quant_paged(PageDims pg, QuantDims qd, int64_t q_tok, const T* __restrict__ q,
-                                                           const int32_t* __restrict__ table, const int32_t* __restrict__ len,
-                                                           PartView part, T* __restrict__ out, float* __restrict__ lse, PagedWs ws) {
+template <typename T, int D, int FMT>
+__global__ __launch_bounds__(PA_T, (quant_waves<T, D, FMT>())) void k_quant_paged(
+    PageDims pg, QuantDims qd, int64_t q_tok, const T* __restrict__ q, const int32_t* __restrict__ table, const int32_t* __restrict__ len,
+    PartView part, T* __restrict__ out, float* __restrict__ lse, PagedWs ws) {
   constexpr bool BF = sizeof(T) == 2;
   constexpr int NS = 2, TILE = 16 * NS;
   constexpr int BITS = code_bits<FMT>();
@@ -69,12 +76,11 @@ __global__ __launch_bounds__(PA_T, OCC) void k_quant_paged(PageDims pg, QuantDim
   const int bid = groups > 1 ? blockIdx.x / groups : blockIdx.x, group = groups > 1 ? blockIdx.x % groups : 0;
   Chunk ck;
   const int places = groups > 1 ? gridDim.x / groups : gridDim.x;
-  if (!find_chunk<TILE, false>(pg, PrefixView{}, len, bid, places, join_cost(pg.hpg, D) * QP_COST, ck)) return;
+  if (!find_chunk<TILE, false>(pg, PrefixView{}, len, bid, places, join_cost(pg.hpg, D), ck)) return;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i16 = lane & 15, g4 = lane >> 4;
   const int h0 = group * PA_HEADS, heads = min(PA_HEADS, pg.hpg - h0);
   constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
   const float scale = 1.0f / sqrtf((float)D), sc2 = scale * LOG2E;
-  constexpr float LAG = 8.f;
   const int seq = ck.b, kv = ck.g;
   const int64_t n_page = held_len(pg, len[seq]);
   // the lane's dims of product s: the eight from 4 PD (s / (PD / 8)) + PD g4 + 8 (s % (PD / 8)) on
@@ -347,12 +353,12 @@ __global__ __launch_bounds__(PA_T, OCC) void k_quant_paged(PageDims pg, QuantDim
 hipError_t launch_quant_paged(const PageDims& pg, int format, const QuantDims& qd, int64_t q_tok, const void* q, const int32_t* table,
                               const int32_t* len, const PartView& part, void* out, float* lse, void* ws, hipStream_t st) {
   const PagedWs v = paged_view(ws, pg);
-  const int64_t room = chunk_room(pg, 0, 32, QP_FEW, QP_MANY);
+  const int64_t room = chunk_room(pg, 0, 32);
   const dim3 grid((unsigned)(((int64_t)pg.n_seq * pg.G + room) * ((pg.hpg + PA_HEADS - 1) / PA_HEADS)));
   by_type(pg, format, [&](auto type, auto dim, auto fmt) {
     using T = decltype(type);
     constexpr int D = decltype(dim)::value, FMT = decltype(fmt)::value;
-    hipLaunchKernelGGL((k_quant_paged<T, D, FMT, QP_OCC>), grid, dim3(PA_T), 0, st, pg, qd, q_tok, (const T*)q, table, len, part, (T*)out, lse, v);
+    hipLaunchKernelGGL((k_quant_paged<T, D, FMT>), grid, dim3(PA_T), 0, st, pg, qd, q_tok, (const T*)q, table, len, part, (T*)out, lse, v);
   });
   return hipGetLastError();
 }

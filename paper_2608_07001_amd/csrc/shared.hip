@@ -7,17 +7,29 @@
 //
 // The rows that share keys, hpg of every sequence of the group, fill the tiles of a matrix product, so
 // the entries are gone through once a row tile instead of once a sequence.  One pass with a running maximum and
-// sum, products transposed and tiles in LDS as in prompt.hip; there is no diagonal here, but
-// every entry has a log m, and one of -inf has no weight: its value is replaced by 0 in
-// LDS, since 0 times an infinity is not 0.
+// sum; every entry has a log m, and one of -inf has no weight: its value is replaced by 0, since 0 times an
+// infinity is not 0.  A row tile's entries are cut into chunks, as many as fill the chip, found on
+// the device by a scan over the groups' lengths (find_item).  Three kernels, chosen by shared_plan (groups.h):
 //
-// Few sequences leave few row tiles, so a tile's entries are cut into chunks, as many as fill
-// the chip, found on the device by a scan over the groups' lengths; each leaves a state, and a second
-// kernel joins them, in their order.  Row tiles of one chunk are neighbours on one XCD, whose L2 then holds the chunk.
+// k_shared_few, 16 rows a workgroup: bound by latency.  Its waves have entries of their own, nothing is in LDS
+// before they are merged, and the last of a row tile's chunks joins the states (tickets.h), so that there
+// is one launch.  16 sequences over 2048 entries a head, 8 KV heads of 128, 32 query heads 15.5 us.
 //
-// bf16 weights are rounded to bf16 (nearest even) for the second product, their sum takes them
-// unrounded, as in prompts: each is off by at most 2^-8 of itself, at random.  fp32 uses the
-// fp32 matrix instructions.
+// k_shared_bf, 64 or 128 rows: bound by what feeds the matrix units.  Products are transposed, keys and values go
+// straight into LDS, as in prompt.hip.  64 sequences over 16384 entries, heads as above (256 rows a KV head in two
+// tiles, a chunk a CU, 34 GFLOP) take 40 us, 860 TFLOP/s: 24 in the loop, 4 to launch and find a
+// chunk, 4 to write the states and 7 for k_shared_join.  A step of 128 keys takes 6500 cycles: 2500 logits (reads of
+// LDS, each wave all of the keys), 1350 values, 850 softmax, 1100 the issue of the next tile's loads
+// (64 KB at 64 bytes a cycle), 700 the barrier.  Tried and slower: tiles of 64 keys in four stages, logits a tile ahead
+// (43.7 us for 41.5), twice the chunks (54 for 41).
+//
+// k_shared_f32, 64 rows: the fp32 matrix instructions, tiles of 32 keys through registers into LDS.
+//
+// The latter two leave states, megabytes of them, to k_shared_join, a second launch in which the whole chip
+// reads them and not one workgroup a row tile.
+//
+// bf16 weights are rounded to bf16 (nearest even) for the second product of k_shared_bf, their sum takes them
+// unrounded, as in prompts: each is off by at most 2^-8 of itself, at random.
 #include <algorithm>
 
 #include "tickets.h"
@@ -187,7 +199,7 @@ __device__ __forceinline__ Row row_of(const SharedDims& sd, const Item& it, int 
 }
 // the row tile's place among all of them
 __device__ __forceinline__ int64_t slot_of(const SharedDims& sd, const Item& it, int R) {
-  return (int64_t)((int)((uint32_t)(it.a * sd.hpg) / (uint32_t)R) + it.b + it.tile) * sd.G + it.g;
+  return (int64_t)(first_tile(sd, it.a, it.b, R) + it.tile) * sd.G + it.g;
 }
 
 // Many rows a group: W waves, pairs of them to the same 32 rows with 32 NU keys each of a tile.  One tile is in

@@ -257,6 +257,55 @@ def test_append_and_read_many_sequences(fmt):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype,G,Hq,d,n", [("bf16", 1, 1, 64, 17003), ("f32", 1, 2, 64, 17003), ("bf16", 8, 32, 128, 2500), ("f32", 2, 2, 128, 4099)])
+@pytest.mark.parametrize("B", [1, 5, 64, 65, 900])
+def test_append_and_read_many_rows(fmt, dtype, G, Hq, d, n, B):
+    # several rows a workgroup, sequences (some empty) that end among them, pages and positions that are none
+    gen = torch.Generator().manual_seed(B + n)
+    page = 32
+    cut = torch.cat([torch.zeros(1), torch.randint(0, n - 9, (B - 1,), generator=gen).sort().values.float(), torch.tensor([n - 9.0])]).long()
+    if B > 4:
+        cut[2] = cut[1]
+    new = (cut[1:] - cut[:-1]).tolist()
+    start = torch.randint(0, 100, (B,), generator=gen).tolist()
+    table, n_pages = _tables(gen, [a + b for a, b in zip(start, new)], page)
+    table[torch.rand(table.shape, generator=gen) < 0.05] = -1
+    seq = torch.repeat_interleave(torch.arange(B), torch.tensor(new))
+    place = torch.cat([torch.arange(a, a + m) for a, m in zip(start, new)])
+    at = table[seq, place // page].long()
+    k, v, q = (_rand(gen, n, x, d, dtype=dtype) for x in (G, G, Hq))
+    pos = torch.randint(-3, 405, (n,), generator=gen).to(torch.int32)
+    cos, sin = _rope(400, d)
+    ok = torch.nonzero((at >= 0) & (pos[:n - 9] >= 0) & (pos[:n - 9] < 400))[:, 0]
+    dev = [torch.zeros_like(x).cuda() for x in _pools(gen, n_pages, G, page, d, fmt)]
+    pages = gk.QuantPages(fmt, *dev)
+    cfg = gk.quant_config(pages, DT[dtype], Hq, table)
+    qd = q.cuda()
+    args = table.cuda(), _i32(*start), _cu(new).cuda()
+    gk.quant_append(cfg, pages, k.cuda(), v.cuda(), *args, pos.cuda(), cos.cuda(), sin.cuda(), qd, qd)
+    want = [torch.zeros(x.shape, dtype=torch.uint8) for x in dev]
+    p = pos.clamp(0, 399).long()
+    kc, ks = Q.quantise(Q.rotated32(k, cos[p], sin[p])[ok].double(), fmt)
+    vc, vs = Q.quantise(v[ok].double(), fmt)
+    for w, x in zip(want, (Q.packed(kc, fmt), Q.packed(vc, fmt), ks, vs)):
+        w[at[ok], :, place[ok] % page] = x
+    for name, got, w in zip(("K", "V", "K_scale", "V_scale"), dev, want):
+        assert torch.equal(got.cpu(), w), name
+    q[ok] = Q.rotated32(q, cos[p], sin[p])[ok].to(DT[dtype])
+    assert torch.equal(qd.cpu(), q)
+    back = [torch.full((n, G, d), 7.0, dtype=DT[dtype], device="cuda") for _ in range(2)]
+    gk.quant_read(cfg, pages, *args, *back)
+    for got, c, s in zip(back, (kc, vc), (ks, vs)):
+        x = torch.zeros(n, G, d, dtype=torch.float64)          # no page: 0; a place that was left out: what it held, 0
+        x[ok] = Q.values(Q.packed(c, fmt), s, fmt)
+        x[n - 9:] = 7
+        x = torch.where(x == 0, 0.0, x)
+        got = got.cpu().double()
+        # a place that held nothing is code 0 under scale 0: 0
+        assert torch.equal(torch.where(got == 0, 0.0, got), x)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
 def test_append_and_read_nothing_or_descending(fmt):
     gen = torch.Generator().manual_seed(5)
     table, n_pages = _tables(gen, [40, 40, 40], 16)

@@ -199,7 +199,7 @@ int main() {
     for (int b = 0; b < S; ++b) {
       const Span sp = span_of(cu.data(), b, B);
       const int mt = tiles_of_group(sd, sp.n, p.rows);
-      const int64_t a = first_tile(sd, cu.data(), b, p.rows);
+      const int64_t a = first_tile(sd, (int)sp.a, b, p.rows);
       if (mt && a <= last) ++bad;
       if (mt) last = a + mt - 1;
       if (mt && (last + 1) * G > p.tiles) ++bad;
