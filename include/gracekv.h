@@ -508,7 +508,7 @@ gracekv_status gracekv_paged_attention(const gracekv_page_config* cfg, const voi
 /* An attention of the same queries over other entries, to be joined to one over pages: out
  * and lse become those over both.  gracekv_shared_attention writes one. */
 typedef struct {
-  float* o;                         /* [n_seq][H][d] fp32: the mean of the values; not out */
+  float* o;                         /* [n_seq][H][d] fp32, 16-byte aligned: the mean of the values; not out */
   float* lse;                       /* [n_seq][H] fp32; -inf: over no entry, whatever its row of o holds */
 } gracekv_part;
 
@@ -597,7 +597,7 @@ gracekv_status gracekv_shared_ws_bytes(const gracekv_shared_config* cfg, size_t*
  *              they descend, the call stays inside the arrays, but what it writes there is
  *              not specified
  *   prefix     host structure, read by the call
- *   part       host structure, read by the call: its arrays are written, o 16-byte aligned;
+ *   part       host structure, read by the call: its arrays are written;
  *              sequences outside every group are left as they are (one without entries belongs to
  *              a group of count 0 and gets 0 and -inf)
  *   ws         gracekv_shared_ws_bytes bytes, which need no initialisation unless a word of
@@ -607,7 +607,7 @@ gracekv_status gracekv_shared_ws_bytes(const gracekv_shared_config* cfg, size_t*
  * bf16: for the product with the values, weights are rounded to bf16, as a prompt's are (groups
  * of many rows), or in two bf16 parts.  An entry whose logm is finite and below -1e36 (the type's
  * lowest value, as masks have it) weighs nothing beside others; where a row has only such entries,
- * the largest of their logm decide, and q.k may be lost beside them.
+ * the largest of their logm decide, and q.k may be lost beside them.  logm has to stay below 1e36.
  * Starts, counts and groups must not change while the call runs. */
 gracekv_status gracekv_shared_attention(const gracekv_shared_config* cfg, const void* q, const int32_t* cu_group,
                                         const gracekv_prefix* prefix, const gracekv_part* part, void* ws,

@@ -686,7 +686,7 @@ gracekv_status gracekv_paged_ws_bytes(const gracekv_page_config* c, size_t* ws_b
 static bool part_view(const gracekv_part* part, PartView* v) {
   *v = PartView{nullptr, nullptr};
   if (!part) return true;
-  if (!part->o || !part->lse || !aligned16(part->o) || !aligned16(part->lse)) return false;
+  if (!part->o || !part->lse || !aligned16(part->o)) return false;
   *v = PartView{part->o, part->lse};
   return true;
 }

@@ -31,6 +31,14 @@ GKV_HD int shared_chunk(uint64_t total, int room, int least) {
   return size < (uint64_t)least ? least : (size > 0x7fffffff ? 0x7fffffff : (int)size);
 }
 
+// The item of workgroup `bid` of `places` (a multiple of 8), `all` items in order: neighbours go to one XCD,
+// workgroups going round the eight.  -1: none.  Groups that descend can make more items than places, of which
+// the last are left out: an item's number is its place in the workspace.
+GKV_HD int item_of(int bid, int all, int places) {
+  const int n = all < places ? all : places, per = (n + 7) / 8, at = bid >> 3, id = (bid & 7) * per + at;
+  return at < per && id < n ? id : -1;
+}
+
 constexpr int SH_T = 256;
 constexpr int SH_W = SH_T / 64;
 struct SharedPlan {

@@ -146,10 +146,9 @@ __device__ __forceinline__ bool find_item(const SharedDims& sd, const int32_t* c
       if (lane >= o) to += y;
     }
     const int all = base + __builtin_amdgcn_readlane(to, 63);
-    if (units <= 64) {                   // neighbouring items to one XCD, workgroups going round the eight
-      const int per = (all + 7) / 8, at = id >> 3;
-      id = (id & 7) * per + at;
-      if (at >= per || id >= all) return false;
+    if (units <= 64) {
+      id = item_of(id, all, gridDim.x);
+      if (id < 0) return false;
     }
     if (id < all) {
       const int at = __popcll(__ballot(base + to <= id));       // the unit's lane
@@ -741,7 +740,8 @@ __global__ __launch_bounds__(SH_T, SF_OCC) void k_shared_few(SharedDims sd, int 
     float4 ov[SF_JOIN][2];
 #pragma unroll
     for (int x = 0; x < SF_JOIN; ++x) {            // past the last: that one again
-      const int64_t p = (first + (int64_t)min(c0 + x, it.chunks - 1) * it.tiles) * ROWS;
+      const int64_t id = first + (int64_t)min(c0 + x, it.chunks - 1) * it.tiles;
+      const int64_t p = (id < gridDim.x ? id : gridDim.x - 1) * ROWS;        // (past the places only where groups descend: item_of)
       ml[x] = ld_agent((const unsigned long long*)(ws.ml + p + r));
       const Buffer from = state_buffer(ws.o + p * D, ROWS * D);
 #pragma unroll

@@ -473,7 +473,7 @@ class Prefix:
     logm: torch.Tensor
 
 
-@dataclasses.dataclass(frozen=True)
+@dataclasses.dataclass(frozen=True, eq=False)
 class Part:
     """An attention of the same queries over other entries (gracekv_part), as shared_attention
     writes it: o [n_seq][H][d] and lse [n_seq][H], fp32.  Looked over once, when it is made; it
@@ -533,7 +533,7 @@ def paged_attention(cfg: PageConfig, q, K_pages, V_pages, block_table, seq_len, 
         "paged_attention")
 
 
-@dataclasses.dataclass(frozen=True)
+@dataclasses.dataclass(frozen=True, eq=False)
 class QuantPages:
     """Quantised pages of one layer (gracekv_quant_pages): codes K, V uint8 [n_pages][G][page_size][d]
     (E4M3) or [..][d / 2] (E2M1), scales K_scale, V_scale uint8 [n_pages][G][page_size][d / 32]; pages

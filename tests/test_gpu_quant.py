@@ -632,6 +632,25 @@ def test_shared_many_units_and_groups():
     Shared("f32", 64, 2, 4, _counts(3, 80, 0, 3), _counts(4, 160, 0, 400), seed=9).check()
 
 
+@pytest.mark.parametrize("rows", [2, 100])
+def test_shared_far_entries(rows):
+    # entries past 2^31 elements and 2^32 bytes of the packed arrays
+    c = Shared("bf16", 128, 2, 4, [rows], [333, 150], seed=4)
+    n, far = c.pre["K"].shape[0], (1 << 24) + 77
+    dev = {k: x.cuda() for k, x in c.pre.items()}
+    for k in ("K", "V", "logm"):
+        x = torch.empty((far + n,) + dev[k].shape[1:], dtype=dev[k].dtype, device="cuda")
+        x[far:] = dev[k]
+        dev[k] = x
+    dev["start"] = dev["start"] + far
+    q = c.q.cuda()
+    cfg = gk.shared_config(q, 2, 1)
+    # (and the part's lse on no boundary of 16 bytes)
+    part = gk.Part(torch.zeros(rows, 4, 128, device="cuda"), torch.zeros(rows * 4 + 1, device="cuda")[1:].view(rows, 4))
+    gk.shared_attention(cfg, q, c.cu.cuda(), gk.Prefix(**dev), part, torch.empty(gk.shared_ws_bytes(cfg), dtype=torch.uint8, device="cuda"))
+    c.check(part)
+
+
 def test_shared_malformed_inputs_stay_inside():
     for dtype, d in TYPES:
         c = Shared(dtype, d, 2, 4, [4, 3, 2], [10, 20, 5, 6, 7, 8], seed=9)
@@ -645,6 +664,19 @@ def test_shared_malformed_inputs_stay_inside():
         for cu in ([9, 3, 7, 0], [0, 9, 0, 9], [-5, 2 ** 31 - 1, -2 ** 31, 7], [9, 9, 9, 9], [0, 0, 0, 0]):
             c.cu = torch.tensor(cu, dtype=torch.int32)
             c.call()
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("B,per,n", [(700, 4, 300), (700, 4, 5), (60, 1, 200)])
+def test_shared_descending_groups_stay_inside(dtype, d, B, per, n):
+    # every second group has all sequences: many more chunks than places, none of them written behind the workspace
+    S = 21
+    c = Shared(dtype, d, 3, 3 * per, [B] + [0] * (S - 1), [n] * (3 * S), seed=10)
+    c.cu = torch.tensor([B * (j % 2) for j in range(S + 1)], dtype=torch.int32)
+    need = gk.shared_ws_bytes(gk.shared_config(c.q, 3, S))
+    ws = torch.full((4 * need + (64 << 20),), 85, dtype=torch.uint8, device="cuda")
+    c.call(ws=ws[:need])                                        # (what the rows hold is not specified)
+    assert (ws[need:] == 85).all()
 
 
 def test_shared_entries_of_no_rows():

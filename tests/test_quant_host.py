@@ -125,7 +125,7 @@ def test_attention_refuses_pointers_and_workspaces():
     assert _attend(c, p, q_tok=4) == -1 and _attend(c, p, q_tok=-4096) == -1
     assert _attend(c, p, n=gk.paged_ws_bytes(c) - 1) == -4
     f = gk.lib().gracekv_paged_attention_part
-    for bad in (_part(o=None), _part(lse=None), _part(o=ODD), _part(lse=ODD)):
+    for bad in (_part(o=None), _part(lse=None), _part(o=ODD)):
         assert _attend(c, p, part=bad) == -1
         assert f(ctypes.byref(c), FAKE, 4096, FAKE, FAKE, FAKE, FAKE, None, ctypes.byref(bad), FAKE, None, FAKE, 0, None) == -1
     assert _attend(c, p, part=_part()) == -4
@@ -241,6 +241,62 @@ def test_groups_are_cut_into_what_the_grid_holds(tmp_path):
     for line, case in zip(out, text):
         assert line.split()[0] == "0", (line, case[:200])
     assert {tuple(line.split()[1:3]) for line in out} == {("1", "4"), ("0", "4"), ("0", "8")}       # every kernel among them
+
+
+DESCENDING = r"""
+#include <stdio.h>
+#include <vector>
+#include "groups.h"
+using namespace gkv;
+int main() {
+  int G, per, B, S, n;
+  while (scanf("%d %d %d %d %d", &G, &per, &B, &S, &n) == 5) {
+    SharedDims sd{1, G, G * per, 128, per, B, S, 0};
+    std::vector<int32_t> cu(S + 1);
+    for (auto& x : cu) if (scanf("%d", &x) != 1) return 1;
+    const SharedPlan p = shared_plan(sd, (int64_t)n * S * G);
+    const int keys = p.few ? 32 : 128, tiles = (n + keys - 1) / keys;
+    int bad = 0, seen = 0;
+    long long all = 0;
+    unsigned long long total = 0;
+    for (int b = 0; b < S; ++b) {
+      const Span sp = span_of(cu.data(), b, B);
+      const int mt = tiles_of_group(sd, sp.n, p.rows);
+      total += (unsigned long long)G * mt * tiles;
+      all += (long long)G * mt;
+      if (mt && (int64_t)(first_tile(sd, (int)sp.a, b, p.rows) + mt) * G > p.tiles) ++bad;        // a ticket of every row tile
+    }
+    const int size = shared_chunk(total, (int)(p.places - p.tiles), p.few ? PA_MIN : 1);
+    all *= p.few ? chunks_of(tiles, size, 1.2f) : (tiles + size - 1) / size;
+    std::vector<char> taken(p.places);
+    for (int bid = 0; bid < p.places; ++bid) {
+      const int id = item_of(bid, (int)all, p.places);
+      if (id < -1 || id >= p.places || (id >= 0 && taken[id])) ++bad;
+      else if (id >= 0) { taken[id] = 1; ++seen; }
+    }
+    if (seen != (all < p.places ? all : p.places)) ++bad;
+    printf("%d %d\n", bad, all > p.places);
+  }
+  return 0;
+}
+"""
+
+
+def test_descending_groups_stay_inside_the_workspace(tmp_path):
+    # bounds that go up and down give rows to several groups: more items than the grid has places
+    (tmp_path / "g.cpp").write_text(DESCENDING)
+    subprocess.run(["g++", "-O1", "-std=c++17", "-Wall", "-Werror", "-I", os.path.join(ROOT, "paper_2608_07001_amd", "csrc"),
+                    str(tmp_path / "g.cpp"), "-o", str(tmp_path / "g")], check=True)
+    r, text = random.Random(2), []
+    for _ in range(1000):
+        G, S, B = r.choice([1, 2, 3]), r.randint(1, 64), int(2 ** r.uniform(0, 13))
+        cu = r.choice([[B * (j % 2) for j in range(S + 1)], [r.randint(-3, B + 3) for _ in range(S + 1)]])
+        text.append(" ".join(map(str, [G, r.choice([1, 4, 8, 20]), B, S, int(2 ** r.uniform(0, 15))] + cu)))
+    out = subprocess.run([str(tmp_path / "g")], input="\n".join(text), capture_output=True, text=True, check=True).stdout.splitlines()
+    assert len(out) == len(text)
+    for line, case in zip(out, text):
+        assert line.split()[0] == "0", (line, case[:200])
+    assert sum(line.split()[1] == "1" for line in out) > 50
 
 
 def test_binding_refuses_other_tensors(monkeypatch):
