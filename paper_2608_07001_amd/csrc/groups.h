@@ -47,21 +47,28 @@ struct SharedPlan {
   int64_t tiles;               // row tiles of all KV heads, at most
 };
 // `entries`: rows of the packed arrays.  The rows and entries of a (group, KV head) are taken as the
-// mean.  Up to 16 rows are few, and up to 64 where they have few entries, which the small tiles spread
-// over the chip with fewer states: the 8B heads, few and many, us: 1 sequence over 512 entries a head 8.8 and
-// 13.9, 8 over 512 10.4 and 13.2, 16 over 2048 15.5 and 15.5, 16 over 16384 40 and 27; fp32 with 64 rows over 2000 12.3 and
-// 15.2.  Beyond, four waves take 64 rows (bf16), eight 128.  The chip holds three of the
-// few's workgroups a CU and one of the others (their tiles fill LDS): with twice the places 64 sequences over 16384
-// entries took 54 us for 41, waiting for a second round.
+// mean.  Small tiles spread little work over the chip with fewer states and one launch, large ones go through keys
+// and values fewer times.  us, small and large tiles, bf16, heads of 128: 4 to 16 rows over 1024 entries 11 and 13, over
+// 16384 25 to 27 and 24 to 26, over 65536 78 and 52 to 64; 64 rows of 8 KV heads over 1024 11.9 and 14.5, over 4096 20.8 and
+// 17.2; 128 over 2048 17.1 and 18.2; 256 over 512 14.7 and 17.5, over 2048 24.7 and 20.6; heads of 64, 2 KV heads,
+// 128 rows over 8192 15.8 and 16.5, 32 over 16384 18.6 and 16.0.  fp32, heads of 128: 8 rows over 65536 124 and 212, 64 over
+// 1024 14.6 and 18.0, over 4096 30.1 and 27.9; 256 over 512 20.8 and 21.7, over 2048 46 and 42.
+// Large tiles have 64 rows (four waves), in bf16 for more rows 128 (eight).  The chip holds three of the
+// small ones' workgroups a CU, two of the fp32 ones (256 rows over 16384 entries 226 us with places for one, 191 for two,
+// over 2048 43.8 and 42.3) and one of the others, whose tiles fill LDS: with twice the places 256 rows over 16384
+// took 54 us for 41, waiting for a second round.
 inline SharedPlan shared_plan(const SharedDims& sd, int64_t entries) {
   const bool bf = sd.dtype == 1;               // GRACEKV_BF16
   const int64_t mean = ((int64_t)sd.n_seq * sd.hpg + sd.n_group - 1) / sd.n_group;
   SharedPlan p;
-  p.few = mean <= 16 || (mean <= 64 && entries / ((int64_t)sd.n_group * sd.G) <= 2048);
+  const int64_t each = entries / ((int64_t)sd.n_group * sd.G), tiles = (mean + 15) / 16, wide = sd.d / 64;
+  // in products of 16 rows, 32 keys and 64 dims, and where no row has a long way to go
+  const bool little = entries / 32 <= (bf ? 10240 : 5120) / (tiles * wide) && each <= (bf && wide > 1 ? 2560 : 10240);
+  p.few = little || (bf ? mean <= 16 && each <= 32768 : mean <= 32);
   p.waves = !p.few && bf && mean > 64 ? 8 : 4;
   p.rows = p.few ? 16 : 16 * p.waves;
   p.tiles = most_tiles(sd, p.rows) * sd.G;
-  const int64_t target = p.few ? 768 : 256;
+  const int64_t target = p.few ? 768 : (bf ? 256 : 512);
   const int64_t room = target - p.tiles / 2 > target / 4 ? target - p.tiles / 2 : target / 4;
   p.places = (int)((p.tiles + room + 7) & ~(int64_t)7);
   return p;

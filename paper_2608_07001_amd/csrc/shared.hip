@@ -11,13 +11,13 @@
 // infinity is not 0.  A row tile's entries are cut into chunks, as many as fill the chip, found on
 // the device by a scan over the groups' lengths (find_item).  Three kernels, chosen by shared_plan (groups.h):
 //
-// k_shared_few, 16 rows a workgroup: bound by latency.  Its waves have entries of their own, nothing is in LDS
+// k_shared_few, 16 rows a workgroup, for little work: bound by latency.  Its waves have entries of their own, nothing is in LDS
 // before they are merged, and the last of a row tile's chunks joins the states (tickets.h), so that there
 // is one launch.  16 sequences over 2048 entries a head, 8 KV heads of 128, 32 query heads 15.5 us.
 //
 // k_shared_bf, 64 or 128 rows: bound by what feeds the matrix units.  Products are transposed, keys and values go
 // straight into LDS, as in prompt.hip.  64 sequences over 16384 entries, heads as above (256 rows a KV head in two
-// tiles, a chunk a CU, 34 GFLOP) take 40 us, 860 TFLOP/s: 24 in the loop, 4 to launch and find a
+// tiles, a chunk a CU, 17 GFLOP) take 40 us, 430 TFLOP/s: 24 in the loop, 4 to launch and find a
 // chunk, 4 to write the states and 7 for k_shared_join.  A step of 128 keys takes 6500 cycles: 2500 logits (reads of
 // LDS, each wave all of the keys), 1350 values, 850 softmax, 1100 the issue of the next tile's loads
 // (64 KB at 64 bytes a cycle), 700 the barrier.  Tried and slower: tiles of 64 keys in four stages, logits a tile ahead
