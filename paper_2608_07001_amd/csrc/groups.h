@@ -46,32 +46,42 @@ struct SharedPlan {
   int waves, rows, places;     // of a workgroup; rows of a tile; workgroups, a multiple of 8
   int64_t tiles;               // row tiles of all KV heads, at most
 };
-// `entries`: rows of the packed arrays.  The rows and entries of a (group, KV head) are taken as the
-// mean.  Small tiles spread little work over the chip with fewer states and one launch, large ones go through keys
-// and values fewer times.  us, small and large tiles, bf16, heads of 128: 4 to 16 rows over 1024 entries 11 and 13, over
-// 16384 25 to 27 and 24 to 26, over 65536 78 and 52 to 64; 64 rows of 8 KV heads over 1024 11.9 and 14.5, over 4096 20.8 and
-// 17.2; 128 over 2048 17.1 and 18.2; 256 over 512 14.7 and 17.5, over 2048 24.7 and 20.6; heads of 64, 2 KV heads,
-// 128 rows over 8192 15.8 and 16.5, 32 over 16384 18.6 and 16.0.  fp32, heads of 128: 8 rows over 65536 124 and 212, 64 over
-// 1024 14.6 and 18.0, over 4096 30.1 and 27.9; 256 over 512 20.8 and 21.7, over 2048 46 and 42.
-// Large tiles have 64 rows (four waves), in bf16 for more rows 128 (eight).  The chip holds three of the
-// small ones' workgroups a CU, two of the fp32 ones (256 rows over 16384 entries 226 us with places for one, 191 for two,
-// over 2048 43.8 and 42.3) and one of the others, whose tiles fill LDS: with twice the places 256 rows over 16384
-// took 54 us for 41, waiting for a second round.
-inline SharedPlan shared_plan(const SharedDims& sd, int64_t entries) {
-  const bool bf = sd.dtype == 1;               // GRACEKV_BF16
-  const int64_t mean = ((int64_t)sd.n_seq * sd.hpg + sd.n_group - 1) / sd.n_group;
+// The chip holds three of the small tiles' workgroups of four waves a CU, one or two of eight (their registers), two of
+// the fp32 ones of large tiles (256 rows over 16384 entries 226 us with places for one, 191 for two) and one of the
+// bf16 ones, whose tiles fill LDS: with twice the places 256 rows over 16384 took 54 us for 41, waiting for a second round.
+inline SharedPlan plan_of(const SharedDims& sd, bool few, int waves) {
   SharedPlan p;
-  const int64_t each = entries / ((int64_t)sd.n_group * sd.G), tiles = (mean + 15) / 16, wide = sd.d / 64;
-  // in products of 16 rows, 32 keys and 64 dims, and where no row has a long way to go
-  const bool little = entries / 32 <= (bf ? 10240 : 5120) / (tiles * wide) && each <= (bf && wide > 1 ? 2560 : 10240);
-  p.few = little || (bf ? mean <= 16 && each <= 32768 : mean <= 32);
-  p.waves = !p.few && bf && mean > 64 ? 8 : 4;
-  p.rows = p.few ? 16 : 16 * p.waves;
+  p.few = few;
+  p.waves = waves;
+  p.rows = few ? 16 : 16 * waves;
   p.tiles = most_tiles(sd, p.rows) * sd.G;
-  const int64_t target = p.few ? 768 : (bf ? 256 : 512);
+  const int64_t target = few ? (waves == 8 ? 256 : 768) : (sd.dtype == 1 ? 256 : 512);
   const int64_t room = target - p.tiles / 2 > target / 4 ? target - p.tiles / 2 : target / 4;
   p.places = (int)((p.tiles + room + 7) & ~(int64_t)7);
   return p;
+}
+// `entries`: rows of the packed arrays.  The rows and entries of a (group, KV head) are taken as the
+// mean.  Small tiles spread little work over the chip with fewer states and one launch, large ones go through keys
+// and values fewer times.  us, heads of 128, small tiles with four waves, with eight, large tiles:
+//   bf16, 8 KV heads, 16 rows each: over 128 entries 9.4, 8.3, 12.4; 1024 11.3, 11.7, 12.8; 4096 18.7, 16.9, 17.4; 16384 27.4, 25.4, 25.6
+//   64 rows: over 256 10.1, 10.6, 13.6; 2048 15.0, 14.1, 15.1; 4096 20.7, 16.8, 17.3; 8192 27.5, 37, 30
+//   256 rows: over 512 14.8, 12.6, 17.3; 1024 19.6, 16.8, 18.1; 2048 24.2, 24.2, 20.6; 8192 50, 54, 29
+//   fp32, 16 rows: over 2048 17.8, 19.7, 18.9; 8192 27, 30, 35; 32 rows: over 4096 21.3, 23.7, 25.5; 16384 78, 55, 68
+//   128 rows: over 256 10.9, 12.8, 16.1; 1024 21.1, 18.0, 22.6; 2048 28.8, 23.4, 26.0; 8192 71, 66, 58
+// and heads of 64 (four waves; eight are slower at all sizes), 2 KV heads: 128 rows over 8192 15.8 and 16.5, 32 over 16384 18.6 and 16.0.
+// Large tiles have 64 rows (four waves), in bf16 for more rows 128 (eight).
+inline SharedPlan shared_plan(const SharedDims& sd, int64_t entries) {
+  const bool bf = sd.dtype == 1;               // GRACEKV_BF16
+  const bool wide = sd.d > 64;
+  const int64_t heads = (int64_t)sd.n_group * sd.G, mean = ((int64_t)sd.n_seq * sd.hpg + sd.n_group - 1) / sd.n_group;
+  const int64_t each = entries / heads, tiles = (mean + 15) / 16;
+  const int64_t steps = tiles * ((entries < (int64_t)1 << 40 ? entries : (int64_t)1 << 40) / 32);       // products of 16 rows and 32 keys
+  const bool little = steps <= (bf && !wide ? 10240 : 4352) && each <= 10240;
+  if (little || (bf ? mean <= 16 && each <= 32768 : mean <= 32)) {
+    const bool eight = wide && (bf ? each > 1536 || each <= 160 || steps >= 960 : mean > 16 && steps * tiles * heads >= 35000);
+    return plan_of(sd, true, eight ? 8 : 4);
+  }
+  return plan_of(sd, false, bf && mean > 64 ? 8 : 4);
 }
 
 }  // namespace gkv

@@ -69,9 +69,12 @@ static SharedWs shared_view(void* base, const SharedDims& sd, const SharedPlan& 
   w.bytes = o;
   return w;
 }
-// (of either kernel: how many entries there are is told with the call)
+// (of any kernel: how many entries there are is told with the call)
 size_t shared_ws_bytes(const SharedDims& sd) {
-  return std::max(shared_view(nullptr, sd, shared_plan(sd, 0)).bytes, shared_view(nullptr, sd, shared_plan(sd, INT64_MAX)).bytes);
+  size_t n = 0;
+  for (bool few : {false, true})
+    for (int waves : {4, 8}) n = std::max(n, shared_view(nullptr, sd, plan_of(sd, few, waves)).bytes);
+  return n;
 }
 
 __device__ __forceinline__ int64_t held_entries(const PrefixView& px, int64_t row, int64_t& start) {
@@ -467,9 +470,10 @@ __device__ __forceinline__ float4 ld_agent16(Buffer b, int byte) {
 // Few rows a group: 16 of them a workgroup, whose waves have a tile of 16 NS entries each at a time, keys
 // straight from memory as the product's operand and values paired up in registers, as over pages
 // (paged.hip), and no LDS before the waves are merged.  The last of a row tile's chunks joins them.
+// Eight waves halve the states of longer rows, which is what four wait for (groups.h has both measured).
 // bf16 weights are in two bf16 parts here, which costs a memory-bound kernel nothing.
-template <typename T, int D, int NS>
-__global__ __launch_bounds__(SH_T, SF_OCC) void k_shared_few(SharedDims sd, int room, const T* __restrict__ q, const int32_t* __restrict__ cu,
+template <typename T, int D, int NS, int W>
+__global__ __launch_bounds__(64 * W, W == 8 ? 2 : SF_OCC) void k_shared_few(SharedDims sd, int room, const T* __restrict__ q, const int32_t* __restrict__ cu,
                                                              PrefixView px, float* __restrict__ out, float* __restrict__ lse, SharedWs ws) {
   constexpr bool BF = sizeof(T) == 2;
   constexpr int ROWS = 16, TILE = 16 * NS;
@@ -478,12 +482,14 @@ __global__ __launch_bounds__(SH_T, SF_OCC) void k_shared_few(SharedDims sd, int 
   constexpr int VD = BF ? D / 16 : 4;         // neighbouring dims of a lane
   constexpr int VB = BF ? 1 : D / 64;         // ... in so many places of the row
   constexpr int VW = VD * (int)sizeof(T) / 4; // words of one place
-  __shared__ float sM[SH_W][ROWS], sL[SH_W][ROWS];
-  __shared__ __align__(16) float sO[SH_W][ROWS][D + 4];      // rows start in other banks
+  __shared__ float sM[W][ROWS], sL[W][ROWS];
+  __shared__ __align__(16) float sO[W][ROWS][D + 4];      // rows start in other banks
   __shared__ int joins;
   Item it;
-  const float join = SF_COST * (D / 64);
-  if (!find_item<ROWS, TILE, PA_MIN, SH_W>(sd, cu, px, room, [&](int n, int size) { return chunks_of(n, size, join); }, it)) return;
+  // (chunks of eight waves are counted in pairs of tiles)
+  constexpr int PAIR = W / SH_W;
+  const float join = SF_COST * (D / 64) / PAIR;
+  if (!find_item<ROWS, TILE * PAIR, PA_MIN, W>(sd, cu, px, room, [&](int n, int size) { return chunks_of(n, size, join); }, it)) return;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i16 = lane & 15, g4 = lane >> 4;
   const float scale = 1.0f / sqrtf((float)D);
   int64_t seq;
@@ -542,14 +548,14 @@ __global__ __launch_bounds__(SH_T, SF_OCC) void k_shared_few(SharedDims sd, int 
 #pragma unroll
     for (int j = 0; j < VD; ++j) o[p][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;               // of row i16, natural units; l: this lane's entries only
-  const int t1 = n_keys > 0 ? it.t1 : it.t0;
-  int ti = it.t0 + w;
+  const int t1 = n_keys > 0 ? min(it.t1 * PAIR, (n_keys + TILE - 1) / TILE) : 0;
+  int ti = it.t0 * PAIR + w;
   if (ti < t1) {
     load_keys(ti);
     load_values(ti);
   }
-  for (; ti < t1; ti += SH_W) {
-    const bool more = ti + SH_W < t1;
+  for (; ti < t1; ti += W) {
+    const bool more = ti + W < t1;
     float x[NS][4];
 #pragma unroll
     for (int h = 0; h < NS; ++h) {
@@ -572,7 +578,7 @@ __global__ __launch_bounds__(SH_T, SF_OCC) void k_shared_few(SharedDims sd, int 
 #pragma unroll
       for (int r = 0; r < 4; ++r) x[h][r] = acc[r] * scale;
     }
-    if (more) load_keys(ti + SH_W);
+    if (more) load_keys(ti + W);
     bool any = false;
 #pragma unroll
     for (int h = 0; h < NS; ++h)
@@ -663,7 +669,7 @@ __global__ __launch_bounds__(SH_T, SF_OCC) void k_shared_few(SharedDims sd, int 
 #pragma unroll
             for (int j = 0; j < VD; ++j) o[p][j] = mfma_f32_16x16x4(__uint_as_float(tv[h][r][p][j]), pr[h][r], o[p][j]);
     }
-    if (more) load_values(ti + SH_W);
+    if (more) load_values(ti + W);
   }
   // the tile's ticket word is made ready now, for its chunks to count themselves in one step
   unsigned long long* ticket = ws.ticket + slot_of(sd, it, ROWS) * ws.step;
@@ -710,7 +716,7 @@ __global__ __launch_bounds__(SH_T, SF_OCC) void k_shared_few(SharedDims sd, int 
   };
   if (mine) {
 #pragma unroll
-    for (int x = 0; x < SH_W; ++x) {
+    for (int x = 0; x < W; ++x) {
       float a[8];
 #pragma unroll
       for (int i = 0; i < 8; i += 4) *(float4*)(a + i) = *(const float4*)&sO[x][r][c + i];
@@ -976,9 +982,13 @@ hipError_t launch_shared(const SharedDims& sd, const void* q, const int32_t* cu,
 #define GKV_SHARED(TT, ...) hipLaunchKernelGGL((__VA_ARGS__), grid, dim3(64 * p.waves), 0, st, sd, room, (const TT*)q, cu, px, out, lse, ws)
   if (p.few) {
     if (bf) {
-      if (sd.d == 128) GKV_SHARED(uint16_t, k_shared_few<uint16_t, 128, 2>); else GKV_SHARED(uint16_t, k_shared_few<uint16_t, 64, 2>);
+      if (sd.d == 64) GKV_SHARED(uint16_t, k_shared_few<uint16_t, 64, 2, 4>);
+      else if (p.waves == 8) GKV_SHARED(uint16_t, k_shared_few<uint16_t, 128, 2, 8>);
+      else GKV_SHARED(uint16_t, k_shared_few<uint16_t, 128, 2, 4>);
     } else {
-      if (sd.d == 128) GKV_SHARED(float, k_shared_few<float, 128, 1>); else GKV_SHARED(float, k_shared_few<float, 64, 2>);
+      if (sd.d == 64) GKV_SHARED(float, k_shared_few<float, 64, 2, 4>);
+      else if (p.waves == 8) GKV_SHARED(float, k_shared_few<float, 128, 1, 8>);
+      else GKV_SHARED(float, k_shared_few<float, 128, 1, 4>);
     }
   } else if (bf) {
     if (sd.d == 128) {

@@ -562,7 +562,8 @@ def test_shared_every_number_of_entries(dtype, d):
 def test_shared_long_and_cut(dtype, d):
     # rows of many chunks, values that rise along the entries: a chunk that is lost or taken twice shows
     for i, (G, Hq, groups, counts) in enumerate([(1, 4, [1], [30001]), (2, 8, [17], [9000, 4001]), (1, 8, [30], [20011]),
-                                                 (2, 4, [1, 50, 3], [3000, 0, 5000, 20, 1, 8000])]):
+                                                 (2, 4, [1, 50, 3], [3000, 0, 5000, 20, 1, 8000]),
+                                                 (2, 16, [40], [1300, 1301]), (1, 4, [8], [40000])]):
         c = Shared(dtype, d, G, Hq, groups, counts, seed=60 + i)
         c.pre["V"] += torch.linspace(0, 4, c.pre["V"].shape[0])[:, None].to(c.pre["V"].dtype)
         c.check()

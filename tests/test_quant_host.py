@@ -177,8 +177,8 @@ GROUPS = r"""
 #include "groups.h"
 using namespace gkv;
 // a key tile's keys, a chunk's fewest tiles and a row's chunks as the kernels have them
-static int keys_of(const SharedPlan& p, bool bf, int d) { return p.few ? (bf || d == 64 ? 32 : 16) : (bf ? 128 : 32); }
-static int chunks(const SharedPlan& p, int n, int size, int d) { return p.few ? chunks_of(n, size, 0.6f * (d / 64)) : (n + size - 1) / size; }
+static int keys_of(const SharedPlan& p, bool bf, int d) { return p.few ? (bf || d == 64 ? 32 : 16) * (p.waves / 4) : (bf ? 128 : 32); }
+static int chunks(const SharedPlan& p, int n, int size, int d) { return p.few ? chunks_of(n, size, 0.6f * (d / 64) / (p.waves / 4)) : (n + size - 1) / size; }
 int main() {
   int bf, G, per, d, B, S;
   while (scanf("%d %d %d %d %d %d", &bf, &G, &per, &d, &B, &S) == 6) {
@@ -240,7 +240,7 @@ def test_groups_are_cut_into_what_the_grid_holds(tmp_path):
     assert len(out) == len(text)
     for line, case in zip(out, text):
         assert line.split()[0] == "0", (line, case[:200])
-    assert {tuple(line.split()[1:3]) for line in out} == {("1", "4"), ("0", "4"), ("0", "8")}       # every kernel among them
+    assert {tuple(line.split()[1:3]) for line in out} == {("1", "4"), ("1", "8"), ("0", "4"), ("0", "8")}       # every kernel among them
 
 
 DESCENDING = r"""
@@ -255,7 +255,7 @@ int main() {
     std::vector<int32_t> cu(S + 1);
     for (auto& x : cu) if (scanf("%d", &x) != 1) return 1;
     const SharedPlan p = shared_plan(sd, (int64_t)n * S * G);
-    const int keys = p.few ? 32 : 128, tiles = (n + keys - 1) / keys;
+    const int keys = p.few ? 8 * p.waves : 128, tiles = (n + keys - 1) / keys;
     int bad = 0, seen = 0;
     long long all = 0;
     unsigned long long total = 0;
@@ -267,7 +267,7 @@ int main() {
       if (mt && (int64_t)(first_tile(sd, (int)sp.a, b, p.rows) + mt) * G > p.tiles) ++bad;        // a ticket of every row tile
     }
     const int size = shared_chunk(total, (int)(p.places - p.tiles), p.few ? PA_MIN : 1);
-    all *= p.few ? chunks_of(tiles, size, 1.2f) : (tiles + size - 1) / size;
+    all *= p.few ? chunks_of(tiles, size, 4.8f / p.waves) : (tiles + size - 1) / size;
     std::vector<char> taken(p.places);
     for (int bid = 0; bid < p.places; ++bid) {
       const int id = item_of(bid, (int)all, p.places);
