@@ -66,8 +66,8 @@ struct Chunk {
 // wave finds it by itself, 64 units at a time; over that few it takes one round of loads
 // and scans without a barrier.  With more units the waves share a first look at them all,
 // which is enough where no row needs a second chunk (4096 sequences of 64 tokens: 860 us
-// with the search, 403 without).
-template <int TILE, bool PREFIX>
+// with the search, 403 without).  W: waves of the workgroup.
+template <int TILE, bool PREFIX, int W = PA_W>
 __device__ __forceinline__ bool find_chunk(const PageDims& pg, const PrefixView& px, const int32_t* len, int bid, int places, float join,
                                            Chunk& out) {
   const int lane = threadIdx.x & 63;
@@ -83,11 +83,11 @@ __device__ __forceinline__ bool find_chunk(const PageDims& pg, const PrefixView&
     first = tiles(lane);
     size = chunk_tiles((uint64_t)(uint32_t)__builtin_amdgcn_readlane(scan_wave(first), 63) * mult, room);
   } else {
-    __shared__ uint64_t part[PA_W];
-    __shared__ int most[PA_W];
+    __shared__ uint64_t part[W];
+    __shared__ int most[W];
     uint64_t sum = 0;
     int mx = 0;
-    for (int u = threadIdx.x; u < units; u += PA_T) {
+    for (int u = threadIdx.x; u < units; u += 64 * W) {
       const int n = tiles(u);
       sum += n;
       mx = max(mx, n);
@@ -101,7 +101,7 @@ __device__ __forceinline__ bool find_chunk(const PageDims& pg, const PrefixView&
     sync_after_lds_stores();
     sum = 0;
 #pragma unroll
-    for (int i = 0; i < PA_W; ++i) { sum += part[i]; mx = max(mx, most[i]); }
+    for (int i = 0; i < W; ++i) { sum += part[i]; mx = max(mx, most[i]); }
     size = __builtin_amdgcn_readfirstlane(chunk_tiles(sum * mult, room));
     if (__builtin_amdgcn_readfirstlane(mx) <= size) {
       if (bid >= units * mult) return false;
@@ -152,7 +152,7 @@ __device__ __forceinline__ bool find_chunk(const PageDims& pg, const PrefixView&
 // result where the chunk is all of it, else left in the workspace, for the last of the row's
 // chunks to join.  `part` (o not null): an attention of the same queries over other entries,
 // joined to the row's as a state of its own, maximum lse, sum 1 and its mean.
-template <typename T, int D, bool RAISED, int JOIN>
+template <typename T, int D, bool RAISED, int JOIN, int W = PA_W>
 __device__ __forceinline__ void finish_row(const PageDims& pg, const Chunk& ck, const PagedWs& ws, const PartView& part, int bid,
                                            int group, int groups, const float (*sM)[PA_HEADS], const float (*sL)[PA_HEADS],
                                            const float (*sO)[PA_HEADS][D + 4], T* __restrict__ out, float* __restrict__ lse) {
@@ -183,11 +183,11 @@ __device__ __forceinline__ void finish_row(const PageDims& pg, const Chunk& ck, 
     if (lse && dd == 0) lse[hd] = M + logf(S);
   };
   const int64_t place = (int64_t)bid * pg.hpg + h0;
-  for (int i = tid; i < heads * (D / 2); i += PA_T) {
+  for (int i = tid; i < heads * (D / 2); i += 64 * W) {
     const int h = i / (D / 2), dd = 2 * (i % (D / 2));
     float M = -INFINITY, S = 0.f, O0 = 0.f, O1 = 0.f;
 #pragma unroll
-    for (int x = 0; x < PA_W; ++x) add(M, S, O0, O1, sM[x][h], sL[x][h], sO[x][h][dd], sO[x][h][dd + 1]);
+    for (int x = 0; x < W; ++x) add(M, S, O0, O1, sM[x][h], sL[x][h], sO[x][h][dd], sO[x][h][dd + 1]);
     if (ck.chunks == 1) {
       finish(h, dd, M, S, O0, O1);
     } else {
@@ -205,7 +205,7 @@ __device__ __forceinline__ void finish_row(const PageDims& pg, const Chunk& ck, 
   // chunks at a time, one each, and pass the weights round.
   constexpr int LH = D / 2;
   const int64_t base = (int64_t)(bid - ck.c) * pg.hpg + h0;              // the row's first chunk
-  for (int i = tid; i < (heads * LH + 63) / 64 * 64; i += PA_T) {               // whole waves
+  for (int i = tid; i < (heads * LH + 63) / 64 * 64; i += 64 * W) {               // whole waves
     const int h = min(i / LH, heads - 1), sub = i % LH, dd = 2 * sub;
     float M = -INFINITY, S = 0.f, O0 = 0.f, O1 = 0.f;
     for (int b0 = 0; b0 < ck.chunks; b0 += LH) {

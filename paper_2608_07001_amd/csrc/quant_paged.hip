@@ -23,10 +23,12 @@
 //
 // Measured, bf16: 64 sequences of 1 to 8192 tokens, 8 KV heads of 128, 32 query heads, e4m3: 44 us (4.0 TB/s; the
 // loads alone take 42: pages of 16 tokens lie 2 KB a head apart); 4 sequences of about 128K, 64 query heads,
-// e2m1: 110 to 125 us as the pages lie (4.3 to 4.8 TB/s; the loads alone 104 to 120); one sequence of 8201 tokens
+// e2m1: 106 to 119 us as the pages lie (4.5 to 5.0 TB/s; the loads alone 104 to 120); one sequence of 8201 tokens
 // 13.1 us, bound by latency: finding the chunk, page ids, two tiles a wave, the states and their join, one
 // after the other.  Two tiles of loads in flight were slower everywhere (15.6, 50.7 and 127 us where one tile
 // in flight took 14.6, 44 and 126): their registers leave a wave less a SIMD.
+#include <algorithm>
+
 #include "paged_rows.h"
 #include "quant.h"
 
@@ -35,7 +37,7 @@ namespace gkv {
 constexpr int QP_JOIN = 8;         // states joined at a time: one sequence 13.9 us with 4, 13.1 with 8, 13.4 with 16
 constexpr float LAG = 8.f;         // (below) a weight is 2^-8 at the row's largest at the least
 
-// Waves a SIMD that the registers have to leave room for.  With four everything spills: 64 sequences
+// Waves a SIMD that the registers have to leave room for, workgroups of four waves.  With four a SIMD everything spills: 64 sequences
 // 106 us for 44.  e4m3 keys beside an fp32 query's three parts do not fit three either: 64 sequences of 4096 tokens,
 // 8 KV heads of 128, 32 query heads 171 us with three and 114 with two; of e2m1 80 and 87.
 template <typename T, int D, int FMT> constexpr int quant_waves() {
@@ -54,12 +56,12 @@ template <int CTRL> __device__ __forceinline__ float quad_of(float x) {
   return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xf, 0xf, true));
 }
 
-template <typename T, int D, int FMT>
-__global__ __launch_bounds__(PA_T, (quant_waves<T, D, FMT>())) void k_quant_paged(
+template <typename T, int D, int FMT, int W>
+__global__ __launch_bounds__(64 * W, (W == 8 ? 2 : quant_waves<T, D, FMT>())) void k_quant_paged(
     PageDims pg, QuantDims qd, int64_t q_tok, const T* __restrict__ q, const int32_t* __restrict__ table, const int32_t* __restrict__ len,
     PartView part, T* __restrict__ out, float* __restrict__ lse, PagedWs ws) {
   constexpr bool BF = sizeof(T) == 2;
-  constexpr int NS = 2, TILE = 16 * NS;
+  constexpr int NS = 2, TILE = 16 * NS, PAIR = W / PA_W;        // (chunks of eight waves are counted in pairs of tiles)
   constexpr int BITS = code_bits<FMT>();
   constexpr int QP = BF ? 1 : 3, PP = BF ? 2 : 3;        // bf16 parts of a query, of a weight
   constexpr int PB = D * BITS / 32 < 16 ? D * BITS / 32 : 16;      // bytes of a lane's piece of a key
@@ -70,13 +72,13 @@ __global__ __launch_bounds__(PA_T, (quant_waves<T, D, FMT>())) void k_quant_page
   constexpr int VB = VD * BITS / 8;                      // ... bytes: 8, 4 or 2
   constexpr int VW = VB < 4 ? 1 : VB / 4;
   constexpr int RB = D * BITS / 8, SB = D / Q_BLOCK;     // bytes of a row and of its scales
-  __shared__ float sM[PA_W][PA_HEADS], sL[PA_W][PA_HEADS];
-  __shared__ __align__(16) float sO[PA_W][PA_HEADS][D + 4];      // rows start in other banks
+  __shared__ float sM[W][PA_HEADS], sL[W][PA_HEADS];
+  __shared__ __align__(16) float sO[W][PA_HEADS][D + 4];      // rows start in other banks
   const int groups = (pg.hpg + PA_HEADS - 1) / PA_HEADS;
   const int bid = groups > 1 ? blockIdx.x / groups : blockIdx.x, group = groups > 1 ? blockIdx.x % groups : 0;
   Chunk ck;
   const int places = groups > 1 ? gridDim.x / groups : gridDim.x;
-  if (!find_chunk<TILE, false>(pg, PrefixView{}, len, bid, places, join_cost(pg.hpg, D), ck)) return;
+  if (!find_chunk<TILE * PAIR, false, W>(pg, PrefixView{}, len, bid, places, join_cost(pg.hpg, D) / PAIR, ck)) return;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i16 = lane & 15, g4 = lane >> 4;
   const int h0 = group * PA_HEADS, heads = min(PA_HEADS, pg.hpg - h0);
   constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
@@ -192,20 +194,21 @@ __global__ __launch_bounds__(PA_T, (quant_waves<T, D, FMT>())) void k_quant_page
   for (int j = 0; j < VD; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;               // of head i16; l: this lane's entries only
 
-  int ti = ck.t0 + w;
+  const int t1 = min(ck.t1 * PAIR, (int)((n_page + TILE - 1) / TILE));
+  int ti = ck.t0 * PAIR + w;
   Where now{}, next{};
   Ids ids{};
-  if (ti < ck.t1) {
+  if (ti < t1) {
     now = where(ti, pages_of(ti));
-    ids = pages_of(min(ti + PA_W, ck.t1 - 1));
+    ids = pages_of(min(ti + W, t1 - 1));
     load_keys(now);
     load_values(now);
   }
-  for (; ti < ck.t1; ti += PA_W) {
-    const bool more = ti + PA_W < ck.t1;
+  for (; ti < t1; ti += W) {
+    const bool more = ti + W < t1;
     if (more) {
-      next = where(ti + PA_W, ids);
-      ids = pages_of(min(ti + 2 * PA_W, ck.t1 - 1));
+      next = where(ti + W, ids);
+      ids = pages_of(min(ti + 2 * W, t1 - 1));
     }
     float x[NS][4];
 #pragma unroll
@@ -347,18 +350,34 @@ __global__ __launch_bounds__(PA_T, (quant_waves<T, D, FMT>())) void k_quant_page
         *(float4*)&sO[w][i16][VD * (4 * g4 + r) + j] = make_float4(o[j][r], o[j + 1][r], o[j + 2][r], o[j + 3][r]);
   }
   sync_after_lds_stores();
-  finish_row<T, D, true, QP_JOIN>(pg, ck, ws, part, bid, group, groups, sM, sL, sO, out, lse);
+  finish_row<T, D, true, QP_JOIN, W>(pg, ck, ws, part, bid, group, groups, sM, sL, sO, out, lse);
+}
+
+// Eight waves a workgroup for few rows that may be long: half the chunks, whose states the last joins in half the time
+// (with more threads, which is what counts for many heads).  us with four and eight, 8 KV heads of 128, bf16 over e4m3: 32 query heads, one
+// sequence of 2048 tokens 9.7 and 9.9, of 8192 13.1 and 12.8, of 32768 22.9 and 20.2, 4 of 8192 21.0 and 18.4, 16 of 1024 14.7 and 13.4; 64
+// query heads, 512 10.4 and 10.0, 2048 11.5 and 10.2, 8192 15.8 and 13.2; fp32, 16 of 4096 43 and 33.  Many rows of different
+// lengths need smaller pieces: 64 of 1 to 8192 44 and 71.  The lengths are not known here: what the table can name counts.
+static bool eight_waves(const PageDims& pg) {
+  const int64_t R = (int64_t)pg.n_seq * pg.G, cap = (int64_t)pg.width << pg.shift;
+  return R < 256 && (pg.hpg > 4 ? cap >= 512 : R * cap >= 131072);
 }
 
 hipError_t launch_quant_paged(const PageDims& pg, int format, const QuantDims& qd, int64_t q_tok, const void* q, const int32_t* table,
                               const int32_t* len, const PartView& part, void* out, float* lse, void* ws, hipStream_t st) {
   const PagedWs v = paged_view(ws, pg);
-  const int64_t room = chunk_room(pg, 0, 32);
-  const dim3 grid((unsigned)(((int64_t)pg.n_seq * pg.G + room) * ((pg.hpg + PA_HEADS - 1) / PA_HEADS)));
+  const int64_t R = (int64_t)pg.n_seq * pg.G;
+  const bool eight = eight_waves(pg);
+  const int64_t room = eight ? std::min<int64_t>(chunk_room(pg, 0, 64), 256 - R / 2) : chunk_room(pg, 0, 32);
+  const dim3 grid((unsigned)((R + room) * ((pg.hpg + PA_HEADS - 1) / PA_HEADS)));
   by_type(pg, format, [&](auto type, auto dim, auto fmt) {
     using T = decltype(type);
     constexpr int D = decltype(dim)::value, FMT = decltype(fmt)::value;
-    hipLaunchKernelGGL((k_quant_paged<T, D, FMT>), grid, dim3(PA_T), 0, st, pg, qd, q_tok, (const T*)q, table, len, part, (T*)out, lse, v);
+    auto run = [&](auto waves) {
+      constexpr int W = decltype(waves)::value;
+      hipLaunchKernelGGL((k_quant_paged<T, D, FMT, W>), grid, dim3(64 * W), 0, st, pg, qd, q_tok, (const T*)q, table, len, part, (T*)out, lse, v);
+    };
+    if (eight) run(std::integral_constant<int, 8>{}); else run(std::integral_constant<int, 4>{});
   });
   return hipGetLastError();
 }

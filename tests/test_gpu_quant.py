@@ -403,6 +403,16 @@ def test_attention_long_and_split(dtype, d, fmt):
 
 @pytest.mark.parametrize("dtype,d", TYPES)
 @pytest.mark.parametrize("fmt", FORMATS)
+def test_attention_few_rows_many_heads(dtype, d, fmt):
+    # eight waves a workgroup: every length about a wave's, a pair's and a chunk's tiles; more sequences than a wave looks at
+    for i, (G, Hq, lens, page) in enumerate([(1, 8, [0, 1, 31, 32, 33, 63, 64, 65, 255, 256, 257, 511, 512, 513, 600, 1025, 2047], 16),
+                                             (2, 12, [1, 3000, 0, 700], 64), (2, 10, [(37 * j) % 700 for j in range(100)], 16),
+                                             (1, 33, [1500, 2], 32)]):
+        Cache(dtype, d, fmt, G, Hq, lens, page, seed=80 + i).check()
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("fmt", FORMATS)
 def test_attention_masked_places_reach_nothing(dtype, d, fmt):
     # what lies past the end, or in pages that are nobody's, stands for NaN; a page of the first sequence is missing
     c = Cache(dtype, d, fmt, 2, 6, [40, 0, 5, 32], 16, seed=6)
