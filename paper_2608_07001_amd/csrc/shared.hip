@@ -284,7 +284,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_shared_bf(SharedDims sd, int 
   auto step = [&](int t, uint4* cur, uint4* next) __attribute__((always_inline)) {
     // the wave's own loads of tile t are there, then everyone's; and everyone is done with tile t - 1
     loaded_barrier<0>();
-    if (t + 1 < t1) load_tile(t + 1, next);
+    if (W == 4 && t + 1 < t1) load_tile(t + 1, next);
     uint4* cV = cur + V0;
     const int left = n_keys - t * KEYS;          // entries from this tile on
     const float* cL = (const float*)(cur + L0 + w * KEYS / 4);
@@ -317,6 +317,9 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_shared_bf(SharedDims sd, int 
     reads_ahead<NU * (KS + 1), 1, 8>();
 #pragma unroll
     for (int u = 0; u < NU; ++u) mfma_done16(s[u]);
+    // eight waves, which the products bound: behind the logits, whose reads the loads would meet (512 rows over 16384 entries 57.6
+    // us in front of them, 55.0 behind); four wait for memory (4 rows over 65536 64 in front and 70 behind)
+    if (W == 8 && t + 1 < t1) load_tile(t + 1, next);
     if (left < KEYS) {
       asm volatile("");                          // (a branch: 64 selects in every tile otherwise)
 #pragma unroll
