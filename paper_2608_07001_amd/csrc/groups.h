@@ -56,7 +56,9 @@ inline SharedPlan plan_of(const SharedDims& sd, bool few, int waves) {
   p.rows = few ? 16 : 16 * waves;
   p.tiles = most_tiles(sd, p.rows) * sd.G;
   const int64_t target = few ? (waves == 8 ? 256 : 768) : (sd.dtype == 1 ? 256 : 512);
-  const int64_t room = target - p.tiles / 2 > target / 4 ? target - p.tiles / 2 : target / 4;
+  // what row tiles' last, unfilled chunks take: all of them where one workgroup more is a second round (64 rows over 8192 entries
+  // 30.2 and 21.4 us, 256 over 4096 25.2 and 23.0), half of them elsewhere (fp32, 256 over 1024 32.0 and 27.7)
+  const int64_t last = !few && sd.dtype == 1 ? p.tiles : p.tiles / 2, room = target - last > target / 4 ? target - last : target / 4;
   p.places = (int)((p.tiles + room + 7) & ~(int64_t)7);
   return p;
 }
@@ -64,7 +66,7 @@ inline SharedPlan plan_of(const SharedDims& sd, bool few, int waves) {
 // mean.  Small tiles spread little work over the chip with fewer states and one launch, large ones go through keys
 // and values fewer times.  us, heads of 128, small tiles with four waves, with eight, large tiles:
 //   bf16, 8 KV heads, 16 rows each: over 128 entries 9.4, 8.3, 12.4; 1024 11.3, 11.7, 12.8; 4096 18.7, 16.9, 17.4; 16384 27.4, 25.4, 25.6
-//   64 rows: over 256 10.1, 10.6, 13.6; 2048 15.0, 14.1, 15.1; 4096 20.7, 16.8, 17.3; 8192 27.5, 37, 30
+//   64 rows: over 256 10.1, 10.6, 13.6; 2048 15.0, 14.1, 15.1; 4096 20.7, 16.8, 17.3; 8192 27.5, 37, 21.4
 //   256 rows: over 512 14.8, 12.6, 17.3; 1024 19.6, 16.8, 18.1; 2048 24.2, 24.2, 20.6; 8192 50, 54, 29
 //   fp32, 16 rows: over 2048 17.8, 19.7, 18.9; 8192 27, 30, 35; 32 rows: over 4096 21.3, 23.7, 25.5; 16384 78, 55, 68
 //   128 rows: over 256 10.9, 12.8, 16.1; 1024 21.1, 18.0, 22.6; 2048 28.8, 23.4, 26.0; 8192 71, 66, 58
@@ -76,7 +78,7 @@ inline SharedPlan shared_plan(const SharedDims& sd, int64_t entries) {
   const int64_t heads = (int64_t)sd.n_group * sd.G, mean = ((int64_t)sd.n_seq * sd.hpg + sd.n_group - 1) / sd.n_group;
   const int64_t each = entries / heads, tiles = (mean + 15) / 16;
   const int64_t steps = tiles * ((entries < (int64_t)1 << 40 ? entries : (int64_t)1 << 40) / 32);       // products of 16 rows and 32 keys
-  const bool little = steps <= (bf && !wide ? 10240 : 4352) && each <= 10240;
+  const bool little = steps <= (bf && !wide ? 10240 : 4352) && each <= (bf && wide ? 5120 : 10240);
   if (little || (bf ? mean <= 16 && each <= 32768 : mean <= 32)) {
     const bool eight = wide && (bf ? each > 1536 || each <= 160 || steps >= 960 : mean > 16 && steps * tiles * heads >= 35000);
     return plan_of(sd, true, eight ? 8 : 4);
