@@ -23,8 +23,9 @@
 //
 // Measured, bf16: 64 sequences of 1 to 8192 tokens, 8 KV heads of 128, 32 query heads, e4m3: 44 us (4.0 TB/s; the
 // loads alone take 42: pages of 16 tokens lie 2 KB a head apart); 4 sequences of about 128K, 64 query heads,
-// e2m1: 106 to 119 us as the pages lie (4.5 to 5.0 TB/s; the loads alone 104 to 120); one sequence of 8201 tokens
-// 13.1 us, bound by latency: finding the chunk, page ids, two tiles a wave, the states and their join, one
+// e2m1: 108 us (4.9 TB/s; the loads alone 104), rising to 120 to 140 where such calls follow one another for
+// milliseconds; one sequence of 8201 tokens
+// 13.1 us, bound by latency: finding the chunk, page ids, the tiles of a wave, the states and their join, one
 // after the other.  Two tiles of loads in flight were slower everywhere (15.6, 50.7 and 127 us where one tile
 // in flight took 14.6, 44 and 126): their registers leave a wave less a SIMD.
 #include <algorithm>
