@@ -73,7 +73,8 @@ static SharedWs shared_view(void* base, const SharedDims& sd, const SharedPlan& 
 size_t shared_ws_bytes(const SharedDims& sd) {
   size_t n = 0;
   for (bool few : {false, true})
-    for (int waves : {4, 8}) n = std::max(n, shared_view(nullptr, sd, plan_of(sd, few, waves)).bytes);
+    for (int waves : {4, 8})
+      if (few || waves == 4 || sd.dtype == GRACEKV_BF16) n = std::max(n, shared_view(nullptr, sd, plan_of(sd, few, waves)).bytes);
   return n;
 }
 

@@ -641,6 +641,8 @@ def test_shared_many_units_and_groups():
         groups = _counts(B, B, 0, 4)
         Shared("bf16", 64, G, 2 * G, groups, _counts(B + 1, B * G, 0, 90), behind=2, seed=B).check()
     Shared("f32", 64, 2, 4, _counts(3, 80, 0, 3), _counts(4, 160, 0, 400), seed=9).check()
+    Shared("bf16", 128, 3, 6, _counts(5, 90, 0, 4), _counts(6, 270, 0, 300), seed=10).check()      # eight waves a workgroup
+    Shared("f32", 128, 2, 8, _counts(7, 40, 0, 20), _counts(8, 80, 0, 300), seed=11).check()
 
 
 @pytest.mark.parametrize("rows", [2, 100])
