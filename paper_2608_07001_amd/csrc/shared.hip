@@ -21,7 +21,8 @@
 // chunk, 4 to write the states and 7 for k_shared_join.  A step of 128 keys takes 6500 cycles: 2500 logits (reads of
 // LDS, each wave all of the keys), 1350 values, 850 softmax, 1100 the issue of the next tile's loads
 // (64 KB at 64 bytes a cycle), 700 the barrier.  Tried and slower: tiles of 64 keys in four stages, logits a tile ahead
-// (43.7 us for 41.5), twice the chunks (54 for 41).
+// (43.7 us for 41.5), twice the chunks (54 for 41), four waves of 64 rows each, which read LDS half as often (50
+// for 39: one wave a SIMD), joining in the same launch, by the chunks' workgroups in slices of the rows (40, and more where chunks are many).
 //
 // k_shared_f32, 64 rows: the fp32 matrix instructions, tiles of 32 keys through registers into LDS.
 //
