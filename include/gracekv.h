@@ -604,10 +604,10 @@ gracekv_status gracekv_shared_ws_bytes(const gracekv_shared_config* cfg, size_t*
  *              them is one that gracekv_paged_attention excludes; calls that overlap on one
  *              workspace race, and what they leave in it, or a call whose cu_group descends, has
  *              to be cleared
- * bf16: for the product with the values, weights are rounded to bf16, as a prompt's are (groups
- * of many rows), or in two bf16 parts.  An entry whose logm is finite and below -1e36 (the type's
- * lowest value, as masks have it) weighs nothing beside others; where a row has only such entries,
- * the largest of their logm decide, and q.k may be lost beside them.  logm has to stay below 1e36.
+ * bf16: for the product with the values, weights are in two bf16 parts, off by at most 2^-15.
+ * An entry whose logm is finite and below -1e36 (the type's lowest value, as masks have it) weighs
+ * nothing beside others; where a row has only such entries, the largest of their logm decide,
+ * and q.k may be lost beside them.  logm has to stay below 1e36.
  * Starts, counts and groups must not change while the call runs. */
 gracekv_status gracekv_shared_attention(const gracekv_shared_config* cfg, const void* q, const int32_t* cu_group,
                                         const gracekv_prefix* prefix, const gracekv_part* part, void* ws,

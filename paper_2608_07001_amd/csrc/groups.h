@@ -48,7 +48,7 @@ struct SharedPlan {
 };
 // The chip holds three of the small tiles' workgroups of four waves a CU, one or two of eight (their registers), two of
 // the fp32 ones of large tiles (256 rows over 16384 entries 226 us with places for one, 191 for two) and one of the
-// bf16 ones, whose tiles fill LDS: with twice the places 256 rows over 16384 took 54 us for 41, waiting for a second round.
+// bf16 ones, whose tiles fill LDS: with twice the places 256 rows over 16384 took 54 us for 41 (weights in one part), waiting for a second round.
 inline SharedPlan plan_of(const SharedDims& sd, bool few, int waves) {
   SharedPlan p;
   p.few = few;
@@ -65,12 +65,13 @@ inline SharedPlan plan_of(const SharedDims& sd, bool few, int waves) {
 // `entries`: rows of the packed arrays.  The rows and entries of a (group, KV head) are taken as the
 // mean.  Small tiles spread little work over the chip with fewer states and one launch, large ones go through keys
 // and values fewer times.  us, heads of 128, small tiles with four waves, with eight, large tiles:
-//   bf16, 8 KV heads, 16 rows each: over 128 entries 9.4, 8.3, 12.4; 1024 11.3, 11.7, 12.8; 4096 18.7, 16.9, 17.4; 16384 27.4, 25.4, 25.6
-//   64 rows: over 256 10.1, 10.6, 13.6; 2048 15.0, 14.1, 15.1; 4096 20.7, 16.8, 17.3; 8192 27.5, 37, 21.4
-//   256 rows: over 512 14.8, 12.6, 17.3; 1024 19.6, 16.8, 18.1; 2048 24.2, 24.2, 20.6; 8192 50, 54, 29
+//   bf16, 8 KV heads, 16 rows each: over 128 entries 9.3, 8.2, 12.6; 1024 11.4, 11.8, 13.1; 4096 18.7, 16.9, 16.9; 16384 27.4, 25.5, 27.2
+//   64 rows: over 256 10.0, 10.6, 13.7; 2048 15.3, 14.0, 15.5; 4096 20.6, 17.0, 17.5; 8192 27.6, 37, 22.3
+//   256 rows: over 512 14.6, 12.5, 17.9; 1024 19.7, 16.8, 18.5; 2048 24.2, 24.1, 21.1; 8192 49, 54, 29.7
+//   4 rows: over 24000 (eight, large) 32.2, 34.7; 65536 64, 68; 16 rows: over 32768 37.6, 37.8; 65536 56, 55; 131072 134, 93
 //   fp32, 16 rows: over 2048 17.8, 19.7, 18.9; 8192 27, 30, 35; 32 rows: over 4096 21.3, 23.7, 25.5; 16384 78, 55, 68
 //   128 rows: over 256 10.9, 12.8, 16.1; 1024 21.1, 18.0, 22.6; 2048 28.8, 23.4, 26.0; 8192 71, 66, 58
-// and heads of 64 (four waves; eight are slower at all sizes), 2 KV heads: 128 rows over 8192 15.8 and 16.5, 32 over 16384 18.6 and 16.0.
+// and heads of 64 (four waves; eight are slower at all sizes), 2 KV heads: 128 rows over 8192 15.8 and 17.0, 32 over 16384 18.7 and 16.4.
 // Large tiles have 64 rows (four waves), in bf16 for more rows 128 (eight).
 inline SharedPlan shared_plan(const SharedDims& sd, int64_t entries) {
   const bool bf = sd.dtype == 1;               // GRACEKV_BF16

@@ -45,13 +45,6 @@ template <typename T, int D, int FMT> constexpr int quant_waves() {
   return sizeof(T) == 4 && D == 128 && FMT == GRACEKV_E4M3 ? 2 : 3;
 }
 
-// a float's upper 16 bits and what is left
-__device__ __forceinline__ float upper(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
-// the upper 16 bits of two floats, low half first
-__device__ __forceinline__ uint32_t uppers(float a, float b) {
-  return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
-}
-
 // the value of one lane of the quad
 template <int CTRL> __device__ __forceinline__ float quad_of(float x) {
   return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xf, 0xf, true));

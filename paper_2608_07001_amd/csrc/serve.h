@@ -80,6 +80,11 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   const f32x2 x = {a, b};
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
 }
+// a float's upper 16 bits, a bf16 number; and those of two floats, low half first
+__device__ __forceinline__ float upper(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
+__device__ __forceinline__ uint32_t uppers(float a, float b) {
+  return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+}
 
 // the sequence b in [0, n) whose span could hold row t: the last with cu[b] <= t (0 if
 // none has).  A wave asks 64 places at a time, so up to 64 sequences take one load.

@@ -17,10 +17,10 @@
 //
 // k_shared_bf, 64 or 128 rows: bound by what feeds the matrix units.  Products are transposed, keys and values go
 // straight into LDS, as in prompt.hip.  64 sequences over 16384 entries, heads as above (256 rows a KV head in two
-// tiles, a chunk a CU, 17 GFLOP) take 40 us, 430 TFLOP/s: 24 in the loop, 4 to launch and find a
-// chunk, 4 to write the states and 7 for k_shared_join.  A step of 128 keys takes 6500 cycles: 2500 logits (reads of
-// LDS, each wave all of the keys), 1350 values, 850 softmax, 1100 the issue of the next tile's loads
-// (64 KB at 64 bytes a cycle), 700 the barrier.  Tried and slower: tiles of 64 keys in four stages, logits a tile ahead
+// tiles, a chunk a CU) take 45 us: 30 in the loop, 4 to launch and find a chunk, 4 to write the states and 7 for
+// k_shared_join.  Of a step of 128 keys a wave has 1770 cycles of logits (reads of LDS, each wave all of the keys), 720 of issuing the
+// next tile's loads, 1250 of softmax and the weights' parts, 1350 of values, 170 of waiting at the barrier.  Tried and slower, with
+// weights in one part: tiles of 64 keys in four stages, logits a tile ahead
 // (43.7 us for 41.5), twice the chunks (54 for 41), four waves of 64 rows each, which read LDS half as often (50
 // for 39: one wave a SIMD), joining in the same launch, by the chunks' workgroups in slices of the rows (40, and more where chunks are many).
 //
@@ -29,8 +29,10 @@
 // The latter two leave states, megabytes of them, to k_shared_join, a second launch in which the whole chip
 // reads them and not one workgroup a row tile.
 //
-// bf16 weights are rounded to bf16 (nearest even) for the second product of k_shared_bf, their sum takes them
-// unrounded, as in prompts: each is off by at most 2^-8 of itself, at random.
+// bf16 weights are held in two bf16 parts for the second product, by both kernels that have it: off by at most 2^-15 of themselves.
+// Which kernel a call takes goes by the work and by rows of the arrays that are no concern of the caller's, and the result is fp32, so
+// they are not held in fewer bits where products are the bound: one part, off by 2^-8, left 64 sequences over 16384 entries
+// 9.5e-4 of the norm away from fp32 arithmetic, two 0.7e-4, for 45 us instead of 40.
 #include <algorithm>
 
 #include "tickets.h"
@@ -319,8 +321,8 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_shared_bf(SharedDims sd, int 
     reads_ahead<NU * (KS + 1), 1, 8>();
 #pragma unroll
     for (int u = 0; u < NU; ++u) mfma_done16(s[u]);
-    // eight waves, which the products bound: behind the logits, whose reads the loads would meet (512 rows over 16384 entries 57.6
-    // us in front of them, 55.0 behind); four wait for memory (4 rows over 65536 64 in front and 70 behind)
+    // eight waves, which the products bound: behind the logits, whose reads the loads would meet (with weights in
+    // one part 512 rows over 16384 entries 57.6 us in front of them, 55.0 behind); four wait for memory (4 rows over 65536 64 and 70)
     if (W == 8 && t + 1 < t1) load_tile(t + 1, next);
     if (left < KEYS) {
       asm volatile("");                          // (a branch: 64 selects in every tile otherwise)
@@ -379,16 +381,21 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_shared_bf(SharedDims sd, int 
             s[u][r] = 8 * (r / 4) + r % 4 < left - 32 * (NU * kw + u) - 4 * half && lm[r] == m ? 0.f : -INFINITY;
       }
     }
-    uint4 pr[NU][2];
+    uint4 pr[NU][2], pl[NU][2];                  // weights in two parts
 #pragma unroll
     for (int u = 0; u < NU; ++u)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        float e[8];
+        float e[8], f[8];
 #pragma unroll
         for (int r = 0; r < 8; ++r) e[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][8 * h + r], sc2, -ms2));
         l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
-        pr[u][h] = make_uint4(pack_bf16(e[0], e[1]), pack_bf16(e[2], e[3]), pack_bf16(e[4], e[5]), pack_bf16(e[6], e[7]));
+        // the second is what the first leaves and 2^-20 of the weight, so that an infinite value does not meet a 0 (a weight
+        // below 2^-113 of one may give NaN for it)
+#pragma unroll
+        for (int r = 0; r < 8; ++r) f[r] = __builtin_fmaf(e[r], 1.f + 0x1p-20f, -upper(e[r]));
+        pr[u][h] = make_uint4(uppers(e[0], e[1]), uppers(e[2], e[3]), uppers(e[4], e[5]), uppers(e[6], e[7]));
+        pl[u][h] = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
       }
     // product step x: keys 16 x + 8 (j / 4) + 4 half + j % 4 in place 8 half + j
 #pragma unroll
@@ -400,9 +407,11 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_shared_bf(SharedDims sd, int 
           const int row = 32 * (NU * kw + u) + 16 * x;
           const uint2 a = lds_read_tr(cV, (v_at ^ (64 * d)) + row * RB);
           const uint2 b = lds_read_tr(cV, (v_at ^ (64 * d + 32)) + (row + 8) * RB);
-          o[d] = mfma_bf16_32x32x16(make_uint4(a.x, a.y, b.x, b.y), pr[u][x], o[d]);
+          const uint4 v8 = make_uint4(a.x, a.y, b.x, b.y);
+          o[d] = mfma_bf16_32x32x16(v8, pl[u][x], o[d]);
+          o[d] = mfma_bf16_32x32x16(v8, pr[u][x], o[d]);
         }
-    reads_ahead<2 * DT * NU, 2, 3>();
+    reads_ahead<2 * DT * NU, 2, 3, 2>();
   };
   if (it.t0 < t1) load_tile(it.t0, st0);
   for (int t = it.t0; t < t1; t += 2) {
@@ -476,7 +485,6 @@ __device__ __forceinline__ float4 ld_agent16(Buffer b, int byte) {
 // straight from memory as the product's operand and values paired up in registers, as over pages
 // (paged.hip), and no LDS before the waves are merged.  The last of a row tile's chunks joins them.
 // Eight waves halve the states of longer rows, which is what four wait for (groups.h has both measured).
-// bf16 weights are in two bf16 parts here, which costs a memory-bound kernel nothing.
 template <typename T, int D, int NS, int W>
 __global__ __launch_bounds__(64 * W, W == 8 ? 2 : SF_OCC) void k_shared_few(SharedDims sd, int room, const T* __restrict__ q, const int32_t* __restrict__ cu,
                                                              PrefixView px, float* __restrict__ out, float* __restrict__ lse, SharedWs ws) {

@@ -14,16 +14,16 @@ __device__ __forceinline__ f32x16 mfma_bf16_32x32x16(uint4 a, uint4 b, f32x16 c)
 // the stated wait for the matrix pipeline (mfma_done) for these accumulators
 __device__ __forceinline__ void mfma_done16(f32x16& x) { asm volatile("s_nop 15\n\ts_nop 4" : "+v"(x)); }
 
-// Orders a block's N products and their LDS reads (R a product): the reads AHEAD products early.
-template <int N, int R, int AHEAD> __device__ __forceinline__ void reads_ahead() {
+// Orders a block's N products, M at a time on the same operand, and their LDS reads (R for each M): the reads AHEAD of them early.
+template <int N, int R, int AHEAD, int M = 1> __device__ __forceinline__ void reads_ahead() {
   constexpr int A = AHEAD < N ? AHEAD : N;
   __builtin_amdgcn_sched_group_barrier(0x100, R * A, 0);        // LDS reads
 #pragma unroll
   for (int i = 0; i < N - A; ++i) {
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);          // products
+    __builtin_amdgcn_sched_group_barrier(0x008, M, 0);          // products
     __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
   }
-  __builtin_amdgcn_sched_group_barrier(0x008, A, 0);
+  __builtin_amdgcn_sched_group_barrier(0x008, M * A, 0);
 }
 
 // 16 bytes of a tile
