@@ -66,7 +66,8 @@ struct Chunk {
 // wave finds it by itself, 64 units at a time; over that few it takes one round of loads
 // and scans without a barrier.  With more units the waves share a first look at them all,
 // which is enough where no row needs a second chunk (4096 sequences of 64 tokens: 860 us
-// with the search, 403 without).  W: waves of the workgroup.
+// with the search, 403 without).  W: waves of the workgroup; of eight, no more chunks than run
+// at once (one_round).
 template <int TILE, bool PREFIX, int W = PA_W>
 __device__ __forceinline__ bool find_chunk(const PageDims& pg, const PrefixView& px, const int32_t* len, int bid, int places, float join,
                                            Chunk& out) {
@@ -78,10 +79,19 @@ __device__ __forceinline__ bool find_chunk(const PageDims& pg, const PrefixView&
     return tiles_of<TILE>(held_len(pg, len[PREFIX ? u / pg.G : u]), PREFIX ? held_count(px, u, s) : 0);
   };
   const int room = places - pg.n_seq * pg.G;
-  int first = 0, size;
+  int first = 0, first_chunks = 0, size;        // of the lane's unit in the first round
   if (units <= 64) {
     first = tiles(lane);
-    size = chunk_tiles((uint64_t)(uint32_t)__builtin_amdgcn_readlane(scan_wave(first), 63) * mult, room);
+    const uint64_t total = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(scan_wave(first), 63) * mult;
+    size = chunk_tiles(total, room);
+    if constexpr (W > PA_W) {
+      first_chunks = first ? chunks_of(first, size, join) : 0;
+      const int fit = one_round(total, pg.n_seq * pg.G, size, (int64_t)__builtin_amdgcn_readlane(scan_wave(first_chunks), 63) * mult);
+      if (fit != size) {
+        size = fit;
+        first_chunks = first ? chunks_of(first, size, join) : 0;
+      }
+    }
   } else {
     __shared__ uint64_t part[W];
     __shared__ int most[W];
@@ -102,7 +112,9 @@ __device__ __forceinline__ bool find_chunk(const PageDims& pg, const PrefixView&
     sum = 0;
 #pragma unroll
     for (int i = 0; i < W; ++i) { sum += part[i]; mx = max(mx, most[i]); }
-    size = __builtin_amdgcn_readfirstlane(chunk_tiles(sum * mult, room));
+    size = chunk_tiles(sum * mult, room);
+    if constexpr (W > PA_W) size = one_round(sum * mult, pg.n_seq * pg.G, size, places);
+    size = __builtin_amdgcn_readfirstlane(size);
     if (__builtin_amdgcn_readfirstlane(mx) <= size) {
       if (bid >= units * mult) return false;
       const int u = bid / mult;
@@ -124,7 +136,7 @@ __device__ __forceinline__ bool find_chunk(const PageDims& pg, const PrefixView&
   for (int many = 1; many >= (ordered ? 0 : 1); --many)
 #pragma unroll 1
     for (int u0 = 0; u0 < units; u0 += 64) {
-      const int n = u0 ? tiles(u0 + lane) : first, x = n ? chunks_of(n, size, join) : 0;
+      const int n = u0 ? tiles(u0 + lane) : first, x = W > PA_W && ordered ? first_chunks : n ? chunks_of(n, size, join) : 0;
       const int c = !ordered || (x > 1) == many ? x * mult : 0;
       const int to = scan_wave(c);     // at most the places: no overflow
       const int all = base + __builtin_amdgcn_readlane(to, 63);

@@ -112,4 +112,28 @@ GKV_HD int chunks_of(int n, int size, float join) {
   return c + (left > 0);
 }
 
+// ---- quantised pages: eight waves a workgroup ----
+constexpr int PA_CUS = 256;        // workgroups of eight waves that run at once (their registers)
+
+// Eight waves for few rows that may be long: half the chunks, whose states the last joins in half the time
+// (with more threads, which is what counts for many heads).  The lengths are not known here: what the table can name counts.
+// us with four and eight, 8 KV heads of 128, bf16 over e4m3, ragged: from 1 to the longest:
+//   32 query heads: one sequence of 2048 tokens 9.7, 9.9, of 8192 13.1, 12.8; 3 of 8192 20.6, 16.7; 8 of 8192 29.4, 28.3; 8 ragged to
+//     4096 14.6, 12.7, to 8192 20.4, 18.4;  64 query heads: 512 10.4, 10.0; 8192 15.8, 13.2; 8 ragged to 8192 23.5, 18.5
+//   fp32, 4 of 8192 26.6, 19.5; heads of 64, 4 of 8192 15.0, 13.0
+// More than 64 rows (9 sequences) are seldom better and often worse, whether their chunks fit the chip or not: 16 ragged to
+// 8192 33.9, 50 (38 where they fit), 20 ragged 37.0, 40 (53), 12 of 4096 23.2, 34 (24), 31 of 4096 47.2, 44.6; fp32, 16 ragged
+// 45, 58 (46).  Of short ones with many heads, which make a chunk or two a row, they stay better: 64 query heads, 12 of 512 11.7, 10.3, 24 of
+// 512 14.3, 10.2, 31 ragged to 768 14.4, 11.7 (20 of 1024 18.2, 23).  More than 16 heads a KV head are two workgroups a chunk: 100 of 768 23, 28.
+inline bool eight_waves(const PageDims& p) {
+  const int64_t R = (int64_t)p.n_seq * p.G, cap = (int64_t)p.width << p.shift;
+  if (R > 64) return R < PA_CUS && p.hpg > 4 && p.hpg <= PA_HEADS && cap >= 512 && cap <= 768;
+  return p.hpg > 4 ? cap >= 512 : R * cap >= 131072;
+}
+// Tiles of their chunks: where those of `size` tiles would be more than the chip runs at once, longer ones, which are no
+// more (a few in a second round: 7 sequences of 32768 tokens 129 us for 90, 53 of 8192 of one KV head 38 for 25).
+GKV_HD int one_round(uint64_t total, int rows, int size, int64_t chunks) {
+  return chunks > PA_CUS ? chunk_tiles(total, PA_CUS - rows) : size;
+}
+
 }  // namespace gkv

@@ -347,16 +347,6 @@ __global__ __launch_bounds__(64 * W, (W == 8 ? 2 : quant_waves<T, D, FMT>())) vo
   finish_row<T, D, true, QP_JOIN, W>(pg, ck, ws, part, bid, group, groups, sM, sL, sO, out, lse);
 }
 
-// Eight waves a workgroup for few rows that may be long: half the chunks, whose states the last joins in half the time
-// (with more threads, which is what counts for many heads).  us with four and eight, 8 KV heads of 128, bf16 over e4m3: 32 query heads, one
-// sequence of 2048 tokens 9.7 and 9.9, of 8192 13.1 and 12.8, of 32768 22.9 and 20.2, 4 of 8192 21.0 and 18.4, 16 of 1024 14.7 and 13.4; 64
-// query heads, 512 10.4 and 10.0, 2048 11.5 and 10.2, 8192 15.8 and 13.2; fp32, 16 of 4096 43 and 33.  Many rows of different
-// lengths need smaller pieces: 64 of 1 to 8192 44 and 71.  The lengths are not known here: what the table can name counts.
-static bool eight_waves(const PageDims& pg) {
-  const int64_t R = (int64_t)pg.n_seq * pg.G, cap = (int64_t)pg.width << pg.shift;
-  return R < 256 && (pg.hpg > 4 ? cap >= 512 : R * cap >= 131072);
-}
-
 hipError_t launch_quant_paged(const PageDims& pg, int format, const QuantDims& qd, int64_t q_tok, const void* q, const int32_t* table,
                               const int32_t* len, const PartView& part, void* out, float* lse, void* ws, hipStream_t st) {
   const PagedWs v = paged_view(ws, pg);
