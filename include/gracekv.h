@@ -559,8 +559,8 @@ typedef struct {
 } gracekv_read_config;
 
 /* Keys and values back from quantised pages: row cu_rows[b] + i of k and v becomes what
- * place start[b] + i of sequence b stands for, exactly (fp32; bf16 holds it too; past their
- * range, where no append leaves a value, infinite).
+ * place start[b] + i of sequence b stands for, exactly.  (Where no append leaves a value: past the
+ * types' range it becomes infinite, and in bf16, of E4M3 under s = 0, 1 or 2, the nearest multiple of 2^-133.)
  *   k, v       [n_rows] x G (cfg->dtype), written; either may be NULL: not wanted
  *   start      [n_seq] int32: the first place of each sequence
  *   cu_rows    [n_seq + 1] int32, ascending, as cu_new above
@@ -570,9 +570,10 @@ gracekv_status gracekv_quant_read(const gracekv_page_config* cfg, const gracekv_
                                   const int32_t* cu_rows, void* k, void* v, void* stream);
 
 /* gracekv_paged_attention_part over quantised pages, without packed entries of its own
- * (those of a compressed context come as a part: gracekv_shared_attention).  Codes
- * and scales are taken exactly; queries and weights in bf16 parts, one and two (bf16 rows:
- * weights off by at most 2^-15) or three (fp32 rows).  ws: gracekv_paged_ws_bytes(cfg) bytes, as there. */
+ * (those of a compressed context come as a part: gracekv_shared_attention).  Codes and scales
+ * are taken exactly, as far as bf16 holds their values (above); queries and weights in bf16 parts,
+ * one and two (bf16 rows: weights off by at most 2^-15) or three (fp32 rows).
+ * ws: gracekv_paged_ws_bytes(cfg) bytes, as there. */
 gracekv_status gracekv_quant_attention(const gracekv_page_config* cfg, const gracekv_quant_pages* pages, const void* q,
                                        int64_t q_tok, const int32_t* block_table, const int32_t* seq_len,
                                        const gracekv_part* part, void* out, float* lse, void* ws, size_t ws_bytes,

@@ -11,7 +11,8 @@
 // taken.  Multiplying by 2^(127 - s) is exact, so that each value is rounded once, to the nearest
 // code and the even one in the middle, as the conversion instruction does; what stands for it
 // is exact in bf16 as well.  s is at least 10 (2^-117), so that no value stands below fp32's normal
-// range, and a block with a size of 2^127 or more, an infinity or NaN has s = 255.
+// range, and a block with a size of 2^127 or more, an infinity or NaN has s = 255.  (Of pages from elsewhere, e4m3 under s = 0, 1
+// and 2 has values below bf16's smallest, 2^-133: they become the nearest multiple of it, except in fp32.)
 #pragma once
 
 #include "serve.h"
@@ -86,6 +87,24 @@ template <int FMT> __device__ __forceinline__ uint4 eight_bf16(const uint32_t* w
   else
     return make_uint4(pair_bf16<FMT, 0>(w[0], scale), pair_bf16<FMT, 1>(w[0], scale), pair_bf16<FMT, 2>(w[0], scale),
                       pair_bf16<FMT, 3>(w[0], scale));
+}
+
+// eight values as floats, from the words that hold them
+template <int FMT> __device__ __forceinline__ void eight_f32(const uint32_t* w, float scale, float* x) {
+  f32x2 p[4];
+  if constexpr (FMT == GRACEKV_E4M3) {
+    p[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[0], scale, false);
+    p[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[0], scale, true);
+    p[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[1], scale, false);
+    p[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[1], scale, true);
+  } else {
+    p[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[0], scale, 0);
+    p[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[0], scale, 1);
+    p[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[0], scale, 2);
+    p[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[0], scale, 3);
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = p[i / 2][i & 1];
 }
 
 // the kernel's template arguments from the shapes

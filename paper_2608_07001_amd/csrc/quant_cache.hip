@@ -7,7 +7,7 @@
 //
 // A rotated key is quantised from fp32, where its two products and their sum are each rounded
 // (no fused multiply and add: the same codes wherever the rotation is formed like that), and
-// not rounded to the rows' type before.  Reading back is exact in bf16 and fp32.
+// not rounded to the rows' type before.  Reading back is exact in fp32, and in bf16 wherever bf16 holds the value.
 #include <algorithm>
 
 #include "quant.h"
@@ -273,12 +273,11 @@ __global__ __launch_bounds__(QC_T) void k_quant_read(PageDims pg, QuantDims qd, 
       const bool key = k && s < pg.G;
       const int head = s < pg.G ? s : s - pg.G;
       T* dst = (key ? k + (t0 + r) * rd.k_tok + head * rd.k_head : v + (t0 + r) * rd.v_tok + head * rd.v_head) + c;
-      const uint4 y = eight_bf16<FMT>(w[i], sc[i]);
       if constexpr (sizeof(T) == 2) {
-        put_past(dst, y);
+        put_past(dst, eight_bf16<FMT>(w[i], sc[i]));
       } else {
         float f[8];
-        Eight<uint16_t>{y}.get(f);
+        eight_f32<FMT>(w[i], sc[i], f);
         Eight<float>::put(dst, f);
       }
     }
