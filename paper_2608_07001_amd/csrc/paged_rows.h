@@ -37,14 +37,6 @@ static inline PagedWs paged_view(void* base, const PageDims& pg) {
   return w;
 }
 
-__device__ __forceinline__ int64_t held_count(const PrefixView& px, int64_t row, int64_t& start) {
-  int64_t s = px.start[row], c = px.count[row];
-  s = s < 0 ? 0 : (s > px.rows ? px.rows : s);
-  c = c < 0 ? 0 : (c > px.rows - s ? px.rows - s : c);
-  start = s;
-  return c > PAGED_ROWS ? PAGED_ROWS : c;
-}
-
 // inclusive sum over the lanes of the wave
 __device__ __forceinline__ int scan_wave(int v) {
   v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);     // row_shr 1, 2, 4, 8

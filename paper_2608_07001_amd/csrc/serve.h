@@ -35,6 +35,15 @@ struct PrefixView {
   int64_t rows;
 };
 
+// the entries of a row (sequence or group, KV head), held inside the arrays
+__device__ __forceinline__ int64_t held_count(const PrefixView& px, int64_t row, int64_t& start) {
+  int64_t s = px.start[row], c = px.count[row];
+  s = s < 0 ? 0 : (s > px.rows ? px.rows : s);
+  c = c < 0 ? 0 : (c > px.rows - s ? px.rows - s : c);
+  start = s;
+  return c > PAGED_ROWS ? PAGED_ROWS : c;
+}
+
 // the pages of a quantised cache: bytes from page to page, of the codes and of their scales
 struct QuantDims {
   int64_t code_stride, scale_stride;

@@ -42,7 +42,7 @@ namespace gkv {
 
 constexpr int SF_OCC = 3;                      // few rows: waves a SIMD
 constexpr int SF_JOIN = 8;                     // ... and states that the last of a tile's chunks joins at a time
-constexpr float SF_COST = 0.6f;                // ... and what joining one costs, in steps of a tile, at d = 64 (chunks_of)
+constexpr float SF_COST = PA_COST;             // ... and what joining one costs, as over pages, in steps of a tile, at d = 64 (chunks_of)
 constexpr float SH_LAG = 8.f, SH_TOP = 256.f;  // as in prompt.hip: base-2 units, and as a factor
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 
@@ -81,14 +81,6 @@ size_t shared_ws_bytes(const SharedDims& sd) {
   return n;
 }
 
-__device__ __forceinline__ int64_t held_entries(const PrefixView& px, int64_t row, int64_t& start) {
-  int64_t s = px.start[row], c = px.count[row];
-  s = s < 0 ? 0 : (s > px.rows ? px.rows : s);
-  c = c < 0 ? 0 : (c > px.rows - s ? px.rows - s : c);
-  start = s;
-  return c > PAGED_ROWS ? PAGED_ROWS : c;
-}
-
 // What a workgroup works on: key tiles [t0, t1), chunk c of `chunks`, of row tile `tile` of (group b, KV head g)
 struct Item {
   int b, g, tile, tiles, c, chunks, t0, t1, id;
@@ -110,7 +102,7 @@ __device__ __forceinline__ bool find_item(const SharedDims& sd, const int32_t* c
     if (u >= units) return;
     sp = span_of(cu, u / sd.G, sd.n_seq);
     mt = tiles_of_group(sd, sp.n, ROWS);
-    count = held_entries(px, u, start);
+    count = held_count(px, u, start);
     n = (int)((count + KEYS - 1) / KEYS);
     if (n == 0) n = 1;                 // its zeros are written too
   };
