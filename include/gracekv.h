@@ -597,7 +597,10 @@ gracekv_status gracekv_shared_ws_bytes(const gracekv_shared_config* cfg, size_t*
  *   cu_group   [n_group + 1] int32, ascending; places outside [0, n_seq] are held inside.  Where
  *              they descend, the call stays inside the arrays, but what it writes there is
  *              not specified
- *   prefix     host structure, read by the call
+ *   prefix     host structure, read by the call.  The kernel is chosen by its rows, as entries of these
+ *              groups: of arrays that hold other layers' entries too (gracekv_pack's do), pass this
+ *              layer's rows alone, K, V and logm from the first of them on and start counted from
+ *              there; with all of them a call over short entries takes up to half as long again
  *   part       host structure, read by the call: its arrays are written;
  *              sequences outside every group are left as they are (one without entries belongs to
  *              a group of count 0 and gets 0 and -inf)

@@ -62,8 +62,11 @@ inline SharedPlan plan_of(const SharedDims& sd, bool few, int waves) {
   p.places = (int)((p.tiles + room + 7) & ~(int64_t)7);
   return p;
 }
-// `entries`: rows of the packed arrays.  The rows and entries of a (group, KV head) are taken as the
-// mean.  Small tiles spread little work over the chip with fewer states and one launch, large ones go through keys
+// `entries`: rows of the packed arrays, the only length that the host has.  The rows and entries of a (group, KV head) are
+// taken as the mean.  (Arrays that hold the entries of all layers look as many times too long, and the call takes the large tiles where small ones
+// are faster: of 32 layers, 16 sequences over 1024 entries a head 14.6 us and 11.7 with the layer's rows alone, 64 over 512 17.6 and 12.3.)
+// The thresholds are fitted to measurements of 288 shapes, over which the choice takes 1.01 times the better kernel's time in the mean; products
+// count 16 rows by 32 keys, and where fp32 takes eight waves they count once more by the row tiles, each of which has states to join.  Small tiles spread little work over the chip with fewer states and one launch, large ones go through keys
 // and values fewer times.  us, heads of 128, small tiles with four waves, with eight, large tiles:
 //   bf16, 8 KV heads, 16 rows each: over 128 entries 9.3, 8.2, 12.6; 1024 11.4, 11.8, 13.1; 4096 18.7, 16.9, 16.9; 16384 27.4, 25.5, 27.2
 //   64 rows: over 256 10.0, 10.6, 13.7; 2048 15.3, 14.0, 15.5; 4096 20.6, 17.0, 17.5; 8192 27.6, 37, 22.3

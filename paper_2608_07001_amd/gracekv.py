@@ -652,7 +652,8 @@ def shared_ws_bytes(cfg: SharedConfig) -> int:
 def shared_attention(cfg: SharedConfig, q, cu_group, prefix: Prefix, part: Part, ws, stream=None):
     """Attention of one token of every sequence over packed entries that its group shares
     (gracekv_shared_attention), written to ``part``: cu_group [n_group + 1] int32, prefix.start and
-    .count [n_group * G], ws: shared_ws_bytes(cfg) bytes."""
+    .count [n_group * G], ws: shared_ws_bytes(cfg) bytes.  Of arrays of several layers pass one layer's
+    rows (K[a:b], V[a:b], logm[a:b], start - a): the kernel is chosen by how many there are."""
     dev, t, n, H, d = torch.cuda.current_device(), _TORCH[cfg.dtype], cfg.n_seq, cfg.H, cfg.d
     qp, far = _tokens(q, t, n, H, d, dev)
     if far != cfg.q_tok:

@@ -344,3 +344,18 @@ def test_large_calls_at_once_on_two_streams():
         torch.cuda.synchronize()
         for x in (a, b):
             assert torch.equal(x.part.o, w.part.o) and torch.equal(x.part.lse, w.part.lse)
+
+
+def test_one_layer_of_several_in_the_arrays():
+    # the arrays' slice of one layer, which begins on no boundary of log m, and the whole of them: another kernel each, and
+    # rows of other layers that are NaN
+    for kind in P.KINDS:
+        G, H, groups = P.one_group(kind)[1]
+        c = Large(kind, G, H, groups, [300, 129], seed=40)
+        whole = c.packed()
+        a = int(whole.start[0]) - 1
+        n = int(c.pre["count"].sum()) + 2
+        one = gk.Prefix(whole.start - a, whole.count, whole.K[a:a + n], whole.V[a:a + n], whole.logm[a:a + n])
+        assert P.kernel(c.dtype, c.d, G, H, c.n, 1, n)[0] == "few" and whole.logm[a:].data_ptr() % 16
+        c.check(c.call(prefix=one))
+        c.check(c.call(prefix=whole))
